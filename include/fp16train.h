@@ -477,6 +477,146 @@ fp16_status fp16_softmax_ce(int32_t n, int32_t k, const fp16_t* z, const fp16_t*
 enum { FP16_FORM_ADDEND = 1, FP16_FORM_STATS = 2 };
 const char* fp16_conv_kernel(const fp16_conv_desc* desc, int32_t pass, int32_t form);
 
+/* ---- orthogonalised momentum for weight matrices (the Muon update) ----
+ * Beside the momentum SGD of Section 5.1, for the parameters that are matrices:
+ * a dense layer's [outputs][inputs], a KRSC filter as [K][R*S*C].  Weights,
+ * gradients and momentum are binary16 with no copy in higher precision, as for
+ * fp16_sgd_step. */
+
+/* One matrix, row-major and contiguous, 1 <= rows, cols <= 65536, the shorter
+ * side at most 16384 and rows * cols < 2^30.  scale multiplies its
+ * orthogonalised update (finite): often sqrt(max(1, rows / cols)). */
+typedef struct {
+  int32_t rows, cols;
+  float scale;
+} fp16_muon_desc;
+
+/* Most matrices of one call, and most steps. */
+#define FP16_MUON_MAX 1024
+#define FP16_MUON_MAX_STEPS 32
+
+/* Bytes of workspace for fp16_orthogonalize and fp16_muon_step on these
+ * matrices with this many products (see there); 0 for an invalid list. */
+size_t fp16_muon_workspace_bytes(int32_t count, const fp16_muon_desc* descs, int32_t products);
+
+/* Side of the tiles the products of such a call run on (256, 128 or 64), for
+ * tests and profiles; 0 for an invalid list. */
+int32_t fp16_muon_tile(int32_t count, const fp16_muon_desc* descs, int32_t products);
+
+/* Orthogonalisation by Newton-Schulz products, of `count` matrices at once
+ * (host arrays, read during the call only):
+ *   X = x / ||x||_F;  steps times:  A = X X^T,  X <- a X + (b A + c A^2) X;
+ *   y = round_to_binary16(scale * X)
+ * with A taken over the shorter side (a tall matrix runs transposed).  coef holds
+ * (a, b, c) for each step, or is NULL for (3.4445, -4.7750, 2.0315) in every step,
+ * which takes all singular values that are not tiny to [0.7, 1.2].  A zero matrix
+ * gives zeros and a zero row a zero row; a matrix with an element that is not
+ * finite gives NaN throughout.
+ * products says how the matrix products are formed (float32 sums either way):
+ *   1  from operands rounded to binary16, X itself kept to 22 bits between steps:
+ *      y is within about 2e-3 of the exact result (2-norm, relative);
+ *   3  from operands of 22 bits, as high and low binary16 parts and three
+ *      products for one: within 5e-5, below the rounding of y.
+ * Coefficients have to keep |X| < 16 and |b A + c A^2| < 32 elementwise; beyond,
+ * operands overflow.
+ * 1 <= steps <= FP16_MUON_MAX_STEPS, products 1 or 3, finite coef (FP16_ERR_SHAPE);
+ * count = 0 is a no-op.  y[i] may equal x[i]; no y[i] may overlap anything else. */
+fp16_status fp16_orthogonalize(int32_t count, const fp16_muon_desc* descs, const fp16_t* const* x,
+                               fp16_t* const* y, int32_t steps, const float* coef,
+                               int32_t products, void* ws, size_t ws_bytes, fp16_stream_t stream);
+
+/* One update of `count` weight matrices, in place:
+ *   m = round_to_binary16(fma(momentum, m, g));
+ *   u = nesterov ? fma(momentum, m, g) : m           (float32, the rounded m)
+ *   O = u orthogonalised as above, in float32
+ *   w = round_to_binary16(fma(-fl(lr * scale), O, fl(fl(1 - lr*weight_decay) * w)))
+ * lr, momentum, weight_decay finite (FP16_ERR_SHAPE); other rules as
+ * fp16_orthogonalize.  No w[i] or m[i] may overlap any other argument. */
+fp16_status fp16_muon_step(int32_t count, const fp16_muon_desc* descs, fp16_t* const* w,
+                           const fp16_t* const* g, fp16_t* const* m, float lr, float momentum,
+                           float weight_decay, int32_t nesterov, int32_t steps, const float* coef,
+                           int32_t products, void* ws, size_t ws_bytes, fp16_stream_t stream);
+
+/* ---- dense layers in 8-bit integers ----
+ * The product of a dense layer (ResNet-50's classifier, Section 5.1, or any
+ * other) from operands quantised to 8 bits with a scale for each row: for each
+ * token of the activations, for each output channel of the weights.
+ *
+ * A quantised operand [rows][n] holds signed bytes, rows fp16_int8_row_bytes(n)
+ * apart (n rounded up to 16), and a float32 scale for each row.  The bytes past n
+ * are zeros; the quantisers write them so. */
+size_t fp16_int8_row_bytes(int32_t n);
+
+/* Quantises x [rows][cols] by rows:
+ *   scale[i] = fl(max_j |x[i][j]| / 127)
+ *   q[i][j]  = 127 x[i][j] / max_j |x[i][j]| to the nearest integer, ties to even
+ * A zero row has scale 0 and q 0; a row with an infinity or a NaN has scale NaN
+ * and q 0, so that every product with it is NaN.  q is [rows][cols] as above.
+ * 1 <= rows, cols < 2^24, rows * cols < 2^40 (FP16_ERR_SHAPE). */
+fp16_status fp16_int8_quant_rows(int32_t rows, int32_t cols, const fp16_t* x, int8_t* q,
+                                 float* scale, fp16_stream_t stream);
+
+/* The same by columns: q is the transpose, [cols][rows] as above, and scale has
+ * cols values.  Workspace: fp16_int8_quant_workspace_bytes(rows, cols). */
+size_t fp16_int8_quant_workspace_bytes(int32_t rows, int32_t cols);
+fp16_status fp16_int8_quant_cols(int32_t rows, int32_t cols, const fp16_t* x, int8_t* q,
+                                 float* scale, void* ws, size_t ws_bytes, fp16_stream_t stream);
+
+/* The product of quantised a [m][k] and b [n][k]:
+ *   y[i][j] = round_to_binary16(fl(sa[i] * sb[j]) * fl(sum_k a[i][k] * b[j][k]) + bias[j])
+ * with the sum exact in 32 bits and the rest in float32; bias [n] may be NULL.
+ * y is [m][n].  1 <= m, n < 2^24, 1 <= k <= 131071, m * n < 2^40
+ * (FP16_ERR_SHAPE).  In every row of a or of b the bytes past k must be zero.  y
+ * must not overlap an input. */
+fp16_status fp16_int8_matmul(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa,
+                             const int8_t* b, const float* sb, const fp16_t* bias, fp16_t* y,
+                             fp16_stream_t stream);
+
+/* The kernel such a product runs on ("few rows", "tile 128", ...), for tests and
+ * profiles; "" for invalid sizes.  No contract. */
+const char* fp16_int8_kernel(int32_t m, int32_t n, int32_t k);
+
+/* A dense layer y = x W^T + bias over `tokens` rows: x [tokens][inputs],
+ * W [outputs][inputs], y [tokens][outputs], each 1 to 131071. */
+typedef struct {
+  int32_t tokens, inputs, outputs;
+} fp16_int8_dense_desc;
+
+typedef enum {
+  FP16_INT8_FWD = 0,
+  FP16_INT8_BWD = 1,
+  FP16_INT8_WEIGHTS = 2
+} fp16_int8_call;
+
+/* Bytes of workspace one of the three calls below needs; 0 if invalid. */
+size_t fp16_int8_dense_workspace_bytes(const fp16_int8_dense_desc* desc, int32_t call);
+
+/* The layer's weights quantised for the forward (wq [outputs][inputs] and sw
+ * [outputs], by rows) and, unless NULL, for the backward (wqt [inputs][outputs]
+ * and swt [inputs], by columns); wqt and swt are given together.  (tokens is not
+ * used.) */
+fp16_status fp16_int8_dense_weights(const fp16_int8_dense_desc* desc, const fp16_t* w, int8_t* wq,
+                                    float* sw, int8_t* wqt, float* swt, void* ws, size_t ws_bytes,
+                                    fp16_stream_t stream);
+
+/* Forward: x quantised by rows, then fp16_int8_matmul of it and (wq, sw), with
+ * identical results.  bias may be NULL. */
+fp16_status fp16_int8_dense_fwd(const fp16_int8_dense_desc* desc, const fp16_t* x, const int8_t* wq,
+                                const float* sw, const fp16_t* bias, fp16_t* y, void* ws,
+                                size_t ws_bytes, fp16_stream_t stream);
+
+/* Backward, each gradient from operands quantised along the axis it sums over
+ * (the rounding to integers passes gradients through unchanged):
+ *   dx = dy quantised by rows    x  W quantised by columns (wqt, swt)
+ *   dw = dy quantised by columns x  x quantised by columns
+ *   dbias[j] = round_to_binary16(sum_i dy[i][j])   (float32 partial sums, added in
+ *              float64)
+ * dx (with wqt, swt), dw (with x) and dbias may each be NULL if not wanted; dbias
+ * needs dw. */
+fp16_status fp16_int8_dense_bwd(const fp16_int8_dense_desc* desc, const fp16_t* x, const fp16_t* dy,
+                                const int8_t* wqt, const float* swt, fp16_t* dx, fp16_t* dw,
+                                fp16_t* dbias, void* ws, size_t ws_bytes, fp16_stream_t stream);
+
 /* Human-readable name of a status code (static string). */
 const char* fp16_status_string(fp16_status status);
 

@@ -37,7 +37,11 @@ EXPORTS = ["fp16_conv_out_dims", "fp16_conv_workspace_bytes", "fp16_conv_fwd", "
            "fp16_conv_dgrad_wf", "fp16_conv_kernel", "fp16_noalloc_scratch_bytes", "fp16_conv_wgrad_noalloc",
            "fp16_bn_mask_bytes", "fp16_bn_relu_m", "fp16_bn_relu_bwd_m", "fp16_conv_bn_relu_fwd_m",
            "fp16_conv_dgrad_wf_m", "fp16_bn_relu_maxpool", "fp16_conv_wgrad_ex",
-           "fp16_conv_dgrad_wf_ex"]
+           "fp16_conv_dgrad_wf_ex", "fp16_muon_workspace_bytes", "fp16_muon_tile", "fp16_orthogonalize",
+           "fp16_muon_step", "fp16_int8_row_bytes", "fp16_int8_quant_rows",
+           "fp16_int8_quant_workspace_bytes", "fp16_int8_quant_cols", "fp16_int8_matmul",
+           "fp16_int8_kernel", "fp16_int8_dense_workspace_bytes", "fp16_int8_dense_weights",
+           "fp16_int8_dense_fwd", "fp16_int8_dense_bwd"]
 
 
 class Fp16Error(RuntimeError):
@@ -62,6 +66,14 @@ class BnDesc(ctypes.Structure):
 class PoolDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("n", "c", "h", "w", "r", "s", "stride_h", "stride_w", "pad_h", "pad_w", "layout")]
+
+
+class MuonDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class Int8DenseDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "inputs", "outputs")]
 
 
 _lib = None
@@ -104,6 +116,21 @@ _SIGS = {
     "fp16_conv_bn_workspace_bytes": (_SZ, [_P, _P]),
     "fp16_conv_bn_relu_fwd": (ctypes.c_int, [_P] * 11 + [_SZ, _P]),
     "fp16_conv_kernel": (ctypes.c_char_p, [_P, _I32, _I32]),
+    "fp16_muon_workspace_bytes": (_SZ, [_I32, _P, _I32]),
+    "fp16_muon_tile": (_I32, [_I32, _P, _I32]),
+    "fp16_orthogonalize": (ctypes.c_int, [_I32, _P, _P, _P, _I32, _P, _I32, _P, _SZ, _P]),
+    "fp16_muon_step": (ctypes.c_int, [_I32, _P, _P, _P, _P, _F, _F, _F, _I32, _I32, _P, _I32, _P,
+                                      _SZ, _P]),
+    "fp16_int8_row_bytes": (_SZ, [_I32]),
+    "fp16_int8_quant_rows": (ctypes.c_int, [_I32, _I32, _P, _P, _P, _P]),
+    "fp16_int8_quant_workspace_bytes": (_SZ, [_I32, _I32]),
+    "fp16_int8_quant_cols": (ctypes.c_int, [_I32, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "fp16_int8_matmul": (ctypes.c_int, [_I32] * 3 + [_P] * 7),
+    "fp16_int8_kernel": (ctypes.c_char_p, [_I32] * 3),
+    "fp16_int8_dense_workspace_bytes": (_SZ, [_P, _I32]),
+    "fp16_int8_dense_weights": (ctypes.c_int, [_P] * 7 + [_SZ, _P]),
+    "fp16_int8_dense_fwd": (ctypes.c_int, [_P] * 7 + [_SZ, _P]),
+    "fp16_int8_dense_bwd": (ctypes.c_int, [_P] * 9 + [_SZ, _P]),
     "fp16_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "fp16_version": (ctypes.c_char_p, []),
 }
@@ -155,9 +182,9 @@ def _ptr(t):
 def _check_dtype(t) -> None:
     global _DTYPES
     import torch
-    _DTYPES = frozenset((torch.float16, torch.float32, torch.uint8, torch.int32))
+    _DTYPES = frozenset((torch.float16, torch.float32, torch.uint8, torch.int8, torch.int32))
     if t.dtype not in _DTYPES:
-        raise TypeError(f"expected float16/float32/uint8/int32 tensor, got {t.dtype}")
+        raise TypeError(f"expected float16/float32/uint8/int8/int32 tensor, got {t.dtype}")
 
 
 def _first_current_stream():
@@ -424,6 +451,134 @@ def fp16_conv_bn_relu_fwd_m(conv, bn, x, w, gamma, beta, residual, y, z, stats, 
         ctypes.byref(conv), ctypes.byref(bn), _ptr(x), _ptr(w), _ptr(gamma), _ptr(beta),
         _ptr(residual), _ptr(y), _ptr(z), _ptr(stats), _ptr(mask), _ptr(ws), _wsb(ws, ws_bytes),
         _stream(stream)))
+
+
+# ---- orthogonalised momentum ------------------------------------------------
+
+def muon_descs(shapes):
+    """The descriptors of a set of matrices: (rows, cols) or (rows, cols, scale) each."""
+    return (MuonDesc * max(len(shapes), 1))(*[MuonDesc(*s) if len(s) == 3 else MuonDesc(*s, 1.0)
+                                              for s in shapes])
+
+
+def _muon_list(descs, *lists):
+    """The number of matrices and an array of pointers for each list of tensors."""
+    n = len(lists[0])
+    if any(len(l) != n for l in lists) or len(descs) < n:
+        raise ValueError("descs and the lists of tensors differ in length")
+    return [n] + [(_P * max(n, 1))(*[_ptr(t) for t in l]) for l in lists]
+
+
+def _coef(coef, steps):
+    """None, one (a, b, c) for every step, or one for each step."""
+    if coef is None:
+        return None
+    flat = [float(v) for c in coef for v in (c if isinstance(c, (tuple, list)) else (c,))]
+    if len(flat) == 3:
+        flat *= int(steps)
+    if len(flat) != 3 * int(steps):
+        raise ValueError("coef holds (a, b, c), or steps of them")
+    return (_F * max(len(flat), 1))(*flat)
+
+
+def fp16_muon_workspace_bytes(descs, products=1) -> int:
+    return int(lib().fp16_muon_workspace_bytes(len(descs), descs, int(products)))
+
+
+def fp16_muon_tile(descs, products=1) -> int:
+    """The side of the tiles the products run on (for tests and profiles)."""
+    return int(lib().fp16_muon_tile(len(descs), descs, int(products)))
+
+
+def fp16_orthogonalize(descs, xs, ys, steps=5, coef=None, products=3, ws=None, ws_bytes=None,
+                       stream=None) -> None:
+    """Each x of xs orthogonalised into the y of ys (lists of tensors)."""
+    n, x, y = _muon_list(descs, xs, ys)
+    _check("fp16_orthogonalize", lib().fp16_orthogonalize(
+        n, descs, x, y, int(steps), _coef(coef, steps), int(products), _ptr(ws),
+        _wsb(ws, ws_bytes), _stream(stream)))
+
+
+def fp16_muon_step(descs, ws_, gs, ms, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True,
+                   steps=5, coef=None, products=1, ws=None, ws_bytes=None, stream=None) -> None:
+    """One update of the weights ws_ from the gradients gs with the momenta ms."""
+    n, w, g, m = _muon_list(descs, ws_, gs, ms)
+    _check("fp16_muon_step", lib().fp16_muon_step(
+        n, descs, w, g, m, float(lr), float(momentum), float(weight_decay), int(bool(nesterov)),
+        int(steps), _coef(coef, steps), int(products), _ptr(ws), _wsb(ws, ws_bytes),
+        _stream(stream)))
+
+
+# ---- dense layers in 8-bit integers -----------------------------------------
+
+INT8_FWD, INT8_BWD, INT8_WEIGHTS = 0, 1, 2
+
+
+def int8_dense_desc(tokens, inputs, outputs) -> Int8DenseDesc:
+    return Int8DenseDesc(int(tokens), int(inputs), int(outputs))
+
+
+def fp16_int8_row_bytes(n: int) -> int:
+    return int(lib().fp16_int8_row_bytes(int(n)))
+
+
+def int8_operand(rows, n, device="cuda"):
+    """Buffers of a quantised operand [rows][n]: its bytes and its scales."""
+    import torch
+    return (torch.empty((int(rows), fp16_int8_row_bytes(n)), dtype=torch.int8, device=device),
+            torch.empty(int(rows), dtype=torch.float32, device=device))
+
+
+def fp16_int8_quant_rows(rows, cols, x, q, scale, stream=None) -> None:
+    _check("fp16_int8_quant_rows", lib().fp16_int8_quant_rows(
+        int(rows), int(cols), _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def fp16_int8_quant_workspace_bytes(rows, cols) -> int:
+    return int(lib().fp16_int8_quant_workspace_bytes(int(rows), int(cols)))
+
+
+def fp16_int8_quant_cols(rows, cols, x, q, scale, ws=None, ws_bytes=None, stream=None) -> None:
+    _check("fp16_int8_quant_cols", lib().fp16_int8_quant_cols(
+        int(rows), int(cols), _ptr(x), _ptr(q), _ptr(scale), _ptr(ws), _wsb(ws, ws_bytes),
+        _stream(stream)))
+
+
+def fp16_int8_matmul(m, n, k, a, sa, b, sb, bias, y, stream=None) -> None:
+    _check("fp16_int8_matmul", lib().fp16_int8_matmul(
+        int(m), int(n), int(k), _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), _ptr(bias), _ptr(y),
+        _stream(stream)))
+
+
+def fp16_int8_kernel(m, n, k) -> str:
+    """The kernel a product runs on (for tests and profiles)."""
+    return lib().fp16_int8_kernel(int(m), int(n), int(k)).decode()
+
+
+def fp16_int8_dense_workspace_bytes(desc: Int8DenseDesc, call=None) -> int:
+    """Workspace of one of the layer's calls, or (None) enough for all three."""
+    calls = (INT8_FWD, INT8_BWD, INT8_WEIGHTS) if call is None else (int(call),)
+    return max(int(lib().fp16_int8_dense_workspace_bytes(ctypes.byref(desc), c)) for c in calls)
+
+
+def fp16_int8_dense_weights(desc, w, wq, sw, wqt=None, swt=None, ws=None, ws_bytes=None,
+                            stream=None) -> None:
+    _check("fp16_int8_dense_weights", lib().fp16_int8_dense_weights(
+        ctypes.byref(desc), _ptr(w), _ptr(wq), _ptr(sw), _ptr(wqt), _ptr(swt), _ptr(ws),
+        _wsb(ws, ws_bytes), _stream(stream)))
+
+
+def fp16_int8_dense_fwd(desc, x, wq, sw, bias, y, ws=None, ws_bytes=None, stream=None) -> None:
+    _check("fp16_int8_dense_fwd", lib().fp16_int8_dense_fwd(
+        ctypes.byref(desc), _ptr(x), _ptr(wq), _ptr(sw), _ptr(bias), _ptr(y), _ptr(ws),
+        _wsb(ws, ws_bytes), _stream(stream)))
+
+
+def fp16_int8_dense_bwd(desc, x, dy, wqt, swt, dx, dw, dbias=None, ws=None, ws_bytes=None,
+                        stream=None) -> None:
+    _check("fp16_int8_dense_bwd", lib().fp16_int8_dense_bwd(
+        ctypes.byref(desc), _ptr(x), _ptr(dy), _ptr(wqt), _ptr(swt), _ptr(dx), _ptr(dw),
+        _ptr(dbias), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
 
 
 def _wsb(ws, ws_bytes):

@@ -3,6 +3,7 @@
 // enqueued on the caller's stream.
 
 #include "../../include/fp16train.h"
+#include "api_util.hpp"
 #include "kernels.hpp"
 
 #include <stdint.h>
@@ -15,16 +16,7 @@ namespace {
 
 constexpr int64_t kMaxElems = (int64_t)1 << 30;  // buffer-load offsets are 32-bit byte offsets
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  if (!a || !b || na == 0 || nb == 0) return false;
-  const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
-  return pa < pb + nb && pb < pa + na;
-}
-
 int round8(int v) { return (v + 7) / 8 * 8; }
-size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct ConvDims {
   int N, C, H, W, K, R, S, sh, sw, ph, pw, P, Q, layout, Cp, Kp, accum;
@@ -213,14 +205,6 @@ hipError_t dgrad_launches(const ConvDims& d, IgemmArgs a, const h16* wf, Launch 
 ConvChainArgs chain_args(const ConvDims& d) {
   return ConvChainArgs{d.N, d.C, d.H, d.W, d.K, d.R, d.S, d.sh, d.sw, d.ph, d.pw, d.P, d.Q};
 }
-
-fp16_status hip_status(hipError_t e) { return e == hipSuccess ? FP16_OK : FP16_ERR_HIP; }
-
-#define TRY(expr)                                  \
-  do {                                             \
-    const hipError_t e_ = (expr);                  \
-    if (e_ != hipSuccess) return FP16_ERR_HIP;     \
-  } while (0)
 
 fp16_status check_ws(const ConvWs& L, const void* ws, size_t ws_bytes) {
   if (L.total == 0) return FP16_OK;

@@ -1,0 +1,450 @@
+// Dense layers in 8-bit integers: rows or columns of a binary16 matrix quantised
+// with a scale each, and the product of two quantised operands.
+//
+//   s = max |x| / 127,  q = 127 x / max |x| to the nearest, ties to even;
+//   y[i][j] = rne16(fl(sa[i] sb[j]) * (sum_k qa[i][k] qb[j][k]) + bias[j]).
+//
+// 127 x of a binary16 x is exact in float32 and the quotient is one float32
+// division, within 2^-24 of the exact one.  Exact quotients differ from a halfway
+// value by at least 2^-20 of it or not at all (254 x and (2k+1) max are integers
+// below 2^20 on a common scale), so q is the exact quotient's rounding.  A zero row
+// has s = 0 and q = 0; a row with an infinity or NaN has s = NaN, so every product
+// with it is NaN.  The sums are exact: 32-bit integers, k <= 131071.
+
+#include "gemm_nt.hpp"
+#include "products.hpp"
+
+#include <algorithm>
+
+namespace fp16k {
+namespace {
+
+// ---- quantising ------------------------------------------------------------------
+
+// Magnitudes as bit patterns, which order as integers: an infinity is 0x7c00, a
+// NaN above it, so that the maximum finds both.
+__device__ __forceinline__ uint32_t i8_mag(uint32_t bits) { return bits & 0x7fffu; }
+__device__ __forceinline__ uint32_t i8_mag8(const V8& v, uint32_t top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t m = i8_mag(v.s[e]);
+    top = m > top ? m : top;
+  }
+  return top;
+}
+__device__ __forceinline__ float i8_top(uint32_t mag) {
+  return to_f32(__builtin_bit_cast(h16, (uint16_t)mag));
+}
+__device__ __forceinline__ float i8_scale(uint32_t mag) {
+  return mag >= 0x7c00u ? __builtin_nanf("") : i8_top(mag) / 127.0f;
+}
+// q of x for a row whose largest magnitude is `mag` (0 for a zero row and for one
+// that is not finite).
+__device__ __forceinline__ int i8_q(h16 x, float top, bool live) {
+  const float r = __builtin_rintf((127.0f * to_f32(x)) / top);
+  return live ? (int)r : 0;
+}
+__device__ __forceinline__ bool i8_live(uint32_t mag) { return mag != 0 && mag < 0x7c00u; }
+
+__device__ __forceinline__ uint32_t i8_wave_max(uint32_t v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)v, off, 64);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+
+// eight elements from p of a row that ends `left` elements further on
+__device__ __forceinline__ V8 i8_load8(const h16* p, int left, bool whole) {
+  if (whole && left >= 8) return load16(p);
+  V8 v = zero8();
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) v.h[e] = p[e];
+  return v;
+}
+
+__device__ __forceinline__ uint2 i8_pack(const V8& v, float top, bool live) {
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(uint8_t)i8_q(v.h[e], top, live) << (8 * (e & 3));
+  return make_uint2(w[0], w[1]);
+}
+
+// One workgroup a row; up to 8192 elements stay in registers between the maximum
+// and the quantising, further ones are read again.  Bandwidth-bound: 3 bytes an
+// element.
+constexpr int kRowKeep = 4;
+__global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __restrict__ x,
+                                               int8_t* __restrict__ q, float* __restrict__ scale) {
+  __shared__ uint32_t red[4];
+  const int tid = threadIdx.x;
+  const h16* xr = x + (int64_t)blockIdx.x * cols;
+  int8_t* qr = q + (int64_t)blockIdx.x * ld;
+  const bool whole = cols % 8 == 0;
+  V8 keep[kRowKeep];
+  uint32_t mag = 0;
+#pragma unroll
+  for (int i = 0; i < kRowKeep; ++i) {
+    const int c = (i * 256 + tid) * 8;
+    keep[i] = c < cols ? i8_load8(xr + c, cols - c, whole) : zero8();
+  }
+#pragma unroll
+  for (int i = 0; i < kRowKeep; ++i) mag = i8_mag8(keep[i], mag);
+  for (int c = (kRowKeep * 256 + tid) * 8; c < cols; c += 2048)
+    mag = i8_mag8(i8_load8(xr + c, cols - c, whole), mag);
+  mag = i8_wave_max(mag);
+  if ((tid & 63) == 0) red[tid >> 6] = mag;
+  __syncthreads();
+  mag = std::max(std::max(red[0], red[1]), std::max(red[2], red[3]));
+  if (tid == 0) scale[blockIdx.x] = i8_scale(mag);
+  const float top = i8_top(mag);
+  const bool live = i8_live(mag);
+#pragma unroll
+  for (int i = 0; i < kRowKeep; ++i) {
+    const int c = (i * 256 + tid) * 8;
+    if (c < ld) *reinterpret_cast<uint2*>(qr + c) = i8_pack(keep[i], top, live);
+  }
+  for (int c = (kRowKeep * 256 + tid) * 8; c < ld; c += 2048)
+    *reinterpret_cast<uint2*>(qr + c) =
+        i8_pack(c < cols ? i8_load8(xr + c, cols - c, whole) : zero8(), top, live);
+}
+
+// Columns, first pass: the largest magnitude (and the sum) of 256 columns over a
+// range of rows.  Thread: 8 columns, every eighth row.
+constexpr int kColChunks = 64;  // ranges of rows, at most
+__global__ __launch_bounds__(256) void i8_cols_max(int rows, int cols, int per,
+                                                   const h16* __restrict__ x,
+                                                   uint32_t* __restrict__ mag,
+                                                   float* __restrict__ sum) {
+  __shared__ uint32_t rm[8][256];
+  __shared__ float rs[8][256];
+  const int tid = threadIdx.x, cg = tid & 31, rg = tid >> 5;
+  const int c = blockIdx.x * 256 + cg * 8;
+  const bool whole = cols % 8 == 0;
+  const int r1 = std::min(rows, (int)(blockIdx.y + 1) * per);
+  uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (c < cols) {
+    for (int r = blockIdx.y * per + rg; r < r1; r += 8) {
+      const V8 v = i8_load8(x + (int64_t)r * cols + c, cols - c, whole);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t b = i8_mag(v.s[e]);
+        m[e] = b > m[e] ? b : m[e];
+        s[e] += to_f32(v.h[e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    rm[rg][cg * 8 + e] = m[e];
+    rs[rg][cg * 8 + e] = s[e];
+  }
+  __syncthreads();
+  const int cc = blockIdx.x * 256 + tid;
+  if (cc >= cols) return;
+  uint32_t a = 0;
+  float t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    a = rm[i][tid] > a ? rm[i][tid] : a;
+    t += rs[i][tid];
+  }
+  mag[(int64_t)blockIdx.y * cols + cc] = a;
+  if (sum) sum[(int64_t)blockIdx.y * cols + cc] = t;
+}
+
+// Columns, second pass: 128 rows x 64 columns quantised and written transposed, a
+// 128-byte run of each column, through LDS.
+__global__ __launch_bounds__(256) void i8_cols_write(int rows, int cols, int chunks, int ld,
+                                                     const h16* __restrict__ x,
+                                                     const uint32_t* __restrict__ mag,
+                                                     const float* __restrict__ psum,
+                                                     int8_t* __restrict__ q,
+                                                     float* __restrict__ scale,
+                                                     h16* __restrict__ sum) {
+  constexpr int LD = 144;  // bytes from column to column of the tile
+  __shared__ uint32_t cm[64];
+  __shared__ __attribute__((aligned(16))) int8_t tile[64 * LD];
+  const int tid = threadIdx.x;
+  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 128;
+  if (tid < 64) {
+    const int c = c0 + tid;
+    uint32_t a = 0;
+    double s = 0.0;
+    if (c < cols) {
+      for (int i = 0; i < chunks; ++i) {
+        const uint32_t b = mag[(int64_t)i * cols + c];
+        a = b > a ? b : a;
+        if (sum && blockIdx.y == 0) s += (double)psum[(int64_t)i * cols + c];
+      }
+      if (blockIdx.y == 0) {
+        scale[c] = i8_scale(a);
+        if (sum) sum[c] = dbl_to_h16(s);
+      }
+    }
+    cm[tid] = a;
+  }
+  __syncthreads();
+  const bool whole = cols % 8 == 0;
+  const int cg = tid & 7, rq = tid >> 3;  // 8 columns, rows 4 rq .. + 3
+  const int c = c0 + cg * 8;
+  uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + rq * 4 + i;
+    V8 v = zero8();
+    if (r < rows && c < cols) v = i8_load8(x + (int64_t)r * cols + c, cols - c, whole);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t m = cm[cg * 8 + e];
+      w[e] |= (uint32_t)(uint8_t)i8_q(v.h[e], i8_top(m), i8_live(m)) << (8 * i);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    *reinterpret_cast<uint32_t*>(tile + (cg * 8 + e) * LD + rq * 4) = w[e];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int cc = (i * 256 + tid) >> 3, k = ((i * 256 + tid) & 7) * 16;
+    if (c0 + cc < cols && r0 + k < ld)
+      *reinterpret_cast<u32x4*>(q + (int64_t)(c0 + cc) * ld + r0 + k) =
+          *reinterpret_cast<const u32x4*>(tile + cc * LD + k);
+  }
+}
+
+// ---- the product --------------------------------------------------------------------
+
+// fl(sa sb) * sum + bias, the sum rounded to float32 first
+__device__ __forceinline__ h16 i8_out(int acc, float sa, float sb, bool has_bias, float bias) {
+  const float v = (sa * sb) * (float)acc;
+  return to_h16(has_bias ? v + bias : v);
+}
+
+// Tile rows p are rows of b (outputs), q rows of a (tokens): a lane's runs of 8 lie
+// along a row of y.
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product g, int tp, int tq) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int t = nt_xcd(blockIdx.x, tp * tq);
+  if (t >= tp * tq) return;
+  const int gr = t / (4 * tq), w = t - gr * 4 * tq;
+  const int gw = tp - 4 * gr < 4 ? tp - 4 * gr : 4;
+  const int pt = (4 * gr + w % gw) * C::BP, qt = (w / gw) * C::BQ;
+  NtTile<1> nt;
+  nt.ldp = nt.ldq = (uint32_t)((g.k + 15) & ~15);
+  nt.p[0] = g.b + (int64_t)pt * nt.ldp;
+  nt.q[0] = g.a + (int64_t)qt * nt.ldq;
+  nt.prows = g.n - pt;
+  nt.qrows = g.m - qt;
+  nt.kbytes = g.k;
+  intx16 acc[C::TP][C::TQ];
+  nt_product<NtByte, C, 1>(nt, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lrow = lane & 31, lhi = lane >> 5;
+  const int p0 = pt + (wave / C::WQ) * 32 * C::TP, q0 = qt + (wave % C::WQ) * 32 * C::TQ;
+  const bool whole = g.n % 8 == 0, has_bias = g.bias != nullptr;
+#pragma unroll
+  for (int a = 0; a < C::TP; ++a)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int p = p0 + 32 * a + 16 * h + 8 * lhi;
+      float sp[8], bp[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool in = p + e < g.n;
+        sp[e] = in ? g.sb[p + e] : 0.0f;
+        bp[e] = in && has_bias ? to_f32(g.bias[p + e]) : 0.0f;
+      }
+#pragma unroll
+      for (int b = 0; b < C::TQ; ++b) {
+        const int q = q0 + 32 * b + lrow;
+        unsigned v[16];
+        nt_rows(acc[a][b], v);
+        if (q >= g.m || p >= g.n) continue;
+        const float sq = g.sa[q];
+        V8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o.h[e] = i8_out((int)v[8 * h + e], sq, sp[e], has_bias, bp[e]);
+        h16* yp = g.y + (int64_t)q * g.n + p;
+        if (whole) {
+          store16(yp, o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (p + e < g.n) yp[e] = o.h[e];
+        }
+      }
+    }
+}
+
+// Few rows (at most 16 tokens): bound by reading b once.  A workgroup takes 16
+// outputs; its eight waves split the reduction, each lane loading 16 bytes of one
+// row of b straight into the operand, and add their 32-bit sums in LDS.  FUSED: the
+// rows of x are quantised by every workgroup for itself into LDS (they are small and
+// come from the L2), which saves a launch; otherwise a is read from memory.
+constexpr int kFewRows = 16, kFewWaves = 8, kFewLds = 48 * 1024;
+template <bool FUSED>
+__global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, const h16* __restrict__ x) {
+  extern __shared__ __attribute__((aligned(16))) char dyn[];  // FUSED: [m][ld + 16]
+  __shared__ int part[kFewWaves][16][17];
+  __shared__ float ss[kFewRows];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ld = (g.k + 15) & ~15, lq = ld + 16;
+  if (FUSED) {
+    const bool whole = g.k % 8 == 0;
+    for (int r = wave; r < g.m; r += kFewWaves) {
+      const h16* xr = x + (int64_t)r * g.k;
+      uint32_t mag = 0;
+      for (int c = lane * 8; c < g.k; c += 512) mag = i8_mag8(i8_load8(xr + c, g.k - c, whole), mag);
+      mag = i8_wave_max(mag);
+      if (lane == 0) ss[r] = i8_scale(mag);
+      const float top = i8_top(mag);
+      const bool live = i8_live(mag);
+      for (int c = lane * 8; c < ld; c += 512)
+        *reinterpret_cast<uint2*>(dyn + r * lq + c) =
+            i8_pack(c < g.k ? i8_load8(xr + c, g.k - c, whole) : zero8(), top, live);
+    }
+    __syncthreads();
+  } else if (tid < g.m) {
+    ss[tid] = g.sa[tid];
+  }
+  const int n0 = blockIdx.x * 16;
+  const int row = lane & 15, kc = (lane >> 4) * 16;
+  const bool bin = n0 + row < g.n, ain = row < g.m;
+  const int8_t* bp = g.b + (int64_t)(n0 + row) * ld;
+  const intx4 zero = {0, 0, 0, 0};
+  intx4 acc = zero;
+  const int steps = (ld + 63) / 64, per = (steps + kFewWaves - 1) / kFewWaves;
+  const int s1 = std::min(steps, (wave + 1) * per);
+  constexpr int U = 4;
+  for (int s = wave * per; s < s1; s += U) {
+    intx4 fb[U], fa[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = (s + u) * 64 + kc;
+      fb[u] = s + u < s1 && bin && k < ld ? *reinterpret_cast<const intx4*>(bp + k) : zero;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = (s + u) * 64 + kc;
+      const bool in = s + u < s1 && ain && k < ld;
+      if (FUSED)
+        fa[u] = in ? *reinterpret_cast<const intx4*>(dyn + row * lq + k) : zero;
+      else
+        fa[u] = in ? *reinterpret_cast<const intx4*>(g.a + (int64_t)row * ld + k) : zero;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u], fa[u], acc, 0, 0, 0);
+  }
+  // lane: outputs 4 (lane / 16) + i of token lane % 16
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[wave][row][4 * (lane >> 4) + i] = acc[i];
+  __syncthreads();
+  if (tid < 256) {
+    const int q = tid >> 4, p = tid & 15;
+    if (q < g.m && n0 + p < g.n) {
+      int s = 0;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) s += part[w][q][p];
+      const bool has_bias = g.bias != nullptr;
+      g.y[(int64_t)q * g.n + n0 + p] =
+          i8_out(s, ss[q], g.sb[n0 + p], has_bias, has_bias ? to_f32(g.bias[n0 + p]) : 0.0f);
+    }
+  }
+}
+
+template <class C>
+hipError_t i8_launch(const I8Product& a, hipStream_t st) {
+  const int tp = ceil_div(a.n, C::BP), tq = ceil_div(a.m, C::BQ);
+  const int64_t n = (int64_t)tp * tq;
+  hipLaunchKernelGGL((i8_product<C>), dim3((unsigned)(8 * ((n + 7) / 8))), dim3(C::THREADS), 0, st,
+                     a, tp, tq);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_i8_rows(int rows, int cols, const h16* x, int8_t* q, float* scale,
+                          hipStream_t st) {
+  hipLaunchKernelGGL(i8_rows, dim3((unsigned)rows), dim3(256), 0, st, cols, (int)i8_row(cols), x, q,
+                     scale);
+  return hipGetLastError();
+}
+
+namespace {
+// rows of a range and how many ranges: at least 64 rows each, enough workgroups
+void i8_chunks(int rows, int cols, int* per, int* chunks) {
+  const int want = std::max(1, std::min(kColChunks, 1024 / std::max(1, ceil_div(cols, 256))));
+  *per = std::max(64, ceil_div(rows, want));
+  *chunks = ceil_div(rows, *per);
+}
+}  // namespace
+
+size_t i8_cols_ws_bytes(int rows, int cols) {
+  int per, chunks;
+  i8_chunks(rows, cols, &per, &chunks);
+  return (size_t)chunks * cols * 8;
+}
+
+hipError_t launch_i8_cols(int rows, int cols, const h16* x, int8_t* q, float* scale, h16* sum,
+                          void* ws, hipStream_t st) {
+  int per, chunks;
+  i8_chunks(rows, cols, &per, &chunks);
+  uint32_t* mag = static_cast<uint32_t*>(ws);
+  float* ps = reinterpret_cast<float*>(mag + (size_t)chunks * cols);
+  const int ld = (int)i8_row(rows);
+  hipLaunchKernelGGL(i8_cols_max, dim3((unsigned)ceil_div(cols, 256), (unsigned)chunks), dim3(256),
+                     0, st, rows, cols, per, x, mag, sum ? ps : nullptr);
+  hipLaunchKernelGGL(i8_cols_write, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(ld, 128)),
+                     dim3(256), 0, st, rows, cols, chunks, ld, x, mag, ps, q, scale, sum);
+  return hipGetLastError();
+}
+
+bool i8_fused_ok(int m, int n, int k) {
+  return m <= kFewRows && (int64_t)m * (i8_row(k) + 16) <= kFewLds;
+}
+
+hipError_t launch_i8_fused(const I8Product& a, const h16* x, hipStream_t st) {
+  const size_t lds = (size_t)a.m * (i8_row(a.k) + 16);
+  hipLaunchKernelGGL((i8_few<true>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), lds,
+                     st, a, x);
+  return hipGetLastError();
+}
+
+namespace {
+// The tile of a product: the largest that fills the CUs.
+int i8_tile(int m, int n) {
+  if (m <= kFewRows) return 0;
+  if ((int64_t)ceil_div(m, 256) * ceil_div(n, 256) >= 200) return 256;
+  return (int64_t)ceil_div(m, 128) * ceil_div(n, 128) >= 256 ? 128 : 64;
+}
+}  // namespace
+
+const char* i8_product_name(int m, int n, int k) {
+  (void)k;
+  switch (i8_tile(m, n)) {
+    case 0: return "few rows";
+    case 256: return "tile 256";
+    case 128: return "tile 128";
+    default: return "tile 64";
+  }
+}
+
+hipError_t launch_i8_product(const I8Product& a, hipStream_t st) {
+  switch (i8_tile(a.m, a.n)) {
+    case 0:
+      hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0,
+                         st, a, (const h16*)nullptr);
+      return hipGetLastError();
+    case 256: return i8_launch<Nt256>(a, st);
+    case 128: return i8_launch<Nt128>(a, st);
+    default: return i8_launch<Nt64>(a, st);
+  }
+}
+
+}  // namespace fp16k

@@ -1,0 +1,83 @@
+// Internal launch interface of the matrix-product operators beside the
+// convolutions: orthogonalised momentum (muon.hip) and 8-bit integer dense
+// layers (int8.hip).  Arguments have already been validated.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "common.hpp"
+
+namespace fp16k {
+
+// ---- orthogonalised momentum (muon.hip) --------------------------------------
+constexpr int kNsMaxJobs = 1024, kNsMaxSteps = 32, kNsMaxSide = 65536, kNsMaxShort = 16384;
+constexpr int kNsParts = 256;  // partial sums of a matrix's squares, at most
+
+// One matrix [rows][cols].  Workspace arrays are given in units of 256 bytes from
+// the workspace's start; "nat" holds X as the matrix is laid out, "mir" its
+// transpose, each padded with zeros to [rp][cp] ([cp][rp]); the operand of the
+// update that is not also its elementwise argument alternates between two.
+struct NsJob {
+  const h16* g;  // the gradient, or the matrix itself
+  h16* m;        // the momentum, or null
+  h16* w;        // the weights, or the result
+  float alpha;   // factor of the orthogonalised matrix
+  int rows, cols, rp, cp, tall;
+  uint32_t nat[2], mir[2], natl[2], mirl[2];  // X (high parts, low parts)
+  uint32_t a, al, b, bl;                      // A and B off the diagonal
+  uint32_t d, e;                              // their diagonals, float32
+  uint32_t part;                              // float64 partial sums
+  int nparts;
+  int t_sym, t_x, t_pre;  // first tile of this matrix in each kind of launch
+};
+
+struct NsPlan {
+  int tile;                    // 64, 128 or 256
+  int count;
+  int n_sym, n_x, n_pre;       // tiles of a symmetric product, of X', of the first pass
+  uint32_t table, map_sym, map_x, map_pre;  // in the workspace
+  size_t bytes;
+  int order[kNsMaxJobs];       // jobs[i] is the caller's matrix order[i]
+  NsJob jobs[kNsMaxJobs];
+};
+
+// Fills the plan's sizes, tiles and workspace places from rows[i], cols[i].
+void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, NsPlan* plan);
+
+struct NsArgs {
+  int steps, products;
+  const float* coef;  // [steps][3], host
+  float momentum, keep;
+  int nesterov;
+};
+hipError_t launch_ns(const NsPlan& plan, const NsArgs& a, void* ws, hipStream_t st);
+
+// ---- 8-bit integer dense layers (int8.hip) ------------------------------------
+constexpr int kI8MaxK = 131071;  // 32-bit sums of products of bytes: k * 2^14 < 2^31
+inline int64_t i8_row(int64_t n) { return (n + 15) & ~(int64_t)15; }  // bytes of a row
+
+// x [rows][cols] by rows: q [rows][i8_row(cols)] and scale [rows].
+hipError_t launch_i8_rows(int rows, int cols, const h16* x, int8_t* q, float* scale,
+                          hipStream_t st);
+// x [rows][cols] by columns: q [cols][i8_row(rows)] and scale [cols]; sum (nullable):
+// the columns' sums, rounded.  ws: i8_cols_ws_bytes.
+size_t i8_cols_ws_bytes(int rows, int cols);
+hipError_t launch_i8_cols(int rows, int cols, const h16* x, int8_t* q, float* scale, h16* sum,
+                          void* ws, hipStream_t st);
+// y [m][n] = rne16(sa sb (a b^T) + bias): a [m][i8_row(k)], b [n][i8_row(k)].
+struct I8Product {
+  int m, n, k;
+  const int8_t *a, *b;
+  const float *sa, *sb;
+  const h16* bias;
+  h16* y;
+};
+hipError_t launch_i8_product(const I8Product& a, hipStream_t st);
+const char* i8_product_name(int m, int n, int k);
+// Whether a product of few rows quantises its binary16 rows itself, and that call.
+bool i8_fused_ok(int m, int n, int k);
+hipError_t launch_i8_fused(const I8Product& a, const h16* x, hipStream_t st);
+
+}  // namespace fp16k

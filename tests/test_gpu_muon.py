@@ -1,0 +1,262 @@
+"""GPU parity of fp16_orthogonalize and fp16_muon_step against float64.
+
+Bars (2-norm, relative).  A step is X <- p(X) on the singular values with
+p(s) = as + bs^3 + cs^5, |p'| <= 3.9 up to s = 1.2, so an error entering at step k
+is multiplied by at most 3.9^(steps - k).
+  products = 3: operands carry 22 bits, an error of a few 2^-22 a step; five steps
+    give 2^-22 * 3 * (3.9^5 - 1) / 2.9 = 2.2e-4 at most; plus the rounding of the
+    result, 2^-11.
+  products = 1: A, B and X as operands are each rounded by up to 2^-11 in the last
+    step, and that is multiplied by at most 3.9: 3 * 3.9 * 2^-11 = 5.8e-3 (what
+    earlier steps leave is within that: X itself keeps 22 bits); plus 2^-11.
+"""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_1911_07384_amd as F
+from gpu_util import dev, host, note, require_gpu
+
+pytestmark = pytest.mark.gpu
+
+QUINTIC = (3.4445, -4.7750, 2.0315)
+BAR = {1: 3 * 3.9 * 2.0 ** -11 + 2.0 ** -11,
+       3: 2.0 ** -22 * 3 * (3.9 ** 5 - 1) / 2.9 + 2.0 ** -11}
+
+
+def matrix(rows, cols, seed, kind="noisy", scale=1e-3):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((rows, cols), generator=g, dtype=torch.float64)
+    if kind == "noisy":  # a few strong directions over noise, as gradients are
+        r = max(1, min(rows, cols) // 16)
+        u = torch.randn((rows, r), generator=g, dtype=torch.float64)
+        v = torch.randn((r, cols), generator=g, dtype=torch.float64)
+        x = 0.1 * x + (u * torch.logspace(0, -1, r, dtype=torch.float64)) @ v / math.sqrt(r)
+    return (x * scale).half()
+
+
+def ns64(u, steps=5, coef=None, scale=1.0):
+    """Newton-Schulz in float64 on the device (or 0 for a zero matrix)."""
+    x = u.double().cuda()
+    n = x.norm()
+    if n == 0:
+        return x
+    x = x / n
+    if x.shape[0] > x.shape[1]:
+        x = x.t().contiguous()
+    for s in range(steps):
+        a, b, c = QUINTIC if coef is None else coef[s] if isinstance(coef, list) else coef
+        p = x @ x.t()
+        x = a * x + (b * p + c * (p @ p)) @ x
+    return (x if u.shape[0] <= u.shape[1] else x.t()) * scale
+
+
+def off(got, ref):
+    n = ref.norm().item()
+    return (got.double() - ref).norm().item() / n if n else got.double().norm().item()
+
+
+def orth(xs, products, steps=5, coef=None, scales=None, ws=None, out=None):
+    require_gpu()
+    scales = scales or [1.0] * len(xs)
+    d = F.muon_descs([(x.shape[0], x.shape[1], s) for x, s in zip(xs, scales)])
+    X = [x.cuda() for x in xs]
+    Y = out or [torch.full_like(x, float("nan")) for x in X]
+    ws = F.workspace(F.fp16_muon_workspace_bytes(d, products)) if ws is None else ws
+    note(f"[gpu] orthogonalize {[tuple(x.shape) for x in xs][:6]} products={products}")
+    F.fp16_orthogonalize(d, X, Y, steps, coef, products, ws)
+    torch.cuda.synchronize()
+    return Y
+
+
+SHAPES = [(1, 1), (1, 7), (5, 1), (2, 2), (3, 3), (8, 8), (16, 200), (200, 16), (63, 65), (64, 64),
+          (65, 63), (64, 147), (147, 64), (64, 576), (129, 300), (256, 256), (300, 520), (1000, 257),
+          (257, 1000), (512, 512)]
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{s[0]}x{s[1]}")
+def test_shapes(shape, products):
+    x = matrix(*shape, seed=sum(shape))
+    y, = orth([x], products)
+    assert off(y, ns64(x)) <= BAR[products]
+
+
+# tile, matrices: the rule has to give each tile
+TILES = [(64, [(96, 700)]), (128, [(1500, 1024), (1024, 1024), (1000, 2048)] * 2),
+         (256, [(4096, 2304)])]
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("tile,shapes", TILES, ids=lambda t: str(t) if isinstance(t, int) else "")
+def test_every_tile(tile, shapes, products):
+    d = F.muon_descs(shapes)
+    assert F.fp16_muon_tile(d, products) == tile
+    xs = [matrix(*s, seed=i) for i, s in enumerate(shapes)]
+    for x, y in zip(xs, orth(xs, products)):
+        assert off(y, ns64(x)) <= BAR[products]
+    # transposed
+    if len(shapes) == 1:
+        x = xs[0].t().contiguous()
+        assert off(orth([x], products)[0], ns64(x)) <= BAR[products]
+
+
+@pytest.mark.parametrize("products", [1, 3])
+def test_many_matrices_at_once_as_one_by_one(products):
+    """1024 small matrices and a large one among them; each within the bar."""
+    shapes = [(1 + (7 * i) % 40, 1 + (13 * i) % 50) for i in range(1023)] + [(200, 300)]
+    xs = [matrix(*s, seed=i, kind="normal") for i, s in enumerate(shapes)]
+    ys = orth(xs, products)
+    for i, (x, y) in enumerate(zip(xs, ys)):
+        if i % 31 == 0 or i >= 1020:
+            assert off(y, ns64(x)) <= BAR[products], shapes[i]
+        assert torch.isfinite(y).all(), shapes[i]
+
+
+def test_steps_and_coefficients():
+    x = matrix(100, 160, 3)
+    cubic = [(1.5, -0.5, 0.0)] * 8
+    mixed = [(3.0, -3.2, 1.2), (2.5, -2.0, 0.5), (1.875, -1.25, 0.375)]
+    for steps, coef in [(1, None), (2, QUINTIC), (8, cubic), (3, mixed)]:
+        y, = orth([x], 3, steps, coef)
+        assert off(y, ns64(x, steps, coef)) <= BAR[3], (steps, coef)
+
+
+def test_scale_and_size_of_the_input():
+    """The result does not depend on the input's size, down to subnormal entries."""
+    for scale in (3e4, 1.0, 2.0 ** -20):
+        x = matrix(48, 80, 5, "normal", scale)
+        x = x.clamp(-65504, 65504)
+        y, = orth([x], 3, scales=[0.25])
+        assert off(y, ns64(x, scale=0.25)) <= BAR[3], scale
+    one = torch.zeros((3, 5), dtype=torch.float16)
+    one[1, 2] = 2.0 ** -24
+    y, = orth([one], 3)
+    assert off(y, ns64(one)) <= BAR[3]
+
+
+def test_zero_and_not_finite():
+    z = torch.zeros((70, 90), dtype=torch.float16)
+    rows = matrix(70, 90, 1)
+    rows[10:60] = 0
+    cols = matrix(70, 90, 2)
+    cols[:, 3:] = 0
+    nan, inf = matrix(70, 90, 3), matrix(70, 90, 4)
+    nan[4, 5] = float("nan")
+    inf[69, 89] = float("-inf")
+    for products in (1, 3):
+        y = orth([z, rows, nan, cols, inf, rows], products)
+        assert (y[0] == 0).all()
+        assert (y[1][10:60] == 0).all() and off(y[1], ns64(rows)) <= BAR[products]
+        assert (y[3][:, 3:] == 0).all() and off(y[3], ns64(cols)) <= BAR[products]
+        assert torch.isnan(y[2]).all() and torch.isnan(y[4]).all()
+        assert torch.equal(y[5], y[1])
+
+
+def test_in_place_and_nothing_else_written():
+    x = matrix(37, 41, 7)
+    ref = ns64(x)
+    n = x.numel()
+    buf = torch.full((n + 64,), 3.0, dtype=torch.float16, device="cuda")
+    v = buf[8:8 + n].view(37, 41)
+    v.copy_(x)
+    d = F.muon_descs([(37, 41)])
+    need = F.fp16_muon_workspace_bytes(d, 3)
+    ws = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    F.fp16_orthogonalize(d, [v], [v], products=3, ws=ws, ws_bytes=need)
+    torch.cuda.synchronize()
+    assert off(v, ref) <= BAR[3]
+    assert (buf[:8] == 3).all() and (buf[8 + n:] == 3).all() and (ws[need:] == 0xA5).all()
+
+
+def test_same_bits_again_and_on_another_stream():
+    xs = [matrix(300, 200, 1), matrix(64, 576, 2)]
+    a, b = orth(xs, 1), orth(xs, 1)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        c = orth(xs, 1)
+    for x, y, z in zip(a, b, c):
+        assert torch.equal(x, y) and torch.equal(x, z)
+
+
+# ---- the update --------------------------------------------------------------------
+
+def step(ws_, gs, ms, scales, lr, mu, wd, nesterov, products, steps=5):
+    require_gpu()
+    d = F.muon_descs([(w.shape[0], w.shape[1], s) for w, s in zip(ws_, scales)])
+    work = F.workspace(F.fp16_muon_workspace_bytes(d, products))
+    note(f"[gpu] muon {[tuple(w.shape) for w in ws_][:6]} products={products}")
+    F.fp16_muon_step(d, ws_, gs, ms, lr, mu, wd, nesterov, steps, None, products, work)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("products", [1, 3])
+def test_update(products, nesterov):
+    """Momentum bit for bit; the weights from the float64 direction: the update's
+    relative error as above, one rounding of w and float32's of the rest."""
+    shapes, scales = [(64, 147), (200, 72), (33, 130)], [1.0, 1.5, 0.7]
+    lr, mu, wd = 0.02, 0.95, 0.1
+    g = [matrix(*s, seed=10 + i) for i, s in enumerate(shapes)]
+    m = [matrix(*s, seed=20 + i) for i, s in enumerate(shapes)]
+    w = [matrix(*s, seed=30 + i, kind="normal", scale=0.1) for i, s in enumerate(shapes)]
+    W, G, M = ([t.cuda() for t in l] for l in (w, g, m))
+    for _ in range(2):  # the second update starts from the first's results
+        w0, m0 = [t.cpu() for t in W], [t.cpu() for t in M]
+        step(W, G, M, scales, lr, mu, wd, nesterov, products)
+        for i in range(len(shapes)):
+            _, mr = oracle.sgd_f32(np.zeros(g[i].numel(), np.float16), g[i].numpy().ravel(),
+                                   m0[i].numpy().ravel(), 0.1, mu, 0.0)
+            assert np.array_equal(host(M[i]).ravel().view(np.uint16), mr.view(np.uint16))
+            md = torch.from_numpy(mr).view(*shapes[i]).double()
+            o = ns64(g[i].double() + float(np.float32(mu)) * md if nesterov else md)
+            upd = lr * scales[i] * o
+            ref = (1 - lr * wd) * w0[i].double().cuda() - upd
+            err = (W[i].double() - ref).norm().item()
+            bar = BAR[products] * upd.norm().item() + (2.0 ** -11 + 2.0 ** -20) * ref.norm().item()
+            assert err <= bar + 2.0 ** -25 * math.sqrt(ref.numel())
+
+
+def test_update_alone():
+    """From zero weights, without decay: w = -lr scale O, held to O's bar."""
+    for shape in [(64, 576), (300, 520), (1000, 257)]:
+        g = matrix(*shape, seed=4)
+        W, M = (torch.zeros(shape, dtype=torch.float16, device="cuda") for _ in range(2))
+        step([W], [g.cuda()], [M], [2.0], 0.5, 0.9, 0.0, True, 1)
+        assert torch.equal(M.cpu(), g)
+        assert off(W, -ns64(g)) <= BAR[1]
+
+
+def test_update_in_a_graph():
+    """Captured once, replayed with eager work between the replays: each replay as
+    the eager update from the same state."""
+    require_gpu()
+    shapes = [(64, 147), (256, 128), (40, 700)]
+    d = F.muon_descs([(*s, 1.0) for s in shapes])
+    mk = lambda o, sc: [matrix(*s, seed=o + i, scale=sc).cuda() for i, s in enumerate(shapes)]
+    W, G, M = mk(1, 0.1), mk(2, 1e-3), mk(3, 1e-3)
+    ws = F.workspace(F.fp16_muon_workspace_bytes(d, 1))
+    We, Me = [t.clone() for t in W], [t.clone() for t in M]
+    run = lambda a, b: F.fp16_muon_step(d, a, G, b, 0.02, 0.95, 0.01, ws=ws)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run([t.clone() for t in W], [t.clone() for t in M])
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(W, M)
+    for i in range(4):
+        G[i % 3].mul_(1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        run(We, Me)
+        torch.cuda.synchronize()
+        for a, b in zip(W + M, We + Me):
+            assert torch.equal(a, b), i
