@@ -485,7 +485,9 @@ const char* fp16_conv_kernel(const fp16_conv_desc* desc, int32_t pass, int32_t f
 
 /* One matrix, row-major and contiguous, 1 <= rows, cols <= 65536, the shorter
  * side at most 16384 and rows * cols < 2^30.  scale multiplies its
- * orthogonalised update (finite): often sqrt(max(1, rows / cols)). */
+ * orthogonalised update (finite): often sqrt(max(1, rows / cols)).  Matrices need
+ * the alignment of an element only (views into a flat parameter buffer); where they
+ * are 16-byte aligned and cols is a multiple of 8 they move 16 bytes at a time. */
 typedef struct {
   int32_t rows, cols;
   float scale;
@@ -499,9 +501,10 @@ typedef struct {
  * matrices with this many products (see there); 0 for an invalid list. */
 size_t fp16_muon_workspace_bytes(int32_t count, const fp16_muon_desc* descs, int32_t products);
 
-/* Side of the tiles the products of such a call run on (256, 128 or 64), for
- * tests and profiles; 0 for an invalid list. */
-int32_t fp16_muon_tile(int32_t count, const fp16_muon_desc* descs, int32_t products);
+/* Sides of the tiles that A, B and X of such a call run on, e.g. "192, 192, 256"
+ * (" split": the reduction split within a workgroup), for tests and profiles; ""
+ * for an invalid list.  No contract; valid until the thread's next call. */
+const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_t products);
 
 /* Orthogonalisation by Newton-Schulz products, of `count` matrices at once
  * (host arrays, read during the call only):

@@ -37,7 +37,7 @@ EXPORTS = ["fp16_conv_out_dims", "fp16_conv_workspace_bytes", "fp16_conv_fwd", "
            "fp16_conv_dgrad_wf", "fp16_conv_kernel", "fp16_noalloc_scratch_bytes", "fp16_conv_wgrad_noalloc",
            "fp16_bn_mask_bytes", "fp16_bn_relu_m", "fp16_bn_relu_bwd_m", "fp16_conv_bn_relu_fwd_m",
            "fp16_conv_dgrad_wf_m", "fp16_bn_relu_maxpool", "fp16_conv_wgrad_ex",
-           "fp16_conv_dgrad_wf_ex", "fp16_muon_workspace_bytes", "fp16_muon_tile", "fp16_orthogonalize",
+           "fp16_conv_dgrad_wf_ex", "fp16_muon_workspace_bytes", "fp16_muon_kernels", "fp16_orthogonalize",
            "fp16_muon_step", "fp16_int8_row_bytes", "fp16_int8_quant_rows",
            "fp16_int8_quant_workspace_bytes", "fp16_int8_quant_cols", "fp16_int8_matmul",
            "fp16_int8_kernel", "fp16_int8_dense_workspace_bytes", "fp16_int8_dense_weights",
@@ -117,7 +117,7 @@ _SIGS = {
     "fp16_conv_bn_relu_fwd": (ctypes.c_int, [_P] * 11 + [_SZ, _P]),
     "fp16_conv_kernel": (ctypes.c_char_p, [_P, _I32, _I32]),
     "fp16_muon_workspace_bytes": (_SZ, [_I32, _P, _I32]),
-    "fp16_muon_tile": (_I32, [_I32, _P, _I32]),
+    "fp16_muon_kernels": (ctypes.c_char_p, [_I32, _P, _I32]),
     "fp16_orthogonalize": (ctypes.c_int, [_I32, _P, _P, _P, _I32, _P, _I32, _P, _SZ, _P]),
     "fp16_muon_step": (ctypes.c_int, [_I32, _P, _P, _P, _P, _F, _F, _F, _I32, _I32, _P, _I32, _P,
                                       _SZ, _P]),
@@ -485,9 +485,9 @@ def fp16_muon_workspace_bytes(descs, products=1) -> int:
     return int(lib().fp16_muon_workspace_bytes(len(descs), descs, int(products)))
 
 
-def fp16_muon_tile(descs, products=1) -> int:
-    """The side of the tiles the products run on (for tests and profiles)."""
-    return int(lib().fp16_muon_tile(len(descs), descs, int(products)))
+def fp16_muon_kernels(descs, products=1) -> str:
+    """The tiles that the products run on (for tests and profiles)."""
+    return lib().fp16_muon_kernels(len(descs), descs, int(products)).decode()
 
 
 def fp16_orthogonalize(descs, xs, ys, steps=5, coef=None, products=3, ws=None, ws_bytes=None,

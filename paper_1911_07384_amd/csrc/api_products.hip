@@ -7,6 +7,7 @@
 #include "products.hpp"
 
 #include <math.h>
+#include <stdio.h>
 
 #include <algorithm>
 
@@ -37,12 +38,10 @@ void ns_make_plan(int32_t count, const fp16_muon_desc* d, int32_t products, NsPl
   ns_plan(count, rows, cols, products, plan);
 }
 
-// Buffers of one call: a written one may overlap no other, except where both are
-// the same matrix's in and out.
+// Buffers of one call: a written one may overlap no other.
 struct Span {
   uintptr_t at;
   size_t bytes;
-  int owner;  // of the matrix, for a result that may be its input
   bool written;
 };
 bool spans_clash(Span* s, int n) {
@@ -75,7 +74,7 @@ fp16_status ns_call(int32_t count, const fp16_muon_desc* descs, fp16_t* const* w
   }
   for (int i = 0; i < count; ++i) {
     if (!w[i] || !g[i] || (update && !m[i])) return FP16_ERR_NULL;
-    if (!aligned16(w[i]) || !aligned16(g[i]) || (update && !aligned16(m[i])))
+    if (((uintptr_t)w[i] | (uintptr_t)g[i] | (update ? (uintptr_t)m[i] : 0)) & 1u)
       return FP16_ERR_MISALIGNED;
   }
   NsPlan plan;
@@ -86,17 +85,19 @@ fp16_status ns_call(int32_t count, const fp16_muon_desc* descs, fp16_t* const* w
   int n = 0;
   for (int i = 0; i < count; ++i) {
     const size_t b = (size_t)descs[i].rows * descs[i].cols * 2;
-    spans[n++] = {(uintptr_t)w[i], b, i, true};
-    if (update) spans[n++] = {(uintptr_t)m[i], b, i, true};
-    if (update || w[i] != g[i]) spans[n++] = {(uintptr_t)g[i], b, i, false};
+    spans[n++] = {(uintptr_t)w[i], b, true};
+    if (update) spans[n++] = {(uintptr_t)m[i], b, true};
+    if (update || w[i] != g[i]) spans[n++] = {(uintptr_t)g[i], b, false};
   }
-  spans[n++] = {(uintptr_t)ws, plan.bytes, -1, true};
+  spans[n++] = {(uintptr_t)ws, plan.bytes, true};
   if (spans_clash(spans, n)) return FP16_ERR_ALIASING;
   for (int i = 0; i < count; ++i) {
     const int o = plan.order[i];
     plan.jobs[i].g = reinterpret_cast<const h16*>(g[o]);
     plan.jobs[i].w = reinterpret_cast<h16*>(w[o]);
     plan.jobs[i].m = update ? reinterpret_cast<h16*>(m[o]) : nullptr;
+    plan.jobs[i].aligned = aligned16(w[o]) && aligned16(g[o]) && (!update || aligned16(m[o]));
+    plan.jobs[i].whole = plan.jobs[i].aligned && descs[o].cols % 8 == 0;
     plan.jobs[i].alpha = update ? lr * descs[o].scale : descs[o].scale;
   }
   NsArgs a;
@@ -197,11 +198,16 @@ size_t fp16_muon_workspace_bytes(int32_t count, const fp16_muon_desc* descs, int
   return plan.bytes;
 }
 
-int32_t fp16_muon_tile(int32_t count, const fp16_muon_desc* descs, int32_t products) {
-  if (!ns_list_ok(count, descs, products)) return 0;
+const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_t products) {
+  thread_local char name[64];
+  if (!ns_list_ok(count, descs, products)) return "";
   NsPlan plan;
   ns_make_plan(count, descs, products, &plan);
-  return plan.tile;
+  char* at = name;
+  for (const NsTile& k : plan.kind)
+    at += snprintf(at, sizeof(name) - (size_t)(at - name), "%s%d%s", at == name ? "" : ", ", k.tile,
+                   k.groups > 1 ? " split" : "");
+  return name;
 }
 
 fp16_status fp16_orthogonalize(int32_t count, const fp16_muon_desc* descs, const fp16_t* const* x,

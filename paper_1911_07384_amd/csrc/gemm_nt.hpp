@@ -5,8 +5,9 @@
 // same way: a lane's fragment is 16 bytes of one row (8 halves or 16 integers),
 // a slice of the reduction is 128 bytes of every row.
 //
-// A workgroup of WP x WQ waves owns BP x BQ outputs, each wave TP x TQ tiles of
-// 32 x 32.  The slices go through S stages of LDS, loaded past the registers
+// A workgroup owns BP x BQ outputs, WP x WQ waves TP x TQ tiles of 32 x 32 each; KG
+// such groups split the reduction where few tiles have a long one, and add up in
+// LDS.  The slices go through S stages of LDS, loaded past the registers
 // (8 rows of one slice, 1 KB, an instruction and wave) S - 1 slices ahead and a
 // few between the products of every sub-step, one barrier a slice.  Rows of LDS
 // are whole 128-byte lines; the 16-byte chunk c of row r lies at c ^ ((r/2) % 8),
@@ -40,15 +41,18 @@ struct NtByte {  // 8-bit integers, 32-bit sums (exact below 2^31)
   }
 };
 
-template <int WP_, int WQ_, int TP_, int TQ_, int S_, int OCC_>
+template <int WP_, int WQ_, int TP_, int TQ_, int S_, int KG_, int OCC_>
 struct NtCfg {
-  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, S = S_, OCC = OCC_;
-  static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES;
+  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, S = S_, KG = KG_, OCC = OCC_;
+  static constexpr int WAVES = WP * WQ;            // of one group
+  static constexpr int THREADS = 64 * WAVES * KG;
   static constexpr int BP = 32 * TP * WP, BQ = 32 * TQ * WQ;
   static constexpr int IP = BP / (8 * WAVES), IQ = BQ / (8 * WAVES);  // loads a wave and slice
-  static constexpr int STAGE = (BP + BQ) * 128, LDS = S * STAGE;
+  static constexpr int STAGE = (BP + BQ) * 128, RING = S * STAGE;
+  static constexpr int LDS = KG * RING;
+  static constexpr int SUM = 1024 * TP * TQ * 4 * WAVES;  // one group's sums
   static_assert(IP % 2 == 0 && IQ % 2 == 0, "the chunk order goes by pairs of loads");
-  static_assert(LDS * OCC <= 160 * 1024, "LDS");
+  static_assert(LDS * OCC <= 160 * 1024 && (KG - 1) * SUM <= LDS, "LDS");
 };
 
 // One 16-byte-per-lane load from a buffer resource into LDS (1 KB a wave).
@@ -74,15 +78,17 @@ struct NtTile {
 };
 
 template <class T, class C, int NSEG>
-__device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
+__device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
                                            typename T::Acc (&acc)[C::TP][C::TQ]) {
   typedef typename T::Frag Frag;
   constexpr int TP = C::TP, TQ = C::TQ, S = C::S, IP = C::IP, IQ = C::IQ, I = IP + IQ;
   constexpr uint32_t OOB = 0x80000000u;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = all % C::WAVES, grp = all / C::WAVES;
   const int wp = wave / C::WQ, wq = wave % C::WQ;
   const int lrow = lane & 31, lhi = lane >> 5;
+  char* const lds = lds0 + grp * C::RING;
 
   // loads: instruction i of a wave takes rows 8 * (wave * I. + i) .. + 7, lane l
   // row l / 8 of them and the chunk that lies at l % 8 of that row
@@ -96,12 +102,31 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
     pv[h] = (uint32_t)(wave * IP * 8 + (lane >> 3)) * t.ldp + (uint32_t)ck[h];
     qv[h] = (uint32_t)(wave * IQ * 8 + (lane >> 3)) * t.ldq + (uint32_t)ck[h];
   }
+  // the slices of all pairs in order, a range of them for each group
+  const int per1 = (t.kbytes + 127) / 128;  // of one pair
+  const int KT = (NSEG * per1 + C::KG - 1) / C::KG;
   int k0 = 0, seg = 0;  // the slice loaded next
+  int left = KT;        // and how many there are from it
+  if (C::KG > 1) {
+    const int s0 = grp * KT;
+    seg = s0 / per1;
+    k0 = (s0 - seg * per1) * 128;
+    left = NSEG * per1 - s0 < KT ? NSEG * per1 - s0 : KT;
+  }
   const void *pp = t.p[0], *qp = t.q[0];
+  auto pair = [&]() {
+#pragma unroll
+    for (int s = 1; s < NSEG; ++s)
+      if (seg == s) {
+        pp = t.p[s];
+        qp = t.q[s];
+      }
+  };
+  if (C::KG > 1) pair();
   bool in[2];
   auto begin = [&]() {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) in[h] = k0 + ck[h] < t.kbytes;
+    for (int h = 0; h < 2; ++h) in[h] = k0 + ck[h] < t.kbytes && (C::KG == 1 || left > 0);
   };
   auto load = [&](char* buf, int i) {
     if (i < IP) {
@@ -116,15 +141,11 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
   };
   auto advance = [&]() {
     k0 += 128;
+    --left;
     if (NSEG > 1 && k0 >= t.kbytes && seg + 1 < NSEG) {
       k0 = 0;
       ++seg;
-#pragma unroll
-      for (int s = 1; s < NSEG; ++s)
-        if (seg == s) {
-          pp = t.p[s];
-          qp = t.q[s];
-        }
+      pair();
     }
   };
 
@@ -146,14 +167,33 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
     for (int a = 0; a < TP; ++a)
       p[a] = *reinterpret_cast<const Frag*>(buf + ((wp * TP + a) * 32 + lrow) * 128 + pos);
   };
-  auto mma = [&](const Frag (&p)[TP], const Frag (&q)[TQ]) {
+  // One sub-step: the products of one set of fragments, between them the reads of
+  // the next set (sub-step ks of `from`) and loads L0 .. L1 - 1 into `to`, an
+  // instruction or two after each product (kept there by the scheduling barriers;
+  // left to itself the compiler issues them in bursts that hold the products up).
+  auto substep = [&](const Frag (&p)[TP], const Frag (&q)[TQ], const char* from, int ks,
+                     Frag (&np)[TP], Frag (&nq)[TQ], char* to, auto l0, auto l1) {
+    constexpr int M = TP * TQ, R = TP + TQ, L0 = decltype(l0)::value, V = decltype(l1)::value - L0;
+    const int pos = ((ks * 2 + lhi) ^ swz) * 16;
 #pragma unroll
-    for (int a = 0; a < TP; ++a)
+    for (int i = 0; i < M; ++i) {
+      const int a = i / TQ, b = i % TQ;
+      acc[a][b] = T::mma(p[a], q[b], acc[a][b]);
 #pragma unroll
-      for (int b = 0; b < TQ; ++b) acc[a][b] = T::mma(p[a], q[b], acc[a][b]);
+      for (int r = R * i / M; r < R * (i + 1) / M; ++r) {
+        if (r < TQ)
+          nq[r < TQ ? r : 0] = *reinterpret_cast<const Frag*>(
+              from + C::BP * 128 + ((wq * TQ + r) * 32 + lrow) * 128 + pos);
+        else
+          np[r < TQ ? 0 : r - TQ] = *reinterpret_cast<const Frag*>(
+              from + ((wp * TP + r - TQ) * 32 + lrow) * 128 + pos);
+      }
+#pragma unroll
+      for (int v = V * i / M; v < V * (i + 1) / M; ++v) load(to, L0 + v);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
-  const int KT = NSEG * ((t.kbytes + 127) / 128);
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) {
     begin();
@@ -172,56 +212,45 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
   for (int kt = 0; kt < KT; ++kt) {
     const char* cur = lds + rd * C::STAGE;
     char* nxt = lds + wr * C::STAGE;
-    constexpr int Q1 = (I + 2) / 3, Q2 = 2 * Q1 < I ? 2 * Q1 : I;
+    constexpr std::integral_constant<int, 0> L0{};
+    constexpr std::integral_constant<int, (I + 1) / 2> L1{};
+    constexpr std::integral_constant<int, I> L2{};
     begin();
-    fetch(cur, 1, fp[1], fq[1]);
-#pragma unroll
-    for (int i = 0; i < Q1; ++i) load(nxt, i);
-    mma(fp[0], fq[0]);
-    __builtin_amdgcn_sched_barrier(0);
-    fetch(cur, 2, fp[0], fq[0]);
-#pragma unroll
-    for (int i = Q1; i < Q2; ++i) load(nxt, i);
-    mma(fp[1], fq[1]);
-    __builtin_amdgcn_sched_barrier(0);
-    fetch(cur, 3, fp[1], fq[1]);
-#pragma unroll
-    for (int i = Q2; i < I; ++i) load(nxt, i);
-    mma(fp[0], fq[0]);
+    substep(fp[0], fq[0], cur, 1, fp[1], fq[1], nxt, L0, L1);
+    substep(fp[1], fq[1], cur, 2, fp[0], fq[0], nxt, L1, L2);
     advance();
-    __builtin_amdgcn_sched_barrier(0);
+    substep(fp[0], fq[0], cur, 3, fp[1], fq[1], nxt, L2, L2);
     // this wave's reads of the stage are complete and its part of the next one
     // has landed: publish it, and free this stage
     __builtin_amdgcn_s_waitcnt(WAIT);
     nt_barrier();
     rd = rd + 1 == S ? 0 : rd + 1;
     wr = wr + 1 == S ? 0 : wr + 1;
-    fetch(lds + rd * C::STAGE, 0, fp[0], fq[0]);
-    mma(fp[1], fq[1]);
-    __builtin_amdgcn_sched_barrier(0);
+    substep(fp[1], fq[1], lds + rd * C::STAGE, 0, fp[0], fq[0], nxt, L2, L2);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // every load has landed and every read is done: LDS is free
-}
-
-// A wave's 32 x 32 tile as the products leave it has rows p = 8 (e/4) + 4 (l/32)
-// + e%4 of column q = l % 32 in lane l; afterwards v[8h + i] is row 16h + 8 (l/32)
-// + i of that column: runs of 8.
-template <class Acc>
-__device__ __forceinline__ void nt_rows(const Acc& acc, unsigned (&v)[16]) {
+  if (C::KG > 1) {
+    // the groups' sums into the first one's, in order
+    typedef typename T::Acc Acc;
+    Acc* sums = reinterpret_cast<Acc*>(lds0);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const auto x = acc[e];  // (a bit cast of a vector's element itself takes element 0)
-    v[e] = __builtin_bit_cast(unsigned, x);
-  }
+    for (int a = 0; a < TP; ++a)
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+      for (int b = 0; b < TQ; ++b)
+        if (grp > 0) sums[(((grp - 1) * C::WAVES + wave) * TP * TQ + a * TQ + b) * 64 + lane] = acc[a][b];
+    __syncthreads();
+    if (grp == 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const auto r = __builtin_amdgcn_permlane32_swap(v[8 * h + i], v[8 * h + 4 + i], false, false);
-      v[8 * h + i] = (unsigned)r[0];
-      v[8 * h + 4 + i] = (unsigned)r[1];
+      for (int g = 1; g < C::KG; ++g)
+#pragma unroll
+        for (int a = 0; a < TP; ++a)
+#pragma unroll
+          for (int b = 0; b < TQ; ++b)
+            acc[a][b] += sums[(((g - 1) * C::WAVES + wave) * TP * TQ + a * TQ + b) * 64 + lane];
     }
+    __syncthreads();
+  }
 }
 
 // Workgroup b of a grid of 8 * ceil(n / 8): the workgroups that one XCD takes
@@ -236,8 +265,99 @@ __device__ __forceinline__ void nt_wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-typedef NtCfg<2, 2, 4, 4, 2, 1> Nt256;  // 256 x 256
-typedef NtCfg<2, 2, 2, 2, 2, 2> Nt128;  // 128 x 128
-typedef NtCfg<2, 2, 1, 1, 3, 3> Nt64;   // 64 x 64
+// A wave's outputs to memory, 32 columns q of its 32 TP rows p at a time.  The
+// products leave rows p = 8 (e/4) + 4 (l/32) + e%4 of column q = l%32 in lane l, so
+// that memory would see runs of 32 bytes; through LDS each lane gets 8 consecutive
+// p of one q and 4 TP lanes a whole run of 32 TP:
+//   epi.apply(b, i, p, q, v, out)  v[8] the sums of block b, pass i = 0 .. 2 TP - 1;
+//                                  stores there what goes out[q][p ..], and sets
+//                                  out[PARTS] for `mirror`
+//   epi.load(b, i, p, q)           the same one block ahead: reads what apply needs
+// With `mirror`, out is also stored transposed, mir[s][p * ldm + q] (its 16-byte
+// chunks in LDS exclusive-ored with the row, since the writes step 8 rows a lane).  Blocks of 32
+// rows or columns past plim, qlim are left out (apply and load guard within them).
+template <class C, int PARTS>
+struct NtEpi {
+  static constexpr int TP = C::TP, TQ = C::TQ;
+  static constexpr int GB = TQ % 2 == 0 && PARTS == 1 ? 2 : 1;  // blocks a mirrored run
+  static constexpr int FLD = 32 * TP + 4, MLD = 32 * GB + 8;    // floats, halves
+  static constexpr int WAVE = 32 * FLD * 4 + PARTS * 32 * TP * MLD * 2;
+  static constexpr int LDS = WAVE * C::WAVES > C::LDS ? WAVE * C::WAVES : C::LDS;
+  static_assert(LDS * C::OCC <= 160 * 1024, "LDS");
+};
+
+template <class C, int PARTS, class Acc, class Epi>
+__device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* lds, int p0, int q0,
+                                         int plim, int qlim, bool mirror, h16* const (&mir)[PARTS],
+                                         int ldm, Epi& epi) {
+  typedef NtEpi<C, PARTS> E;
+  constexpr int TP = E::TP, TQ = E::TQ, GB = E::GB, FLD = E::FLD, MLD = E::MLD;
+  constexpr int CPR = 4 * TP, IT = 2 * TP;  // chunks of a run, passes of a block
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lrow = lane & 31, lhi = lane >> 5;
+  typedef decltype(acc[0][0][0] + 0) V;
+  V* const f = reinterpret_cast<V*>(lds + wave * E::WAVE);
+  h16* const m = reinterpret_cast<h16*>(f + 32 * FLD);
+  auto load = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int r = (i * 64 + lane) / CPR, c = (i * 64 + lane) % CPR;
+      if (b < TQ) epi.load(b, i, p0 + 8 * c, q0 + 32 * b + r);
+    }
+  };
+  load(0);
+#pragma unroll
+  for (int b = 0; b < TQ; ++b) {
+    load(b + 1);
+#pragma unroll
+    for (int a = 0; a < TP; ++a)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        typedef V V4 __attribute__((ext_vector_type(4)));
+        const V4 v = {acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2],
+                      acc[a][b][4 * e + 3]};
+        *reinterpret_cast<V4*>(f + lrow * FLD + 32 * a + 8 * e + 4 * lhi) = v;
+      }
+    nt_wave_sync();
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int r = (i * 64 + lane) / CPR, c = (i * 64 + lane) % CPR;
+      V v[8];
+      __builtin_memcpy(v, f + r * FLD + 8 * c, 32);
+      V8 out[PARTS];
+      epi.apply(b, i, p0 + 8 * c, q0 + 32 * b + r, v, out);
+      if (mirror) {
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            m[s * 32 * TP * MLD + (8 * c + e) * MLD + (((4 * (b % GB) + r / 8) ^ ((c >> 1) & (4 * GB - 1))) * 8) +
+              r % 8] = out[s].h[e];
+      }
+    }
+    nt_wave_sync();
+    if (mirror && b % GB == GB - 1) {
+      constexpr int MC = 4 * GB;  // chunks of a mirrored run
+#pragma unroll
+      for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+        for (int i = 0; i < 32 * TP * MC / 64; ++i) {
+          const int r = (i * 64 + lane) / MC, c = (i * 64 + lane) % MC;
+          const int q = q0 + 32 * (b - GB + 1) + 8 * c;
+          if (p0 + r < plim && q < qlim)
+            store16(mir[s] + (int64_t)(p0 + r) * ldm + q,
+                    load16(m + s * 32 * TP * MLD + r * MLD + 8 * (c ^ ((r >> 4) & (4 * GB - 1)))));
+        }
+      nt_wave_sync();
+    }
+  }
+}
+
+//             waves  tile  stages  groups  workgroups a CU
+typedef NtCfg<2, 2, 4, 4, 2, 1, 1> Nt256;   // 256 x 256
+typedef NtCfg<2, 2, 3, 3, 3, 1, 1> Nt192;   // 192 x 192
+typedef NtCfg<2, 2, 2, 2, 2, 1, 2> Nt128;   // 128 x 128
+typedef NtCfg<2, 2, 1, 1, 3, 1, 3> Nt64;    // 64 x 64
+typedef NtCfg<2, 2, 1, 1, 2, 4, 1> Nt64k;   // 64 x 64, the reduction split in four
 
 }  // namespace fp16k

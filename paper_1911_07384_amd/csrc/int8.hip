@@ -224,11 +224,44 @@ __device__ __forceinline__ h16 i8_out(int acc, float sa, float sb, bool has_bias
   return to_h16(has_bias ? v + bias : v);
 }
 
-// Tile rows p are rows of b (outputs), q rows of a (tokens): a lane's runs of 8 lie
-// along a row of y.
+// What a tile stores, see nt_store: p along a row of y.
+template <class C>
+struct I8Epi {
+  const I8Product& g;
+  bool whole, has_bias;
+  float sq[2][2 * C::TP], sp[2 * C::TP][8], bp[2 * C::TP][8];
+
+  __device__ __forceinline__ void load(int b, int i, int p, int q) {
+    if (p >= g.n) return;
+    if (q < g.m) sq[b & 1][i] = g.sa[q];
+    if (b > 0) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool in = p + k < g.n;
+      sp[i][k] = in ? g.sb[p + k] : 0.0f;
+      bp[i][k] = in && has_bias ? to_f32(g.bias[p + k]) : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void apply(int b, int i, int p, int q, const int (&v)[8], V8 (&)[1]) {
+    if (p >= g.n || q >= g.m) return;
+    V8 o;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o.h[k] = i8_out(v[k], sq[b & 1][i], sp[i][k], has_bias, bp[i][k]);
+    h16* yp = g.y + (int64_t)q * g.n + p;
+    if (whole) {
+      store16(yp, o);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (p + k < g.n) yp[k] = o.h[k];
+    }
+  }
+};
+
+// Tile rows p are rows of b (outputs), q rows of a (tokens).
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product g, int tp, int tq) {
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, 1>::LDS];
   const int t = nt_xcd(blockIdx.x, tp * tq);
   if (t >= tp * tq) return;
   const int gr = t / (4 * tq), w = t - gr * 4 * tq;
@@ -243,42 +276,12 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
   nt.kbytes = g.k;
   intx16 acc[C::TP][C::TQ];
   nt_product<NtByte, C, 1>(nt, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int lrow = lane & 31, lhi = lane >> 5;
-  const int p0 = pt + (wave / C::WQ) * 32 * C::TP, q0 = qt + (wave % C::WQ) * 32 * C::TQ;
-  const bool whole = g.n % 8 == 0, has_bias = g.bias != nullptr;
-#pragma unroll
-  for (int a = 0; a < C::TP; ++a)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int p = p0 + 32 * a + 16 * h + 8 * lhi;
-      float sp[8], bp[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool in = p + e < g.n;
-        sp[e] = in ? g.sb[p + e] : 0.0f;
-        bp[e] = in && has_bias ? to_f32(g.bias[p + e]) : 0.0f;
-      }
-#pragma unroll
-      for (int b = 0; b < C::TQ; ++b) {
-        const int q = q0 + 32 * b + lrow;
-        unsigned v[16];
-        nt_rows(acc[a][b], v);
-        if (q >= g.m || p >= g.n) continue;
-        const float sq = g.sa[q];
-        V8 o;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o.h[e] = i8_out((int)v[8 * h + e], sq, sp[e], has_bias, bp[e]);
-        h16* yp = g.y + (int64_t)q * g.n + p;
-        if (whole) {
-          store16(yp, o);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (p + e < g.n) yp[e] = o.h[e];
-        }
-      }
-    }
+  const int wave = threadIdx.x >> 6;
+  if (wave >= C::WAVES) return;
+  I8Epi<C> epi{g, g.n % 8 == 0, g.bias != nullptr};
+  h16* none[1] = {nullptr};
+  nt_store<C, 1>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ, g.n,
+                 g.m, false, none, 0, epi);
 }
 
 // Few rows (at most 16 tokens): bound by reading b once.  A workgroup takes 16
@@ -417,34 +420,53 @@ hipError_t launch_i8_fused(const I8Product& a, const h16* x, hipStream_t st) {
 }
 
 namespace {
-// The tile of a product: the largest that fills the CUs.
-int i8_tile(int m, int n) {
-  if (m <= kFewRows) return 0;
-  if ((int64_t)ceil_div(m, 256) * ceil_div(n, 256) >= 200) return 256;
-  return (int64_t)ceil_div(m, 128) * ceil_div(n, 128) >= 256 ? 128 : 64;
+// The tiles of a product: side, parts of the reduction, workgroups the device holds
+// at once, microseconds a 128-byte slice of the reduction and a launch take.
+struct I8Tile {
+  int tile, groups, slots;
+  double slice, fixed;
+  const char* name;
+};
+constexpr I8Tile kI8Tiles[6] = {{256, 1, 256, 1.15, 8.0, "tile 256"},
+                                {192, 1, 256, 0.75, 6.0, "tile 192"},
+                                {128, 1, 512, 0.72, 4.5, "tile 128"},
+                                {64, 1, 768, 0.40, 3.0, "tile 64"},
+                                {64, 4, 256, 0.30, 3.5, "tile 64 split"},
+                                {0, 8, 0, 0.0, 0.0, "few rows"}};
+
+// The one that finishes soonest by that estimate: rounds of workgroups over the
+// device, or one workgroup's reduction if that takes longer.
+const I8Tile& i8_tile(int m, int n, int k) {
+  if (m <= kFewRows) return kI8Tiles[5];
+  int best = 0;
+  double bt = 0;
+  for (int i = 0; i < 5; ++i) {
+    const I8Tile& c = kI8Tiles[i];
+    const double tiles = (double)ceil_div(m, c.tile) * ceil_div(n, c.tile);
+    const double slices = ceil_div(ceil_div(k, 128), c.groups);
+    const double t = c.fixed + c.slice * slices * std::max(tiles / c.slots, 1.0);
+    if (i == 0 || t < bt) {
+      bt = t;
+      best = i;
+    }
+  }
+  return kI8Tiles[best];
 }
 }  // namespace
 
-const char* i8_product_name(int m, int n, int k) {
-  (void)k;
-  switch (i8_tile(m, n)) {
-    case 0: return "few rows";
-    case 256: return "tile 256";
-    case 128: return "tile 128";
-    default: return "tile 64";
-  }
-}
+const char* i8_product_name(int m, int n, int k) { return i8_tile(m, n, k).name; }
 
 hipError_t launch_i8_product(const I8Product& a, hipStream_t st) {
-  switch (i8_tile(a.m, a.n)) {
-    case 0:
-      hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0,
-                         st, a, (const h16*)nullptr);
-      return hipGetLastError();
-    case 256: return i8_launch<Nt256>(a, st);
-    case 128: return i8_launch<Nt128>(a, st);
-    default: return i8_launch<Nt64>(a, st);
+  const I8Tile& c = i8_tile(a.m, a.n, a.k);
+  if (c.tile == 0) {
+    hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0,
+                       st, a, (const h16*)nullptr);
+    return hipGetLastError();
   }
+  if (c.tile == 256) return i8_launch<Nt256>(a, st);
+  if (c.tile == 192) return i8_launch<Nt192>(a, st);
+  if (c.tile == 128) return i8_launch<Nt128>(a, st);
+  return c.groups == 1 ? i8_launch<Nt64>(a, st) : i8_launch<Nt64k>(a, st);
 }
 
 }  // namespace fp16k

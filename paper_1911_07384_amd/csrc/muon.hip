@@ -65,7 +65,7 @@ static_assert(sizeof(NsChunk) <= 3584, "kernel arguments");
 
 struct NsPlaces {
   uint32_t table, map_sym, map_x, map_pre;
-  int tile;
+  int tile_sym, tile_x;
 };
 
 __device__ __forceinline__ double ns_block_sum(double v, double* red) {
@@ -74,6 +74,15 @@ __device__ __forceinline__ double ns_block_sum(double v, double* red) {
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   return ((red[0] + red[1]) + red[2]) + red[3];
+}
+
+// eight elements, at once where the matrix is 16-byte aligned
+__device__ __forceinline__ V8 ns_load8(const h16* p, bool aligned) {
+  if (aligned) return load16(p);
+  V8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v.h[e] = p[e];
+  return v;
 }
 
 // the float32 update direction before normalisation
@@ -94,8 +103,9 @@ __global__ __launch_bounds__(256) void ns_first(const NsChunk c, char* ws, NsPla
   if (blockIdx.x == 0) {
     const int idx = first + blockIdx.y;
     if (tid == 0) at<NsJob>(ws, pl.table)[idx] = j;
-    const int m = j.tall ? j.cp : j.rp, tm = m / pl.tile;
-    const int nsym = tm * (tm + 1) / 2, nx = (j.rp / pl.tile) * (j.cp / pl.tile);
+    const int m = j.tall ? j.cp : j.rp, tm = (m + pl.tile_sym - 1) / pl.tile_sym;
+    const int nsym = tm * (tm + 1) / 2;
+    const int nx = ((j.rp + pl.tile_x - 1) / pl.tile_x) * ((j.cp + pl.tile_x - 1) / pl.tile_x);
     const int npre = (j.rp / 64) * (j.cp / 64);
     for (int i = tid; i < nsym; i += 256) at<uint16_t>(ws, pl.map_sym)[j.t_sym + i] = (uint16_t)idx;
     for (int i = tid; i < nx; i += 256) at<uint16_t>(ws, pl.map_x)[j.t_x + i] = (uint16_t)idx;
@@ -105,13 +115,18 @@ __global__ __launch_bounds__(256) void ns_first(const NsChunk c, char* ws, NsPla
   const int64_t n = (int64_t)j.rows * j.cols, nvec = n / 8;
   double s = 0.0;
   for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < nvec; i += (int64_t)j.nparts * 256) {
-    const V8 g = load16(j.g + i * 8);
+    const V8 g = ns_load8(j.g + i * 8, j.aligned);
     V8 m = zero8();
     if (has_m) {
-      m = load16(j.m + i * 8);
+      m = ns_load8(j.m + i * 8, j.aligned);
 #pragma unroll
       for (int e = 0; e < 8; ++e) m.h[e] = to_h16(__builtin_fmaf(mu, to_f32(m.h[e]), to_f32(g.h[e])));
-      store16(j.m + i * 8, m);
+      if (j.aligned) {
+        store16(j.m + i * 8, m);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) j.m[i * 8 + e] = m.h[e];
+      }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -152,7 +167,7 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
   const int local = blockIdx.x - j.t_pre, tc = j.cp / 64;
   const int r0 = (local / tc) * 64, c0 = (local % tc) * 64;
   const int row = r0 + tid / 4;
-  const bool has_m = j.m != nullptr, whole = j.cols % 8 == 0;
+  const bool has_m = j.m != nullptr, whole = j.whole;
   h16* nat = at<h16>(dv.ws, j.nat[0]) + (int64_t)row * j.cp;
   h16* natl = at<h16>(dv.ws, j.natl[0]) + (int64_t)row * j.cp;
 #pragma unroll
@@ -198,56 +213,7 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
 
 // ---- the three products of a step -----------------------------------------------
 
-// Walks a wave's tiles in runs of 8 rows p of one column q: value(p, q, v[8]) gives
-// the run's halves to store there (natural, out[q][p ..]) in n_out parts; with
-// `mirror` the same halves go out[p][q ..] as well, through this wave's LDS.
-template <class C, int PARTS, class Value>
-__device__ __forceinline__ void ns_store(const typename NtHalf::Acc (&acc)[C::TP][C::TQ], char* lds,
-                                         int p0, int q0, bool mirror, h16* const (&mir)[PARTS],
-                                         int ldm, Value value) {
-  constexpr int TP = C::TP, TQ = C::TQ, LD = 32 * TQ + 8;  // halves
-  static_assert(PARTS * 32 * LD * 2 * C::WAVES <= C::LDS, "LDS");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int lrow = lane & 31, lhi = lane >> 5;
-  h16* buf = reinterpret_cast<h16*>(lds) + wave * (PARTS * 32 * LD);
-#pragma unroll
-  for (int a = 0; a < TP; ++a) {
-#pragma unroll
-    for (int b = 0; b < TQ; ++b) {
-      unsigned v[16];
-      nt_rows(acc[a][b], v);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int p = 32 * a + 16 * h + 8 * lhi, q = 32 * b + lrow;
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, v[8 * h + e]);
-        V8 out[PARTS];
-        value(p0 + p, q0 + q, f, out);
-        if (mirror) {
-#pragma unroll
-          for (int s = 0; s < PARTS; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) buf[s * 32 * LD + (16 * h + 8 * lhi + e) * LD + q] = out[s].h[e];
-        }
-      }
-    }
-    if (mirror) {
-      nt_wave_sync();
-#pragma unroll
-      for (int s = 0; s < PARTS; ++s)
-#pragma unroll
-        for (int i = 0; i < 2 * TQ; ++i) {
-          const int r = (i * 64 + lane) / (4 * TQ), c = (i * 64 + lane) % (4 * TQ);
-          store16(mir[s] + (int64_t)(p0 + 32 * a + r) * ldm + q0 + c * 8,
-                  load16(buf + s * 32 * LD + r * LD + c * 8));
-        }
-      nt_wave_sync();
-    }
-  }
-}
-
-// This workgroup's matrix and its tile of the launch, or -1.
+// This workgroup's matrix and its tile of the launch, or null.
 __device__ __forceinline__ const NsJob* ns_job(const NsDev& dv, int* t) {
   *t = nt_xcd(blockIdx.x, dv.tiles);
   if (*t >= dv.tiles) return nullptr;
@@ -263,11 +229,64 @@ __device__ __forceinline__ void ns_triangle(int t, int* i, int* j) {
   *j = t - r * (r + 1) / 2;
 }
 
+// What a tile of A (STEP 0) or B (STEP 1) stores, see nt_store.
+template <class C, int STEP, int PARTS>
+struct NsSymEpi {
+  int m;
+  const h16 *ah, *al;  // A, for B
+  h16 *oh, *ol;
+  float *d, *e;
+  float cb, cc;
+  V8 va[2][2 * C::TP], vl[PARTS == 2 ? 2 : 1][2 * C::TP];
+
+  __device__ __forceinline__ void load(int b, int i, int p, int q) {
+    if (STEP == 0 || p >= m || q >= m) return;
+    const int64_t o = (int64_t)q * m + p;
+    va[b & 1][i] = load16(ah + o);
+    if (PARTS == 2) vl[PARTS == 2 ? b & 1 : 0][i] = load16(al + o);
+  }
+  __device__ __forceinline__ void apply(int b, int i, int p, int q, const float (&f)[8],
+                                        V8 (&out)[PARTS]) {
+    if (p >= m || q >= m) return;
+    const int64_t o = (int64_t)q * m + p;
+    float dp[8], dq = 0.0f;
+    if (STEP == 1) {
+      dq = d[q];
+      __builtin_memcpy(dp, d + p, 32);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float r;
+      if (STEP == 0) {
+        r = f[k] * (kSa / (kSx * kSx));
+        if (p + k == q) {
+          d[q] = f[k] * (1.0f / (kSx * kSx));
+          r = 0.0f;
+        }
+      } else {
+        float a = to_f32(va[b & 1][i].h[k]);
+        if (PARTS == 2) a += to_f32(vl[PARTS == 2 ? b & 1 : 0][i].h[k]);
+        a *= 1.0f / kSa;
+        const float a2 = f[k] * (1.0f / (kSa * kSa));
+        r = kSb * __builtin_fmaf(cc, __builtin_fmaf(dq + dp[k], a, a2), cb * a);
+        if (p + k == q) {
+          e[q] = __builtin_fmaf(cc, __builtin_fmaf(dq, dq, a2), cb * dq);
+          r = 0.0f;
+        }
+      }
+      out[0].h[k] = to_h16(r);
+      if (PARTS == 2) out[PARTS - 1].h[k] = to_h16(r - to_f32(out[0].h[k]));
+    }
+    store16(oh + o, out[0]);
+    if (PARTS == 2) store16(ol + o, out[PARTS - 1]);
+  }
+};
+
 // A = X X^T (STEP 0) or B = bA + cA^2 (STEP 1), off the diagonal, and the diagonal.
 template <class C, int STEP, int PROD>
-__global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, int cur, float cb,
-                                                             float cc) {
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+__global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, float cb, float cc) {
+  constexpr int PARTS = PROD == 3 ? 2 : 1;
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PARTS>::LDS];
   int t;
   const NsJob* jp = ns_job(dv, &t);
   if (!jp) return;
@@ -294,75 +313,123 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, int
   nt.p[PROD - 1] = hi + (int64_t)pt * k;
   nt.q[PROD - 1] = hi + (int64_t)qt * k;
   nt.ldp = nt.ldq = (uint32_t)k * 2u;
-  nt.prows = nt.qrows = C::BP;
+  nt.prows = m - pt;
+  nt.qrows = m - qt;
   nt.kbytes = k * 2;
   floatx16 acc[C::TP][C::TQ];
   nt_product<NtHalf, C, PROD>(nt, lds, acc);
-  constexpr int PARTS = PROD == 3 ? 2 : 1;
   const int wave = threadIdx.x >> 6;
-  const int p0 = pt + (wave / C::WQ) * 32 * C::TP, q0 = qt + (wave % C::WQ) * 32 * C::TQ;
-  h16* const oh = at<h16>(dv.ws, STEP == 0 ? j.a : j.b);
-  h16* const ol = at<h16>(dv.ws, STEP == 0 ? j.al : j.bl);
+  if (wave >= C::WAVES) return;
+  NsSymEpi<C, STEP, PARTS> epi;
+  epi.m = m;
+  epi.ah = ah;
+  epi.al = al;
+  epi.oh = at<h16>(dv.ws, STEP == 0 ? j.a : j.b);
+  epi.ol = at<h16>(dv.ws, STEP == 0 ? j.al : j.bl);
+  epi.d = at<float>(dv.ws, j.d);
+  epi.e = at<float>(dv.ws, j.e);
+  epi.cb = cb;
+  epi.cc = cc;
   h16* mir[PARTS];
-  mir[0] = oh;
-  mir[PARTS - 1] = PARTS == 2 ? ol : oh;
-  float* const d = at<float>(dv.ws, j.d);
-  float* const ev = at<float>(dv.ws, j.e);
-  ns_store<C, PARTS>(acc, lds, p0, q0, ti != tj, mir, m, [&](int p, int q, const float (&f)[8],
-                                                            V8 (&out)[PARTS]) {
-    const int64_t o = (int64_t)q * m + p;
-    V8 va, vl;
-    float dp[8], dq = 0.0f;
-    if (STEP == 1) {
-      va = load16(ah + o);
-      if (PROD == 3) vl = load16(al + o);
-      dq = d[q];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dp[e] = d[p + e];
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float r;
-      if (STEP == 0) {
-        r = f[e] * (kSa / (kSx * kSx));
-        if (p + e == q) {
-          d[q] = f[e] * (1.0f / (kSx * kSx));
-          r = 0.0f;
-        }
-      } else {
-        float a = to_f32(va.h[e]);
-        if (PROD == 3) a += to_f32(vl.h[e]);
-        a *= 1.0f / kSa;
-        const float a2 = f[e] * (1.0f / (kSa * kSa));
-        if (p + e == q) {
-          ev[q] = __builtin_fmaf(cc, __builtin_fmaf(dq, dq, a2), cb * dq);
-          r = 0.0f;
-        } else {
-          r = kSb * __builtin_fmaf(cc, __builtin_fmaf(dq + dp[e], a, a2), cb * a);
-        }
-      }
-      out[0].h[e] = to_h16(r);
-      if (PARTS == 2) out[PARTS - 1].h[e] = to_h16(r - to_f32(out[0].h[e]));
-    }
-    store16(oh + o, out[0]);
-    if (PARTS == 2) store16(ol + o, out[PARTS - 1]);
-  });
+  mir[0] = epi.oh;
+  mir[PARTS - 1] = PARTS == 2 ? epi.ol : epi.oh;
+  nt_store<C, PARTS>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ, m,
+                     m, ti != tj, mir, m, epi);
 }
 
+// What a tile of X' stores: X' as laid out in two parts (its transpose through
+// nt_store), or with LAST the weights' update or the result.
+template <class C, int PARTS, bool LAST>
+struct NsXEpi {
+  int rows, cols, rp, cp, tall;
+  const h16 *nh, *nl;
+  h16 *nho, *nlo, *w;
+  const float* e;
+  float ca, keep, alpha;
+  bool update, whole;
+  V8 vh[2][2 * C::TP], vl[2][2 * C::TP], vw[LAST ? 2 : 1][2 * C::TP];
+
+  __device__ __forceinline__ void load(int b, int i, int p, int q) {
+    if (p >= cp || q >= rp) return;
+    const int64_t o = (int64_t)q * cp + p;
+    vh[b & 1][i] = load16(nh + o);
+    vl[b & 1][i] = load16(nl + o);
+    if (LAST && update && q < rows && p < cols) {
+      const h16* wp = w + (int64_t)q * cols + p;
+      if (whole) {
+        vw[LAST ? b & 1 : 0][i] = load16(wp);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (p + k < cols) vw[LAST ? b & 1 : 0][i].h[k] = wp[k];
+      }
+    }
+  }
+  __device__ __forceinline__ void apply(int b, int i, int p, int q, const float (&f)[8],
+                                        V8 (&out)[PARTS]) {
+    // (X' comes out as zeros in the padding, which is part of the next operands)
+    if (LAST ? p >= cols || q >= rows : p >= cp || q >= rp) return;
+    const int64_t o = (int64_t)q * cp + p;
+    float x[8], ep[8];
+    if (tall) {
+      __builtin_memcpy(ep, e + p, 32);
+    } else {
+      const float eq = e[q];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ep[k] = eq;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float h = to_f32(vh[b & 1][i].h[k]), l = to_f32(vl[b & 1][i].h[k]);
+      // (products = 1: the low part takes part in aX only, as in B'X)
+      const float y = __builtin_fmaf(PARTS == 2 ? ca + ep[k] : ca, l, f[k] * (1.0f / kSb));
+      x[k] = __builtin_fmaf(ca + ep[k], h, y);
+    }
+    if (!LAST) {
+      V8 lo;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        out[0].h[k] = to_h16(x[k]);
+        lo.h[k] = to_h16(x[k] - to_f32(out[0].h[k]));
+      }
+      if (PARTS == 2) out[PARTS - 1] = lo;
+      store16(nho + o, out[0]);
+      store16(nlo + o, lo);
+    } else {
+      h16* const wp = w + (int64_t)q * cols + p;
+      V8 v;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float ox = x[k] * (1.0f / kSx);
+        v.h[k] = to_h16(update ? __builtin_fmaf(-alpha, ox, keep * to_f32(vw[LAST ? b & 1 : 0][i].h[k]))
+                               : alpha * ox);
+      }
+      if (whole) {
+        store16(wp, v);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (p + k < cols) wp[k] = v.h[k];
+      }
+    }
+  }
+};
+
 // X' = (a + E) X + B'X, tile rows p along the columns of the matrix as laid out and
-// q along its rows.  LAST: the weights' update (or the result) instead of X'.
+// q along its rows.
 template <class C, int PROD, bool LAST>
 __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int cur, float ca,
                                                            float keep) {
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  constexpr int PARTS = PROD == 3 ? 2 : 1;
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PARTS>::LDS];
   int t;
   const NsJob* jp = ns_job(dv, &t);
   if (!jp) return;
   const NsJob& j = *jp;
   t -= j.t_x;
-  const int tp = j.cp / C::BP;
   // four tiles of rows p at a time, their rows q in turn
-  const int tq = j.rp / C::BQ, g = t / (4 * tq), w = t - g * 4 * tq;
+  const int tp = (j.cp + C::BP - 1) / C::BP, tq = (j.rp + C::BQ - 1) / C::BQ;
+  const int g = t / (4 * tq), w = t - g * 4 * tq;
   const int gw = tp - 4 * g < 4 ? tp - 4 * g : 4;
   const int pt = (4 * g + w % gw) * C::BP, qt = (w / gw) * C::BQ;
   const int tall = j.tall, m = tall ? j.cp : j.rp;
@@ -382,138 +449,88 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
   nt.p[PROD - 1] = (tall ? bh : xh) + po;
   nt.q[PROD - 1] = (tall ? xh : bh) + qo;
   nt.ldp = nt.ldq = (uint32_t)m * 2u;
-  nt.prows = C::BP;
-  nt.qrows = C::BQ;
+  nt.prows = j.cp - pt;
+  nt.qrows = j.rp - qt;
   nt.kbytes = m * 2;
   floatx16 acc[C::TP][C::TQ];
   nt_product<NtHalf, C, PROD>(nt, lds, acc);
-
-  constexpr int PARTS = PROD == 3 ? 2 : 1;
   const int wave = threadIdx.x >> 6;
-  const int p0 = pt + (wave / C::WQ) * 32 * C::TP, q0 = qt + (wave % C::WQ) * 32 * C::TQ;
-  const int cp = j.cp, rows = j.rows, cols = j.cols;
-  const int nc = tall ? cur : 0, nn = tall ? cur ^ 1 : 0;  // X as laid out, now and next
-  const int lc = PROD == 3 ? nc : 0, ln = PROD == 3 ? nn : 0;
-  const int mn = tall ? 0 : cur ^ 1;
-  const h16* nh = at<h16>(dv.ws, j.nat[nc]);
-  const h16* nl = at<h16>(dv.ws, j.natl[lc]);
-  h16* const nho = at<h16>(dv.ws, j.nat[nn]);
-  h16* const nlo = at<h16>(dv.ws, j.natl[ln]);
-  const float* ev = at<float>(dv.ws, j.e);
+  if (wave >= C::WAVES) return;
+  // X as laid out, now and next; its low part is an operand (and alternates) only
+  // with three products
+  const int nc = tall ? cur : 0, nn = tall ? cur ^ 1 : 0, mn = tall ? 0 : cur ^ 1;
+  NsXEpi<C, PARTS, LAST> epi;
+  epi.rows = j.rows;
+  epi.cols = j.cols;
+  epi.rp = j.rp;
+  epi.cp = j.cp;
+  epi.tall = tall;
+  epi.nh = at<h16>(dv.ws, j.nat[nc]);
+  epi.nl = at<h16>(dv.ws, j.natl[PARTS == 2 ? nc : 0]);
+  epi.nho = at<h16>(dv.ws, j.nat[nn]);
+  epi.nlo = at<h16>(dv.ws, j.natl[PARTS == 2 ? nn : 0]);
+  epi.w = j.w;
+  epi.e = at<float>(dv.ws, j.e);
+  epi.ca = ca;
+  epi.keep = keep;
+  epi.alpha = j.alpha;
+  epi.update = j.m != nullptr;
+  epi.whole = j.whole;
   h16* mir[PARTS];
   mir[0] = at<h16>(dv.ws, j.mir[mn]);
   mir[PARTS - 1] = at<h16>(dv.ws, PARTS == 2 ? j.mirl[mn] : j.mir[mn]);
-  h16* const wt = j.w;
-  const bool update = j.m != nullptr, whole = cols % 8 == 0;
-  const float alpha = j.alpha;
-  ns_store<C, PARTS>(acc, lds, p0, q0, !LAST, mir, j.rp, [&](int p, int q, const float (&f)[8],
-                                                             V8 (&out)[PARTS]) {
-    const int64_t o = (int64_t)q * cp + p;
-    if (LAST && (q >= rows || p >= cols)) return;
-    const V8 vh = load16(nh + o), vl = load16(nl + o);
-    float x[8];
-    const float eq = tall ? 0.0f : ev[q];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float E = tall ? ev[p + e] : eq;
-      const float h = to_f32(vh.h[e]), l = to_f32(vl.h[e]);
-      // (products = 1: the low part takes part in aX only, as in B'X)
-      const float y = __builtin_fmaf(PROD == 3 ? ca + E : ca, l, f[e] * (1.0f / kSb));
-      x[e] = __builtin_fmaf(ca + E, h, y);
-    }
-    if (!LAST) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        out[0].h[e] = to_h16(x[e]);
-        const h16 lo = to_h16(x[e] - to_f32(out[0].h[e]));
-        if (PARTS == 2)
-          out[PARTS - 1].h[e] = lo;
-        else
-          x[e] = to_f32(lo);
-      }
-      store16(nho + o, out[0]);
-      V8 lo;
-      if (PARTS == 2) {
-        lo = out[PARTS - 1];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) lo.h[e] = (h16)x[e];
-      }
-      store16(nlo + o, lo);
-    } else {
-      h16* const wp = wt + (int64_t)q * cols + p;
-      V8 v = zero8();
-      if (update) {
-        if (whole) {
-          v = load16(wp);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (p + e < cols) v.h[e] = wp[e];
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float ox = x[e] * (1.0f / kSx);
-        v.h[e] = to_h16(update ? __builtin_fmaf(-alpha, ox, keep * to_f32(v.h[e])) : alpha * ox);
-      }
-      if (whole) {
-        store16(wp, v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (p + e < cols) wp[e] = v.h[e];
-      }
-    }
-  });
+  nt_store<C, PARTS>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ,
+                     j.cp, j.rp, !LAST, mir, j.rp, epi);
 }
 
 // ---- the plan ------------------------------------------------------------------
 
 int up(int v, int t) { return (v + t - 1) / t * t; }
 
-// Estimated time of one step with tiles of side T, in microseconds: rounds of
-// workgroups over the device at so long a slice each.
-struct NsTileCost {
-  int tile, slots;
-  double slice, fixed;
-};
-constexpr NsTileCost kNsTiles[3] = {{256, 256, 1.25, 8.0}, {128, 512, 0.70, 4.0}, {64, 768, 0.45, 3.0}};
+// The tiles a product may run on: workgroups the device holds at once, microseconds
+// a 128-byte slice of the reduction takes and a launch takes besides.
+constexpr NsTile kNsTiles[5] = {{256, 1, 256, 1.15, 12.0},
+                                {192, 1, 256, 0.75, 9.0},
+                                {128, 1, 512, 0.72, 6.0},
+                                {64, 1, 768, 0.40, 4.0},
+                                {64, 4, 256, 0.30, 5.0}};
 
-double ns_cost(const NsTileCost& c, int count, const int32_t* rows, const int32_t* cols) {
-  double work[3] = {0, 0, 0}, longest[3] = {0, 0, 0};
-  for (int i = 0; i < count; ++i) {
-    const int m = up(std::min(rows[i], cols[i]), c.tile), n = up(std::max(rows[i], cols[i]), c.tile);
-    const double tm = m / c.tile, tn = n / c.tile, sym = tm * (tm + 1) / 2;
-    const double w[3] = {sym * (n / 64), sym * (m / 64), tm * tn * (m / 64)};
-    const double k[3] = {n / 64.0, m / 64.0, m / 64.0};
-    for (int s = 0; s < 3; ++s) {
-      work[s] += w[s];
-      longest[s] = std::max(longest[s], k[s]);
+// The tile that a product of the set finishes soonest on, by that estimate: rounds
+// of workgroups over the device, or the longest reduction if that takes longer.
+// stage 0: A, 1: B, 2: X'.
+NsTile ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, int products) {
+  NsTile best = kNsTiles[0];
+  double bt = 0;
+  for (const NsTile& c : kNsTiles) {
+    double work = 0, longest = 0;
+    for (int i = 0; i < count; ++i) {
+      const int m = up(std::min(rows[i], cols[i]), 64), n = up(std::max(rows[i], cols[i]), 64);
+      const double tm = ceil_div(m, c.tile), tn = ceil_div(n, c.tile);
+      const double k = ceil_div(products * ((stage == 0 ? n : m) / 64), c.groups);
+      work += (stage == 2 ? tm * tn : tm * (tm + 1) / 2) * k;
+      longest = std::max(longest, k);
+    }
+    const double t = c.fixed + c.slice * std::max(work / c.slots, longest);
+    if (bt == 0 || t < bt) {
+      bt = t;
+      best = c;
     }
   }
-  double t = 0;
-  for (int s = 0; s < 3; ++s) t += c.fixed + c.slice * std::max(work[s] / c.slots, longest[s]);
-  return t;
+  return best;
 }
 
 template <class C, int PROD>
-hipError_t ns_steps(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
-  const NsDev sym{ws, p.table, p.map_sym, p.n_sym}, x{ws, p.table, p.map_x, p.n_x};
-  const dim3 gs((unsigned)(8 * ((p.n_sym + 7) / 8))), gx((unsigned)(8 * ((p.n_x + 7) / 8)));
-  for (int s = 0; s < a.steps; ++s) {
-    const float ca = a.coef[3 * s], cb = a.coef[3 * s + 1], cc = a.coef[3 * s + 2];
-    const int cur = s & 1;
-    hipLaunchKernelGGL((ns_sym<C, 0, PROD>), gs, dim3(C::THREADS), 0, st, sym, cur, cb, cc);
-    hipLaunchKernelGGL((ns_sym<C, 1, PROD>), gs, dim3(C::THREADS), 0, st, sym, cur, cb, cc);
-    if (s + 1 < a.steps)
-      hipLaunchKernelGGL((ns_x<C, PROD, false>), gx, dim3(C::THREADS), 0, st, x, cur, ca, a.keep);
-    else
-      hipLaunchKernelGGL((ns_x<C, PROD, true>), gx, dim3(C::THREADS), 0, st, x, cur, ca, a.keep);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+void ns_launch(int stage, bool last, const NsDev& d, int cur, float ca, float cb, float cc,
+               float keep, hipStream_t st) {
+  const dim3 grid((unsigned)(8 * ((d.tiles + 7) / 8))), block(C::THREADS);
+  if (stage == 0)
+    hipLaunchKernelGGL((ns_sym<C, 0, PROD>), grid, block, 0, st, d, cb, cc);
+  else if (stage == 1)
+    hipLaunchKernelGGL((ns_sym<C, 1, PROD>), grid, block, 0, st, d, cb, cc);
+  else if (!last)
+    hipLaunchKernelGGL((ns_x<C, PROD, false>), grid, block, 0, st, d, cur, ca, keep);
+  else
+    hipLaunchKernelGGL((ns_x<C, PROD, true>), grid, block, 0, st, d, cur, ca, keep);
 }
 
 template <int PROD>
@@ -521,11 +538,28 @@ hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
   const NsDev pre{ws, p.table, p.map_pre, p.n_pre};
   hipLaunchKernelGGL((ns_split<PROD>), dim3((unsigned)p.n_pre), dim3(256), 0, st, pre, a.momentum,
                      a.nesterov);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (p.tile == 256) return ns_steps<Nt256, PROD>(p, a, ws, st);
-  if (p.tile == 128) return ns_steps<Nt128, PROD>(p, a, ws, st);
-  return ns_steps<Nt64, PROD>(p, a, ws, st);
+  const NsDev sym{ws, p.table, p.map_sym, p.n_sym}, x{ws, p.table, p.map_x, p.n_x};
+  for (int s = 0; s < a.steps; ++s) {
+    const float ca = a.coef[3 * s], cb = a.coef[3 * s + 1], cc = a.coef[3 * s + 2];
+    for (int stage = 0; stage < 3; ++stage) {
+      const NsDev& d = stage == 2 ? x : sym;
+      const NsTile& k = p.kind[stage];
+      const bool last = s + 1 == a.steps;
+      if (k.tile == 256)
+        ns_launch<Nt256, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
+      else if (k.tile == 192)
+        ns_launch<Nt192, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
+      else if (k.tile == 128)
+        ns_launch<Nt128, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
+      else if (k.groups == 1)
+        ns_launch<Nt64, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
+      else
+        ns_launch<Nt64k, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -533,15 +567,11 @@ hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
 void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, NsPlan* plan) {
   NsPlan& P = *plan;
   P.count = count;
-  double best = 0;
-  P.tile = 0;
-  for (const NsTileCost& c : kNsTiles) {
-    const double t = ns_cost(c, count, rows, cols);
-    if (P.tile == 0 || t < best) {
-      best = t;
-      P.tile = c.tile;
-    }
-  }
+  // (A and B share their tiles' map, so their tile sides are one choice)
+  P.kind[0] = ns_choose(0, count, rows, cols, products);
+  P.kind[1] = ns_choose(1, count, rows, cols, products);
+  if (P.kind[1].tile != P.kind[0].tile) P.kind[1] = P.kind[0];
+  P.kind[2] = ns_choose(2, count, rows, cols, products);
   // the longest products first
   for (int i = 0; i < count; ++i) P.order[i] = i;
   std::sort(P.order, P.order + count, [&](int x, int y) {
@@ -563,14 +593,14 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
     j.rows = rows[o];
     j.cols = cols[o];
     j.tall = j.rows > j.cols;
-    j.rp = up(j.rows, P.tile);
-    j.cp = up(j.cols, P.tile);
-    const int m = j.tall ? j.cp : j.rp, tm = m / P.tile;
+    j.rp = up(j.rows, 64);
+    j.cp = up(j.cols, 64);
+    const int m = j.tall ? j.cp : j.rp, tm = ceil_div(m, P.kind[0].tile);
     j.t_sym = P.n_sym;
     j.t_x = P.n_x;
     j.t_pre = P.n_pre;
     P.n_sym += tm * (tm + 1) / 2;
-    P.n_x += (j.rp / P.tile) * (j.cp / P.tile);
+    P.n_x += ceil_div(j.rp, P.kind[2].tile) * ceil_div(j.cp, P.kind[2].tile);
     P.n_pre += (j.rp / 64) * (j.cp / 64);
     const int64_t n = (int64_t)j.rows * j.cols;
     j.nparts = (int)std::min<int64_t>(kNsParts, (n + 8191) / 8192);
@@ -600,7 +630,7 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
 
 hipError_t launch_ns(const NsPlan& p, const NsArgs& a, void* ws, hipStream_t st) {
   char* w = static_cast<char*>(ws);
-  const NsPlaces pl{p.table, p.map_sym, p.map_x, p.map_pre, p.tile};
+  const NsPlaces pl{p.table, p.map_sym, p.map_x, p.map_pre, p.kind[0].tile, p.kind[2].tile};
   for (int first = 0; first < p.count; first += kJobsPerLaunch) {
     NsChunk c{};
     const int n = std::min(kJobsPerLaunch, p.count - first);

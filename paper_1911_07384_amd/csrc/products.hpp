@@ -17,7 +17,7 @@ constexpr int kNsParts = 256;  // partial sums of a matrix's squares, at most
 
 // One matrix [rows][cols].  Workspace arrays are given in units of 256 bytes from
 // the workspace's start; "nat" holds X as the matrix is laid out, "mir" its
-// transpose, each padded with zeros to [rp][cp] ([cp][rp]); the operand of the
+// transpose, each padded with zeros to multiples of 64, [rp][cp] ([cp][rp]); the operand of the
 // update that is not also its elementwise argument alternates between two.
 struct NsJob {
   const h16* g;  // the gradient, or the matrix itself
@@ -25,6 +25,7 @@ struct NsJob {
   h16* w;        // the weights, or the result
   float alpha;   // factor of the orthogonalised matrix
   int rows, cols, rp, cp, tall;
+  int aligned, whole;  // 16-byte aligned; and rows of whole 16 bytes
   uint32_t nat[2], mir[2], natl[2], mirl[2];  // X (high parts, low parts)
   uint32_t a, al, b, bl;                      // A and B off the diagonal
   uint32_t d, e;                              // their diagonals, float32
@@ -33,8 +34,13 @@ struct NsJob {
   int t_sym, t_x, t_pre;  // first tile of this matrix in each kind of launch
 };
 
+struct NsTile {
+  int tile, groups, slots;  // side, parts of the reduction, workgroups at once
+  double slice, fixed;      // microseconds: a slice of the reduction, a launch
+};
+
 struct NsPlan {
-  int tile;                    // 64, 128 or 256
+  NsTile kind[3];              // of A, B and X'
   int count;
   int n_sym, n_x, n_pre;       // tiles of a symmetric product, of X', of the first pass
   uint32_t table, map_sym, map_x, map_pre;  // in the workspace

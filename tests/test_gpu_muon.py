@@ -86,23 +86,45 @@ def test_shapes(shape, products):
     assert off(y, ns64(x)) <= BAR[products]
 
 
-# tile, matrices: the rule has to give each tile
-TILES = [(64, [(96, 700)]), (128, [(1500, 1024), (1024, 1024), (1000, 2048)] * 2),
-         (256, [(4096, 2304)])]
+# sets that between them run on every tile (test_product_choice.py holds which)
+SETS = [[(96, 700)], [(64, 4608)], [(700, 600)] * 3, [(1500, 1024), (1024, 1024), (1000, 2048)] * 2,
+        [(2304, 2304)], [(4096, 2304)], [(2304, 4096)], [(3000, 3100)]]
 
 
 @pytest.mark.parametrize("products", [1, 3])
-@pytest.mark.parametrize("tile,shapes", TILES, ids=lambda t: str(t) if isinstance(t, int) else "")
-def test_every_tile(tile, shapes, products):
-    d = F.muon_descs(shapes)
-    assert F.fp16_muon_tile(d, products) == tile
+@pytest.mark.parametrize("shapes", SETS, ids=lambda s: "x".join(map(str, s[0])))
+def test_every_tile(shapes, products):
     xs = [matrix(*s, seed=i) for i, s in enumerate(shapes)]
     for x, y in zip(xs, orth(xs, products)):
         assert off(y, ns64(x)) <= BAR[products]
-    # transposed
-    if len(shapes) == 1:
-        x = xs[0].t().contiguous()
-        assert off(orth([x], products)[0], ns64(x)) <= BAR[products]
+
+
+def test_views_of_a_flat_buffer():
+    """Matrices that start at any element (no 16-byte accesses): the same bits as
+    aligned copies, and nothing else written."""
+    shapes = [(77, 90), (64, 72), (33, 41)]
+    d = F.muon_descs(shapes)
+    ws = F.workspace(F.fp16_muon_workspace_bytes(d, 1))
+    bufs = []
+    for k, scale in ((1, 0.1), (2, 1e-3), (3, 1e-3)):
+        flat = torch.full((1 + sum(a * b for a, b in shapes) + 9,), 7.0, dtype=torch.float16,
+                          device="cuda")
+        views, at = [], 1
+        for i, s in enumerate(shapes):
+            v = flat[at:at + s[0] * s[1]].view(s)
+            v.copy_(matrix(*s, seed=10 * k + i, kind="normal", scale=scale))
+            views.append(v)
+            at += s[0] * s[1]
+        bufs.append((flat, views, at))
+    copies = [[v.clone() for v in views] for _, views, _ in bufs]
+    run = lambda l: F.fp16_muon_step(d, l[0], l[1], l[2], 0.02, 0.9, 0.1, ws=ws)
+    note("[gpu] muon on views")
+    run([b[1] for b in bufs])
+    run(copies)
+    torch.cuda.synchronize()
+    for (flat, views, at), cs in zip(bufs, copies):
+        assert all(torch.equal(v, c) for v, c in zip(views, cs))
+        assert flat[0] == 7 and (flat[at:] == 7).all()
 
 
 @pytest.mark.parametrize("products", [1, 3])
