@@ -41,17 +41,18 @@ struct NtByte {  // 8-bit integers, 32-bit sums (exact below 2^31)
   }
 };
 
-template <int WP_, int WQ_, int TP_, int TQ_, int S_, int KG_, int OCC_>
+template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int KG_, int OCC_>
 struct NtCfg {
-  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, S = S_, KG = KG_, OCC = OCC_;
+  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, SB = SB_, S = S_, KG = KG_, OCC = OCC_;
   static constexpr int WAVES = WP * WQ;            // of one group
   static constexpr int THREADS = 64 * WAVES * KG;
   static constexpr int BP = 32 * TP * WP, BQ = 32 * TQ * WQ;
-  static constexpr int IP = BP / (8 * WAVES), IQ = BQ / (8 * WAVES);  // loads a wave and slice
-  static constexpr int STAGE = (BP + BQ) * 128, RING = S * STAGE;
+  static constexpr int STAGE = (BP + BQ) * SB, RING = S * STAGE;
+  static constexpr int IP = BP * SB / (1024 * WAVES), IQ = BQ * SB / (1024 * WAVES);  // loads
   static constexpr int LDS = KG * RING;
   static constexpr int SUM = 1024 * TP * TQ * 4 * WAVES;  // one group's sums
-  static_assert(IP % 2 == 0 && IQ % 2 == 0, "the chunk order goes by pairs of loads");
+  static_assert(SB == 64 || (SB == 128 && IP % 2 == 0 && IQ % 2 == 0), "the chunks' order");
+  static_assert(IP * 1024 * WAVES == BP * SB && IQ * 1024 * WAVES == BQ * SB, "whole loads");
   static_assert(LDS * OCC <= 160 * 1024 && (KG - 1) * SUM <= LDS, "LDS");
 };
 
@@ -81,7 +82,7 @@ template <class T, class C, int NSEG>
 __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
                                            typename T::Acc (&acc)[C::TP][C::TQ]) {
   typedef typename T::Frag Frag;
-  constexpr int TP = C::TP, TQ = C::TQ, S = C::S, IP = C::IP, IQ = C::IQ, I = IP + IQ;
+  constexpr int TP = C::TP, TQ = C::TQ, S = C::S, SB = C::SB, IP = C::IP, IQ = C::IQ, I = IP + IQ;
   constexpr uint32_t OOB = 0x80000000u;
   const int lane = threadIdx.x & 63;
   const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -90,27 +91,36 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
   const int lrow = lane & 31, lhi = lane >> 5;
   char* const lds = lds0 + grp * C::RING;
 
-  // loads: instruction i of a wave takes rows 8 * (wave * I. + i) .. + 7, lane l
-  // row l / 8 of them and the chunk that lies at l % 8 of that row
+  // loads: an instruction fills 8 lines of 128 bytes, lane l the 16 bytes l % 8 of
+  // line l / 8: rows RI (wave * I. + i) .. + RI - 1 (see the layout above)
+  constexpr int RI = 1024 / SB;
   const int prec = (t.prows < C::BP ? t.prows : C::BP) * (int)t.ldp;
   const int qrec = (t.qrows < C::BQ ? t.qrows : C::BQ) * (int)t.ldq;
   int ck[2];           // byte of the chunk in its row's slice, even and odd instructions
   uint32_t pv[2], qv[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    ck[h] = ((lane & 7) ^ ((h * 4 + (lane >> 4)) & 7)) * 16;
-    pv[h] = (uint32_t)(wave * IP * 8 + (lane >> 3)) * t.ldp + (uint32_t)ck[h];
-    qv[h] = (uint32_t)(wave * IQ * 8 + (lane >> 3)) * t.ldq + (uint32_t)ck[h];
+    int row;
+    if (SB == 128) {
+      row = lane >> 3;
+      ck[h] = ((lane & 7) ^ ((h * 4 + (lane >> 4)) & 7)) * 16;
+    } else {
+      const int c = (lane & 7) ^ ((lane >> 4) & 3);
+      row = (lane >> 3) * 2 + (c >> 2);
+      ck[h] = (c & 3) * 16;
+    }
+    pv[h] = (uint32_t)(wave * IP * RI + row) * t.ldp + (uint32_t)ck[h];
+    qv[h] = (uint32_t)(wave * IQ * RI + row) * t.ldq + (uint32_t)ck[h];
   }
   // the slices of all pairs in order, a range of them for each group
-  const int per1 = (t.kbytes + 127) / 128;  // of one pair
+  const int per1 = (t.kbytes + SB - 1) / SB;  // of one pair
   const int KT = (NSEG * per1 + C::KG - 1) / C::KG;
   int k0 = 0, seg = 0;  // the slice loaded next
   int left = KT;        // and how many there are from it
   if (C::KG > 1) {
     const int s0 = grp * KT;
     seg = s0 / per1;
-    k0 = (s0 - seg * per1) * 128;
+    k0 = (s0 - seg * per1) * SB;
     left = NSEG * per1 - s0 < KT ? NSEG * per1 - s0 : KT;
   }
   const void *pp = t.p[0], *qp = t.q[0];
@@ -130,17 +140,17 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
   };
   auto load = [&](char* buf, int i) {
     if (i < IP) {
-      const uint32_t off = pv[i & 1] + ((uint32_t)(i * 8) * t.ldp + (uint32_t)k0);
+      const uint32_t off = pv[i & 1] + ((uint32_t)(i * RI) * t.ldp + (uint32_t)k0);
       nt_load(nt_rsrc(pp, prec), buf + (wave * IP + i) * 1024, in[i & 1] ? off : OOB);
     } else {
       const int j = i - IP;
-      const uint32_t off = qv[j & 1] + ((uint32_t)(j * 8) * t.ldq + (uint32_t)k0);
-      nt_load(nt_rsrc(qp, qrec), buf + C::BP * 128 + (wave * IQ + j) * 1024,
+      const uint32_t off = qv[j & 1] + ((uint32_t)(j * RI) * t.ldq + (uint32_t)k0);
+      nt_load(nt_rsrc(qp, qrec), buf + C::BP * SB + (wave * IQ + j) * 1024,
               in[j & 1] ? off : OOB);
     }
   };
   auto advance = [&]() {
-    k0 += 128;
+    k0 += SB;
     --left;
     if (NSEG > 1 && k0 >= t.kbytes && seg + 1 < NSEG) {
       k0 = 0;
@@ -156,16 +166,17 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[a][b][e] = 0;
 
-  const int swz = (lrow >> 1) & 7;
   Frag fp[2][TP], fq[2][TQ];
-  auto fetch = [&](const char* buf, int ks, Frag (&p)[TP], Frag (&q)[TQ]) {
-    const int pos = ((ks * 2 + lhi) ^ swz) * 16;
-#pragma unroll
-    for (int b = 0; b < TQ; ++b)
-      q[b] = *reinterpret_cast<const Frag*>(buf + C::BP * 128 + ((wq * TQ + b) * 32 + lrow) * 128 + pos);
-#pragma unroll
-    for (int a = 0; a < TP; ++a)
-      p[a] = *reinterpret_cast<const Frag*>(buf + ((wp * TP + a) * 32 + lrow) * 128 + pos);
+  // byte of this lane's fragment of sub-step ks in a block of 32 rows
+  auto place = [&](int ks) {
+    if (SB == 128) return lrow * 128 + ((ks * 2 + lhi) ^ ((lrow >> 1) & 7)) * 16;
+    return (lrow >> 1) * 128 + (((lrow & 1) * 4 + ks * 2 + lhi) ^ ((lrow >> 2) & 3)) * 16;
+  };
+  auto fetch_p = [&](const char* buf, int ks, int a) {
+    return *reinterpret_cast<const Frag*>(buf + (wp * TP + a) * 32 * SB + place(ks));
+  };
+  auto fetch_q = [&](const char* buf, int ks, int b) {
+    return *reinterpret_cast<const Frag*>(buf + C::BP * SB + (wq * TQ + b) * 32 * SB + place(ks));
   };
   // One sub-step: the products of one set of fragments, between them the reads of
   // the next set (sub-step ks of `from`) and loads L0 .. L1 - 1 into `to`, an
@@ -174,7 +185,6 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
   auto substep = [&](const Frag (&p)[TP], const Frag (&q)[TQ], const char* from, int ks,
                      Frag (&np)[TP], Frag (&nq)[TQ], char* to, auto l0, auto l1) {
     constexpr int M = TP * TQ, R = TP + TQ, L0 = decltype(l0)::value, V = decltype(l1)::value - L0;
-    const int pos = ((ks * 2 + lhi) ^ swz) * 16;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
       const int a = i / TQ, b = i % TQ;
@@ -182,11 +192,9 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
 #pragma unroll
       for (int r = R * i / M; r < R * (i + 1) / M; ++r) {
         if (r < TQ)
-          nq[r < TQ ? r : 0] = *reinterpret_cast<const Frag*>(
-              from + C::BP * 128 + ((wq * TQ + r) * 32 + lrow) * 128 + pos);
+          nq[r < TQ ? r : 0] = fetch_q(from, ks, r);
         else
-          np[r < TQ ? 0 : r - TQ] = *reinterpret_cast<const Frag*>(
-              from + ((wp * TP + r - TQ) * 32 + lrow) * 128 + pos);
+          np[r < TQ ? 0 : r - TQ] = fetch_p(from, ks, r - TQ);
       }
 #pragma unroll
       for (int v = V * i / M; v < V * (i + 1) / M; ++v) load(to, L0 + v);
@@ -207,19 +215,24 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
   constexpr int WAIT = (0x0 << 8) | (0x7 << 4) | (OUT & 0xF) | ((OUT >> 4) << 14);
   __builtin_amdgcn_s_waitcnt(WAIT);
   nt_barrier();
-  fetch(lds, 0, fp[0], fq[0]);
+#pragma unroll
+  for (int b = 0; b < TQ; ++b) fq[0][b] = fetch_q(lds, 0, b);
+#pragma unroll
+  for (int a = 0; a < TP; ++a) fp[0][a] = fetch_p(lds, 0, a);
   int rd = 0, wr = S - 1;
   for (int kt = 0; kt < KT; ++kt) {
     const char* cur = lds + rd * C::STAGE;
     char* nxt = lds + wr * C::STAGE;
     constexpr std::integral_constant<int, 0> L0{};
-    constexpr std::integral_constant<int, (I + 1) / 2> L1{};
+    constexpr std::integral_constant<int, SB == 64 ? I : (I + 1) / 2> L1{};
     constexpr std::integral_constant<int, I> L2{};
     begin();
     substep(fp[0], fq[0], cur, 1, fp[1], fq[1], nxt, L0, L1);
-    substep(fp[1], fq[1], cur, 2, fp[0], fq[0], nxt, L1, L2);
+    if constexpr (SB == 128) {
+      substep(fp[1], fq[1], cur, 2, fp[0], fq[0], nxt, L1, L2);
+      substep(fp[0], fq[0], cur, 3, fp[1], fq[1], nxt, L2, L2);
+    }
     advance();
-    substep(fp[0], fq[0], cur, 3, fp[1], fq[1], nxt, L2, L2);
     // this wave's reads of the stage are complete and its part of the next one
     // has landed: publish it, and free this stage
     __builtin_amdgcn_s_waitcnt(WAIT);
@@ -269,18 +282,21 @@ __device__ __forceinline__ void nt_wave_sync() {
 // products leave rows p = 8 (e/4) + 4 (l/32) + e%4 of column q = l%32 in lane l, so
 // that memory would see runs of 32 bytes; through LDS each lane gets 8 consecutive
 // p of one q and 4 TP lanes a whole run of 32 TP:
-//   epi.apply(b, i, p, q, v, out)  v[8] the sums of block b, pass i = 0 .. 2 TP - 1;
-//                                  stores there what goes out[q][p ..], and sets
-//                                  out[PARTS] for `mirror`
-//   epi.load(b, i, p, q)           the same one block ahead: reads what apply needs
-// With `mirror`, out is also stored transposed, mir[s][p * ldm + q] (its 16-byte
-// chunks in LDS exclusive-ored with the row, since the writes step 8 rows a lane).  Blocks of 32
-// rows or columns past plim, qlim are left out (apply and load guard within them).
+//   epi.load(p, q)                what compute needs of memory, read a group of
+//                                 passes ahead; any p, q (reads within bounds)
+//   epi.compute(p, q, v, pre, out) out[OUTS] from the sums v[8]; any p, q
+//   epi.store(p, q, out)          what goes out[q][p ..], if p and q are within
+//   epi.diagonal(q, v)            (DIAGONAL) the sum of p = q
+// With `mirror`, out[0 .. PARTS - 1] are also stored transposed, mir[s][p * ldm + q]
+// (their 16-byte chunks in LDS exclusive-ored with the row, since the writes step 8
+// rows a lane), where p < plim and q < qlim.
+// A workgroup runs this once, at one wave a SIMD for the large tiles: the passes of
+// a group are done side by side without branches, so that they hide each other's
+// latency (one at a time with a test each: 4 us a pass of a 256 x 256 tile).
 template <class C, int PARTS>
 struct NtEpi {
-  static constexpr int TP = C::TP, TQ = C::TQ;
-  static constexpr int GB = TQ % 2 == 0 && PARTS == 1 ? 2 : 1;  // blocks a mirrored run
-  static constexpr int FLD = 32 * TP + 4, MLD = 32 * GB + 8;    // floats, halves
+  static constexpr int TP = C::TP, TQ = C::TQ, U = TP;
+  static constexpr int FLD = 32 * TP + 4, MLD = 40;  // floats, halves
   static constexpr int WAVE = 32 * FLD * 4 + PARTS * 32 * TP * MLD * 2;
   static constexpr int LDS = WAVE * C::WAVES > C::LDS ? WAVE * C::WAVES : C::LDS;
   static_assert(LDS * C::OCC <= 160 * 1024, "LDS");
@@ -289,75 +305,110 @@ struct NtEpi {
 template <class C, int PARTS, class Acc, class Epi>
 __device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* lds, int p0, int q0,
                                          int plim, int qlim, bool mirror, h16* const (&mir)[PARTS],
-                                         int ldm, Epi& epi) {
+                                         int ldm, const Epi& epi) {
   typedef NtEpi<C, PARTS> E;
-  constexpr int TP = E::TP, TQ = E::TQ, GB = E::GB, FLD = E::FLD, MLD = E::MLD;
-  constexpr int CPR = 4 * TP, IT = 2 * TP;  // chunks of a run, passes of a block
+  constexpr int TP = E::TP, TQ = E::TQ, U = E::U, FLD = E::FLD, MLD = E::MLD;
+  constexpr int CPR = 4 * TP;  // chunks of a run; 2 TP passes a block, U at a time
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int lrow = lane & 31, lhi = lane >> 5;
   typedef decltype(acc[0][0][0] + 0) V;
+  typedef V V4 __attribute__((ext_vector_type(4)));
   V* const f = reinterpret_cast<V*>(lds + wave * E::WAVE);
   h16* const m = reinterpret_cast<h16*>(f + 32 * FLD);
-  auto load = [&](int b) {
+  typename Epi::Pre pre[U];
+  // passes n U .. n U + U - 1 of the wave's 2 TP TQ: columns and chunks' first rows
+  auto load = [&](int n) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int r = (i * 64 + lane) / CPR, c = (i * 64 + lane) % CPR;
-      if (b < TQ) epi.load(b, i, p0 + 8 * c, q0 + 32 * b + r);
+    for (int u = 0; u < U; ++u) {
+      const int i = (n % 2) * U + u;
+      pre[u] = epi.load(p0 + 8 * ((i * 64 + lane) % CPR), q0 + 32 * (n / 2) + (i * 64 + lane) / CPR);
     }
   };
   load(0);
-#pragma unroll
+#pragma unroll 1
   for (int b = 0; b < TQ; ++b) {
-    load(b + 1);
 #pragma unroll
-    for (int a = 0; a < TP; ++a)
+    for (int s = 0; s < TQ; ++s) {
+      if (s != b) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        typedef V V4 __attribute__((ext_vector_type(4)));
-        const V4 v = {acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2],
-                      acc[a][b][4 * e + 3]};
-        *reinterpret_cast<V4*>(f + lrow * FLD + 32 * a + 8 * e + 4 * lhi) = v;
-      }
+      for (int a = 0; a < TP; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const V4 v = {acc[a][s][4 * e], acc[a][s][4 * e + 1], acc[a][s][4 * e + 2],
+                        acc[a][s][4 * e + 3]};
+          *reinterpret_cast<V4*>(f + lrow * FLD + 32 * a + 8 * e + 4 * lhi) = v;
+        }
+    }
     nt_wave_sync();
+    const int qb = q0 + 32 * b;
+    if constexpr (Epi::DIAGONAL) {
+      if (qb >= p0 && qb < p0 + 32 * TP) {
+        if (lane < 32) epi.diagonal(qb + lane, f[lane * FLD + qb - p0 + lane]);
+      }
+    }
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+      typename Epi::Pre now[U];
+      V v[U][8];
+      V8 out[U][Epi::OUTS];
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int r = (i * 64 + lane) / CPR, c = (i * 64 + lane) % CPR;
-      V v[8];
-      __builtin_memcpy(v, f + r * FLD + 8 * c, 32);
-      V8 out[PARTS];
-      epi.apply(b, i, p0 + 8 * c, q0 + 32 * b + r, v, out);
-      if (mirror) {
+      for (int u = 0; u < U; ++u) {
+        const int r = ((h * U + u) * 64 + lane) / CPR, c = ((h * U + u) * 64 + lane) % CPR;
+        const V4* from = reinterpret_cast<const V4*>(f + r * FLD + 8 * c);
+        const V4 x = from[0], y = from[1];
 #pragma unroll
-        for (int s = 0; s < PARTS; ++s)
+        for (int k = 0; k < 4; ++k) {
+          v[u][k] = x[k];
+          v[u][4 + k] = y[k];
+        }
+        now[u] = pre[u];
+      }
+      if (2 * b + h + 1 < 2 * TQ) load(2 * b + h + 1);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            m[s * 32 * TP * MLD + (8 * c + e) * MLD + (((4 * (b % GB) + r / 8) ^ ((c >> 1) & (4 * GB - 1))) * 8) +
-              r % 8] = out[s].h[e];
+      for (int u = 0; u < U; ++u) {
+        const int r = ((h * U + u) * 64 + lane) / CPR, c = ((h * U + u) * 64 + lane) % CPR;
+        epi.compute(p0 + 8 * c, qb + r, v[u], now[u], out[u]);
+        if (mirror) {
+#pragma unroll
+          for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              m[s * 32 * TP * MLD + (8 * c + e) * MLD + ((r / 8) ^ ((c >> 1) & 3)) * 8 + r % 8] =
+                  out[u][s].h[e];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int r = ((h * U + u) * 64 + lane) / CPR, c = ((h * U + u) * 64 + lane) % CPR;
+        epi.store(p0 + 8 * c, qb + r, out[u]);
       }
     }
     nt_wave_sync();
-    if (mirror && b % GB == GB - 1) {
-      constexpr int MC = 4 * GB;  // chunks of a mirrored run
+    if (mirror) {
 #pragma unroll
-      for (int s = 0; s < PARTS; ++s)
+      for (int s = 0; s < PARTS; ++s) {
+        V8 w[2 * TP];
 #pragma unroll
-        for (int i = 0; i < 32 * TP * MC / 64; ++i) {
-          const int r = (i * 64 + lane) / MC, c = (i * 64 + lane) % MC;
-          const int q = q0 + 32 * (b - GB + 1) + 8 * c;
-          if (p0 + r < plim && q < qlim)
-            store16(mir[s] + (int64_t)(p0 + r) * ldm + q,
-                    load16(m + s * 32 * TP * MLD + r * MLD + 8 * (c ^ ((r >> 4) & (4 * GB - 1)))));
+        for (int i = 0; i < 2 * TP; ++i) {
+          const int r = (i * 64 + lane) / 4, c = (i * 64 + lane) % 4;
+          w[i] = load16(m + s * 32 * TP * MLD + r * MLD + 8 * (c ^ ((r >> 4) & 3)));
         }
+#pragma unroll
+        for (int i = 0; i < 2 * TP; ++i) {
+          const int r = (i * 64 + lane) / 4, q = qb + 8 * ((i * 64 + lane) % 4);
+          if (p0 + r < plim && q < qlim) store16(mir[s] + (int64_t)(p0 + r) * ldm + q, w[i]);
+        }
+      }
       nt_wave_sync();
     }
   }
 }
 
-//             waves  tile  stages  groups  workgroups a CU
-typedef NtCfg<2, 2, 4, 4, 2, 1, 1> Nt256;   // 256 x 256
-typedef NtCfg<2, 2, 3, 3, 3, 1, 1> Nt192;   // 192 x 192
-typedef NtCfg<2, 2, 2, 2, 2, 1, 2> Nt128;   // 128 x 128
-typedef NtCfg<2, 2, 1, 1, 3, 1, 3> Nt64;    // 64 x 64
-typedef NtCfg<2, 2, 1, 1, 2, 4, 1> Nt64k;   // 64 x 64, the reduction split in four
+//            waves  tile  slice  stages  groups  workgroups a CU
+typedef NtCfg<2, 2, 4, 4, 128, 2, 1, 1> Nt256;    // 256 x 256
+typedef NtCfg<2, 2, 3, 3, 128, 3, 1, 1> Nt192;    // 192 x 192
+typedef NtCfg<2, 2, 2, 2, 64, 5, 1, 2> Nt128;    // 128 x 128
+typedef NtCfg<2, 2, 1, 1, 128, 5, 1, 2> Nt64;    // 64 x 64
+typedef NtCfg<2, 2, 1, 1, 128, 5, 2, 1> Nt64k;   // 64 x 64, the reduction split in two
 
 }  // namespace fp16k

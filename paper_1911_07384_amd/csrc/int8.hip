@@ -225,35 +225,54 @@ __device__ __forceinline__ h16 i8_out(int acc, float sa, float sb, bool has_bias
 }
 
 // What a tile stores, see nt_store: p along a row of y.
-template <class C>
 struct I8Epi {
   const I8Product& g;
   bool whole, has_bias;
-  float sq[2][2 * C::TP], sp[2 * C::TP][8], bp[2 * C::TP][8];
+  static constexpr int OUTS = 1;
+  static constexpr bool DIAGONAL = false;
+  struct Pre {
+    float sq, sp[8];
+    V8 bp;
+  };
 
-  __device__ __forceinline__ void load(int b, int i, int p, int q) {
-    if (p >= g.n) return;
-    if (q < g.m) sq[b & 1][i] = g.sa[q];
-    if (b > 0) return;
+  __device__ __forceinline__ Pre load(int p, int q) const {
+    Pre r;
+    r.sq = g.sa[q < g.m ? q : 0];
+    p = p < g.n ? p : 0;
+    if (whole) {
+      const floatx4* sv = reinterpret_cast<const floatx4*>(g.sb + p);
+      const floatx4 x = sv[0], y = sv[1];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const bool in = p + k < g.n;
-      sp[i][k] = in ? g.sb[p + k] : 0.0f;
-      bp[i][k] = in && has_bias ? to_f32(g.bias[p + k]) : 0.0f;
+      for (int k = 0; k < 4; ++k) {
+        r.sp[k] = x[k];
+        r.sp[4 + k] = y[k];
+      }
+      if (has_bias) r.bp = load16(g.bias + p);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = p + k < g.n ? p + k : 0;
+        r.sp[k] = g.sb[i];
+        if (has_bias) r.bp.h[k] = g.bias[i];
+      }
     }
+    return r;
   }
-  __device__ __forceinline__ void apply(int b, int i, int p, int q, const int (&v)[8], V8 (&)[1]) {
-    if (p >= g.n || q >= g.m) return;
-    V8 o;
+  __device__ __forceinline__ void compute(int, int, const int (&v)[8], const Pre& pre,
+                                          V8 (&out)[1]) const {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o.h[k] = i8_out(v[k], sq[b & 1][i], sp[i][k], has_bias, bp[i][k]);
+    for (int k = 0; k < 8; ++k)
+      out[0].h[k] = i8_out(v[k], pre.sq, pre.sp[k], has_bias, to_f32(pre.bp.h[k]));
+  }
+  __device__ __forceinline__ void store(int p, int q, const V8 (&out)[1]) const {
+    if (p >= g.n || q >= g.m) return;
     h16* yp = g.y + (int64_t)q * g.n + p;
     if (whole) {
-      store16(yp, o);
+      store16(yp, out[0]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
-        if (p + k < g.n) yp[k] = o.h[k];
+        if (p + k < g.n) yp[k] = out[0].h[k];
     }
   }
 };
@@ -278,7 +297,7 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
   nt_product<NtByte, C, 1>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
   if (wave >= C::WAVES) return;
-  I8Epi<C> epi{g, g.n % 8 == 0, g.bias != nullptr};
+  const I8Epi epi{g, g.n % 8 == 0, g.bias != nullptr};
   h16* none[1] = {nullptr};
   nt_store<C, 1>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ, g.n,
                  g.m, false, none, 0, epi);
@@ -430,8 +449,8 @@ struct I8Tile {
 constexpr I8Tile kI8Tiles[6] = {{256, 1, 256, 1.15, 8.0, "tile 256"},
                                 {192, 1, 256, 0.75, 6.0, "tile 192"},
                                 {128, 1, 512, 0.72, 4.5, "tile 128"},
-                                {64, 1, 768, 0.40, 3.0, "tile 64"},
-                                {64, 4, 256, 0.30, 3.5, "tile 64 split"},
+                                {64, 1, 512, 0.40, 3.0, "tile 64"},
+                                {64, 2, 256, 0.30, 3.5, "tile 64 split"},
                                 {0, 8, 0, 0.0, 0.0, "few rows"}};
 
 // The one that finishes soonest by that estimate: rounds of workgroups over the

@@ -230,55 +230,72 @@ __device__ __forceinline__ void ns_triangle(int t, int* i, int* j) {
 }
 
 // What a tile of A (STEP 0) or B (STEP 1) stores, see nt_store.
-template <class C, int STEP, int PARTS>
+template <int STEP, int PARTS>
 struct NsSymEpi {
   int m;
   const h16 *ah, *al;  // A, for B
   h16 *oh, *ol;
   float *d, *e;
   float cb, cc;
-  V8 va[2][2 * C::TP], vl[PARTS == 2 ? 2 : 1][2 * C::TP];
+  static constexpr int OUTS = PARTS;
+  static constexpr bool DIAGONAL = true;
+  struct Pre {
+    V8 a[STEP == 1 ? PARTS : 1];
+    float dp[8], dq;
+  };
 
-  __device__ __forceinline__ void load(int b, int i, int p, int q) {
-    if (STEP == 0 || p >= m || q >= m) return;
-    const int64_t o = (int64_t)q * m + p;
-    va[b & 1][i] = load16(ah + o);
-    if (PARTS == 2) vl[PARTS == 2 ? b & 1 : 0][i] = load16(al + o);
-  }
-  __device__ __forceinline__ void apply(int b, int i, int p, int q, const float (&f)[8],
-                                        V8 (&out)[PARTS]) {
-    if (p >= m || q >= m) return;
-    const int64_t o = (int64_t)q * m + p;
-    float dp[8], dq = 0.0f;
+  __device__ __forceinline__ Pre load(int p, int q) const {
+    Pre r;
     if (STEP == 1) {
-      dq = d[q];
-      __builtin_memcpy(dp, d + p, 32);
+      p = p < m ? p : 0;
+      q = q < m ? q : 0;
+      const int64_t o = (int64_t)q * m + p;
+      r.a[0] = load16(ah + o);
+      if (PARTS == 2) r.a[PARTS - 1] = load16(al + o);
+      r.dq = d[q];
+      const floatx4* dv = reinterpret_cast<const floatx4*>(d + p);
+      const floatx4 x = dv[0], y = dv[1];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        r.dp[k] = x[k];
+        r.dp[4 + k] = y[k];
+      }
     }
+    return r;
+  }
+  __device__ __forceinline__ void compute(int p, int q, const float (&f)[8], const Pre& pre,
+                                          V8 (&out)[PARTS]) const {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       float r;
       if (STEP == 0) {
         r = f[k] * (kSa / (kSx * kSx));
-        if (p + k == q) {
-          d[q] = f[k] * (1.0f / (kSx * kSx));
-          r = 0.0f;
-        }
       } else {
-        float a = to_f32(va[b & 1][i].h[k]);
-        if (PARTS == 2) a += to_f32(vl[PARTS == 2 ? b & 1 : 0][i].h[k]);
+        float a = to_f32(pre.a[0].h[k]);
+        if (PARTS == 2) a += to_f32(pre.a[PARTS - 1].h[k]);
         a *= 1.0f / kSa;
         const float a2 = f[k] * (1.0f / (kSa * kSa));
-        r = kSb * __builtin_fmaf(cc, __builtin_fmaf(dq + dp[k], a, a2), cb * a);
-        if (p + k == q) {
-          e[q] = __builtin_fmaf(cc, __builtin_fmaf(dq, dq, a2), cb * dq);
-          r = 0.0f;
-        }
+        r = kSb * __builtin_fmaf(cc, __builtin_fmaf(pre.dq + pre.dp[k], a, a2), cb * a);
       }
+      if (p + k == q) r = 0.0f;
       out[0].h[k] = to_h16(r);
       if (PARTS == 2) out[PARTS - 1].h[k] = to_h16(r - to_f32(out[0].h[k]));
     }
+  }
+  __device__ __forceinline__ void store(int p, int q, const V8 (&out)[PARTS]) const {
+    if (p >= m || q >= m) return;
+    const int64_t o = (int64_t)q * m + p;
     store16(oh + o, out[0]);
     if (PARTS == 2) store16(ol + o, out[PARTS - 1]);
+  }
+  __device__ __forceinline__ void diagonal(int q, float v) const {
+    if (q >= m) return;
+    if (STEP == 0) {
+      d[q] = v * (1.0f / (kSx * kSx));
+    } else {
+      const float dq = d[q];
+      e[q] = __builtin_fmaf(cc, __builtin_fmaf(dq, dq, v * (1.0f / (kSa * kSa))), cb * dq);
+    }
   }
 };
 
@@ -320,7 +337,7 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, flo
   nt_product<NtHalf, C, PROD>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
   if (wave >= C::WAVES) return;
-  NsSymEpi<C, STEP, PARTS> epi;
+  NsSymEpi<STEP, PARTS> epi;
   epi.m = m;
   epi.ah = ah;
   epi.al = al;
@@ -339,7 +356,7 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, flo
 
 // What a tile of X' stores: X' as laid out in two parts (its transpose through
 // nt_store), or with LAST the weights' update or the result.
-template <class C, int PARTS, bool LAST>
+template <int PARTS, bool LAST>
 struct NsXEpi {
   int rows, cols, rp, cp, tall;
   const h16 *nh, *nl;
@@ -347,70 +364,82 @@ struct NsXEpi {
   const float* e;
   float ca, keep, alpha;
   bool update, whole;
-  V8 vh[2][2 * C::TP], vl[2][2 * C::TP], vw[LAST ? 2 : 1][2 * C::TP];
+  static constexpr int OUTS = 2;  // X' in two parts, or the weights in the first
+  static constexpr bool DIAGONAL = false;
+  struct Pre {
+    V8 h, l, w;
+    float e[8];
+  };
 
-  __device__ __forceinline__ void load(int b, int i, int p, int q) {
-    if (p >= cp || q >= rp) return;
-    const int64_t o = (int64_t)q * cp + p;
-    vh[b & 1][i] = load16(nh + o);
-    vl[b & 1][i] = load16(nl + o);
-    if (LAST && update && q < rows && p < cols) {
-      const h16* wp = w + (int64_t)q * cols + p;
+  __device__ __forceinline__ Pre load(int p, int q) const {
+    Pre r;
+    if (LAST && update) {
+      const int pw = p < cols ? p : 0, qw = q < rows ? q : 0;
+      const h16* wp = w + (int64_t)qw * cols + pw;
       if (whole) {
-        vw[LAST ? b & 1 : 0][i] = load16(wp);
+        r.w = load16(wp);
       } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (p + k < cols) vw[LAST ? b & 1 : 0][i].h[k] = wp[k];
+        for (int k = 0; k < 8; ++k) r.w.h[k] = wp[pw + k < cols ? k : 0];
+      }
+    }
+    p = p < cp ? p : 0;
+    q = q < rp ? q : 0;
+    const int64_t o = (int64_t)q * cp + p;
+    r.h = load16(nh + o);
+    r.l = load16(nl + o);
+    // (a tall matrix's diagonal runs along p)
+    const floatx4* ev = reinterpret_cast<const floatx4*>(e + (tall ? p : q & ~7));
+    const floatx4 x = ev[0], y = ev[1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      r.e[k] = x[k];
+      r.e[4 + k] = y[k];
+    }
+    if (!tall) {
+      float eq = r.e[0];
+#pragma unroll
+      for (int k = 1; k < 8; ++k) eq = (q & 7) == k ? r.e[k] : eq;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r.e[k] = eq;
+    }
+    return r;
+  }
+  __device__ __forceinline__ void compute(int p, int q, const float (&f)[8], const Pre& pre,
+                                          V8 (&out)[2]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float h = to_f32(pre.h.h[k]), l = to_f32(pre.l.h[k]), E = pre.e[k];
+      // (products = 1: the low part takes part in aX only, as in B'X)
+      const float y = __builtin_fmaf(PARTS == 2 ? ca + E : ca, l, f[k] * (1.0f / kSb));
+      const float x = __builtin_fmaf(ca + E, h, y);
+      if (!LAST) {
+        out[0].h[k] = to_h16(x);
+        out[1].h[k] = to_h16(x - to_f32(out[0].h[k]));
+      } else {
+        const float ox = x * (1.0f / kSx);
+        out[0].h[k] =
+            to_h16(update ? __builtin_fmaf(-alpha, ox, keep * to_f32(pre.w.h[k])) : alpha * ox);
       }
     }
   }
-  __device__ __forceinline__ void apply(int b, int i, int p, int q, const float (&f)[8],
-                                        V8 (&out)[PARTS]) {
-    // (X' comes out as zeros in the padding, which is part of the next operands)
-    if (LAST ? p >= cols || q >= rows : p >= cp || q >= rp) return;
-    const int64_t o = (int64_t)q * cp + p;
-    float x[8], ep[8];
-    if (tall) {
-      __builtin_memcpy(ep, e + p, 32);
-    } else {
-      const float eq = e[q];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) ep[k] = eq;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float h = to_f32(vh[b & 1][i].h[k]), l = to_f32(vl[b & 1][i].h[k]);
-      // (products = 1: the low part takes part in aX only, as in B'X)
-      const float y = __builtin_fmaf(PARTS == 2 ? ca + ep[k] : ca, l, f[k] * (1.0f / kSb));
-      x[k] = __builtin_fmaf(ca + ep[k], h, y);
-    }
+  __device__ __forceinline__ void store(int p, int q, const V8 (&out)[2]) const {
     if (!LAST) {
-      V8 lo;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        out[0].h[k] = to_h16(x[k]);
-        lo.h[k] = to_h16(x[k] - to_f32(out[0].h[k]));
-      }
-      if (PARTS == 2) out[PARTS - 1] = lo;
+      // (X' is zero in the padding, which is part of the next operands)
+      if (p >= cp || q >= rp) return;
+      const int64_t o = (int64_t)q * cp + p;
       store16(nho + o, out[0]);
-      store16(nlo + o, lo);
+      store16(nlo + o, out[1]);
+      return;
+    }
+    if (p >= cols || q >= rows) return;
+    h16* const wp = w + (int64_t)q * cols + p;
+    if (whole) {
+      store16(wp, out[0]);
     } else {
-      h16* const wp = w + (int64_t)q * cols + p;
-      V8 v;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float ox = x[k] * (1.0f / kSx);
-        v.h[k] = to_h16(update ? __builtin_fmaf(-alpha, ox, keep * to_f32(vw[LAST ? b & 1 : 0][i].h[k]))
-                               : alpha * ox);
-      }
-      if (whole) {
-        store16(wp, v);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (p + k < cols) wp[k] = v.h[k];
-      }
+      for (int k = 0; k < 8; ++k)
+        if (p + k < cols) wp[k] = out[0].h[k];
     }
   }
 };
@@ -459,7 +488,7 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
   // X as laid out, now and next; its low part is an operand (and alternates) only
   // with three products
   const int nc = tall ? cur : 0, nn = tall ? cur ^ 1 : 0, mn = tall ? 0 : cur ^ 1;
-  NsXEpi<C, PARTS, LAST> epi;
+  NsXEpi<PARTS, LAST> epi;
   epi.rows = j.rows;
   epi.cols = j.cols;
   epi.rp = j.rp;
@@ -492,8 +521,8 @@ int up(int v, int t) { return (v + t - 1) / t * t; }
 constexpr NsTile kNsTiles[5] = {{256, 1, 256, 1.15, 12.0},
                                 {192, 1, 256, 0.75, 9.0},
                                 {128, 1, 512, 0.72, 6.0},
-                                {64, 1, 768, 0.40, 4.0},
-                                {64, 4, 256, 0.30, 5.0}};
+                                {64, 1, 512, 0.40, 4.0},
+                                {64, 2, 256, 0.30, 5.0}};
 
 // The tile that a product of the set finishes soonest on, by that estimate: rounds
 // of workgroups over the device, or the longest reduction if that takes longer.
