@@ -204,9 +204,10 @@ const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_
   NsPlan plan;
   ns_make_plan(count, descs, products, &plan);
   char* at = name;
-  for (const NsTile& k : plan.kind)
-    at += snprintf(at, sizeof(name) - (size_t)(at - name), "%s%d%s", at == name ? "" : ", ", k.tile,
-                   k.groups > 1 ? " split" : "");
+  for (const NsTile& k : plan.kind) {
+    at += snprintf(at, sizeof(name) - (size_t)(at - name), "%s%s", at == name ? "" : ", ", k.name);
+    if (k.parts > 1) at += snprintf(at, sizeof(name) - (size_t)(at - name), " in %d", k.parts);
+  }
   return name;
 }
 

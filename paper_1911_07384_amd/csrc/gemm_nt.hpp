@@ -5,9 +5,8 @@
 // same way: a lane's fragment is 16 bytes of one row (8 halves or 16 integers),
 // a slice of the reduction is 128 bytes of every row.
 //
-// A workgroup owns BP x BQ outputs, WP x WQ waves TP x TQ tiles of 32 x 32 each; KG
-// such groups split the reduction where few tiles have a long one, and add up in
-// LDS.  The slices go through S stages of LDS, loaded past the registers
+// A workgroup owns BP x BQ outputs, WP x WQ waves TP x TQ tiles of 32 x 32 each, over
+// the whole reduction or one of several parts of it.  The slices go through S stages of LDS, loaded past the registers
 // (8 rows of one slice, 1 KB, an instruction and wave) S - 1 slices ahead and a
 // few between the products of every sub-step, one barrier a slice.  Rows of LDS
 // are whole 128-byte lines; the 16-byte chunk c of row r lies at c ^ ((r/2) % 8),
@@ -41,19 +40,16 @@ struct NtByte {  // 8-bit integers, 32-bit sums (exact below 2^31)
   }
 };
 
-template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int KG_, int OCC_>
+template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int OCC_>
 struct NtCfg {
-  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, SB = SB_, S = S_, KG = KG_, OCC = OCC_;
-  static constexpr int WAVES = WP * WQ;            // of one group
-  static constexpr int THREADS = 64 * WAVES * KG;
+  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, SB = SB_, S = S_, OCC = OCC_;
+  static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES;
   static constexpr int BP = 32 * TP * WP, BQ = 32 * TQ * WQ;
-  static constexpr int STAGE = (BP + BQ) * SB, RING = S * STAGE;
+  static constexpr int STAGE = (BP + BQ) * SB, LDS = S * STAGE;
   static constexpr int IP = BP * SB / (1024 * WAVES), IQ = BQ * SB / (1024 * WAVES);  // loads
-  static constexpr int LDS = KG * RING;
-  static constexpr int SUM = 1024 * TP * TQ * 4 * WAVES;  // one group's sums
   static_assert(SB == 64 || (SB == 128 && IP % 2 == 0 && IQ % 2 == 0), "the chunks' order");
   static_assert(IP * 1024 * WAVES == BP * SB && IQ * 1024 * WAVES == BQ * SB, "whole loads");
-  static_assert(LDS * OCC <= 160 * 1024 && (KG - 1) * SUM <= LDS, "LDS");
+  static_assert(LDS * OCC <= 160 * 1024, "LDS");
 };
 
 // One 16-byte-per-lane load from a buffer resource into LDS (1 KB a wave).
@@ -76,20 +72,19 @@ struct NtTile {
   uint32_t ldp, ldq;   // bytes from row to row, multiples of 16
   int prows, qrows;    // rows there are from the tile's first; others read as zeros
   int kbytes;          // of a row; a last chunk's bytes past it are multiplied too
+  int part, parts;     // which of so many ranges of the slices
 };
 
 template <class T, class C, int NSEG>
-__device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
+__device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
                                            typename T::Acc (&acc)[C::TP][C::TQ]) {
   typedef typename T::Frag Frag;
   constexpr int TP = C::TP, TQ = C::TQ, S = C::S, SB = C::SB, IP = C::IP, IQ = C::IQ, I = IP + IQ;
   constexpr uint32_t OOB = 0x80000000u;
   const int lane = threadIdx.x & 63;
-  const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wave = all % C::WAVES, grp = all / C::WAVES;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave / C::WQ, wq = wave % C::WQ;
   const int lrow = lane & 31, lhi = lane >> 5;
-  char* const lds = lds0 + grp * C::RING;
 
   // loads: an instruction fills 8 lines of 128 bytes, lane l the 16 bytes l % 8 of
   // line l / 8: rows RI (wave * I. + i) .. + RI - 1 (see the layout above)
@@ -112,17 +107,12 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
     pv[h] = (uint32_t)(wave * IP * RI + row) * t.ldp + (uint32_t)ck[h];
     qv[h] = (uint32_t)(wave * IQ * RI + row) * t.ldq + (uint32_t)ck[h];
   }
-  // the slices of all pairs in order, a range of them for each group
+  // the slices of all pairs in order, this part's range of them
   const int per1 = (t.kbytes + SB - 1) / SB;  // of one pair
-  const int KT = (NSEG * per1 + C::KG - 1) / C::KG;
-  int k0 = 0, seg = 0;  // the slice loaded next
-  int left = KT;        // and how many there are from it
-  if (C::KG > 1) {
-    const int s0 = grp * KT;
-    seg = s0 / per1;
-    k0 = (s0 - seg * per1) * SB;
-    left = NSEG * per1 - s0 < KT ? NSEG * per1 - s0 : KT;
-  }
+  const int KT = (NSEG * per1 + t.parts - 1) / t.parts;
+  int seg = t.part * KT / per1;                // the slice loaded next: its pair,
+  int k0 = (t.part * KT - seg * per1) * SB;    // its first byte,
+  int left = NSEG * per1 - t.part * KT < KT ? NSEG * per1 - t.part * KT : KT;  // and how many
   const void *pp = t.p[0], *qp = t.q[0];
   auto pair = [&]() {
 #pragma unroll
@@ -132,11 +122,11 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
         qp = t.q[s];
       }
   };
-  if (C::KG > 1) pair();
+  pair();
   bool in[2];
   auto begin = [&]() {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) in[h] = k0 + ck[h] < t.kbytes && (C::KG == 1 || left > 0);
+    for (int h = 0; h < 2; ++h) in[h] = left > 0 && k0 + ck[h] < t.kbytes;
   };
   auto load = [&](char* buf, int i) {
     if (i < IP) {
@@ -243,27 +233,6 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds0,
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // every load has landed and every read is done: LDS is free
-  if (C::KG > 1) {
-    // the groups' sums into the first one's, in order
-    typedef typename T::Acc Acc;
-    Acc* sums = reinterpret_cast<Acc*>(lds0);
-#pragma unroll
-    for (int a = 0; a < TP; ++a)
-#pragma unroll
-      for (int b = 0; b < TQ; ++b)
-        if (grp > 0) sums[(((grp - 1) * C::WAVES + wave) * TP * TQ + a * TQ + b) * 64 + lane] = acc[a][b];
-    __syncthreads();
-    if (grp == 0) {
-#pragma unroll
-      for (int g = 1; g < C::KG; ++g)
-#pragma unroll
-        for (int a = 0; a < TP; ++a)
-#pragma unroll
-          for (int b = 0; b < TQ; ++b)
-            acc[a][b] += sums[(((g - 1) * C::WAVES + wave) * TP * TQ + a * TQ + b) * 64 + lane];
-    }
-    __syncthreads();
-  }
 }
 
 // Workgroup b of a grid of 8 * ceil(n / 8): the workgroups that one XCD takes
@@ -404,11 +373,47 @@ __device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* l
   }
 }
 
-//            waves  tile  slice  stages  groups  workgroups a CU
-typedef NtCfg<2, 2, 4, 4, 128, 2, 1, 1> Nt256;    // 256 x 256
-typedef NtCfg<2, 2, 3, 3, 128, 3, 1, 1> Nt192;    // 192 x 192
-typedef NtCfg<2, 2, 2, 2, 64, 5, 1, 2> Nt128;    // 128 x 128
-typedef NtCfg<2, 2, 1, 1, 128, 5, 1, 2> Nt64;    // 64 x 64
-typedef NtCfg<2, 2, 1, 1, 128, 5, 2, 1> Nt64k;   // 64 x 64, the reduction split in two
+// The sums of a workgroup as they lie in registers, to memory and back, for a
+// reduction split over workgroups: 1 KB a wave and instruction.
+template <class C, class Acc>
+__device__ __forceinline__ void nt_put(const Acc (&acc)[C::TP][C::TQ], floatx4* to) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int a = 0; a < C::TP; ++a)
+#pragma unroll
+    for (int b = 0; b < C::TQ; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const floatx4 v = {acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2],
+                           acc[a][b][4 * e + 3]};
+        to[(((wave * C::TP + a) * C::TQ + b) * 4 + e) * 64 + lane] = v;
+      }
+}
+// One 32 x 32 tile (wave, a, b) of the sums that `parts` workgroups put there.
+template <class C>
+__device__ __forceinline__ floatx16 nt_get(const floatx4* from, int parts, int wave, int a, int b) {
+  const int lane = threadIdx.x & 63;
+  floatx16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) {
+    const floatx4* f = from + (size_t)s * (C::BP * C::BQ / 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const floatx4 v = f[(((wave * C::TP + a) * C::TQ + b) * 4 + e) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[4 * e + i] += v[i];
+    }
+  }
+  return acc;
+}
+
+//            waves  tile  slice  stages  workgroups a CU
+typedef NtCfg<4, 2, 2, 4, 128, 2, 1> Nt256;   // 256 x 256
+typedef NtCfg<2, 2, 3, 3, 128, 3, 1> Nt192;   // 192 x 192
+typedef NtCfg<2, 2, 2, 2, 128, 2, 2> Nt128;   // 128 x 128, two workgroups
+typedef NtCfg<2, 2, 2, 2, 128, 4, 1> Nt128d;  // 128 x 128, one, loads further ahead
+typedef NtCfg<2, 2, 1, 1, 128, 5, 2> Nt64;    // 64 x 64
 
 }  // namespace fp16k

@@ -293,10 +293,11 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
   nt.prows = g.n - pt;
   nt.qrows = g.m - qt;
   nt.kbytes = g.k;
+  nt.part = 0;
+  nt.parts = 1;
   intx16 acc[C::TP][C::TQ];
   nt_product<NtByte, C, 1>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
-  if (wave >= C::WAVES) return;
   const I8Epi epi{g, g.n % 8 == 0, g.bias != nullptr};
   h16* none[1] = {nullptr};
   nt_store<C, 1>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ, g.n,
@@ -439,53 +440,56 @@ hipError_t launch_i8_fused(const I8Product& a, const h16* x, hipStream_t st) {
 }
 
 namespace {
-// The tiles of a product: side, parts of the reduction, workgroups the device holds
-// at once, microseconds a 128-byte slice of the reduction and a launch take.
+// The square tiles of a product: workgroups a CU holds, microseconds that a
+// 128-byte slice of the reduction takes one workgroup alone and a CU whatever it
+// holds, and a launch takes besides.  Fits, e.g. to (us)
+//                              256   192   128  128 deep   64
+//   4096 x 4096 x 4096          65    81    75        89  127
+//   128 x 1000 x 2048 (train)   21    18    12        11    6
 struct I8Tile {
-  int tile, groups, slots;
-  double slice, fixed;
+  int side, occ;
+  double alone, cu, fixed;
   const char* name;
 };
-constexpr I8Tile kI8Tiles[6] = {{256, 1, 256, 1.15, 8.0, "tile 256"},
-                                {192, 1, 256, 0.75, 6.0, "tile 192"},
-                                {128, 1, 512, 0.72, 4.5, "tile 128"},
-                                {64, 1, 512, 0.40, 3.0, "tile 64"},
-                                {64, 2, 256, 0.30, 3.5, "tile 64 split"},
-                                {0, 8, 0, 0.0, 0.0, "few rows"}};
+constexpr int kI8Kinds = 5;
+constexpr I8Tile kI8Tiles[kI8Kinds + 1] = {
+    {256, 1, 1.10, 1.65, 11.0, "tile 256"},     {192, 1, 0.65, 1.10, 9.0, "tile 192"},
+    {128, 2, 0.60, 0.53, 7.0, "tile 128"},      {128, 1, 0.33, 0.62, 8.0, "tile 128 deep"},
+    {64, 2, 0.21, 0.24, 4.0, "tile 64"},        {0, 0, 0.0, 0.0, 0.0, "few rows"}};
 
-// The one that finishes soonest by that estimate: rounds of workgroups over the
-// device, or one workgroup's reduction if that takes longer.
-const I8Tile& i8_tile(int m, int n, int k) {
-  if (m <= kFewRows) return kI8Tiles[5];
+// The one that finishes soonest by that estimate: the work spread over the CUs (and
+// half a reduction for the last round), or one reduction if that takes longer.
+int i8_tile(int m, int n, int k) {
+  if (m <= kFewRows) return kI8Kinds;
   int best = 0;
   double bt = 0;
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 0; i < kI8Kinds; ++i) {
     const I8Tile& c = kI8Tiles[i];
-    const double tiles = (double)ceil_div(m, c.tile) * ceil_div(n, c.tile);
-    const double slices = ceil_div(ceil_div(k, 128), c.groups);
-    const double t = c.fixed + c.slice * slices * std::max(tiles / c.slots, 1.0);
+    const double tiles = (double)ceil_div(n, c.side) * ceil_div(m, c.side), slices = ceil_div(k, 128);
+    const double tail = tiles > 256.0 * c.occ ? 0.5 * c.alone : 0.0;
+    const double t = c.fixed + slices * std::max(c.alone, c.cu * tiles / 256.0 + tail);
     if (i == 0 || t < bt) {
       bt = t;
       best = i;
     }
   }
-  return kI8Tiles[best];
+  return best;
 }
 }  // namespace
 
-const char* i8_product_name(int m, int n, int k) { return i8_tile(m, n, k).name; }
+const char* i8_product_name(int m, int n, int k) { return kI8Tiles[i8_tile(m, n, k)].name; }
 
 hipError_t launch_i8_product(const I8Product& a, hipStream_t st) {
-  const I8Tile& c = i8_tile(a.m, a.n, a.k);
-  if (c.tile == 0) {
-    hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0,
-                       st, a, (const h16*)nullptr);
-    return hipGetLastError();
+  switch (i8_tile(a.m, a.n, a.k)) {
+    case 0: return i8_launch<Nt256>(a, st);
+    case 1: return i8_launch<Nt192>(a, st);
+    case 2: return i8_launch<Nt128>(a, st);
+    case 3: return i8_launch<Nt128d>(a, st);
+    case 4: return i8_launch<Nt64>(a, st);
   }
-  if (c.tile == 256) return i8_launch<Nt256>(a, st);
-  if (c.tile == 192) return i8_launch<Nt192>(a, st);
-  if (c.tile == 128) return i8_launch<Nt128>(a, st);
-  return c.groups == 1 ? i8_launch<Nt64>(a, st) : i8_launch<Nt64k>(a, st);
+  hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0, st,
+                     a, (const h16*)nullptr);
+  return hipGetLastError();
 }
 
 }  // namespace fp16k

@@ -37,6 +37,8 @@
 #include "gemm_nt.hpp"
 #include "products.hpp"
 
+#include <math.h>
+
 #include <algorithm>
 
 namespace fp16k {
@@ -46,13 +48,20 @@ constexpr float kSx = 4096.0f, kSa = 4096.0f, kSb = 2048.0f;
 
 struct NsDev {
   char* ws;
-  uint32_t table, map;  // in units of 256 bytes
+  uint32_t table, map, sums;  // in units of 256 bytes
   int tiles;
 };
 
 template <class T>
 __device__ __forceinline__ T* at(char* ws, uint32_t place) {
   return reinterpret_cast<T*>(ws + (size_t)place * 256);
+}
+
+// Tiles of one matrix in a launch for A (stage 0), B (1) or X' (2).
+__host__ __device__ inline int ns_tiles(const NsJob& j, int stage, int side) {
+  const int tr = (j.rp + side - 1) / side, tc = (j.cp + side - 1) / side;
+  const int tm = j.tall ? tc : tr;
+  return stage == 2 ? tr * tc : tm * (tm + 1) / 2;
 }
 
 // ---- pass 1: momentum, squares, and the table ---------------------------------
@@ -64,8 +73,8 @@ struct NsChunk {
 static_assert(sizeof(NsChunk) <= 3584, "kernel arguments");
 
 struct NsPlaces {
-  uint32_t table, map_sym, map_x, map_pre;
-  int tile_sym, tile_x;
+  uint32_t table, map[3], map_pre;
+  int side[3];
 };
 
 __device__ __forceinline__ double ns_block_sum(double v, double* red) {
@@ -103,12 +112,12 @@ __global__ __launch_bounds__(256) void ns_first(const NsChunk c, char* ws, NsPla
   if (blockIdx.x == 0) {
     const int idx = first + blockIdx.y;
     if (tid == 0) at<NsJob>(ws, pl.table)[idx] = j;
-    const int m = j.tall ? j.cp : j.rp, tm = (m + pl.tile_sym - 1) / pl.tile_sym;
-    const int nsym = tm * (tm + 1) / 2;
-    const int nx = ((j.rp + pl.tile_x - 1) / pl.tile_x) * ((j.cp + pl.tile_x - 1) / pl.tile_x);
+    for (int stage = 0; stage < 3; ++stage) {
+      const int n = ns_tiles(j, stage, pl.side[stage]);
+      uint16_t* const map = at<uint16_t>(ws, pl.map[stage]) + j.t[stage];
+      for (int i = tid; i < n; i += 256) map[i] = (uint16_t)idx;
+    }
     const int npre = (j.rp / 64) * (j.cp / 64);
-    for (int i = tid; i < nsym; i += 256) at<uint16_t>(ws, pl.map_sym)[j.t_sym + i] = (uint16_t)idx;
-    for (int i = tid; i < nx; i += 256) at<uint16_t>(ws, pl.map_x)[j.t_x + i] = (uint16_t)idx;
     for (int i = tid; i < npre; i += 256) at<uint16_t>(ws, pl.map_pre)[j.t_pre + i] = (uint16_t)idx;
   }
   const bool has_m = j.m != nullptr;
@@ -213,11 +222,9 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
 
 // ---- the three products of a step -----------------------------------------------
 
-// This workgroup's matrix and its tile of the launch, or null.
-__device__ __forceinline__ const NsJob* ns_job(const NsDev& dv, int* t) {
-  *t = nt_xcd(blockIdx.x, dv.tiles);
-  if (*t >= dv.tiles) return nullptr;
-  return at<NsJob>(dv.ws, dv.table) + at<uint16_t>(dv.ws, dv.map)[*t];
+// The matrix that tile t of the launch belongs to.
+__device__ __forceinline__ const NsJob& ns_job(const NsDev& dv, int t) {
+  return at<NsJob>(dv.ws, dv.table)[at<uint16_t>(dv.ws, dv.map)[t]];
 }
 
 // tile t of a lower triangle, rows in order
@@ -299,48 +306,41 @@ struct NsSymEpi {
   }
 };
 
-// A = X X^T (STEP 0) or B = bA + cA^2 (STEP 1), off the diagonal, and the diagonal.
-template <class C, int STEP, int PROD>
-__global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, float cb, float cc) {
-  constexpr int PARTS = PROD == 3 ? 2 : 1;
-  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PARTS>::LDS];
-  int t;
-  const NsJob* jp = ns_job(dv, &t);
-  if (!jp) return;
-  const NsJob& j = *jp;
+// The operands of one tile of A or B.
+template <int STEP, int PROD>
+__device__ __forceinline__ void ns_sym_tile(const NsDev& dv, const NsJob& j, int pt, int qt,
+                                            NtTile<PROD>* nt) {
   const int m = j.tall ? j.cp : j.rp, n = j.tall ? j.rp : j.cp;
-  int ti, tj;
-  ns_triangle(t - j.t_sym, &ti, &tj);
-  const int pt = ti * C::BP, qt = tj * C::BQ;
   // X as [m][n]: laid out so, or the transpose of a tall matrix
-  const h16* xh = at<h16>(dv.ws, j.tall ? j.mir[0] : j.nat[0]);
-  const h16* xl = at<h16>(dv.ws, j.tall ? j.mirl[0] : j.natl[0]);
-  const h16* ah = at<h16>(dv.ws, j.a);
-  const h16* al = at<h16>(dv.ws, j.al);
-  const h16* hi = STEP == 0 ? xh : ah;
-  const h16* lo = STEP == 0 ? xl : al;
+  const h16* hi = at<h16>(dv.ws, STEP == 1 ? j.a : j.tall ? j.mir[0] : j.nat[0]);
+  const h16* lo = at<h16>(dv.ws, STEP == 1 ? j.al : j.tall ? j.mirl[0] : j.natl[0]);
   const int k = STEP == 0 ? n : m;
-  NtTile<PROD> nt;
+  const int64_t po = (int64_t)pt * k, qo = (int64_t)qt * k;
   if (PROD == 3) {
-    nt.p[0] = hi + (int64_t)pt * k;
-    nt.q[0] = lo + (int64_t)qt * k;
-    nt.p[PROD / 2] = lo + (int64_t)pt * k;
-    nt.q[PROD / 2] = hi + (int64_t)qt * k;
+    nt->p[0] = hi + po;
+    nt->q[0] = lo + qo;
+    nt->p[PROD / 2] = lo + po;
+    nt->q[PROD / 2] = hi + qo;
   }
-  nt.p[PROD - 1] = hi + (int64_t)pt * k;
-  nt.q[PROD - 1] = hi + (int64_t)qt * k;
-  nt.ldp = nt.ldq = (uint32_t)k * 2u;
-  nt.prows = m - pt;
-  nt.qrows = m - qt;
-  nt.kbytes = k * 2;
-  floatx16 acc[C::TP][C::TQ];
-  nt_product<NtHalf, C, PROD>(nt, lds, acc);
-  const int wave = threadIdx.x >> 6;
-  if (wave >= C::WAVES) return;
+  nt->p[PROD - 1] = hi + po;
+  nt->q[PROD - 1] = hi + qo;
+  nt->ldp = nt->ldq = (uint32_t)k * 2u;
+  nt->prows = m - pt;
+  nt->qrows = m - qt;
+  nt->kbytes = k * 2;
+}
+
+// Stores a tile of A or B at rows p0, q0 (those of this wave).
+template <class C, int STEP, int PROD>
+__device__ __forceinline__ void ns_sym_out(const NsDev& dv, const NsJob& j, float cb, float cc,
+                                           const floatx16 (&acc)[C::TP][C::TQ], char* lds, int p0,
+                                           int q0, bool mirror) {
+  constexpr int PARTS = PROD == 3 ? 2 : 1;
+  const int m = j.tall ? j.cp : j.rp;
   NsSymEpi<STEP, PARTS> epi;
   epi.m = m;
-  epi.ah = ah;
-  epi.al = al;
+  epi.ah = at<h16>(dv.ws, j.a);
+  epi.al = at<h16>(dv.ws, j.al);
   epi.oh = at<h16>(dv.ws, STEP == 0 ? j.a : j.b);
   epi.ol = at<h16>(dv.ws, STEP == 0 ? j.al : j.bl);
   epi.d = at<float>(dv.ws, j.d);
@@ -350,8 +350,27 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, flo
   h16* mir[PARTS];
   mir[0] = epi.oh;
   mir[PARTS - 1] = PARTS == 2 ? epi.ol : epi.oh;
-  nt_store<C, PARTS>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ, m,
-                     m, ti != tj, mir, m, epi);
+  nt_store<C, PARTS>(acc, lds, p0, q0, m, m, mirror, mir, m, epi);
+}
+
+// A = X X^T (STEP 0) or B = bA + cA^2 (STEP 1), off the diagonal, and the diagonal.
+template <class C, int STEP, int PROD>
+__global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, float cb, float cc) {
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PROD == 3 ? 2 : 1>::LDS];
+  const int t = nt_xcd(blockIdx.x, dv.tiles);
+  if (t >= dv.tiles) return;
+  const NsJob& j = ns_job(dv, t);
+  int ti, tj;
+  ns_triangle(t - j.t[STEP], &ti, &tj);
+  NtTile<PROD> nt;
+  ns_sym_tile<STEP>(dv, j, ti * C::BP, tj * C::BQ, &nt);
+  nt.part = 0;
+  nt.parts = 1;
+  floatx16 acc[C::TP][C::TQ];
+  nt_product<NtHalf, C, PROD>(nt, lds, acc);
+  const int wave = threadIdx.x >> 6;
+  ns_sym_out<C, STEP, PROD>(dv, j, cb, cc, acc, lds, ti * C::BP + (wave / C::WQ) * 32 * C::TP,
+                            tj * C::BQ + (wave % C::WQ) * 32 * C::TQ, ti != tj);
 }
 
 // What a tile of X' stores: X' as laid out in two parts (its transpose through
@@ -444,23 +463,11 @@ struct NsXEpi {
   }
 };
 
-// X' = (a + E) X + B'X, tile rows p along the columns of the matrix as laid out and
-// q along its rows.
-template <class C, int PROD, bool LAST>
-__global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int cur, float ca,
-                                                           float keep) {
-  constexpr int PARTS = PROD == 3 ? 2 : 1;
-  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PARTS>::LDS];
-  int t;
-  const NsJob* jp = ns_job(dv, &t);
-  if (!jp) return;
-  const NsJob& j = *jp;
-  t -= j.t_x;
-  // four tiles of rows p at a time, their rows q in turn
-  const int tp = (j.cp + C::BP - 1) / C::BP, tq = (j.rp + C::BQ - 1) / C::BQ;
-  const int g = t / (4 * tq), w = t - g * 4 * tq;
-  const int gw = tp - 4 * g < 4 ? tp - 4 * g : 4;
-  const int pt = (4 * g + w % gw) * C::BP, qt = (w / gw) * C::BQ;
+// The operands of one tile of X'; rows p run along the columns of the matrix as
+// laid out, q along its rows.
+template <int PROD>
+__device__ __forceinline__ void ns_x_tile(const NsDev& dv, const NsJob& j, int cur, int pt, int qt,
+                                          NtTile<PROD>* nt) {
   const int tall = j.tall, m = tall ? j.cp : j.rp;
   const h16* bh = at<h16>(dv.ws, j.b);
   const h16* bl = at<h16>(dv.ws, j.bl);
@@ -468,23 +475,36 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
   const h16* xh = at<h16>(dv.ws, tall ? j.nat[cur] : j.mir[cur]);
   const h16* xl = at<h16>(dv.ws, tall ? j.natl[cur] : j.mirl[cur]);
   const int64_t po = (int64_t)pt * m, qo = (int64_t)qt * m;
-  NtTile<PROD> nt;
   if (PROD == 3) {
-    nt.p[0] = (tall ? bh : xh) + po;
-    nt.q[0] = (tall ? xl : bl) + qo;
-    nt.p[PROD / 2] = (tall ? bl : xl) + po;
-    nt.q[PROD / 2] = (tall ? xh : bh) + qo;
+    nt->p[0] = (tall ? bh : xh) + po;
+    nt->q[0] = (tall ? xl : bl) + qo;
+    nt->p[PROD / 2] = (tall ? bl : xl) + po;
+    nt->q[PROD / 2] = (tall ? xh : bh) + qo;
   }
-  nt.p[PROD - 1] = (tall ? bh : xh) + po;
-  nt.q[PROD - 1] = (tall ? xh : bh) + qo;
-  nt.ldp = nt.ldq = (uint32_t)m * 2u;
-  nt.prows = j.cp - pt;
-  nt.qrows = j.rp - qt;
-  nt.kbytes = m * 2;
-  floatx16 acc[C::TP][C::TQ];
-  nt_product<NtHalf, C, PROD>(nt, lds, acc);
-  const int wave = threadIdx.x >> 6;
-  if (wave >= C::WAVES) return;
+  nt->p[PROD - 1] = (tall ? bh : xh) + po;
+  nt->q[PROD - 1] = (tall ? xh : bh) + qo;
+  nt->ldp = nt->ldq = (uint32_t)m * 2u;
+  nt->prows = j.cp - pt;
+  nt->qrows = j.rp - qt;
+  nt->kbytes = m * 2;
+}
+
+// Tile t of X' of a matrix: four tiles of rows p at a time, their rows q in turn.
+template <class C>
+__device__ __forceinline__ void ns_x_place(const NsJob& j, int t, int* pt, int* qt) {
+  const int tp = (j.cp + C::BP - 1) / C::BP, tq = (j.rp + C::BQ - 1) / C::BQ;
+  const int g = t / (4 * tq), w = t - g * 4 * tq;
+  const int gw = tp - 4 * g < 4 ? tp - 4 * g : 4;
+  *pt = (4 * g + w % gw) * C::BP;
+  *qt = (w / gw) * C::BQ;
+}
+
+template <class C, int PROD, bool LAST>
+__device__ __forceinline__ void ns_x_out(const NsDev& dv, const NsJob& j, int cur, float ca,
+                                         float keep, const floatx16 (&acc)[C::TP][C::TQ], char* lds,
+                                         int p0, int q0) {
+  constexpr int PARTS = PROD == 3 ? 2 : 1;
+  const int tall = j.tall;
   // X as laid out, now and next; its low part is an operand (and alternates) only
   // with three products
   const int nc = tall ? cur : 0, nn = tall ? cur ^ 1 : 0, mn = tall ? 0 : cur ^ 1;
@@ -508,82 +528,200 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
   h16* mir[PARTS];
   mir[0] = at<h16>(dv.ws, j.mir[mn]);
   mir[PARTS - 1] = at<h16>(dv.ws, PARTS == 2 ? j.mirl[mn] : j.mir[mn]);
-  nt_store<C, PARTS>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ,
-                     j.cp, j.rp, !LAST, mir, j.rp, epi);
+  nt_store<C, PARTS>(acc, lds, p0, q0, j.cp, j.rp, !LAST, mir, j.rp, epi);
+}
+
+// X' = (a + E) X + B'X.
+template <class C, int PROD, bool LAST>
+__global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int cur, float ca,
+                                                           float keep) {
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PROD == 3 ? 2 : 1>::LDS];
+  const int t = nt_xcd(blockIdx.x, dv.tiles);
+  if (t >= dv.tiles) return;
+  const NsJob& j = ns_job(dv, t);
+  int pt, qt;
+  ns_x_place<C>(j, t - j.t[2], &pt, &qt);
+  NtTile<PROD> nt;
+  ns_x_tile(dv, j, cur, pt, qt, &nt);
+  nt.part = 0;
+  nt.parts = 1;
+  floatx16 acc[C::TP][C::TQ];
+  nt_product<NtHalf, C, PROD>(nt, lds, acc);
+  const int wave = threadIdx.x >> 6;
+  ns_x_out<C, PROD, LAST>(dv, j, cur, ca, keep, acc, lds, pt + (wave / C::WQ) * 32 * C::TP,
+                          qt + (wave % C::WQ) * 32 * C::TQ);
+}
+
+// Few tiles with a long reduction: each reduction in `parts` workgroups, whose sums
+// a second launch adds in order (64 x 64 of a tile a workgroup) and stores.  The
+// workgroups of one part are neighbours: they share operands in the L2.
+// (1000 x 2048, three products, A: 36 tiles of 96 slices; 26 us on 64 x 64 tiles.)
+template <int STAGE, int PROD>
+__global__ __launch_bounds__(Nt128d::THREADS, Nt128d::OCC) void ns_part(const NsDev dv, int cur,
+                                                                       int parts) {
+  typedef Nt128d C;
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int x = nt_xcd(blockIdx.x, dv.tiles * parts);
+  if (x >= dv.tiles * parts) return;
+  const int part = x / dv.tiles, t = x - part * dv.tiles;
+  const NsJob& j = ns_job(dv, t);
+  NtTile<PROD> nt;
+  if (STAGE < 2) {
+    int ti, tj;
+    ns_triangle(t - j.t[STAGE], &ti, &tj);
+    ns_sym_tile<STAGE>(dv, j, ti * C::BP, tj * C::BQ, &nt);
+  } else {
+    int pt, qt;
+    ns_x_place<C>(j, t - j.t[2], &pt, &qt);
+    ns_x_tile(dv, j, cur, pt, qt, &nt);
+  }
+  nt.part = part;
+  nt.parts = parts;
+  floatx16 acc[C::TP][C::TQ];
+  nt_product<NtHalf, C, PROD>(nt, lds, acc);
+  nt_put<C>(acc, at<floatx4>(dv.ws, dv.sums) + ((size_t)t * parts + part) * (C::BP * C::BQ / 4));
+}
+
+template <int STAGE, int PROD, bool LAST>
+__global__ __launch_bounds__(Nt64::THREADS) void ns_sum(const NsDev dv, int cur, int parts, float ca,
+                                                        float cb, float cc, float keep) {
+  typedef Nt128d C;
+  typedef NtCfg<2, 2, 1, 1, 128, 1, 1> O;  // 64 x 64, 32 x 32 a wave
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<O, PROD == 3 ? 2 : 1>::LDS];
+  const int t = blockIdx.x / C::WAVES, w = blockIdx.x % C::WAVES;  // tile and wave of it
+  const NsJob& j = ns_job(dv, t);
+  const int wave = threadIdx.x >> 6;
+  const floatx4* from = at<floatx4>(dv.ws, dv.sums) + (size_t)t * parts * (C::BP * C::BQ / 4);
+  floatx16 acc[1][1] = {{nt_get<C>(from, parts, w, wave / 2, wave % 2)}};
+  const int dp = (w / C::WQ) * 64 + (wave / 2) * 32, dq = (w % C::WQ) * 64 + (wave % 2) * 32;
+  if constexpr (STAGE < 2) {
+    int ti, tj;
+    ns_triangle(t - j.t[STAGE], &ti, &tj);
+    ns_sym_out<O, STAGE, PROD>(dv, j, cb, cc, acc, lds, ti * C::BP + dp, tj * C::BQ + dq, ti != tj);
+  } else {
+    int pt, qt;
+    ns_x_place<C>(j, t - j.t[2], &pt, &qt);
+    ns_x_out<O, PROD, LAST>(dv, j, cur, ca, keep, acc, lds, pt + dp, qt + dq);
+  }
 }
 
 // ---- the plan ------------------------------------------------------------------
 
 int up(int v, int t) { return (v + t - 1) / t * t; }
 
-// The tiles a product may run on: workgroups the device holds at once, microseconds
-// a 128-byte slice of the reduction takes and a launch takes besides.
-constexpr NsTile kNsTiles[5] = {{256, 1, 256, 1.15, 12.0},
-                                {192, 1, 256, 0.75, 9.0},
-                                {128, 1, 512, 0.72, 6.0},
-                                {64, 1, 512, 0.40, 4.0},
-                                {64, 2, 256, 0.30, 5.0}};
+// The tiles a product may run on.  Times of a 128-byte slice of the reduction in
+// microseconds: for one workgroup alone (alone), and for a CU whatever it holds (cu);
+// and of a launch besides, for A or B and for X', whose outputs read more.  They are
+// fits to what each tile took where it is at home and where it is not, e.g. (us)
+//                                     256   192   128  128 deep   64  128 in 7
+//   A, 4096 x 4096, products 1        107    82   120       113  162         -
+//   X', the same                      139   182   156       182  256         -
+//   A, 1000 x 2048, products 3        116    72    65        42   26        20
+//   X', the same                       76    55    40        31   27        31
+//   A, ResNet-50's 54 matrices         95    60    58        40   56         -
+//   X', the same                       93   115    92       101  116         -
+constexpr int kNsKinds = 6;
+constexpr NsTile kNsTiles[kNsKinds] = {{"256", 256, 1, 1, 1.10, 1.40, {30.0, 35.0}},
+                                       {"192", 192, 1, 1, 0.65, 0.98, {19.0, 29.0}},
+                                       {"128", 128, 1, 2, 0.70, 0.57, {7.0, 11.0}},
+                                       {"128 deep", 128, 1, 1, 0.33, 0.56, {11.0, 15.0}},
+                                       {"64", 64, 1, 2, 0.21, 0.26, {5.5, 5.5}},
+                                       {"128", 128, 2, 1, 0.33, 0.60, {10.0, 13.0}}};
 
-// The tile that a product of the set finishes soonest on, by that estimate: rounds
-// of workgroups over the device, or the longest reduction if that takes longer.
+// The tile that a product of the set finishes soonest on, by that estimate: the
+// work spread over the CUs (and half of the longest reduction for the last round),
+// or the longest reduction if that takes longer.  The last kind splits reductions in
+// as many parts as give every CU one; its sums go to memory and back.
 // stage 0: A, 1: B, 2: X'.
-NsTile ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, int products) {
-  NsTile best = kNsTiles[0];
+int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, int products,
+              NsTile* tile) {
+  constexpr double cus = 256.0;
+  int best = -1;
   double bt = 0;
-  for (const NsTile& c : kNsTiles) {
-    double work = 0, longest = 0;
-    for (int i = 0; i < count; ++i) {
-      const int m = up(std::min(rows[i], cols[i]), 64), n = up(std::max(rows[i], cols[i]), 64);
-      const double tm = ceil_div(m, c.tile), tn = ceil_div(n, c.tile);
-      const double k = ceil_div(products * ((stage == 0 ? n : m) / 64), c.groups);
-      work += (stage == 2 ? tm * tn : tm * (tm + 1) / 2) * k;
+  for (int i = 0; i < kNsKinds; ++i) {
+    NsTile c = kNsTiles[i];
+    double tiles = 0, work = 0, longest = 0;
+    for (int n = 0; n < count; ++n) {
+      const int r = up(rows[n], 64), l = up(cols[n], 64), m = std::min(r, l);
+      const double k = products * ((stage == 0 ? std::max(r, l) : m) / 64), tm = ceil_div(m, c.side);
+      const double t =
+          stage == 2 ? (double)ceil_div(l, c.side) * ceil_div(r, c.side) : tm * (tm + 1) / 2;
+      tiles += t;
+      work += t * k;
       longest = std::max(longest, k);
     }
-    const double t = c.fixed + c.slice * std::max(work / c.slots, longest);
-    if (bt == 0 || t < bt) {
+    double t = c.fixed[stage == 2];
+    if (c.parts > 1) {
+      c.parts = (int)std::min(std::min(cus / tiles, longest / 2), 16.0);
+      if (c.parts < 2) continue;
+      longest = ceil(longest / c.parts);
+      t += 2 * tiles * c.parts * (65536.0 / 4e6);
+    }
+    const double tail = tiles > cus * c.occ ? 0.5 * longest * c.alone : 0.0;
+    t += std::max(work / cus * c.cu + tail, longest * c.alone);
+    if (best < 0 || t < bt) {
       bt = t;
-      best = c;
+      best = i;
+      *tile = c;
     }
   }
   return best;
 }
 
+struct NsStep {
+  int stage, cur;
+  bool last;
+  float ca, cb, cc, keep;
+};
+
 template <class C, int PROD>
-void ns_launch(int stage, bool last, const NsDev& d, int cur, float ca, float cb, float cc,
-               float keep, hipStream_t st) {
+void ns_launch(const NsStep& s, const NsDev& d, hipStream_t st) {
   const dim3 grid((unsigned)(8 * ((d.tiles + 7) / 8))), block(C::THREADS);
-  if (stage == 0)
-    hipLaunchKernelGGL((ns_sym<C, 0, PROD>), grid, block, 0, st, d, cb, cc);
-  else if (stage == 1)
-    hipLaunchKernelGGL((ns_sym<C, 1, PROD>), grid, block, 0, st, d, cb, cc);
-  else if (!last)
-    hipLaunchKernelGGL((ns_x<C, PROD, false>), grid, block, 0, st, d, cur, ca, keep);
+  if (s.stage == 0)
+    hipLaunchKernelGGL((ns_sym<C, 0, PROD>), grid, block, 0, st, d, s.cb, s.cc);
+  else if (s.stage == 1)
+    hipLaunchKernelGGL((ns_sym<C, 1, PROD>), grid, block, 0, st, d, s.cb, s.cc);
+  else if (!s.last)
+    hipLaunchKernelGGL((ns_x<C, PROD, false>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
   else
-    hipLaunchKernelGGL((ns_x<C, PROD, true>), grid, block, 0, st, d, cur, ca, keep);
+    hipLaunchKernelGGL((ns_x<C, PROD, true>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
+}
+
+template <int STAGE, int PROD, bool LAST>
+void ns_launch_parts(const NsStep& s, const NsDev& d, int parts, hipStream_t st) {
+  hipLaunchKernelGGL((ns_part<STAGE, PROD>), dim3((unsigned)(8 * ((d.tiles * parts + 7) / 8))),
+                     dim3(Nt128d::THREADS), 0, st, d, s.cur, parts);
+  hipLaunchKernelGGL((ns_sum<STAGE, PROD, LAST>), dim3((unsigned)(d.tiles * Nt128d::WAVES)),
+                     dim3(Nt64::THREADS), 0, st, d, s.cur, parts, s.ca, s.cb, s.cc, s.keep);
 }
 
 template <int PROD>
 hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
-  const NsDev pre{ws, p.table, p.map_pre, p.n_pre};
+  const NsDev pre{ws, p.table, p.map_pre, 0, p.n_pre};
   hipLaunchKernelGGL((ns_split<PROD>), dim3((unsigned)p.n_pre), dim3(256), 0, st, pre, a.momentum,
                      a.nesterov);
-  const NsDev sym{ws, p.table, p.map_sym, p.n_sym}, x{ws, p.table, p.map_x, p.n_x};
-  for (int s = 0; s < a.steps; ++s) {
-    const float ca = a.coef[3 * s], cb = a.coef[3 * s + 1], cc = a.coef[3 * s + 2];
+  for (int i = 0; i < a.steps; ++i) {
     for (int stage = 0; stage < 3; ++stage) {
-      const NsDev& d = stage == 2 ? x : sym;
-      const NsTile& k = p.kind[stage];
-      const bool last = s + 1 == a.steps;
-      if (k.tile == 256)
-        ns_launch<Nt256, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
-      else if (k.tile == 192)
-        ns_launch<Nt192, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
-      else if (k.tile == 128)
-        ns_launch<Nt128, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
-      else if (k.groups == 1)
-        ns_launch<Nt64, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
-      else
-        ns_launch<Nt64k, PROD>(stage, last, d, s & 1, ca, cb, cc, a.keep, st);
+      const NsStep s{stage, i & 1, i + 1 == a.steps, a.coef[3 * i], a.coef[3 * i + 1],
+                     a.coef[3 * i + 2], a.keep};
+      const NsDev d{ws, p.table, p.map[stage], p.sums, p.tiles[stage]};
+      const int parts = p.kind[stage].parts;
+      switch (p.variant[stage]) {
+        case 0: ns_launch<Nt256, PROD>(s, d, st); break;
+        case 1: ns_launch<Nt192, PROD>(s, d, st); break;
+        case 2: ns_launch<Nt128, PROD>(s, d, st); break;
+        case 3: ns_launch<Nt128d, PROD>(s, d, st); break;
+        case 4: ns_launch<Nt64, PROD>(s, d, st); break;
+        default:
+          if (stage == 0)
+            ns_launch_parts<0, PROD, false>(s, d, parts, st);
+          else if (stage == 1)
+            ns_launch_parts<1, PROD, false>(s, d, parts, st);
+          else if (!s.last)
+            ns_launch_parts<2, PROD, false>(s, d, parts, st);
+          else
+            ns_launch_parts<2, PROD, true>(s, d, parts, st);
+      }
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -596,11 +734,8 @@ hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
 void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, NsPlan* plan) {
   NsPlan& P = *plan;
   P.count = count;
-  // (A and B share their tiles' map, so their tile sides are one choice)
-  P.kind[0] = ns_choose(0, count, rows, cols, products);
-  P.kind[1] = ns_choose(1, count, rows, cols, products);
-  if (P.kind[1].tile != P.kind[0].tile) P.kind[1] = P.kind[0];
-  P.kind[2] = ns_choose(2, count, rows, cols, products);
+  for (int stage = 0; stage < 3; ++stage)
+    P.variant[stage] = ns_choose(stage, count, rows, cols, products, &P.kind[stage]);
   // the longest products first
   for (int i = 0; i < count; ++i) P.order[i] = i;
   std::sort(P.order, P.order + count, [&](int x, int y) {
@@ -614,7 +749,7 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
     return (uint32_t)o;
   };
   P.table = take((uint64_t)count * sizeof(NsJob));
-  P.n_sym = P.n_x = P.n_pre = 0;
+  P.tiles[0] = P.tiles[1] = P.tiles[2] = P.n_pre = 0;
   for (int i = 0; i < count; ++i) {
     NsJob& j = P.jobs[i];
     const int o = P.order[i];
@@ -624,12 +759,12 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
     j.tall = j.rows > j.cols;
     j.rp = up(j.rows, 64);
     j.cp = up(j.cols, 64);
-    const int m = j.tall ? j.cp : j.rp, tm = ceil_div(m, P.kind[0].tile);
-    j.t_sym = P.n_sym;
-    j.t_x = P.n_x;
+    const int m = j.tall ? j.cp : j.rp;
+    for (int stage = 0; stage < 3; ++stage) {
+      j.t[stage] = P.tiles[stage];
+      P.tiles[stage] += ns_tiles(j, stage, P.kind[stage].side);
+    }
     j.t_pre = P.n_pre;
-    P.n_sym += tm * (tm + 1) / 2;
-    P.n_x += ceil_div(j.rp, P.kind[2].tile) * ceil_div(j.cp, P.kind[2].tile);
     P.n_pre += (j.rp / 64) * (j.cp / 64);
     const int64_t n = (int64_t)j.rows * j.cols;
     j.nparts = (int)std::min<int64_t>(kNsParts, (n + 8191) / 8192);
@@ -651,15 +786,20 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
     j.e = take((uint64_t)m * 4);
     j.part = take((uint64_t)j.nparts * 8);
   }
-  P.map_sym = take((uint64_t)P.n_sym * 2);
-  P.map_x = take((uint64_t)P.n_x * 2);
+  for (int stage = 0; stage < 3; ++stage) P.map[stage] = take((uint64_t)P.tiles[stage] * 2);
   P.map_pre = take((uint64_t)P.n_pre * 2);
+  size_t sums = 0;
+  for (int stage = 0; stage < 3; ++stage)
+    if (P.kind[stage].parts > 1)
+      sums = std::max(sums, (size_t)P.tiles[stage] * P.kind[stage].parts * 65536);
+  P.sums = take(sums);
   P.bytes = (size_t)off * 256;
 }
 
 hipError_t launch_ns(const NsPlan& p, const NsArgs& a, void* ws, hipStream_t st) {
   char* w = static_cast<char*>(ws);
-  const NsPlaces pl{p.table, p.map_sym, p.map_x, p.map_pre, p.kind[0].tile, p.kind[2].tile};
+  const NsPlaces pl{p.table, {p.map[0], p.map[1], p.map[2]}, p.map_pre,
+                    {p.kind[0].side, p.kind[1].side, p.kind[2].side}};
   for (int first = 0; first < p.count; first += kJobsPerLaunch) {
     NsChunk c{};
     const int n = std::min(kJobsPerLaunch, p.count - first);

@@ -31,19 +31,23 @@ struct NsJob {
   uint32_t d, e;                              // their diagonals, float32
   uint32_t part;                              // float64 partial sums
   int nparts;
-  int t_sym, t_x, t_pre;  // first tile of this matrix in each kind of launch
+  int t[3], t_pre;  // its first tile in the launches for A, B, X' and the first pass
 };
 
+// A square tile that a product may run on: its side, the parts of the reduction,
+// workgroups a CU holds, and times in microseconds (see ns_choose).
 struct NsTile {
-  int tile, groups, slots;  // side, parts of the reduction, workgroups at once
-  double slice, fixed;      // microseconds: a slice of the reduction, a launch
+  const char* name;
+  int side, parts, occ;
+  double alone, cu, fixed[2];
 };
 
 struct NsPlan {
   NsTile kind[3];              // of A, B and X'
+  int variant[3];              // their places in the list of tiles
   int count;
-  int n_sym, n_x, n_pre;       // tiles of a symmetric product, of X', of the first pass
-  uint32_t table, map_sym, map_x, map_pre;  // in the workspace
+  int tiles[3], n_pre;         // in all
+  uint32_t table, map[3], map_pre, sums;  // in the workspace
   size_t bytes;
   int order[kNsMaxJobs];       // jobs[i] is the caller's matrix order[i]
   NsJob jobs[kNsMaxJobs];
