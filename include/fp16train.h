@@ -486,8 +486,7 @@ const char* fp16_conv_kernel(const fp16_conv_desc* desc, int32_t pass, int32_t f
 /* One matrix, row-major and contiguous, 1 <= rows, cols <= 65536, the shorter
  * side at most 16384 and rows * cols < 2^30.  scale multiplies its
  * orthogonalised update (finite): often sqrt(max(1, rows / cols)).  Matrices need
- * the alignment of an element only (views into a flat parameter buffer); where they
- * are 16-byte aligned and cols is a multiple of 8 they move 16 bytes at a time. */
+ * the alignment of an element only (views into a flat parameter buffer). */
 typedef struct {
   int32_t rows, cols;
   float scale;
@@ -555,7 +554,7 @@ size_t fp16_int8_row_bytes(int32_t n);
  *   q[i][j]  = 127 x[i][j] / max_j |x[i][j]| to the nearest integer, ties to even
  * A zero row has scale 0 and q 0; a row with an infinity or a NaN has scale NaN
  * and q 0, so that every product with it is NaN.  q is [rows][cols] as above.
- * 1 <= rows, cols < 2^24, rows * cols < 2^40 (FP16_ERR_SHAPE). */
+ * 1 <= rows, cols < 2^22, rows * cols < 2^40 (FP16_ERR_SHAPE). */
 fp16_status fp16_int8_quant_rows(int32_t rows, int32_t cols, const fp16_t* x, int8_t* q,
                                  float* scale, fp16_stream_t stream);
 
@@ -568,7 +567,7 @@ fp16_status fp16_int8_quant_cols(int32_t rows, int32_t cols, const fp16_t* x, in
 /* The product of quantised a [m][k] and b [n][k]:
  *   y[i][j] = round_to_binary16(fl(sa[i] * sb[j]) * fl(sum_k a[i][k] * b[j][k]) + bias[j])
  * with the sum exact in 32 bits and the rest in float32; bias [n] may be NULL.
- * y is [m][n].  1 <= m, n < 2^24, 1 <= k <= 131071, m * n < 2^40
+ * y is [m][n].  1 <= m, n < 2^22, 1 <= k <= 131071, m * n < 2^40
  * (FP16_ERR_SHAPE).  In every row of a or of b the bytes past k must be zero.  y
  * must not overlap an input. */
 fp16_status fp16_int8_matmul(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa,

@@ -96,8 +96,6 @@ fp16_status ns_call(int32_t count, const fp16_muon_desc* descs, fp16_t* const* w
     plan.jobs[i].g = reinterpret_cast<const h16*>(g[o]);
     plan.jobs[i].w = reinterpret_cast<h16*>(w[o]);
     plan.jobs[i].m = update ? reinterpret_cast<h16*>(m[o]) : nullptr;
-    plan.jobs[i].aligned = aligned16(w[o]) && aligned16(g[o]) && (!update || aligned16(m[o]));
-    plan.jobs[i].whole = plan.jobs[i].aligned && descs[o].cols % 8 == 0;
     plan.jobs[i].alpha = update ? lr * descs[o].scale : descs[o].scale;
   }
   NsArgs a;
@@ -113,7 +111,7 @@ fp16_status ns_call(int32_t count, const fp16_muon_desc* descs, fp16_t* const* w
 // ---- 8-bit integer dense layers -----------------------------------------------------
 
 bool i8_sides_ok(int64_t a, int64_t b) {
-  return a >= 1 && b >= 1 && a < (1 << 24) && b < (1 << 24) && a * b < ((int64_t)1 << 40);
+  return a >= 1 && b >= 1 && a < (1 << 22) && b < (1 << 22) && a * b < ((int64_t)1 << 40);
 }
 size_t i8_bytes(int64_t rows, int64_t n) { return (size_t)(rows * i8_row(n)); }
 
@@ -124,7 +122,7 @@ bool dense_ok(const fp16_int8_dense_desc* d) {
 
 // Workspace places of the three calls.
 struct DenseWs {
-  size_t q1 = 0, s1 = 0, q2 = 0, s2 = 0, cols = 0, total = 0;
+  size_t q1 = 0, s1 = 0, q2 = 0, s2 = 0, q3 = 0, s3 = 0, part = 0, part2 = 0, total = 0;
 };
 DenseWs dense_ws(const fp16_int8_dense_desc* d, int call) {
   DenseWs L;
@@ -135,20 +133,22 @@ DenseWs dense_ws(const fp16_int8_dense_desc* d, int call) {
     return at;
   };
   if (call == FP16_INT8_WEIGHTS) {
-    L.cols = take(i8_cols_ws_bytes(O, I));
+    L.part = take(i8_cols_ws_bytes(O, I, true, false));
   } else if (call == FP16_INT8_FWD) {
     if (!i8_fused_ok(T, O, I)) {
       L.q1 = take(i8_bytes(T, I));
       L.s1 = take((size_t)T * 4);
     }
   } else {
-    // dy by rows for dx, then dy and x by columns for dw in the same place
-    const size_t rows = i8_bytes(T, O), cols = i8_bytes(O, T);
-    L.q1 = take(std::max(rows, cols));
-    L.s1 = take((size_t)std::max(T, O) * 4);
-    L.q2 = take(i8_bytes(I, T));
-    L.s2 = take((size_t)I * 4);
-    L.cols = take(std::max(i8_cols_ws_bytes(T, O), i8_cols_ws_bytes(T, I)));
+    // dy by rows, dy by columns, x by columns
+    L.q1 = take(i8_bytes(T, O));
+    L.s1 = take((size_t)T * 4);
+    L.q2 = take(i8_bytes(O, T));
+    L.s2 = take((size_t)O * 4);
+    L.q3 = take(i8_bytes(I, T));
+    L.s3 = take((size_t)I * 4);
+    L.part = take(i8_cols_ws_bytes(T, O, true, true));
+    L.part2 = take(i8_cols_ws_bytes(T, I, false, false));
   }
   return L;
 }
@@ -241,14 +241,14 @@ fp16_status fp16_int8_quant_rows(int32_t rows, int32_t cols, const fp16_t* x, in
 }
 
 size_t fp16_int8_quant_workspace_bytes(int32_t rows, int32_t cols) {
-  return i8_sides_ok(rows, cols) ? i8_cols_ws_bytes(rows, cols) : 0;
+  return i8_sides_ok(rows, cols) ? i8_cols_ws_bytes(rows, cols, false, false) : 0;
 }
 
 fp16_status fp16_int8_quant_cols(int32_t rows, int32_t cols, const fp16_t* x, int8_t* q,
                                  float* scale, void* ws, size_t ws_bytes, fp16_stream_t stream) {
   if (!i8_sides_ok(rows, cols)) return FP16_ERR_SHAPE;
   if (!x || !q || !scale) return FP16_ERR_NULL;
-  const size_t need = i8_cols_ws_bytes(rows, cols);
+  const size_t need = i8_cols_ws_bytes(rows, cols, false, false);
   const fp16_status s = ws_ok(ws, ws_bytes, need);
   if (s != FP16_OK) return s;
   const Buf b[] = {{x, (size_t)rows * cols * 2, false},
@@ -257,8 +257,8 @@ fp16_status fp16_int8_quant_cols(int32_t rows, int32_t cols, const fp16_t* x, in
                    {ws, need, true}};
   if (!bufs_aligned(b)) return FP16_ERR_MISALIGNED;
   if (bufs_clash(b)) return FP16_ERR_ALIASING;
-  return hip_status(
-      launch_i8_cols(rows, cols, hp(x), q, scale, nullptr, ws, static_cast<hipStream_t>(stream)));
+  const I8Cols j = i8_cols_job(rows, cols, hp(x), q, scale, nullptr, nullptr, nullptr, ws);
+  return hip_status(launch_i8_cols(&j, 1, static_cast<hipStream_t>(stream)));
 }
 
 fp16_status fp16_int8_matmul(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa,
@@ -304,9 +304,9 @@ fp16_status fp16_int8_dense_weights(const fp16_int8_dense_desc* desc, const fp16
   if (!bufs_aligned(b)) return FP16_ERR_MISALIGNED;
   if (bufs_clash(b)) return FP16_ERR_ALIASING;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  TRY(launch_i8_rows(O, I, hp(w), wq, sw, st));
-  if (wqt) TRY(launch_i8_cols(O, I, hp(w), wqt, swt, nullptr, ws_at<void>(ws, L.cols), st));
-  return FP16_OK;
+  if (!wqt) return hip_status(launch_i8_rows(O, I, hp(w), wq, sw, st));
+  const I8Cols j = i8_cols_job(O, I, hp(w), wqt, swt, wq, sw, nullptr, ws_at<void>(ws, L.part));
+  return hip_status(launch_i8_cols(&j, 1, st));
 }
 
 fp16_status fp16_int8_dense_fwd(const fp16_int8_dense_desc* desc, const fp16_t* x, const int8_t* wq,
@@ -357,17 +357,23 @@ fp16_status fp16_int8_dense_bwd(const fp16_int8_dense_desc* desc, const fp16_t* 
   if (!bufs_aligned(b)) return FP16_ERR_MISALIGNED;
   if (bufs_clash(b)) return FP16_ERR_ALIASING;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  int8_t *q1 = ws_at<int8_t>(ws, L.q1), *q2 = ws_at<int8_t>(ws, L.q2);
-  float *s1 = ws_at<float>(ws, L.s1), *s2 = ws_at<float>(ws, L.s2);
-  if (dx) {
+  int8_t *q1 = ws_at<int8_t>(ws, L.q1), *q2 = ws_at<int8_t>(ws, L.q2), *q3 = ws_at<int8_t>(ws, L.q3);
+  float *s1 = ws_at<float>(ws, L.s1), *s2 = ws_at<float>(ws, L.s2), *s3 = ws_at<float>(ws, L.s3);
+  if (dw) {
+    const I8Cols j[2] = {i8_cols_job(T, O, hp(dy), q2, s2, dx ? q1 : nullptr, dx ? s1 : nullptr,
+                                     hp(dbias), ws_at<void>(ws, L.part)),
+                         i8_cols_job(T, I, hp(x), q3, s3, nullptr, nullptr, nullptr,
+                                     ws_at<void>(ws, L.part2))};
+    TRY(launch_i8_cols(j, 2, st));
+  } else if (dx) {
     TRY(launch_i8_rows(T, O, hp(dy), q1, s1, st));
+  }
+  if (dx) {
     const I8Product p{T, I, O, q1, wqt, s1, swt, nullptr, hp(dx)};
     TRY(launch_i8_product(p, st));
   }
   if (dw) {
-    TRY(launch_i8_cols(T, O, hp(dy), q1, s1, hp(dbias), ws_at<void>(ws, L.cols), st));
-    TRY(launch_i8_cols(T, I, hp(x), q2, s2, nullptr, ws_at<void>(ws, L.cols), st));
-    const I8Product p{O, I, T, q1, q2, s1, s2, nullptr, hp(dw)};
+    const I8Product p{O, I, T, q2, q3, s2, s3, nullptr, hp(dw)};
     TRY(launch_i8_product(p, st));
   }
   return FP16_OK;

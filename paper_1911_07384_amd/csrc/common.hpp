@@ -29,6 +29,14 @@ __device__ __forceinline__ void store16(void* p, const V8& v) {
   *reinterpret_cast<u32x4*>(p) = v.u;
 }
 
+// The same at any element's address (one access; it need not be aligned).
+__device__ __forceinline__ V8 load16u(const h16* p) {
+  V8 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+__device__ __forceinline__ void store16u(h16* p, const V8& v) { __builtin_memcpy(p, &v, 16); }
+
 __device__ __forceinline__ V8 zero8() {
   V8 v;
   v.u = u32x4{0u, 0u, 0u, 0u};

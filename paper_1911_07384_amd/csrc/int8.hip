@@ -38,13 +38,33 @@ __device__ __forceinline__ float i8_top(uint32_t mag) {
 __device__ __forceinline__ float i8_scale(uint32_t mag) {
   return mag >= 0x7c00u ? __builtin_nanf("") : i8_top(mag) / 127.0f;
 }
-// q of x for a row whose largest magnitude is `mag` (0 for a zero row and for one
-// that is not finite).
-__device__ __forceinline__ int i8_q(h16 x, float top, bool live) {
-  const float r = __builtin_rintf((127.0f * to_f32(x)) / top);
-  return live ? (int)r : 0;
+// A row's (or column's) quantiser: the quotient t = 127 x / top as x * 127 * inv and
+// one correction by its exact remainder, which leaves a halfway quotient exact and
+// any other within 2^-24 of it (a division costs three times as many instructions);
+// then t + 1.5 * 2^23, whose last byte is t to the nearest, ties to even.  inv = 0
+// for a zero row and for one that is not finite, which makes every byte 0 (a NaN's
+// last byte is 0 too).
+struct I8Quant {
+  float top, inv;
+};
+__device__ __forceinline__ I8Quant i8_quant(uint32_t mag) {
+  const bool live = mag != 0 && mag < 0x7c00u;
+  const float top = live ? i8_top(mag) : 0.0f;
+  return I8Quant{top, live ? 1.0f / top : 0.0f};
 }
-__device__ __forceinline__ bool i8_live(uint32_t mag) { return mag != 0 && mag < 0x7c00u; }
+// (x127: 127 x, exact)
+__device__ __forceinline__ uint32_t i8_byte(float x127, const I8Quant& k) {
+  const float t = x127 * k.inv;
+  const float u = __builtin_fmaf(__builtin_fmaf(-t, k.top, x127), k.inv, t) + 12582912.0f;
+  return __builtin_bit_cast(uint32_t, u);
+}
+__device__ __forceinline__ float i8_x127(h16 x) { return 127.0f * to_f32(x); }
+// the last bytes of four words
+__device__ __forceinline__ uint32_t i8_pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+  return lo | hi;
+}
 
 __device__ __forceinline__ uint32_t i8_wave_max(uint32_t v) {
 #pragma unroll
@@ -55,9 +75,9 @@ __device__ __forceinline__ uint32_t i8_wave_max(uint32_t v) {
   return v;
 }
 
-// eight elements from p of a row that ends `left` elements further on
-__device__ __forceinline__ V8 i8_load8(const h16* p, int left, bool whole) {
-  if (whole && left >= 8) return load16(p);
+// Eight elements from p of a row that ends `left` elements further on, zeros past it.
+__device__ __forceinline__ V8 i8_load8(const h16* p, int left) {
+  if (left >= 8) return load16u(p);
   V8 v = zero8();
 #pragma unroll
   for (int e = 0; e < 8; ++e)
@@ -65,11 +85,11 @@ __device__ __forceinline__ V8 i8_load8(const h16* p, int left, bool whole) {
   return v;
 }
 
-__device__ __forceinline__ uint2 i8_pack(const V8& v, float top, bool live) {
-  uint32_t w[2] = {0, 0};
+__device__ __forceinline__ uint2 i8_pack(const V8& v, const I8Quant& k) {
+  uint32_t b[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(uint8_t)i8_q(v.h[e], top, live) << (8 * (e & 3));
-  return make_uint2(w[0], w[1]);
+  for (int e = 0; e < 8; ++e) b[e] = i8_byte(i8_x127(v.h[e]), k);
+  return make_uint2(i8_pack4(b[0], b[1], b[2], b[3]), i8_pack4(b[4], b[5], b[6], b[7]));
 }
 
 // One workgroup a row; up to 8192 elements stay in registers between the maximum
@@ -82,58 +102,72 @@ __global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __re
   const int tid = threadIdx.x;
   const h16* xr = x + (int64_t)blockIdx.x * cols;
   int8_t* qr = q + (int64_t)blockIdx.x * ld;
-  const bool whole = cols % 8 == 0;
   V8 keep[kRowKeep];
   uint32_t mag = 0;
 #pragma unroll
   for (int i = 0; i < kRowKeep; ++i) {
     const int c = (i * 256 + tid) * 8;
-    keep[i] = c < cols ? i8_load8(xr + c, cols - c, whole) : zero8();
+    keep[i] = i8_load8(xr + (c < cols ? c : 0), cols - c);
   }
 #pragma unroll
   for (int i = 0; i < kRowKeep; ++i) mag = i8_mag8(keep[i], mag);
   for (int c = (kRowKeep * 256 + tid) * 8; c < cols; c += 2048)
-    mag = i8_mag8(i8_load8(xr + c, cols - c, whole), mag);
+    mag = i8_mag8(i8_load8(xr + c, cols - c), mag);
   mag = i8_wave_max(mag);
   if ((tid & 63) == 0) red[tid >> 6] = mag;
   __syncthreads();
   mag = std::max(std::max(red[0], red[1]), std::max(red[2], red[3]));
   if (tid == 0) scale[blockIdx.x] = i8_scale(mag);
-  const float top = i8_top(mag);
-  const bool live = i8_live(mag);
+  const I8Quant k = i8_quant(mag);
 #pragma unroll
   for (int i = 0; i < kRowKeep; ++i) {
     const int c = (i * 256 + tid) * 8;
-    if (c < ld) *reinterpret_cast<uint2*>(qr + c) = i8_pack(keep[i], top, live);
+    if (c < ld) *reinterpret_cast<uint2*>(qr + c) = i8_pack(keep[i], k);
   }
   for (int c = (kRowKeep * 256 + tid) * 8; c < ld; c += 2048)
-    *reinterpret_cast<uint2*>(qr + c) =
-        i8_pack(c < cols ? i8_load8(xr + c, cols - c, whole) : zero8(), top, live);
+    *reinterpret_cast<uint2*>(qr + c) = i8_pack(i8_load8(xr + (c < cols ? c : 0), cols - c), k);
 }
 
-// Columns, first pass: the largest magnitude (and the sum) of 256 columns over a
-// range of rows.  Thread: 8 columns, every eighth row.
-constexpr int kColChunks = 64;  // ranges of rows, at most
-__global__ __launch_bounds__(256) void i8_cols_max(int rows, int cols, int per,
-                                                   const h16* __restrict__ x,
-                                                   uint32_t* __restrict__ mag,
-                                                   float* __restrict__ sum) {
+// Columns, or rows and columns, of up to two matrices (blockIdx.z) in two passes.
+//
+// First pass: 256 columns of a range of rows a workgroup, a thread 8 columns of
+// every eighth row: the largest magnitude (and the sum) of each column over the
+// range and, for the rows, of each row over the 256 columns.
+constexpr int kColChunks = 16;  // ranges of rows, at most
+__global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
+  const I8Cols& j = both.job[blockIdx.z];
+  if ((int)blockIdx.x * 256 >= j.cols || (int)blockIdx.y >= j.chunks) return;
   __shared__ uint32_t rm[8][256];
   __shared__ float rs[8][256];
   const int tid = threadIdx.x, cg = tid & 31, rg = tid >> 5;
   const int c = blockIdx.x * 256 + cg * 8;
-  const bool whole = cols % 8 == 0;
-  const int r1 = std::min(rows, (int)(blockIdx.y + 1) * per);
+  const int r0 = blockIdx.y * j.per, r1 = std::min(j.rows, r0 + j.per);
+  const bool want_rows = j.rmag != nullptr, want_sum = j.psum != nullptr;
   uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (c < cols) {
-    for (int r = blockIdx.y * per + rg; r < r1; r += 8) {
-      const V8 v = i8_load8(x + (int64_t)r * cols + c, cols - c, whole);
+  constexpr int U = 4;
+  for (int r = r0 + rg; r < r1; r += 8 * U) {
+    V8 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = c < j.cols && r + 8 * u < r1 ? i8_load8(j.x + (int64_t)(r + 8 * u) * j.cols + c, j.cols - c)
+                                          : zero8();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t b = i8_mag(v.s[e]);
+        const uint32_t b = i8_mag(v[u].s[e]);
         m[e] = b > m[e] ? b : m[e];
-        s[e] += to_f32(v.h[e]);
+        if (want_sum) s[e] += to_f32(v[u].h[e]);
+      }
+      if (want_rows) {
+        uint32_t top = i8_mag8(v[u], 0);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+          const uint32_t o = (uint32_t)__shfl_xor((int)top, off, 64);
+          top = o > top ? o : top;
+        }
+        if (cg == 0 && r + 8 * u < r1) j.rmag[(int64_t)blockIdx.x * j.rows + r + 8 * u] = top;
       }
     }
   }
@@ -144,7 +178,7 @@ __global__ __launch_bounds__(256) void i8_cols_max(int rows, int cols, int per,
   }
   __syncthreads();
   const int cc = blockIdx.x * 256 + tid;
-  if (cc >= cols) return;
+  if (cc >= j.cols) return;
   uint32_t a = 0;
   float t = 0.0f;
 #pragma unroll
@@ -152,66 +186,86 @@ __global__ __launch_bounds__(256) void i8_cols_max(int rows, int cols, int per,
     a = rm[i][tid] > a ? rm[i][tid] : a;
     t += rs[i][tid];
   }
-  mag[(int64_t)blockIdx.y * cols + cc] = a;
-  if (sum) sum[(int64_t)blockIdx.y * cols + cc] = t;
+  j.cmag[(int64_t)blockIdx.y * j.cols + cc] = a;
+  if (want_sum) j.psum[(int64_t)blockIdx.y * j.cols + cc] = t;
 }
 
-// Columns, second pass: 128 rows x 64 columns quantised and written transposed, a
-// 128-byte run of each column, through LDS.
-__global__ __launch_bounds__(256) void i8_cols_write(int rows, int cols, int chunks, int ld,
-                                                     const h16* __restrict__ x,
-                                                     const uint32_t* __restrict__ mag,
-                                                     const float* __restrict__ psum,
-                                                     int8_t* __restrict__ q,
-                                                     float* __restrict__ scale,
-                                                     h16* __restrict__ sum) {
+// Second pass: 128 rows x 128 columns quantised and written transposed, a 128-byte
+// run of each column through LDS, and as laid out, a run of each row.
+__global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
+  const I8Cols& j = both.job[blockIdx.z];
+  const int c0 = blockIdx.x * 128, r0 = blockIdx.y * 128;
+  if (c0 >= j.ldr || r0 >= j.ldc) return;
   constexpr int LD = 144;  // bytes from column to column of the tile
-  __shared__ uint32_t cm[64];
-  __shared__ __attribute__((aligned(16))) int8_t tile[64 * LD];
+  __shared__ I8Quant cq[128], rq[128];
+  __shared__ __attribute__((aligned(16))) int8_t tile[128 * LD];
   const int tid = threadIdx.x;
-  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 128;
-  if (tid < 64) {
-    const int c = c0 + tid;
+  const bool want_rows = j.rmag != nullptr;
+  const int cg = tid & 15, rg = tid >> 4;  // 8 columns, rows 8 rg .. + 7
+  const int c = c0 + cg * 8;
+  V8 v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + rg * 8 + i;
+    v[i] = r < j.rows && c < j.cols ? i8_load8(j.x + (int64_t)r * j.cols + c, j.cols - c) : zero8();
+  }
+  if (tid < 128) {
+    const int k = c0 + tid;
     uint32_t a = 0;
     double s = 0.0;
-    if (c < cols) {
-      for (int i = 0; i < chunks; ++i) {
-        const uint32_t b = mag[(int64_t)i * cols + c];
+    if (k < j.cols) {
+#pragma unroll 8
+      for (int i = 0; i < j.chunks; ++i) {
+        const uint32_t b = j.cmag[(int64_t)i * j.cols + k];
         a = b > a ? b : a;
-        if (sum && blockIdx.y == 0) s += (double)psum[(int64_t)i * cols + c];
       }
       if (blockIdx.y == 0) {
-        scale[c] = i8_scale(a);
-        if (sum) sum[c] = dbl_to_h16(s);
+        j.scale_c[k] = i8_scale(a);
+        if (j.psum) {
+          for (int i = 0; i < j.chunks; ++i) s += (double)j.psum[(int64_t)i * j.cols + k];
+          j.sum[k] = dbl_to_h16(s);
+        }
       }
     }
-    cm[tid] = a;
+    cq[tid] = i8_quant(a);
+  } else if (want_rows) {
+    const int k = r0 + tid - 128;
+    uint32_t a = 0;
+    if (k < j.rows) {
+      const int n = (j.cols + 255) / 256;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const uint32_t b = j.rmag[(int64_t)i * j.rows + k];
+        a = b > a ? b : a;
+      }
+      if (blockIdx.x == 0) j.scale_r[k] = i8_scale(a);
+    }
+    rq[tid - 128] = i8_quant(a);
   }
   __syncthreads();
-  const bool whole = cols % 8 == 0;
-  const int cg = tid & 7, rq = tid >> 3;  // 8 columns, rows 4 rq .. + 3
-  const int c = c0 + cg * 8;
-  uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (want_rows) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = r0 + rq * 4 + i;
-    V8 v = zero8();
-    if (r < rows && c < cols) v = i8_load8(x + (int64_t)r * cols + c, cols - c, whole);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t m = cm[cg * 8 + e];
-      w[e] |= (uint32_t)(uint8_t)i8_q(v.h[e], i8_top(m), i8_live(m)) << (8 * i);
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + rg * 8 + i;
+      if (r < j.rows && c < j.ldr)
+        *reinterpret_cast<uint2*>(j.qr + (int64_t)r * j.ldr + c) = i8_pack(v[i], rq[rg * 8 + i]);
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    *reinterpret_cast<uint32_t*>(tile + (cg * 8 + e) * LD + rq * 4) = w[e];
+  for (int e = 0; e < 8; ++e) {
+    const I8Quant k = cq[cg * 8 + e];
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = i8_byte(i8_x127(v[i].h[e]), k);
+    *reinterpret_cast<uint2*>(tile + (cg * 8 + e) * LD + rg * 8) =
+        make_uint2(i8_pack4(b[0], b[1], b[2], b[3]), i8_pack4(b[4], b[5], b[6], b[7]));
+  }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const int cc = (i * 256 + tid) >> 3, k = ((i * 256 + tid) & 7) * 16;
-    if (c0 + cc < cols && r0 + k < ld)
-      *reinterpret_cast<u32x4*>(q + (int64_t)(c0 + cc) * ld + r0 + k) =
+    if (c0 + cc < j.cols && r0 + k < j.ldc)
+      *reinterpret_cast<u32x4*>(j.qc + (int64_t)(c0 + cc) * j.ldc + r0 + k) =
           *reinterpret_cast<const u32x4*>(tile + cc * LD + k);
   }
 }
@@ -227,7 +281,7 @@ __device__ __forceinline__ h16 i8_out(int acc, float sa, float sb, bool has_bias
 // What a tile stores, see nt_store: p along a row of y.
 struct I8Epi {
   const I8Product& g;
-  bool whole, has_bias;
+  bool has_bias;
   static constexpr int OUTS = 1;
   static constexpr bool DIAGONAL = false;
   struct Pre {
@@ -239,7 +293,7 @@ struct I8Epi {
     Pre r;
     r.sq = g.sa[q < g.m ? q : 0];
     p = p < g.n ? p : 0;
-    if (whole) {
+    if (p + 8 <= g.n) {
       const floatx4* sv = reinterpret_cast<const floatx4*>(g.sb + p);
       const floatx4 x = sv[0], y = sv[1];
 #pragma unroll
@@ -267,8 +321,8 @@ struct I8Epi {
   __device__ __forceinline__ void store(int p, int q, const V8 (&out)[1]) const {
     if (p >= g.n || q >= g.m) return;
     h16* yp = g.y + (int64_t)q * g.n + p;
-    if (whole) {
-      store16(yp, out[0]);
+    if (p + 8 <= g.n) {
+      store16u(yp, out[0]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -298,7 +352,7 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
   intx16 acc[C::TP][C::TQ];
   nt_product<NtByte, C, 1>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
-  const I8Epi epi{g, g.n % 8 == 0, g.bias != nullptr};
+  const I8Epi epi{g, g.bias != nullptr};
   h16* none[1] = {nullptr};
   nt_store<C, 1>(acc, lds, pt + (wave / C::WQ) * 32 * C::TP, qt + (wave % C::WQ) * 32 * C::TQ, g.n,
                  g.m, false, none, 0, epi);
@@ -306,63 +360,70 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
 
 // Few rows (at most 16 tokens): bound by reading b once.  A workgroup takes 16
 // outputs; its eight waves split the reduction, each lane loading 16 bytes of one
-// row of b straight into the operand, and add their 32-bit sums in LDS.  FUSED: the
-// rows of x are quantised by every workgroup for itself into LDS (they are small and
-// come from the L2), which saves a launch; otherwise a is read from memory.
-constexpr int kFewRows = 16, kFewWaves = 8, kFewLds = 48 * 1024;
+// row of b straight into the operand (the first kFewAhead of them before anything
+// else), and add their 32-bit sums in LDS.  FUSED: the rows of x are quantised by
+// every workgroup for itself into LDS (they are small and come from the L2), which
+// saves a launch; otherwise a is read from memory.
+constexpr int kFewRows = 16, kFewWaves = 8, kFewLds = 48 * 1024, kFewAhead = 8;
 template <bool FUSED>
 __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, const h16* __restrict__ x) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];  // FUSED: [m][ld + 16]
   __shared__ int part[kFewWaves][16][17];
-  __shared__ float ss[kFewRows];
+  __shared__ uint32_t top[kFewRows][kFewWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ld = (g.k + 15) & ~15, lq = ld + 16;
-  if (FUSED) {
-    const bool whole = g.k % 8 == 0;
-    for (int r = wave; r < g.m; r += kFewWaves) {
-      const h16* xr = x + (int64_t)r * g.k;
-      uint32_t mag = 0;
-      for (int c = lane * 8; c < g.k; c += 512) mag = i8_mag8(i8_load8(xr + c, g.k - c, whole), mag);
-      mag = i8_wave_max(mag);
-      if (lane == 0) ss[r] = i8_scale(mag);
-      const float top = i8_top(mag);
-      const bool live = i8_live(mag);
-      for (int c = lane * 8; c < ld; c += 512)
-        *reinterpret_cast<uint2*>(dyn + r * lq + c) =
-            i8_pack(c < g.k ? i8_load8(xr + c, g.k - c, whole) : zero8(), top, live);
-    }
-    __syncthreads();
-  } else if (tid < g.m) {
-    ss[tid] = g.sa[tid];
-  }
   const int n0 = blockIdx.x * 16;
   const int row = lane & 15, kc = (lane >> 4) * 16;
-  const bool bin = n0 + row < g.n, ain = row < g.m;
-  const int8_t* bp = g.b + (int64_t)(n0 + row) * ld;
+  const bool ain = row < g.m;
+  const int8_t* bp = g.b + (int64_t)(n0 + row < g.n ? n0 + row : 0) * ld;
   const intx4 zero = {0, 0, 0, 0};
-  intx4 acc = zero;
   const int steps = (ld + 63) / 64, per = (steps + kFewWaves - 1) / kFewWaves;
-  const int s1 = std::min(steps, (wave + 1) * per);
-  constexpr int U = 4;
-  for (int s = wave * per; s < s1; s += U) {
-    intx4 fb[U], fa[U];
+  const int s0 = wave * per, s1 = std::min(steps, s0 + per);
+  intx4 fb[kFewAhead];
+  auto load = [&](int s) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kFewAhead; ++u) {
       const int k = (s + u) * 64 + kc;
-      fb[u] = s + u < s1 && bin && k < ld ? *reinterpret_cast<const intx4*>(bp + k) : zero;
+      fb[u] = s + u < s1 && k < ld ? *reinterpret_cast<const intx4*>(bp + k) : zero;
     }
+  };
+  load(s0);
+  const int wpr = g.m >= 8 ? 1 : g.m >= 3 ? 2 : g.m == 2 ? 4 : 8;  // waves to a row of x
+  if (FUSED) {
+    const int w = wave % wpr;
+    for (int r = wave / wpr; r < g.m; r += kFewWaves / wpr) {
+      const h16* xr = x + (int64_t)r * g.k;
+      uint32_t mag = 0;
+      for (int c = (w * 64 + lane) * 8; c < g.k; c += 512 * wpr)
+        mag = i8_mag8(i8_load8(xr + c, g.k - c), mag);
+      mag = i8_wave_max(mag);
+      if (lane == 0) top[r][w] = mag;
+    }
+    if (wpr > 1) __syncthreads();
+    for (int r = wave / wpr; r < g.m; r += kFewWaves / wpr) {
+      const h16* xr = x + (int64_t)r * g.k;
+      uint32_t mag = 0;
+      for (int i = 0; i < wpr; ++i) mag = std::max(mag, top[r][i]);
+      const I8Quant k = i8_quant(mag);
+      for (int c = (w * 64 + lane) * 8; c < ld; c += 512 * wpr)
+        *reinterpret_cast<uint2*>(dyn + r * lq + c) =
+            i8_pack(i8_load8(xr + (c < g.k ? c : 0), g.k - c), k);
+    }
+    __syncthreads();
+  }
+  intx4 acc = zero;
+  for (int s = s0; s < s1; s += kFewAhead) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kFewAhead; ++u) {
       const int k = (s + u) * 64 + kc;
       const bool in = s + u < s1 && ain && k < ld;
-      if (FUSED)
-        fa[u] = in ? *reinterpret_cast<const intx4*>(dyn + row * lq + k) : zero;
-      else
-        fa[u] = in ? *reinterpret_cast<const intx4*>(g.a + (int64_t)row * ld + k) : zero;
+      const char* from = FUSED ? dyn + row * lq + k
+                               : reinterpret_cast<const char*>(g.a) + (int64_t)row * ld + k;
+      const intx4 fa = in ? *reinterpret_cast<const intx4*>(from) : zero;
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u], fa, acc, 0, 0, 0);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u], fa[u], acc, 0, 0, 0);
+    if (s + kFewAhead < s1) load(s + kFewAhead);
   }
   // lane: outputs 4 (lane / 16) + i of token lane % 16
 #pragma unroll
@@ -374,9 +435,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, cons
       int s = 0;
 #pragma unroll
       for (int w = 0; w < kFewWaves; ++w) s += part[w][q][p];
+      float sq;
+      if (FUSED) {
+        uint32_t mag = 0;
+        for (int i = 0; i < wpr; ++i) mag = std::max(mag, top[q][i]);
+        sq = i8_scale(mag);
+      } else {
+        sq = g.sa[q];
+      }
       const bool has_bias = g.bias != nullptr;
       g.y[(int64_t)q * g.n + n0 + p] =
-          i8_out(s, ss[q], g.sb[n0 + p], has_bias, has_bias ? to_f32(g.bias[n0 + p]) : 0.0f);
+          i8_out(s, sq, g.sb[n0 + p], has_bias, has_bias ? to_f32(g.bias[n0 + p]) : 0.0f);
     }
   }
 }
@@ -399,32 +468,58 @@ hipError_t launch_i8_rows(int rows, int cols, const h16* x, int8_t* q, float* sc
   return hipGetLastError();
 }
 
-namespace {
-// rows of a range and how many ranges: at least 64 rows each, enough workgroups
-void i8_chunks(int rows, int cols, int* per, int* chunks) {
-  const int want = std::max(1, std::min(kColChunks, 1024 / std::max(1, ceil_div(cols, 256))));
-  *per = std::max(64, ceil_div(rows, want));
-  *chunks = ceil_div(rows, *per);
-}
-}  // namespace
-
-size_t i8_cols_ws_bytes(int rows, int cols) {
-  int per, chunks;
-  i8_chunks(rows, cols, &per, &chunks);
-  return (size_t)chunks * cols * 8;
+void i8_cols_plan(I8Cols* j) {
+  j->per = std::max(64, ceil_div(ceil_div(j->rows, kColChunks), 8) * 8);
+  j->chunks = ceil_div(j->rows, j->per);
+  j->ldc = (int)i8_row(j->rows);
+  j->ldr = (int)i8_row(j->cols);
 }
 
-hipError_t launch_i8_cols(int rows, int cols, const h16* x, int8_t* q, float* scale, h16* sum,
-                          void* ws, hipStream_t st) {
-  int per, chunks;
-  i8_chunks(rows, cols, &per, &chunks);
-  uint32_t* mag = static_cast<uint32_t*>(ws);
-  float* ps = reinterpret_cast<float*>(mag + (size_t)chunks * cols);
-  const int ld = (int)i8_row(rows);
-  hipLaunchKernelGGL(i8_cols_max, dim3((unsigned)ceil_div(cols, 256), (unsigned)chunks), dim3(256),
-                     0, st, rows, cols, per, x, mag, sum ? ps : nullptr);
-  hipLaunchKernelGGL(i8_cols_write, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(ld, 128)),
-                     dim3(256), 0, st, rows, cols, chunks, ld, x, mag, ps, q, scale, sum);
+size_t i8_cols_ws_bytes(int rows, int cols, bool by_rows, bool sum) {
+  I8Cols j{};
+  j.rows = rows;
+  j.cols = cols;
+  i8_cols_plan(&j);
+  return (size_t)j.chunks * cols * (sum ? 8 : 4) +
+         (by_rows ? (size_t)ceil_div(cols, 256) * rows * 4 : 0);
+}
+
+I8Cols i8_cols_job(int rows, int cols, const h16* x, int8_t* qc, float* scale_c, int8_t* qr,
+                   float* scale_r, h16* sum, void* ws) {
+  I8Cols j{};
+  j.rows = rows;
+  j.cols = cols;
+  j.x = x;
+  i8_cols_plan(&j);
+  j.qc = qc;
+  j.scale_c = scale_c;
+  j.qr = qr;
+  j.scale_r = scale_r;
+  j.sum = sum;
+  j.cmag = static_cast<uint32_t*>(ws);
+  uint32_t* next = j.cmag + (size_t)j.chunks * cols;
+  if (sum) {
+    j.psum = reinterpret_cast<float*>(next);
+    next += (size_t)j.chunks * cols;
+  }
+  if (qr) j.rmag = next;
+  return j;
+}
+
+hipError_t launch_i8_cols(const I8Cols* jobs, int count, hipStream_t st) {
+  I8Both b{};
+  int cols = 0, chunks = 0, rows = 0;
+  for (int i = 0; i < count; ++i) {
+    b.job[i] = jobs[i];
+    cols = std::max(cols, jobs[i].ldr);
+    rows = std::max(rows, jobs[i].ldc);
+    chunks = std::max(chunks, jobs[i].chunks);
+  }
+  hipLaunchKernelGGL(i8_cols_max, dim3((unsigned)ceil_div(cols, 256), (unsigned)chunks, (unsigned)count),
+                     dim3(256), 0, st, b);
+  hipLaunchKernelGGL(i8_cols_write,
+                     dim3((unsigned)ceil_div(cols, 128), (unsigned)ceil_div(rows, 128), (unsigned)count),
+                     dim3(256), 0, st, b);
   return hipGetLastError();
 }
 

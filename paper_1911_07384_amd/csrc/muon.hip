@@ -85,15 +85,6 @@ __device__ __forceinline__ double ns_block_sum(double v, double* red) {
   return ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-// eight elements, at once where the matrix is 16-byte aligned
-__device__ __forceinline__ V8 ns_load8(const h16* p, bool aligned) {
-  if (aligned) return load16(p);
-  V8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v.h[e] = p[e];
-  return v;
-}
-
 // the float32 update direction before normalisation
 __device__ __forceinline__ float ns_dir(h16 g, h16 m, float mu, bool has_m, bool nesterov) {
   if (!has_m) return to_f32(g);
@@ -124,18 +115,13 @@ __global__ __launch_bounds__(256) void ns_first(const NsChunk c, char* ws, NsPla
   const int64_t n = (int64_t)j.rows * j.cols, nvec = n / 8;
   double s = 0.0;
   for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < nvec; i += (int64_t)j.nparts * 256) {
-    const V8 g = ns_load8(j.g + i * 8, j.aligned);
+    const V8 g = load16u(j.g + i * 8);
     V8 m = zero8();
     if (has_m) {
-      m = ns_load8(j.m + i * 8, j.aligned);
+      m = load16u(j.m + i * 8);
 #pragma unroll
       for (int e = 0; e < 8; ++e) m.h[e] = to_h16(__builtin_fmaf(mu, to_f32(m.h[e]), to_f32(g.h[e])));
-      if (j.aligned) {
-        store16(j.m + i * 8, m);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) j.m[i * 8 + e] = m.h[e];
-      }
+      store16u(j.m + i * 8, m);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -176,7 +162,7 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
   const int local = blockIdx.x - j.t_pre, tc = j.cp / 64;
   const int r0 = (local / tc) * 64, c0 = (local % tc) * 64;
   const int row = r0 + tid / 4;
-  const bool has_m = j.m != nullptr, whole = j.whole;
+  const bool has_m = j.m != nullptr;
   h16* nat = at<h16>(dv.ws, j.nat[0]) + (int64_t)row * j.cp;
   h16* natl = at<h16>(dv.ws, j.natl[0]) + (int64_t)row * j.cp;
 #pragma unroll
@@ -185,9 +171,9 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
     V8 g = zero8(), m = zero8(), hi, lo;
     const int64_t o = (int64_t)row * j.cols + col;
     if (row < j.rows && col < j.cols) {
-      if (whole) {
-        g = load16(j.g + o);
-        if (has_m) m = load16(j.m + o);
+      if (col + 8 <= j.cols) {
+        g = load16u(j.g + o);
+        if (has_m) m = load16u(j.m + o);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -382,7 +368,7 @@ struct NsXEpi {
   h16 *nho, *nlo, *w;
   const float* e;
   float ca, keep, alpha;
-  bool update, whole;
+  bool update;
   static constexpr int OUTS = 2;  // X' in two parts, or the weights in the first
   static constexpr bool DIAGONAL = false;
   struct Pre {
@@ -395,8 +381,8 @@ struct NsXEpi {
     if (LAST && update) {
       const int pw = p < cols ? p : 0, qw = q < rows ? q : 0;
       const h16* wp = w + (int64_t)qw * cols + pw;
-      if (whole) {
-        r.w = load16(wp);
+      if (pw + 8 <= cols) {
+        r.w = load16u(wp);
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) r.w.h[k] = wp[pw + k < cols ? k : 0];
@@ -453,8 +439,8 @@ struct NsXEpi {
     }
     if (p >= cols || q >= rows) return;
     h16* const wp = w + (int64_t)q * cols + p;
-    if (whole) {
-      store16(wp, out[0]);
+    if (p + 8 <= cols) {
+      store16u(wp, out[0]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -524,7 +510,6 @@ __device__ __forceinline__ void ns_x_out(const NsDev& dv, const NsJob& j, int cu
   epi.keep = keep;
   epi.alpha = j.alpha;
   epi.update = j.m != nullptr;
-  epi.whole = j.whole;
   h16* mir[PARTS];
   mir[0] = at<h16>(dv.ws, j.mir[mn]);
   mir[PARTS - 1] = at<h16>(dv.ws, PARTS == 2 ? j.mirl[mn] : j.mir[mn]);

@@ -25,7 +25,6 @@ struct NsJob {
   h16* w;        // the weights, or the result
   float alpha;   // factor of the orthogonalised matrix
   int rows, cols, rp, cp, tall;
-  int aligned, whole;  // 16-byte aligned; and rows of whole 16 bytes
   uint32_t nat[2], mir[2], natl[2], mirl[2];  // X (high parts, low parts)
   uint32_t a, al, b, bl;                      // A and B off the diagonal
   uint32_t d, e;                              // their diagonals, float32
@@ -71,11 +70,25 @@ inline int64_t i8_row(int64_t n) { return (n + 15) & ~(int64_t)15; }  // bytes o
 // x [rows][cols] by rows: q [rows][i8_row(cols)] and scale [rows].
 hipError_t launch_i8_rows(int rows, int cols, const h16* x, int8_t* q, float* scale,
                           hipStream_t st);
-// x [rows][cols] by columns: q [cols][i8_row(rows)] and scale [cols]; sum (nullable):
-// the columns' sums, rounded.  ws: i8_cols_ws_bytes.
-size_t i8_cols_ws_bytes(int rows, int cols);
-hipError_t launch_i8_cols(int rows, int cols, const h16* x, int8_t* q, float* scale, h16* sum,
-                          void* ws, hipStream_t st);
+// x [rows][cols] by columns, qc [cols][i8_row(rows)] and scale_c [cols]; and unless
+// qr is null by rows, qr [rows][i8_row(cols)] and scale_r [rows]; sum (nullable): the
+// columns' sums, rounded.  ws: i8_cols_ws_bytes.  Up to two of them in a launch.
+struct I8Cols {
+  int rows, cols, per, chunks, ldc, ldr;
+  const h16* x;
+  int8_t *qc, *qr;
+  float *scale_c, *scale_r;
+  h16* sum;
+  uint32_t *cmag, *rmag;  // largest magnitudes: [chunks][cols], [cols / 256][rows]
+  float* psum;            // sums: [chunks][cols]
+};
+struct I8Both {
+  I8Cols job[2];
+};
+size_t i8_cols_ws_bytes(int rows, int cols, bool by_rows, bool sum);
+I8Cols i8_cols_job(int rows, int cols, const h16* x, int8_t* qc, float* scale_c, int8_t* qr,
+                   float* scale_r, h16* sum, void* ws);
+hipError_t launch_i8_cols(const I8Cols* jobs, int count, hipStream_t st);
 // y [m][n] = rne16(sa sb (a b^T) + bias): a [m][i8_row(k)], b [n][i8_row(k)].
 struct I8Product {
   int m, n, k;
