@@ -40,12 +40,13 @@ struct NtByte {  // 8-bit integers, 32-bit sums (exact below 2^31)
   }
 };
 
-template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int OCC_>
+// H = 2: operands in a high and a low part each (see nt_product).
+template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int OCC_, int H_ = 1>
 struct NtCfg {
-  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, SB = SB_, S = S_, OCC = OCC_;
+  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, SB = SB_, S = S_, OCC = OCC_, H = H_;
   static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES;
   static constexpr int BP = 32 * TP * WP, BQ = 32 * TQ * WQ;
-  static constexpr int STAGE = (BP + BQ) * SB, LDS = S * STAGE;
+  static constexpr int PART = (BP + BQ) * SB, STAGE = H * PART, LDS = S * STAGE;
   static constexpr int IP = BP * SB / (1024 * WAVES), IQ = BQ * SB / (1024 * WAVES);  // loads
   static_assert(SB == 64 || (SB == 128 && IP % 2 == 0 && IQ % 2 == 0), "the chunks' order");
   static_assert(IP * 1024 * WAVES == BP * SB && IQ * 1024 * WAVES == BQ * SB, "whole loads");
@@ -63,23 +64,25 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t nt_rsrc(const void* p, int byt
 // workgroup barrier without the implied memory fence; callers wait first
 __device__ __forceinline__ void nt_barrier() { __asm__ volatile("s_barrier" ::: "memory"); }
 
-// The rows of one tile: NSEG pairs of operands whose products add up (the parts
-// of split operands), each from the tile's first row.
-template <int NSEG>
+// The rows of one tile, each operand from the tile's first row (with H = 2 its high
+// and its low part).
 struct NtTile {
-  const void* p[NSEG];
-  const void* q[NSEG];
+  const void* p[2];
+  const void* q[2];
   uint32_t ldp, ldq;   // bytes from row to row, multiples of 16
   int prows, qrows;    // rows there are from the tile's first; others read as zeros
   int kbytes;          // of a row; a last chunk's bytes past it are multiplied too
   int part, parts;     // which of so many ranges of the slices
 };
 
-template <class T, class C, int NSEG>
-__device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
+// acc = the sums of P[p][k] Q[q][k]; with H = 2 of Ph Ql + Pl Qh + Ph Qh, every part
+// loaded once for the three products.
+template <class T, class C>
+__device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
                                            typename T::Acc (&acc)[C::TP][C::TQ]) {
   typedef typename T::Frag Frag;
-  constexpr int TP = C::TP, TQ = C::TQ, S = C::S, SB = C::SB, IP = C::IP, IQ = C::IQ, I = IP + IQ;
+  constexpr int TP = C::TP, TQ = C::TQ, S = C::S, SB = C::SB, H = C::H, IP = C::IP, IQ = C::IQ;
+  constexpr int I1 = IP + IQ, I = H * I1;
   constexpr uint32_t OOB = 0x80000000u;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -107,47 +110,29 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
     pv[h] = (uint32_t)(wave * IP * RI + row) * t.ldp + (uint32_t)ck[h];
     qv[h] = (uint32_t)(wave * IQ * RI + row) * t.ldq + (uint32_t)ck[h];
   }
-  // the slices of all pairs in order, this part's range of them
-  const int per1 = (t.kbytes + SB - 1) / SB;  // of one pair
-  const int KT = (NSEG * per1 + t.parts - 1) / t.parts;
-  int seg = t.part * KT / per1;                // the slice loaded next: its pair,
-  int k0 = (t.part * KT - seg * per1) * SB;    // its first byte,
-  int left = NSEG * per1 - t.part * KT < KT ? NSEG * per1 - t.part * KT : KT;  // and how many
-  const void *pp = t.p[0], *qp = t.q[0];
-  auto pair = [&]() {
-#pragma unroll
-    for (int s = 1; s < NSEG; ++s)
-      if (seg == s) {
-        pp = t.p[s];
-        qp = t.q[s];
-      }
-  };
-  pair();
+  // this part's range of the slices: its length, and the one loaded next
+  const int slices = (t.kbytes + SB - 1) / SB, KT = (slices + t.parts - 1) / t.parts;
+  int k0 = t.part * KT * SB;
+  const int kend = t.kbytes < k0 + KT * SB ? t.kbytes : k0 + KT * SB;
   bool in[2];
   auto begin = [&]() {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) in[h] = left > 0 && k0 + ck[h] < t.kbytes;
+    for (int h = 0; h < 2; ++h) in[h] = k0 + ck[h] < kend;
   };
-  auto load = [&](char* buf, int i) {
+  auto load = [&](char* buf, int n) {
+    const int h = n / I1, i = n % I1;
+    buf += h * C::PART;
     if (i < IP) {
       const uint32_t off = pv[i & 1] + ((uint32_t)(i * RI) * t.ldp + (uint32_t)k0);
-      nt_load(nt_rsrc(pp, prec), buf + (wave * IP + i) * 1024, in[i & 1] ? off : OOB);
+      nt_load(nt_rsrc(t.p[h], prec), buf + (wave * IP + i) * 1024, in[i & 1] ? off : OOB);
     } else {
       const int j = i - IP;
       const uint32_t off = qv[j & 1] + ((uint32_t)(j * RI) * t.ldq + (uint32_t)k0);
-      nt_load(nt_rsrc(qp, qrec), buf + C::BP * SB + (wave * IQ + j) * 1024,
+      nt_load(nt_rsrc(t.q[h], qrec), buf + C::BP * SB + (wave * IQ + j) * 1024,
               in[j & 1] ? off : OOB);
     }
   };
-  auto advance = [&]() {
-    k0 += SB;
-    --left;
-    if (NSEG > 1 && k0 >= t.kbytes && seg + 1 < NSEG) {
-      k0 = 0;
-      ++seg;
-      pair();
-    }
-  };
+  auto advance = [&]() { k0 += SB; };
 
 #pragma unroll
   for (int a = 0; a < TP; ++a)
@@ -156,36 +141,39 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[a][b][e] = 0;
 
-  Frag fp[2][TP], fq[2][TQ];
+  Frag fp[2][H][TP], fq[2][H][TQ];
   // byte of this lane's fragment of sub-step ks in a block of 32 rows
   auto place = [&](int ks) {
     if (SB == 128) return lrow * 128 + ((ks * 2 + lhi) ^ ((lrow >> 1) & 7)) * 16;
     return (lrow >> 1) * 128 + (((lrow & 1) * 4 + ks * 2 + lhi) ^ ((lrow >> 2) & 3)) * 16;
   };
-  auto fetch_p = [&](const char* buf, int ks, int a) {
-    return *reinterpret_cast<const Frag*>(buf + (wp * TP + a) * 32 * SB + place(ks));
+  // read r of the fragments of sub-step ks, in the order they are used in
+  auto fetch = [&](const char* buf, int ks, int r, Frag (&p)[H][TP], Frag (&q)[H][TQ]) {
+    const bool isq = r < TQ || r >= TQ + H * TP;
+    const int h = H == 1 ? 0 : r < TQ ? 1 : r < TQ + TP ? 0 : r < TQ + 2 * TP ? 1 : 0;
+    const int i = r < TQ ? r : r < TQ + TP ? r - TQ : r < TQ + 2 * TP ? r - TQ - TP : r - TQ - 2 * TP;
+    const Frag* from = reinterpret_cast<const Frag*>(
+        buf + h * C::PART + (isq ? C::BP * SB + (wq * TQ + i) * 32 * SB : (wp * TP + i) * 32 * SB) +
+        place(ks));
+    if (isq)
+      q[h][i < TQ ? i : 0] = *from;
+    else
+      p[h][i < TP ? i : 0] = *from;
   };
-  auto fetch_q = [&](const char* buf, int ks, int b) {
-    return *reinterpret_cast<const Frag*>(buf + C::BP * SB + (wq * TQ + b) * 32 * SB + place(ks));
-  };
+  constexpr int R = H * (TP + TQ), M = (H == 2 ? 3 : 1) * TP * TQ;  // reads, products
   // One sub-step: the products of one set of fragments, between them the reads of
   // the next set (sub-step ks of `from`) and loads L0 .. L1 - 1 into `to`, an
   // instruction or two after each product (kept there by the scheduling barriers;
   // left to itself the compiler issues them in bursts that hold the products up).
-  auto substep = [&](const Frag (&p)[TP], const Frag (&q)[TQ], const char* from, int ks,
-                     Frag (&np)[TP], Frag (&nq)[TQ], char* to, auto l0, auto l1) {
-    constexpr int M = TP * TQ, R = TP + TQ, L0 = decltype(l0)::value, V = decltype(l1)::value - L0;
+  auto substep = [&](const Frag (&p)[H][TP], const Frag (&q)[H][TQ], const char* from, int ks,
+                     Frag (&np)[H][TP], Frag (&nq)[H][TQ], char* to, auto l0, auto l1) {
+    constexpr int L0 = decltype(l0)::value, V = decltype(l1)::value - L0;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      const int a = i / TQ, b = i % TQ;
-      acc[a][b] = T::mma(p[a], q[b], acc[a][b]);
+      const int a = i / TQ % TP, b = i % TQ, term = i / (TP * TQ);
+      acc[a][b] = T::mma(p[H == 2 && term == 1][a], q[H == 2 && term == 0][b], acc[a][b]);
 #pragma unroll
-      for (int r = R * i / M; r < R * (i + 1) / M; ++r) {
-        if (r < TQ)
-          nq[r < TQ ? r : 0] = fetch_q(from, ks, r);
-        else
-          np[r < TQ ? 0 : r - TQ] = fetch_p(from, ks, r - TQ);
-      }
+      for (int r = R * i / M; r < R * (i + 1) / M; ++r) fetch(from, ks, r, np, nq);
 #pragma unroll
       for (int v = V * i / M; v < V * (i + 1) / M; ++v) load(to, L0 + v);
       __builtin_amdgcn_sched_barrier(0);
@@ -206,9 +194,7 @@ __device__ __forceinline__ void nt_product(const NtTile<NSEG>& t, char* lds,
   __builtin_amdgcn_s_waitcnt(WAIT);
   nt_barrier();
 #pragma unroll
-  for (int b = 0; b < TQ; ++b) fq[0][b] = fetch_q(lds, 0, b);
-#pragma unroll
-  for (int a = 0; a < TP; ++a) fp[0][a] = fetch_p(lds, 0, a);
+  for (int r = 0; r < R; ++r) fetch(lds, 0, r, fp[0], fq[0]);
   int rd = 0, wr = S - 1;
   for (int kt = 0; kt < KT; ++kt) {
     const char* cur = lds + rd * C::STAGE;

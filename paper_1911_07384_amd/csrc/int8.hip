@@ -340,17 +340,17 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
   const int gr = t / (4 * tq), w = t - gr * 4 * tq;
   const int gw = tp - 4 * gr < 4 ? tp - 4 * gr : 4;
   const int pt = (4 * gr + w % gw) * C::BP, qt = (w / gw) * C::BQ;
-  NtTile<1> nt;
+  NtTile nt;
   nt.ldp = nt.ldq = (uint32_t)((g.k + 15) & ~15);
-  nt.p[0] = g.b + (int64_t)pt * nt.ldp;
-  nt.q[0] = g.a + (int64_t)qt * nt.ldq;
+  nt.p[0] = nt.p[1] = g.b + (int64_t)pt * nt.ldp;
+  nt.q[0] = nt.q[1] = g.a + (int64_t)qt * nt.ldq;
   nt.prows = g.n - pt;
   nt.qrows = g.m - qt;
   nt.kbytes = g.k;
   nt.part = 0;
   nt.parts = 1;
   intx16 acc[C::TP][C::TQ];
-  nt_product<NtByte, C, 1>(nt, lds, acc);
+  nt_product<NtByte, C>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
   const I8Epi epi{g, g.bias != nullptr};
   h16* none[1] = {nullptr};

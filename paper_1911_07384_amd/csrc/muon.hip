@@ -44,12 +44,34 @@
 namespace fp16k {
 namespace {
 
+// The tiles by the number of products: with three, the parts of both operands lie
+// in LDS together, so slices are half as long.
+template <int PROD>
+struct NsTiles {
+  typedef Nt256 T256;
+  typedef Nt192 T192;
+  typedef Nt128 T128;
+  typedef Nt128d T128d;
+  typedef Nt64 T64;
+  typedef NtCfg<2, 2, 1, 1, 128, 8, 1> T64d;
+};
+template <>
+struct NsTiles<3> {
+  typedef NtCfg<2, 2, 4, 4, 64, 2, 1, 2> T256;
+  typedef NtCfg<2, 2, 3, 3, 64, 3, 1, 2> T192;
+  typedef NtCfg<2, 2, 2, 2, 64, 2, 2, 2> T128;
+  typedef NtCfg<2, 2, 2, 2, 64, 4, 1, 2> T128d;
+  typedef NtCfg<2, 2, 1, 1, 128, 2, 2, 2> T64;
+  typedef NtCfg<2, 2, 1, 1, 128, 4, 1, 2> T64d;
+};
+
 constexpr float kSx = 4096.0f, kSa = 4096.0f, kSb = 2048.0f;
 
 struct NsDev {
   char* ws;
   uint32_t table, map, sums;  // in units of 256 bytes
   int tiles;
+  int single;  // one matrix only
 };
 
 template <class T>
@@ -114,19 +136,30 @@ __global__ __launch_bounds__(256) void ns_first(const NsChunk c, char* ws, NsPla
   const bool has_m = j.m != nullptr;
   const int64_t n = (int64_t)j.rows * j.cols, nvec = n / 8;
   double s = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < nvec; i += (int64_t)j.nparts * 256) {
-    const V8 g = load16u(j.g + i * 8);
-    V8 m = zero8();
-    if (has_m) {
-      m = load16u(j.m + i * 8);
+  constexpr int U = 4;
+  const int64_t step = (int64_t)j.nparts * 256;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256 + tid; i0 < nvec; i0 += U * step) {
+    V8 g[U], m[U];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m.h[e] = to_h16(__builtin_fmaf(mu, to_f32(m.h[e]), to_f32(g.h[e])));
-      store16u(j.m + i * 8, m);
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * step;
+      g[u] = i < nvec ? load16u(j.g + i * 8) : zero8();
+      m[u] = has_m && i < nvec ? load16u(j.m + i * 8) : zero8();
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const double u = (double)ns_dir(g.h[e], m.h[e], mu, has_m, nesterov);
-      s = __builtin_fma(u, u, s);
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * step;
+      if (has_m) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          m[u].h[e] = to_h16(__builtin_fmaf(mu, to_f32(m[u].h[e]), to_f32(g[u].h[e])));
+        if (i < nvec) store16u(j.m + i * 8, m[u]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double x = (double)ns_dir(g[u].h[e], m[u].h[e], mu, has_m, nesterov);
+        s = __builtin_fma(x, x, s);
+      }
     }
   }
   if (blockIdx.x == 0 && tid < n - nvec * 8) {  // the last elements
@@ -143,14 +176,20 @@ __global__ __launch_bounds__(256) void ns_first(const NsChunk c, char* ws, NsPla
   if (tid == 0) at<double>(ws, j.part)[blockIdx.x] = s;
 }
 
+// The matrix that tile t of the launch belongs to (without a look at the map, a
+// dependent read, where there is only one).
+__device__ __forceinline__ const NsJob& ns_job(const NsDev& dv, int t) {
+  return at<NsJob>(dv.ws, dv.table)[dv.single ? 0 : at<uint16_t>(dv.ws, dv.map)[t]];
+}
+
 // ---- pass 2: X = u / ||u|| split in two binary16 parts, both ways round --------
 
 template <int PROD>
 __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int nesterov) {
-  constexpr int LD = 72;
+  constexpr int LD = 64;
   __shared__ double red[4];
   __shared__ __attribute__((aligned(16))) h16 tile[PROD == 3 ? 2 : 1][64 * LD];
-  const NsJob& j = at<NsJob>(dv.ws, dv.table)[at<uint16_t>(dv.ws, dv.map)[blockIdx.x]];
+  const NsJob& j = ns_job(dv, blockIdx.x);
   const int tid = threadIdx.x;
   double s = 0.0;
   for (int i = tid; i < j.nparts; i += 256) s += at<double>(dv.ws, j.part)[i];
@@ -161,13 +200,14 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
                                                   : (s == 0.0 ? 0.0f : __builtin_nanf(""));
   const int local = blockIdx.x - j.t_pre, tc = j.cp / 64;
   const int r0 = (local / tc) * 64, c0 = (local % tc) * 64;
-  const int row = r0 + tid / 4;
   const bool has_m = j.m != nullptr;
-  h16* nat = at<h16>(dv.ws, j.nat[0]) + (int64_t)row * j.cp;
-  h16* natl = at<h16>(dv.ws, j.natl[0]) + (int64_t)row * j.cp;
+  // thread: 8 columns of rows tid / 8 and tid / 8 + 32; 8 threads a row's 128 bytes.
+  // Transposed through LDS, the 8-row chunks of a column exclusive-ored with the
+  // column's chunk.
+  const int cg = tid & 7, col = c0 + cg * 8;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
-    const int col = c0 + (tid & 3) * 16 + v * 8;
+    const int rl = tid / 8 + 32 * v, row = r0 + rl;
     V8 g = zero8(), m = zero8(), hi, lo;
     const int64_t o = (int64_t)row * j.cols + col;
     if (row < j.rows && col < j.cols) {
@@ -189,29 +229,26 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
       const float x = row < j.rows && col + e < j.cols ? u * rs : 0.0f;
       hi.h[e] = to_h16(x);
       lo.h[e] = to_h16(x - to_f32(hi.h[e]));
-      tile[0][((tid & 3) * 16 + v * 8 + e) * LD + tid / 4] = hi.h[e];
-      if (PROD == 3) tile[PROD == 3][((tid & 3) * 16 + v * 8 + e) * LD + tid / 4] = lo.h[e];
+      const int to = (cg * 8 + e) * LD + ((rl / 8) ^ cg) * 8 + rl % 8;
+      tile[0][to] = hi.h[e];
+      if (PROD == 3) tile[PROD == 3][to] = lo.h[e];
     }
-    store16(nat + col, hi);
-    store16(natl + col, lo);
+    store16(at<h16>(dv.ws, j.nat[0]) + (int64_t)row * j.cp + col, hi);
+    store16(at<h16>(dv.ws, j.natl[0]) + (int64_t)row * j.cp + col, lo);
   }
   __syncthreads();
-  const int64_t mo = (int64_t)(c0 + tid / 4) * j.rp + r0;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
-    const int k = (tid & 3) * 16 + v * 8;
-    store16(at<h16>(dv.ws, j.mir[0]) + mo + k, load16(&tile[0][(tid / 4) * LD + k]));
-    if (PROD == 3)
-      store16(at<h16>(dv.ws, j.mirl[0]) + mo + k, load16(&tile[PROD == 3][(tid / 4) * LD + k]));
+    const int cl = tid / 8 + 32 * v, k = tid & 7;
+    const int from = cl * LD + (k ^ (cl / 8)) * 8;
+    const int64_t mo = (int64_t)(c0 + cl) * j.rp + r0 + k * 8;
+    store16(at<h16>(dv.ws, j.mir[0]) + mo, load16(&tile[0][from]));
+    if (PROD == 3) store16(at<h16>(dv.ws, j.mirl[0]) + mo, load16(&tile[PROD == 3][from]));
   }
 }
 
 // ---- the three products of a step -----------------------------------------------
 
-// The matrix that tile t of the launch belongs to.
-__device__ __forceinline__ const NsJob& ns_job(const NsDev& dv, int t) {
-  return at<NsJob>(dv.ws, dv.table)[at<uint16_t>(dv.ws, dv.map)[t]];
-}
 
 // tile t of a lower triangle, rows in order
 __device__ __forceinline__ void ns_triangle(int t, int* i, int* j) {
@@ -293,23 +330,19 @@ struct NsSymEpi {
 };
 
 // The operands of one tile of A or B.
-template <int STEP, int PROD>
+template <int STEP>
 __device__ __forceinline__ void ns_sym_tile(const NsDev& dv, const NsJob& j, int pt, int qt,
-                                            NtTile<PROD>* nt) {
+                                            NtTile* nt) {
   const int m = j.tall ? j.cp : j.rp, n = j.tall ? j.rp : j.cp;
   // X as [m][n]: laid out so, or the transpose of a tall matrix
   const h16* hi = at<h16>(dv.ws, STEP == 1 ? j.a : j.tall ? j.mir[0] : j.nat[0]);
   const h16* lo = at<h16>(dv.ws, STEP == 1 ? j.al : j.tall ? j.mirl[0] : j.natl[0]);
   const int k = STEP == 0 ? n : m;
   const int64_t po = (int64_t)pt * k, qo = (int64_t)qt * k;
-  if (PROD == 3) {
-    nt->p[0] = hi + po;
-    nt->q[0] = lo + qo;
-    nt->p[PROD / 2] = lo + po;
-    nt->q[PROD / 2] = hi + qo;
-  }
-  nt->p[PROD - 1] = hi + po;
-  nt->q[PROD - 1] = hi + qo;
+  nt->p[0] = hi + po;
+  nt->q[0] = hi + qo;
+  nt->p[1] = lo + po;
+  nt->q[1] = lo + qo;
   nt->ldp = nt->ldq = (uint32_t)k * 2u;
   nt->prows = m - pt;
   nt->qrows = m - qt;
@@ -348,12 +381,12 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, flo
   const NsJob& j = ns_job(dv, t);
   int ti, tj;
   ns_triangle(t - j.t[STEP], &ti, &tj);
-  NtTile<PROD> nt;
+  NtTile nt;
   ns_sym_tile<STEP>(dv, j, ti * C::BP, tj * C::BQ, &nt);
   nt.part = 0;
   nt.parts = 1;
   floatx16 acc[C::TP][C::TQ];
-  nt_product<NtHalf, C, PROD>(nt, lds, acc);
+  nt_product<NtHalf, C>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
   ns_sym_out<C, STEP, PROD>(dv, j, cb, cc, acc, lds, ti * C::BP + (wave / C::WQ) * 32 * C::TP,
                             tj * C::BQ + (wave % C::WQ) * 32 * C::TQ, ti != tj);
@@ -451,9 +484,8 @@ struct NsXEpi {
 
 // The operands of one tile of X'; rows p run along the columns of the matrix as
 // laid out, q along its rows.
-template <int PROD>
 __device__ __forceinline__ void ns_x_tile(const NsDev& dv, const NsJob& j, int cur, int pt, int qt,
-                                          NtTile<PROD>* nt) {
+                                          NtTile* nt) {
   const int tall = j.tall, m = tall ? j.cp : j.rp;
   const h16* bh = at<h16>(dv.ws, j.b);
   const h16* bl = at<h16>(dv.ws, j.bl);
@@ -461,14 +493,10 @@ __device__ __forceinline__ void ns_x_tile(const NsDev& dv, const NsJob& j, int c
   const h16* xh = at<h16>(dv.ws, tall ? j.nat[cur] : j.mir[cur]);
   const h16* xl = at<h16>(dv.ws, tall ? j.natl[cur] : j.mirl[cur]);
   const int64_t po = (int64_t)pt * m, qo = (int64_t)qt * m;
-  if (PROD == 3) {
-    nt->p[0] = (tall ? bh : xh) + po;
-    nt->q[0] = (tall ? xl : bl) + qo;
-    nt->p[PROD / 2] = (tall ? bl : xl) + po;
-    nt->q[PROD / 2] = (tall ? xh : bh) + qo;
-  }
-  nt->p[PROD - 1] = (tall ? bh : xh) + po;
-  nt->q[PROD - 1] = (tall ? xh : bh) + qo;
+  nt->p[0] = (tall ? bh : xh) + po;
+  nt->q[0] = (tall ? xh : bh) + qo;
+  nt->p[1] = (tall ? bl : xl) + po;
+  nt->q[1] = (tall ? xl : bl) + qo;
   nt->ldp = nt->ldq = (uint32_t)m * 2u;
   nt->prows = j.cp - pt;
   nt->qrows = j.rp - qt;
@@ -526,12 +554,12 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
   const NsJob& j = ns_job(dv, t);
   int pt, qt;
   ns_x_place<C>(j, t - j.t[2], &pt, &qt);
-  NtTile<PROD> nt;
+  NtTile nt;
   ns_x_tile(dv, j, cur, pt, qt, &nt);
   nt.part = 0;
   nt.parts = 1;
   floatx16 acc[C::TP][C::TQ];
-  nt_product<NtHalf, C, PROD>(nt, lds, acc);
+  nt_product<NtHalf, C>(nt, lds, acc);
   const int wave = threadIdx.x >> 6;
   ns_x_out<C, PROD, LAST>(dv, j, cur, ca, keep, acc, lds, pt + (wave / C::WQ) * 32 * C::TP,
                           qt + (wave % C::WQ) * 32 * C::TQ);
@@ -542,15 +570,14 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
 // workgroups of one part are neighbours: they share operands in the L2.
 // (1000 x 2048, three products, A: 36 tiles of 96 slices; 26 us on 64 x 64 tiles.)
 template <int STAGE, int PROD>
-__global__ __launch_bounds__(Nt128d::THREADS, Nt128d::OCC) void ns_part(const NsDev dv, int cur,
-                                                                       int parts) {
-  typedef Nt128d C;
+__global__ __launch_bounds__(256, 1) void ns_part(const NsDev dv, int cur, int parts) {
+  typedef typename NsTiles<PROD>::T128d C;
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int x = nt_xcd(blockIdx.x, dv.tiles * parts);
   if (x >= dv.tiles * parts) return;
   const int part = x / dv.tiles, t = x - part * dv.tiles;
   const NsJob& j = ns_job(dv, t);
-  NtTile<PROD> nt;
+  NtTile nt;
   if (STAGE < 2) {
     int ti, tj;
     ns_triangle(t - j.t[STAGE], &ti, &tj);
@@ -563,14 +590,14 @@ __global__ __launch_bounds__(Nt128d::THREADS, Nt128d::OCC) void ns_part(const Ns
   nt.part = part;
   nt.parts = parts;
   floatx16 acc[C::TP][C::TQ];
-  nt_product<NtHalf, C, PROD>(nt, lds, acc);
+  nt_product<NtHalf, C>(nt, lds, acc);
   nt_put<C>(acc, at<floatx4>(dv.ws, dv.sums) + ((size_t)t * parts + part) * (C::BP * C::BQ / 4));
 }
 
 template <int STAGE, int PROD, bool LAST>
-__global__ __launch_bounds__(Nt64::THREADS) void ns_sum(const NsDev dv, int cur, int parts, float ca,
+__global__ __launch_bounds__(256) void ns_sum(const NsDev dv, int cur, int parts, float ca,
                                                         float cb, float cc, float keep) {
-  typedef Nt128d C;
+  typedef typename NsTiles<PROD>::T128d C;
   typedef NtCfg<2, 2, 1, 1, 128, 1, 1> O;  // 64 x 64, 32 x 32 a wave
   __shared__ __attribute__((aligned(1024))) char lds[NtEpi<O, PROD == 3 ? 2 : 1>::LDS];
   const int t = blockIdx.x / C::WAVES, w = blockIdx.x % C::WAVES;  // tile and wave of it
@@ -594,24 +621,35 @@ __global__ __launch_bounds__(Nt64::THREADS) void ns_sum(const NsDev dv, int cur,
 
 int up(int v, int t) { return (v + t - 1) / t * t; }
 
-// The tiles a product may run on.  Times of a 128-byte slice of the reduction in
-// microseconds: for one workgroup alone (alone), and for a CU whatever it holds (cu);
-// and of a launch besides, for A or B and for X', whose outputs read more.  They are
-// fits to what each tile took where it is at home and where it is not, e.g. (us)
-//                                     256   192   128  128 deep   64  128 in 7
-//   A, 4096 x 4096, products 1        107    82   120       113  162         -
-//   X', the same                      139   182   156       182  256         -
-//   A, 1000 x 2048, products 3        116    72    65        42   26        20
-//   X', the same                       76    55    40        31   27        31
-//   A, ResNet-50's 54 matrices         95    60    58        40   56         -
-//   X', the same                       93   115    92       101  116         -
-constexpr int kNsKinds = 6;
-constexpr NsTile kNsTiles[kNsKinds] = {{"256", 256, 1, 1, 1.10, 1.40, {30.0, 35.0}},
-                                       {"192", 192, 1, 1, 0.65, 0.98, {19.0, 29.0}},
-                                       {"128", 128, 1, 2, 0.70, 0.57, {7.0, 11.0}},
-                                       {"128 deep", 128, 1, 1, 0.33, 0.56, {11.0, 15.0}},
-                                       {"64", 64, 1, 2, 0.21, 0.26, {5.5, 5.5}},
-                                       {"128", 128, 2, 1, 0.33, 0.60, {10.0, 13.0}}};
+// The tiles a product may run on, with one product and with three.  Times of a
+// 128-byte slice of the reduction in microseconds, for one workgroup alone (alone)
+// and for a CU whatever it holds (cu); of a launch besides, for A or B and for X',
+// whose outputs read more; and of the sums of a workgroup to memory and back.  Fits
+// (to 10 %) to what each tile took on ten sets of 256 to 8192 rows and columns, e.g.
+// A / X' in us:
+//                          256       192       128  128 deep        64   64 deep  128 in parts
+//  1: 4096 x 4096      101/136    79/171   114/150   110/177   166/275   184/346       -
+//     1024 x 4096        80/40     49/34     46/25     30/23     18/26     17/33   18/-
+//     3 of 512 x 4608    88/33     53/30     49/22     30/29     18/30     18/41   16/-
+//  3: 4096 x 4096      280/398   193/433   294/430   272/463   319/511   338/544       -
+//     1024 x 4096       227/92    117/54    100/47     67/39     45/40     27/46   26/-
+//     3 of 512 x 4608   258/67    128/43    109/37     75/46     49/45     29/53   24/-
+constexpr int kNsKinds = 7;
+constexpr NsTile kNsTiles[2][kNsKinds] = {
+    {{"256", 256, 1, 1, 1.23, 1.87, {11.1, 19.3}, 0.0},
+     {"192", 192, 1, 1, 0.68, 1.09, {11.8, 21.0}, 0.0},
+     {"128", 128, 1, 2, 0.68, 0.57, {6.4, 13.0}, 0.0},
+     {"128 deep", 128, 1, 1, 0.31, 0.74, {7.7, 10.0}, 0.0},
+     {"64", 64, 1, 2, 0.19, 0.29, {4.7, 6.3}, 0.0},
+     {"64 deep", 64, 1, 1, 0.165, 0.37, {5.1, 6.6}, 0.0},
+     {"128", 128, 2, 1, 0.31, 0.30, {8.0, 7.0}, 0.036}},
+    {{"256", 256, 1, 1, 3.80, 5.50, {15.7, 31.8}, 0.0},
+     {"192", 192, 1, 1, 1.71, 2.82, {14.6, 23.1}, 0.0},
+     {"128", 128, 1, 2, 1.53, 1.76, {7.8, 12.9}, 0.0},
+     {"128 deep", 128, 1, 1, 1.04, 1.72, {8.1, 11.6}, 0.0},
+     {"64", 64, 1, 2, 0.62, 0.53, {5.0, 6.9}, 0.0},
+     {"64 deep", 64, 1, 1, 0.30, 0.60, {5.5, 7.0}, 0.0},
+     {"128", 128, 2, 1, 0.44, 0.59, {11.0, 11.9}, 0.033}}};
 
 // The tile that a product of the set finishes soonest on, by that estimate: the
 // work spread over the CUs (and half of the longest reduction for the last round),
@@ -624,11 +662,11 @@ int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, in
   int best = -1;
   double bt = 0;
   for (int i = 0; i < kNsKinds; ++i) {
-    NsTile c = kNsTiles[i];
+    NsTile c = kNsTiles[products == 3][i];
     double tiles = 0, work = 0, longest = 0;
     for (int n = 0; n < count; ++n) {
       const int r = up(rows[n], 64), l = up(cols[n], 64), m = std::min(r, l);
-      const double k = products * ((stage == 0 ? std::max(r, l) : m) / 64), tm = ceil_div(m, c.side);
+      const double k = (stage == 0 ? std::max(r, l) : m) / 64, tm = ceil_div(m, c.side);
       const double t =
           stage == 2 ? (double)ceil_div(l, c.side) * ceil_div(r, c.side) : tm * (tm + 1) / 2;
       tiles += t;
@@ -640,7 +678,7 @@ int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, in
       c.parts = (int)std::min(std::min(cus / tiles, longest / 2), 16.0);
       if (c.parts < 2) continue;
       longest = ceil(longest / c.parts);
-      t += 2 * tiles * c.parts * (65536.0 / 4e6);
+      t += tiles * c.parts * c.sums;
     }
     const double tail = tiles > cus * c.occ ? 0.5 * longest * c.alone : 0.0;
     t += std::max(work / cus * c.cu + tail, longest * c.alone);
@@ -675,28 +713,29 @@ void ns_launch(const NsStep& s, const NsDev& d, hipStream_t st) {
 template <int STAGE, int PROD, bool LAST>
 void ns_launch_parts(const NsStep& s, const NsDev& d, int parts, hipStream_t st) {
   hipLaunchKernelGGL((ns_part<STAGE, PROD>), dim3((unsigned)(8 * ((d.tiles * parts + 7) / 8))),
-                     dim3(Nt128d::THREADS), 0, st, d, s.cur, parts);
-  hipLaunchKernelGGL((ns_sum<STAGE, PROD, LAST>), dim3((unsigned)(d.tiles * Nt128d::WAVES)),
-                     dim3(Nt64::THREADS), 0, st, d, s.cur, parts, s.ca, s.cb, s.cc, s.keep);
+                     dim3(256), 0, st, d, s.cur, parts);
+  hipLaunchKernelGGL((ns_sum<STAGE, PROD, LAST>), dim3((unsigned)(d.tiles * 4)),
+                     dim3(256), 0, st, d, s.cur, parts, s.ca, s.cb, s.cc, s.keep);
 }
 
 template <int PROD>
 hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
-  const NsDev pre{ws, p.table, p.map_pre, 0, p.n_pre};
+  const NsDev pre{ws, p.table, p.map_pre, 0, p.n_pre, p.count == 1};
   hipLaunchKernelGGL((ns_split<PROD>), dim3((unsigned)p.n_pre), dim3(256), 0, st, pre, a.momentum,
                      a.nesterov);
   for (int i = 0; i < a.steps; ++i) {
     for (int stage = 0; stage < 3; ++stage) {
       const NsStep s{stage, i & 1, i + 1 == a.steps, a.coef[3 * i], a.coef[3 * i + 1],
                      a.coef[3 * i + 2], a.keep};
-      const NsDev d{ws, p.table, p.map[stage], p.sums, p.tiles[stage]};
+      const NsDev d{ws, p.table, p.map[stage], p.sums, p.tiles[stage], p.count == 1};
       const int parts = p.kind[stage].parts;
       switch (p.variant[stage]) {
-        case 0: ns_launch<Nt256, PROD>(s, d, st); break;
-        case 1: ns_launch<Nt192, PROD>(s, d, st); break;
-        case 2: ns_launch<Nt128, PROD>(s, d, st); break;
-        case 3: ns_launch<Nt128d, PROD>(s, d, st); break;
-        case 4: ns_launch<Nt64, PROD>(s, d, st); break;
+        case 0: ns_launch<typename NsTiles<PROD>::T256, PROD>(s, d, st); break;
+        case 1: ns_launch<typename NsTiles<PROD>::T192, PROD>(s, d, st); break;
+        case 2: ns_launch<typename NsTiles<PROD>::T128, PROD>(s, d, st); break;
+        case 3: ns_launch<typename NsTiles<PROD>::T128d, PROD>(s, d, st); break;
+        case 4: ns_launch<typename NsTiles<PROD>::T64, PROD>(s, d, st); break;
+        case 5: ns_launch<typename NsTiles<PROD>::T64d, PROD>(s, d, st); break;
         default:
           if (stage == 0)
             ns_launch_parts<0, PROD, false>(s, d, parts, st);

@@ -38,7 +38,7 @@ struct NsJob {
 struct NsTile {
   const char* name;
   int side, parts, occ;
-  double alone, cu, fixed[2];
+  double alone, cu, fixed[2], sums;
 };
 
 struct NsPlan {
