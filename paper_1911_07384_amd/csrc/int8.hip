@@ -14,6 +14,8 @@
 #include "gemm_nt.hpp"
 #include "products.hpp"
 
+#include <math.h>
+
 #include <algorithm>
 
 namespace fp16k {
@@ -535,34 +537,39 @@ hipError_t launch_i8_fused(const I8Product& a, const h16* x, hipStream_t st) {
 }
 
 namespace {
-// The square tiles of a product: workgroups a CU holds, microseconds that a
-// 128-byte slice of the reduction takes one workgroup alone and a CU whatever it
-// holds, and a launch takes besides.  Fits, e.g. to (us)
-//                              256   192   128  128 deep   64
-//   4096 x 4096 x 4096          65    81    75        89  127
-//   128 x 1000 x 2048 (train)   21    18    12        11    6
+// The square tiles of a product: workgroups a CU holds; microseconds that a
+// 128-byte slice of the reduction takes one workgroup alone, and a CU for each
+// workgroup it holds, that a launch takes besides, and every round of workgroups.
+// Fits (to 10 %) to 22 sizes, e.g. in us:
+//   m x n x k               256    128  128 deep     64
+//   8192 x 4096 x 4096      129    147       168    229
+//   2048 x 2048 x 2048       30     18        15     22
+//   2048 x 4096 x 4096       53     38        45     60
+//   128 x 1000 x 2048        27     14        12      8
+//   8192 x 8192 x 300        67     72       113    113
 struct I8Tile {
   int side, occ;
-  double alone, cu, fixed;
+  double alone, cu, launch, round;
   const char* name;
 };
-constexpr int kI8Kinds = 5;
-constexpr I8Tile kI8Tiles[kI8Kinds + 1] = {
-    {256, 1, 1.10, 1.65, 11.0, "tile 256"},     {192, 1, 0.65, 1.10, 9.0, "tile 192"},
-    {128, 2, 0.60, 0.53, 7.0, "tile 128"},      {128, 1, 0.33, 0.62, 8.0, "tile 128 deep"},
-    {64, 2, 0.21, 0.24, 4.0, "tile 64"},        {0, 0, 0.0, 0.0, 0.0, "few rows"}};
+constexpr int kI8Kinds = 4;
+constexpr I8Tile kI8Tiles[kI8Kinds + 1] = {{256, 1, 1.02, 1.72, 1.5, 11.1, "tile 256"},
+                                           {128, 2, 0.56, 0.50, 0.0, 6.6, "tile 128"},
+                                           {128, 1, 0.33, 0.51, 1.7, 5.3, "tile 128 deep"},
+                                           {64, 2, 0.18, 0.20, 2.7, 2.4, "tile 64"},
+                                           {0, 0, 0.0, 0.0, 0.0, 0.0, "few rows"}};
 
-// The one that finishes soonest by that estimate: the work spread over the CUs (and
-// half a reduction for the last round), or one reduction if that takes longer.
+// The one that finishes soonest by that estimate.
 int i8_tile(int m, int n, int k) {
   if (m <= kFewRows) return kI8Kinds;
   int best = 0;
   double bt = 0;
   for (int i = 0; i < kI8Kinds; ++i) {
     const I8Tile& c = kI8Tiles[i];
-    const double tiles = (double)ceil_div(n, c.side) * ceil_div(m, c.side), slices = ceil_div(k, 128);
-    const double tail = tiles > 256.0 * c.occ ? 0.5 * c.alone : 0.0;
-    const double t = c.fixed + slices * std::max(c.alone, c.cu * tiles / 256.0 + tail);
+    const double tiles = (double)ceil_div(n, c.side) * ceil_div(m, c.side), full = 256.0 * c.occ;
+    const double rounds = ceil(tiles / full), rest = (tiles - (rounds - 1) * full) / 256.0;
+    const double t = c.launch + rounds * c.round +
+                     ceil_div(k, 128) * ((rounds - 1) * c.cu * c.occ + std::max(c.alone, c.cu * rest));
     if (i == 0 || t < bt) {
       bt = t;
       best = i;
@@ -577,10 +584,9 @@ const char* i8_product_name(int m, int n, int k) { return kI8Tiles[i8_tile(m, n,
 hipError_t launch_i8_product(const I8Product& a, hipStream_t st) {
   switch (i8_tile(a.m, a.n, a.k)) {
     case 0: return i8_launch<Nt256>(a, st);
-    case 1: return i8_launch<Nt192>(a, st);
-    case 2: return i8_launch<Nt128>(a, st);
-    case 3: return i8_launch<Nt128d>(a, st);
-    case 4: return i8_launch<Nt64>(a, st);
+    case 1: return i8_launch<Nt128>(a, st);
+    case 2: return i8_launch<Nt128d>(a, st);
+    case 3: return i8_launch<Nt64>(a, st);
   }
   hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0, st,
                      a, (const h16*)nullptr);

@@ -565,28 +565,22 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int c
                           qt + (wave % C::WQ) * 32 * C::TQ);
 }
 
-// Few tiles with a long reduction: each reduction in `parts` workgroups, whose sums
-// a second launch adds in order (64 x 64 of a tile a workgroup) and stores.  The
+// A of few tiles with a long reduction: each reduction in `parts` workgroups, whose
+// sums a second launch adds in order (64 x 64 of a tile a workgroup) and stores.  The
 // workgroups of one part are neighbours: they share operands in the L2.
-// (1000 x 2048, three products, A: 36 tiles of 96 slices; 26 us on 64 x 64 tiles.)
-template <int STAGE, int PROD>
-__global__ __launch_bounds__(256, 1) void ns_part(const NsDev dv, int cur, int parts) {
+// (3 of 512 x 4608, three products: 24 us, 75 on whole 128 x 128 tiles, 29 on 64.)
+template <int PROD>
+__global__ __launch_bounds__(256, 1) void ns_part(const NsDev dv, int parts) {
   typedef typename NsTiles<PROD>::T128d C;
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int x = nt_xcd(blockIdx.x, dv.tiles * parts);
   if (x >= dv.tiles * parts) return;
   const int part = x / dv.tiles, t = x - part * dv.tiles;
   const NsJob& j = ns_job(dv, t);
+  int ti, tj;
+  ns_triangle(t - j.t[0], &ti, &tj);
   NtTile nt;
-  if (STAGE < 2) {
-    int ti, tj;
-    ns_triangle(t - j.t[STAGE], &ti, &tj);
-    ns_sym_tile<STAGE>(dv, j, ti * C::BP, tj * C::BQ, &nt);
-  } else {
-    int pt, qt;
-    ns_x_place<C>(j, t - j.t[2], &pt, &qt);
-    ns_x_tile(dv, j, cur, pt, qt, &nt);
-  }
+  ns_sym_tile<0>(dv, j, ti * C::BP, tj * C::BQ, &nt);
   nt.part = part;
   nt.parts = parts;
   floatx16 acc[C::TP][C::TQ];
@@ -594,9 +588,8 @@ __global__ __launch_bounds__(256, 1) void ns_part(const NsDev dv, int cur, int p
   nt_put<C>(acc, at<floatx4>(dv.ws, dv.sums) + ((size_t)t * parts + part) * (C::BP * C::BQ / 4));
 }
 
-template <int STAGE, int PROD, bool LAST>
-__global__ __launch_bounds__(256) void ns_sum(const NsDev dv, int cur, int parts, float ca,
-                                                        float cb, float cc, float keep) {
+template <int PROD>
+__global__ __launch_bounds__(256) void ns_sum(const NsDev dv, int parts) {
   typedef typename NsTiles<PROD>::T128d C;
   typedef NtCfg<2, 2, 1, 1, 128, 1, 1> O;  // 64 x 64, 32 x 32 a wave
   __shared__ __attribute__((aligned(1024))) char lds[NtEpi<O, PROD == 3 ? 2 : 1>::LDS];
@@ -605,16 +598,11 @@ __global__ __launch_bounds__(256) void ns_sum(const NsDev dv, int cur, int parts
   const int wave = threadIdx.x >> 6;
   const floatx4* from = at<floatx4>(dv.ws, dv.sums) + (size_t)t * parts * (C::BP * C::BQ / 4);
   floatx16 acc[1][1] = {{nt_get<C>(from, parts, w, wave / 2, wave % 2)}};
-  const int dp = (w / C::WQ) * 64 + (wave / 2) * 32, dq = (w % C::WQ) * 64 + (wave % 2) * 32;
-  if constexpr (STAGE < 2) {
-    int ti, tj;
-    ns_triangle(t - j.t[STAGE], &ti, &tj);
-    ns_sym_out<O, STAGE, PROD>(dv, j, cb, cc, acc, lds, ti * C::BP + dp, tj * C::BQ + dq, ti != tj);
-  } else {
-    int pt, qt;
-    ns_x_place<C>(j, t - j.t[2], &pt, &qt);
-    ns_x_out<O, PROD, LAST>(dv, j, cur, ca, keep, acc, lds, pt + dp, qt + dq);
-  }
+  int ti, tj;
+  ns_triangle(t - j.t[0], &ti, &tj);
+  ns_sym_out<O, 0, PROD>(dv, j, 0.0f, 0.0f, acc, lds,
+                         ti * C::BP + (w / C::WQ) * 64 + (wave / 2) * 32,
+                         tj * C::BQ + (w % C::WQ) * 64 + (wave % 2) * 32, ti != tj);
 }
 
 // ---- the plan ------------------------------------------------------------------
@@ -639,10 +627,10 @@ constexpr NsTile kNsTiles[2][kNsKinds] = {
     {{"256", 256, 1, 1, 1.23, 1.87, {11.1, 19.3}, 0.0},
      {"192", 192, 1, 1, 0.68, 1.09, {11.8, 21.0}, 0.0},
      {"128", 128, 1, 2, 0.68, 0.57, {6.4, 13.0}, 0.0},
-     {"128 deep", 128, 1, 1, 0.31, 0.74, {7.7, 10.0}, 0.0},
+     {"128 deep", 128, 1, 1, 0.31, 0.74, {7.7, 8.5}, 0.0},
      {"64", 64, 1, 2, 0.19, 0.29, {4.7, 6.3}, 0.0},
      {"64 deep", 64, 1, 1, 0.165, 0.37, {5.1, 6.6}, 0.0},
-     {"128", 128, 2, 1, 0.31, 0.30, {8.0, 7.0}, 0.036}},
+     {"128", 128, 2, 1, 0.31, 0.30, {9.0, 8.0}, 0.036}},
     {{"256", 256, 1, 1, 3.80, 5.50, {15.7, 31.8}, 0.0},
      {"192", 192, 1, 1, 1.71, 2.82, {14.6, 23.1}, 0.0},
      {"128", 128, 1, 2, 1.53, 1.76, {7.8, 12.9}, 0.0},
@@ -653,8 +641,8 @@ constexpr NsTile kNsTiles[2][kNsKinds] = {
 
 // The tile that a product of the set finishes soonest on, by that estimate: the
 // work spread over the CUs (and half of the longest reduction for the last round),
-// or the longest reduction if that takes longer.  The last kind splits reductions in
-// as many parts as give every CU one; its sums go to memory and back.
+// or the longest reduction if that takes longer.  The last kind, for A only, splits
+// reductions in as many parts as give every CU one; its sums go to memory and back.
 // stage 0: A, 1: B, 2: X'.
 int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, int products,
               NsTile* tile) {
@@ -675,6 +663,7 @@ int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, in
     }
     double t = c.fixed[stage == 2];
     if (c.parts > 1) {
+      if (stage != 0) continue;
       c.parts = (int)std::min(std::min(cus / tiles, longest / 2), 16.0);
       if (c.parts < 2) continue;
       longest = ceil(longest / c.parts);
@@ -710,14 +699,6 @@ void ns_launch(const NsStep& s, const NsDev& d, hipStream_t st) {
     hipLaunchKernelGGL((ns_x<C, PROD, true>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
 }
 
-template <int STAGE, int PROD, bool LAST>
-void ns_launch_parts(const NsStep& s, const NsDev& d, int parts, hipStream_t st) {
-  hipLaunchKernelGGL((ns_part<STAGE, PROD>), dim3((unsigned)(8 * ((d.tiles * parts + 7) / 8))),
-                     dim3(256), 0, st, d, s.cur, parts);
-  hipLaunchKernelGGL((ns_sum<STAGE, PROD, LAST>), dim3((unsigned)(d.tiles * 4)),
-                     dim3(256), 0, st, d, s.cur, parts, s.ca, s.cb, s.cc, s.keep);
-}
-
 template <int PROD>
 hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
   const NsDev pre{ws, p.table, p.map_pre, 0, p.n_pre, p.count == 1};
@@ -737,14 +718,10 @@ hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
         case 4: ns_launch<typename NsTiles<PROD>::T64, PROD>(s, d, st); break;
         case 5: ns_launch<typename NsTiles<PROD>::T64d, PROD>(s, d, st); break;
         default:
-          if (stage == 0)
-            ns_launch_parts<0, PROD, false>(s, d, parts, st);
-          else if (stage == 1)
-            ns_launch_parts<1, PROD, false>(s, d, parts, st);
-          else if (!s.last)
-            ns_launch_parts<2, PROD, false>(s, d, parts, st);
-          else
-            ns_launch_parts<2, PROD, true>(s, d, parts, st);
+          hipLaunchKernelGGL((ns_part<PROD>), dim3((unsigned)(8 * ((d.tiles * parts + 7) / 8))),
+                             dim3(256), 0, st, d, parts);
+          hipLaunchKernelGGL((ns_sum<PROD>), dim3((unsigned)(d.tiles * 4)), dim3(256), 0, st, d,
+                             parts);
       }
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
@@ -812,11 +789,7 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
   }
   for (int stage = 0; stage < 3; ++stage) P.map[stage] = take((uint64_t)P.tiles[stage] * 2);
   P.map_pre = take((uint64_t)P.n_pre * 2);
-  size_t sums = 0;
-  for (int stage = 0; stage < 3; ++stage)
-    if (P.kind[stage].parts > 1)
-      sums = std::max(sums, (size_t)P.tiles[stage] * P.kind[stage].parts * 65536);
-  P.sums = take(sums);
+  P.sums = take(P.kind[0].parts > 1 ? (uint64_t)P.tiles[0] * P.kind[0].parts * 65536 : 0);
   P.bytes = (size_t)off * 256;
 }
 

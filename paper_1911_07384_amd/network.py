@@ -16,7 +16,12 @@ Section 5.1).
 Options: ``bn_swap`` makes every block-last BN the BN swap of Section 4.1
 (the shortcut joins before gamma); ``zero_gamma_last`` starts every
 block-last gamma at 0 (the initialisation of Section 5.1; with the swap it
-also zeroes the shortcut's contribution at the start).
+also zeroes the shortcut's contribution at the start); ``optimizer="muon"``
+updates the convolution filters and the classifier's weights by orthogonalised
+momentum (fp16_muon_step, each filter as a [K, R*S*C] matrix) in one call, and
+the classifier's bias and the BN parameters by SGD as before;
+``classifier="int8"`` runs the classifier's products in 8-bit integers
+(fp16_int8_dense_*), its weights quantised anew in every step.
 
 The step is an explicit program: a list of ``Op`` records, each one ABI call
 with named device buffers.  Running the list in order is one training step.
@@ -66,7 +71,12 @@ class ResNet50:
                  lr: float = 0.1, momentum: float = 0.9, weight_decay: float = 1e-4,
                  post_scale: float = 0.25, eps: float = 1e-5, stages=STAGES, device="cuda",
                  bn_swap: bool = False, zero_gamma_last: bool = False,
-                 fuse_bn_stats: bool = True):
+                 fuse_bn_stats: bool = True, optimizer: str = "sgd", classifier: str = "fp16",
+                 muon_lr: float = 0.02, muon_momentum: float = 0.95, muon_products: int = 1):
+        if optimizer not in ("sgd", "muon") or classifier not in ("fp16", "int8"):
+            raise ValueError(f"optimizer {optimizer!r}, classifier {classifier!r}")
+        self.optimizer, self.classifier = optimizer, classifier
+        self.muon_lr, self.muon_momentum, self.muon_products = muon_lr, muon_momentum, muon_products
         self.n, self.image, self.classes = n, image, classes
         self.lr, self.momentum, self.wd = lr, momentum, weight_decay
         self.post_scale, self.eps = post_scale, eps
@@ -175,6 +185,8 @@ class ResNet50:
         self._buf("gap.y", (n, 1, 1, cin))
         self.fwd.append(Op("avgpool_fwd", "gap", {"desc": gd, "x": xname, "y": "gap.y"}))
         self._conv("fc", self.buffers["gap.y"], "gap.y", cin, self.classes, 1, 1, 0)
+        if self.classifier == "int8":
+            self._int8_classifier(cin)
         self._buf("loss", (n,), torch.float32)
         self._buf("fc.dy", (n, 1, 1, self.classes))
         self.fwd.append(Op("softmax_ce", "loss", {"n": n, "k": self.classes, "z": "fc.y",
@@ -186,6 +198,21 @@ class ResNet50:
         if self.fuse:
             self._fuse_bn_pool()
             self._fuse_conv_bn()
+
+    def _int8_classifier(self, cin):
+        """The classifier's forward on quantised operands: its weights in both
+        layouts, then the product (in place of the convolution just planned)."""
+        d = F.int8_dense_desc(self.n, cin, self.classes)
+        self._ws_need = max(self._ws_need, F.fp16_int8_dense_workspace_bytes(d))
+        for name, rows, cols in (("fc.wq", self.classes, cin), ("fc.wqt", cin, self.classes)):
+            self._buf(name, (rows, F.fp16_int8_row_bytes(cols)), torch.int8)
+            self._buf(name + ".scale", (rows,), torch.float32)
+        self.fwd.pop()
+        self.fwd.append(Op("int8_weights", "fc", {"desc": d, "w": "fc", "wq": "fc.wq",
+                                                  "sw": "fc.wq.scale", "wqt": "fc.wqt",
+                                                  "swt": "fc.wqt.scale"}))
+        self.fwd.append(Op("int8_fwd", "fc", {"desc": d, "x": "gap.y", "wq": "fc.wq",
+                                              "sw": "fc.wq.scale", "y": "fc.y"}))
 
     def _fuse_bn_pool(self):
         """A BN + ReLU whose output only feeds the max pool that follows it
@@ -309,8 +336,14 @@ class ResNet50:
 
     def _plan_backward(self, gd, pd):
         # classifier: the loss kernel wrote fc.dy and the bias gradient
-        self._conv_bwd("fc", "fc.dy")
         dgap = self._grad("gap.y")
+        if self.classifier == "int8":
+            a = next(o for o in self.fwd if o.kind == "int8_weights").a
+            self.bwd.append(Op("int8_bwd", "fc", {"desc": a["desc"], "x": "gap.y", "dy": "fc.dy",
+                                                  "wqt": a["wqt"], "swt": a["swt"], "dx": dgap,
+                                                  "dw": "d:fc"}))
+        else:
+            self._conv_bwd("fc", "fc.dy")
         dlast = self._grad(self._last)
         self.bwd.append(Op("avgpool_bwd", "gap", {"desc": gd, "dy": dgap, "dx": dlast}))
         dout = dlast
@@ -404,13 +437,34 @@ class ResNet50:
             self.buffers[name + ".beta"] = self.bn_arena[off:off + c]
             self.buffers[name + ".dbeta"] = self.dbn_arena[off:off + c]
             off += c
-        self.upd = [
-            Op("sgd", "sgd_weights", {"w": self.w_arena, "g": self.dw_arena, "m": self.mw_arena,
-                                      "wd": self.wd}),
+        if self.optimizer == "muon":
+            weights, at = self._muon_op(), sum(sizes)  # the classifier's bias stays with SGD
+            arenas = [t[at:] for t in (self.w_arena, self.dw_arena, self.mw_arena)]
+            name = "sgd_bias"
+        else:
+            weights, arenas = [], [self.w_arena, self.dw_arena, self.mw_arena]
+            name = "sgd_weights"
+        self.upd = weights + [
+            Op("sgd", name, {"w": arenas[0], "g": arenas[1], "m": arenas[2], "wd": self.wd}),
             Op("sgd", "sgd_bn", {"w": self.bn_arena, "g": self.dbn_arena, "m": self.mbn_arena,
                                  "wd": 0.0}),
         ]
         self.n_weights, self.n_bn = nw, nb
+
+    def _muon_op(self):
+        """One update of every filter as a matrix [K, R*S*C], its scale
+        sqrt(max(1, K / (R*S*C)))."""
+        shapes, views, off = [], ([], [], []), 0
+        for name, sh, _ in self._wspecs:
+            rows, cols = sh[0], int(np.prod(sh[1:]))
+            shapes.append((rows, cols, max(1.0, rows / cols) ** 0.5))
+            for v, arena in zip(views, (self.w_arena, self.dw_arena, self.mw_arena)):
+                v.append(arena[off:off + rows * cols].view(rows, cols))
+            off += rows * cols
+        descs = F.muon_descs(shapes)
+        ws = F.workspace(F.fp16_muon_workspace_bytes(descs, self.muon_products), self.dev)
+        return [Op("muon", "muon_weights", {"descs": descs, "w": views[0], "g": views[1],
+                                            "m": views[2], "ws": ws})]
 
     def load_batch(self, seed: int = 0):
         """Synthetic images ~ N(0, 1) and uniform labels (the ImageNet shapes)."""
@@ -493,6 +547,17 @@ class ResNet50:
         elif k == "softmax_ce":
             F.fp16_softmax_ce(a["n"], a["k"], t(a["z"]), t(a["bias"]), t(a["labels"]),
                               t(a["loss"]), t(a["dz"]), t(a["dbias"]))
+        elif k == "int8_weights":
+            F.fp16_int8_dense_weights(a["desc"], t(a["w"]), t(a["wq"]), t(a["sw"]), t(a["wqt"]),
+                                      t(a["swt"]), ws)
+        elif k == "int8_fwd":
+            F.fp16_int8_dense_fwd(a["desc"], t(a["x"]), t(a["wq"]), t(a["sw"]), None, t(a["y"]), ws)
+        elif k == "int8_bwd":
+            F.fp16_int8_dense_bwd(a["desc"], t(a["x"]), t(a["dy"]), t(a["wqt"]), t(a["swt"]),
+                                  t(a["dx"]), t(a["dw"]), None, ws)
+        elif k == "muon":
+            F.fp16_muon_step(a["descs"], a["w"], a["g"], a["m"], self.muon_lr, self.muon_momentum,
+                             self.wd, products=self.muon_products, ws=a["ws"])
         elif k == "sgd":
             F.fp16_sgd_step(a["w"], a["g"], a["m"], a["w"].numel(), self.lr, self.momentum,
                             a["wd"])
@@ -514,7 +579,9 @@ class ResNet50:
                 "bn_bwd": ("dx", "dgamma", "dbeta", "dres"), "maxpool_fwd": ("y", "idx"),
                 "maxpool_bwd": ("dx",), "avgpool_fwd": ("y",), "avgpool_bwd": ("dx",),
                 "bn_maxpool_fwd": ("stats", "y", "idx"),
-                "softmax_ce": ("loss", "dz", "dbias"), "dgrad_filter": ("wf",)}
+                "softmax_ce": ("loss", "dz", "dbias"), "dgrad_filter": ("wf",),
+                "int8_weights": ("wq", "sw", "wqt", "swt"), "int8_fwd": ("y",),
+                "int8_bwd": ("dx", "dw")}
 
     def _schedule(self):
         """For each weight gradient of the backward, the index (in bwd) of the

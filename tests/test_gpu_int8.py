@@ -119,7 +119,7 @@ def test_halfway_and_special_values(by):
 PRODUCTS = [(1, 1, 1), (1, 33, 100), (3, 1000, 2048), (16, 130, 4111), (2, 40, 131071),
             (17, 1, 15), (17, 40, 16), (64, 64, 128), (65, 129, 129), (128, 1000, 2048),
             (200, 77, 1337), (900, 700, 200), (2049, 2047, 300), (2100, 2056, 64),
-            (2900, 3000, 700), (4001, 3601, 257), (3585, 3700, 128)]
+            (1111, 2501, 1337), (2900, 3000, 700), (4001, 3601, 257), (3585, 3700, 128)]
 
 
 @pytest.mark.parametrize("case", PRODUCTS, ids=lambda c: "x".join(map(str, c)))

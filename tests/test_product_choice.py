@@ -1,0 +1,25 @@
+"""The tiles that the cases of the GPU tests run on, asked of the library on the
+host: a changed estimate must not move a test off the kernel it is for."""
+
+import paper_1911_07384_amd as F
+import test_gpu_int8 as int8
+import test_gpu_muon as muon
+
+def test_every_tile_of_the_products_is_covered():
+    """A, B and X', with one product and with three, on every tile that the rule ever
+    gives them; reductions in parts are offered to A only."""
+    for products in (1, 3):
+        seen = [set(), set(), set()]
+        for shapes in muon.SETS:
+            kinds = F.fp16_muon_kernels(F.muon_descs(shapes), products).split(", ")
+            for s, k in zip(seen, kinds):
+                s.add("parts" if " in " in k else k)
+        plain = {"256", "192", "128", "128 deep", "64"}
+        assert seen[0] == plain | {"64 deep", "parts"}, (products, seen[0])
+        assert seen[1] == plain | ({"64 deep"} if products == 3 else set()), (products, seen[1])
+        assert seen[2] == plain | ({"64 deep"} if products == 3 else set()), (products, seen[2])
+
+
+def test_every_tile_of_the_8_bit_product_is_covered():
+    got = {F.fp16_int8_kernel(*c) for c in int8.PRODUCTS}
+    assert got == {"few rows", "tile 64", "tile 128", "tile 128 deep", "tile 256"}
