@@ -77,6 +77,22 @@ __device__ __forceinline__ uint32_t i8_wave_max(uint32_t v) {
   return v;
 }
 
+// The maximum over the 32 lanes of a half wave, in every one of them, by register
+// permutes alone (quads, eights, sixteens, then the two rows of 16).
+template <int CTRL>
+__device__ __forceinline__ uint32_t i8_max_dpp(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+  return o > v ? o : v;
+}
+__device__ __forceinline__ uint32_t i8_half_max(uint32_t v) {
+  v = i8_max_dpp<0xB1>(v);   // lanes 1 0 3 2 of each quad
+  v = i8_max_dpp<0x4E>(v);   // 2 3 0 1
+  v = i8_max_dpp<0x141>(v);  // 7 .. 0 of each eight
+  v = i8_max_dpp<0x140>(v);  // 15 .. 0 of each sixteen
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return r[0] > r[1] ? r[0] : r[1];
+}
+
 // Eight elements from p of a row that ends `left` elements further on, zeros past it.
 __device__ __forceinline__ V8 i8_load8(const h16* p, int left) {
   if (left >= 8) return load16u(p);
@@ -135,7 +151,7 @@ __global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __re
 // First pass: 256 columns of a range of rows a workgroup, a thread 8 columns of
 // every eighth row: the largest magnitude (and the sum) of each column over the
 // range and, for the rows, of each row over the 256 columns.
-constexpr int kColChunks = 16;  // ranges of rows, at most
+constexpr int kColChunks = 32, kColRows = 32;  // ranges of rows at most, rows of one at least
 __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
   const I8Cols& j = both.job[blockIdx.z];
   if ((int)blockIdx.x * 256 >= j.cols || (int)blockIdx.y >= j.chunks) return;
@@ -163,12 +179,7 @@ __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
         if (want_sum) s[e] += to_f32(v[u].h[e]);
       }
       if (want_rows) {
-        uint32_t top = i8_mag8(v[u], 0);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-          const uint32_t o = (uint32_t)__shfl_xor((int)top, off, 64);
-          top = o > top ? o : top;
-        }
+        const uint32_t top = i8_half_max(i8_mag8(v[u], 0));
         if (cg == 0 && r + 8 * u < r1) j.rmag[(int64_t)blockIdx.x * j.rows + r + 8 * u] = top;
       }
     }
@@ -192,31 +203,35 @@ __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
   if (want_sum) j.psum[(int64_t)blockIdx.y * j.cols + cc] = t;
 }
 
-// Second pass: 128 rows x 128 columns quantised and written transposed, a 128-byte
-// run of each column through LDS, and as laid out, a run of each row.
+// Second pass: T rows x T columns quantised and written transposed, a run of T bytes
+// of each column through LDS, and as laid out, a run of each row.  T = 128 writes
+// whole lines, T = 64 has four times the workgroups for small matrices (128 x 1000
+// and 128 x 2048: 9.0 us on 128).
+template <int T>
 __global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
   const I8Cols& j = both.job[blockIdx.z];
-  const int c0 = blockIdx.x * 128, r0 = blockIdx.y * 128;
+  const int c0 = blockIdx.x * T, r0 = blockIdx.y * T;
   if (c0 >= j.ldr || r0 >= j.ldc) return;
-  constexpr int LD = 144;  // bytes from column to column of the tile
-  __shared__ I8Quant cq[128], rq[128];
-  __shared__ __attribute__((aligned(16))) int8_t tile[128 * LD];
+  constexpr int LD = T + 16;             // bytes from column to column of the tile
+  constexpr int CG = T / 8, R = T * T / 2048;  // groups of 8 columns; rows a thread
+  __shared__ I8Quant cq[T], rq[T];
+  __shared__ __attribute__((aligned(16))) int8_t tile[T * LD];
   const int tid = threadIdx.x;
   const bool want_rows = j.rmag != nullptr;
-  const int cg = tid & 15, rg = tid >> 4;  // 8 columns, rows 8 rg .. + 7
+  const int cg = tid % CG, rg = tid / CG;  // columns 8 cg .. + 7, rows R rg .. + R - 1
   const int c = c0 + cg * 8;
-  V8 v[8];
+  V8 v[R];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + rg * 8 + i;
+  for (int i = 0; i < R; ++i) {
+    const int r = r0 + rg * R + i;
     v[i] = r < j.rows && c < j.cols ? i8_load8(j.x + (int64_t)r * j.cols + c, j.cols - c) : zero8();
   }
-  if (tid < 128) {
+  if (tid < T) {
     const int k = c0 + tid;
     uint32_t a = 0;
     double s = 0.0;
     if (k < j.cols) {
-#pragma unroll 8
+#pragma unroll 16
       for (int i = 0; i < j.chunks; ++i) {
         const uint32_t b = j.cmag[(int64_t)i * j.cols + k];
         a = b > a ? b : a;
@@ -230,27 +245,27 @@ __global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
       }
     }
     cq[tid] = i8_quant(a);
-  } else if (want_rows) {
-    const int k = r0 + tid - 128;
+  } else if (want_rows && tid < 2 * T) {
+    const int k = r0 + tid - T;
     uint32_t a = 0;
     if (k < j.rows) {
       const int n = (j.cols + 255) / 256;
-#pragma unroll 8
+#pragma unroll 16
       for (int i = 0; i < n; ++i) {
         const uint32_t b = j.rmag[(int64_t)i * j.rows + k];
         a = b > a ? b : a;
       }
       if (blockIdx.x == 0) j.scale_r[k] = i8_scale(a);
     }
-    rq[tid - 128] = i8_quant(a);
+    rq[tid - T] = i8_quant(a);
   }
   __syncthreads();
   if (want_rows) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = r0 + rg * 8 + i;
+    for (int i = 0; i < R; ++i) {
+      const int r = r0 + rg * R + i;
       if (r < j.rows && c < j.ldr)
-        *reinterpret_cast<uint2*>(j.qr + (int64_t)r * j.ldr + c) = i8_pack(v[i], rq[rg * 8 + i]);
+        *reinterpret_cast<uint2*>(j.qr + (int64_t)r * j.ldr + c) = i8_pack(v[i], rq[rg * R + i]);
     }
   }
 #pragma unroll
@@ -258,17 +273,24 @@ __global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
     const I8Quant k = cq[cg * 8 + e];
     uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = i8_byte(i8_x127(v[i].h[e]), k);
-    *reinterpret_cast<uint2*>(tile + (cg * 8 + e) * LD + rg * 8) =
-        make_uint2(i8_pack4(b[0], b[1], b[2], b[3]), i8_pack4(b[4], b[5], b[6], b[7]));
+    for (int i = 0; i < 8; ++i) b[i] = i < R ? i8_byte(i8_x127(v[i < R ? i : 0].h[e]), k) : 0u;
+    // (16-byte chunks exclusive-ored with the columns' group: a lane's columns lie 8
+    // lines from its neighbour's)
+    const int at = rg * R;
+    int8_t* to = tile + (cg * 8 + e) * LD + ((at / 16) ^ (cg % (T / 16))) * 16 + at % 16;
+    const uint32_t w = i8_pack4(b[0], b[1], b[2], b[3]);
+    if (R == 8)
+      *reinterpret_cast<uint2*>(to) = make_uint2(w, i8_pack4(b[4], b[5], b[6], b[7]));
+    else
+      *reinterpret_cast<uint16_t*>(to) = (uint16_t)w;
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int cc = (i * 256 + tid) >> 3, k = ((i * 256 + tid) & 7) * 16;
+  for (int i = 0; i < T * T / 4096; ++i) {
+    const int cc = (i * 256 + tid) / (T / 16), k = (i * 256 + tid) % (T / 16) * 16;
     if (c0 + cc < j.cols && r0 + k < j.ldc)
       *reinterpret_cast<u32x4*>(j.qc + (int64_t)(c0 + cc) * j.ldc + r0 + k) =
-          *reinterpret_cast<const u32x4*>(tile + cc * LD + k);
+          *reinterpret_cast<const u32x4*>(tile + cc * LD + ((k / 16) ^ (cc / 8 % (T / 16))) * 16);
   }
 }
 
@@ -471,7 +493,7 @@ hipError_t launch_i8_rows(int rows, int cols, const h16* x, int8_t* q, float* sc
 }
 
 void i8_cols_plan(I8Cols* j) {
-  j->per = std::max(64, ceil_div(ceil_div(j->rows, kColChunks), 8) * 8);
+  j->per = std::max(kColRows, ceil_div(ceil_div(j->rows, kColChunks), 32) * 32);
   j->chunks = ceil_div(j->rows, j->per);
   j->ldc = (int)i8_row(j->rows);
   j->ldr = (int)i8_row(j->cols);
@@ -519,9 +541,13 @@ hipError_t launch_i8_cols(const I8Cols* jobs, int count, hipStream_t st) {
   }
   hipLaunchKernelGGL(i8_cols_max, dim3((unsigned)ceil_div(cols, 256), (unsigned)chunks, (unsigned)count),
                      dim3(256), 0, st, b);
-  hipLaunchKernelGGL(i8_cols_write,
-                     dim3((unsigned)ceil_div(cols, 128), (unsigned)ceil_div(rows, 128), (unsigned)count),
-                     dim3(256), 0, st, b);
+  const bool small = (int64_t)ceil_div(cols, 128) * ceil_div(rows, 128) * count < 512;
+  const int t = small ? 64 : 128;
+  const dim3 grid((unsigned)ceil_div(cols, t), (unsigned)ceil_div(rows, t), (unsigned)count);
+  if (small)
+    hipLaunchKernelGGL(i8_cols_write<64>, grid, dim3(256), 0, st, b);
+  else
+    hipLaunchKernelGGL(i8_cols_write<128>, grid, dim3(256), 0, st, b);
   return hipGetLastError();
 }
 
