@@ -10,7 +10,9 @@
  * rounded once to binary16, to nearest with ties to even, at its store
  * (Section 4.2 leaves the rounding method open; this library uses the IEEE
  * default).  Binary16 subnormals are kept (gradual underflow) and overflow
- * rounds to +-infinity.
+ * rounds to +-infinity.  The exceptions are statistics, losses and masks, and the
+ * quantised operands of the 8-bit dense layers, which say so where they are
+ * declared.
  *
  * Conventions shared by every entry point:
  *   - Buffers are device pointers owned by the caller.  The library never

@@ -457,16 +457,16 @@ def fp16_conv_bn_relu_fwd_m(conv, bn, x, w, gamma, beta, residual, y, z, stats, 
 
 def muon_descs(shapes):
     """The descriptors of a set of matrices: (rows, cols) or (rows, cols, scale) each."""
-    return (MuonDesc * max(len(shapes), 1))(*[MuonDesc(*s) if len(s) == 3 else MuonDesc(*s, 1.0)
-                                              for s in shapes])
+    return (MuonDesc * len(shapes))(*[MuonDesc(*s) if len(s) == 3 else MuonDesc(*s, 1.0)
+                                      for s in shapes])
 
 
 def _muon_list(descs, *lists):
     """The number of matrices and an array of pointers for each list of tensors."""
     n = len(lists[0])
-    if any(len(l) != n for l in lists) or len(descs) < n:
+    if any(len(l) != n for l in (descs, *lists)):
         raise ValueError("descs and the lists of tensors differ in length")
-    return [n] + [(_P * max(n, 1))(*[_ptr(t) for t in l]) for l in lists]
+    return [n] + [(_P * n)(*[_ptr(t) for t in l]) for l in lists]
 
 
 def _coef(coef, steps):

@@ -424,7 +424,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, cons
       mag = i8_wave_max(mag);
       if (lane == 0) top[r][w] = mag;
     }
-    if (wpr > 1) __syncthreads();
+    if (wpr > 1)
+      __syncthreads();
+    else
+      nt_wave_sync();
     for (int r = wave / wpr; r < g.m; r += kFewWaves / wpr) {
       const h16* xr = x + (int64_t)r * g.k;
       uint32_t mag = 0;

@@ -155,6 +155,10 @@ def test_dense_refusals():
 def test_binding_checks():
     with pytest.raises(ValueError):
         F.fp16_orthogonalize(F.muon_descs([(8, 8)]), [A], [B, C], ws=W, ws_bytes=0, stream=0)
+    with pytest.raises(ValueError):  # (a workspace for two, tensors for one)
+        F.fp16_orthogonalize(F.muon_descs([(8, 8)] * 2), [A], [B], ws=W, ws_bytes=0, stream=0)
+    F.fp16_orthogonalize(F.muon_descs([]), [], [], stream=0)  # nothing to do
+    F.fp16_muon_step(F.muon_descs([]), [], [], [], stream=0)
     with pytest.raises(ValueError):
         F.fp16_orthogonalize(F.muon_descs([(8, 8)]), [A], [B], coef=(1.0, 2.0), ws=W, ws_bytes=0,
                              stream=0)

@@ -211,6 +211,51 @@ def test_parts_of_the_backward():
     assert same(a.cpu().numpy(), dx) and same(b.cpu().numpy(), dw)
 
 
+def test_offsets_past_32_bits():
+    """Quantisers of 2.2e9 elements and a product of as many outputs, compared in
+    blocks on the device."""
+    require_gpu()
+    rows, cols = 70001, 31003
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty((rows, cols), dtype=torch.float16, device="cuda").normal_(generator=g)
+    assert x.numel() > 2 ** 31
+    for by in ("rows", "cols"):
+        n, l = (rows, cols) if by == "rows" else (cols, rows)
+        q, s = F.int8_operand(n, l)
+        note(f"[gpu] int8 quant {by} {rows}x{cols}")
+        if by == "rows":
+            F.fp16_int8_quant_rows(rows, cols, x, q, s)
+        else:
+            F.fp16_int8_quant_cols(rows, cols, x, q, s,
+                                   F.workspace(F.fp16_int8_quant_workspace_bytes(rows, cols)))
+        torch.cuda.synchronize()
+        for a in list(range(0, n - 4096, 8192)) + [n - 4096]:
+            b = min(n, a + 4096)
+            t = x[a:b] if by == "rows" else x[:, a:b].t().contiguous()
+            top = t.abs().amax(1, keepdim=True).double()
+            # (quotients in float64 are within 2^-52 of halfway ones or exactly there)
+            assert torch.equal(q[a:b, :l], (127.0 * t.double() / top).round().to(torch.int8))
+            assert not q[a:b, l:].any()
+            assert torch.equal(s[a:b].cpu(), top[:, 0].float().cpu() / np.float32(127.0))
+        del q, s
+    del x, t
+    m, n, k = 70001, 31003, 33
+    (qa, sa), (qb, sb) = F.int8_operand(m, k), F.int8_operand(n, k)
+    for q, s in ((qa, sa), (qb, sb)):
+        q.zero_()
+        q[:, :k] = torch.randint(-127, 128, (len(q), k), generator=g, device="cuda").to(torch.int8)
+        s.uniform_(0.001, 0.002, generator=g)
+    y = torch.empty((m, n), dtype=torch.float16, device="cuda")
+    note(f"[gpu] int8 product {m}x{n}x{k} {F.fp16_int8_kernel(m, n, k)}")
+    F.fp16_int8_matmul(m, n, k, qa, sa, qb, sb, None, y)
+    torch.cuda.synchronize()
+    bt = qb.float().t().contiguous()
+    for a in list(range(0, m - 4096, 8192)) + [m - 4096]:
+        b = min(m, a + 4096)
+        acc = qa[a:b].float() @ bt  # integers below 2^24
+        assert torch.equal(y[a:b], (sa[a:b, None] * sb[None, :] * acc).half())
+
+
 def test_rows_that_are_not_finite_stay_apart():
     """A token with a NaN makes its own outputs NaN, and no other token's."""
     x, w, dy, bias = layer(40, 64, 32)

@@ -212,6 +212,34 @@ def test_same_bits_again_and_on_another_stream():
         assert torch.equal(x, y) and torch.equal(x, z)
 
 
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape", [(16300, 65500), (65500, 16300)], ids=["wide", "tall"])
+def test_the_largest_matrices(shape, products):
+    """Offsets past 2^31 bytes.  One element a row and column of the shorter side, so
+    that the singular values are known, every product of two rows is zero, and the
+    result is the polynomial of each element on its own; everything else stays zero."""
+    require_gpu()
+    m, n = min(shape), max(shape)
+    v = (1.0 + 0.5 * torch.sin(torch.arange(m, dtype=torch.float64))).half()
+    i = torch.arange(m, device="cuda")
+    j = n - 1 - 4 * i  # to the far end of the last row
+    at = i * n + j if shape[0] == m else j * m + i
+    x = torch.zeros(shape, dtype=torch.float16, device="cuda")
+    x.view(-1)[at] = v.cuda()
+    d = F.muon_descs([(*shape, 1.0)])
+    ws = F.workspace(F.fp16_muon_workspace_bytes(d, products))
+    note(f"[gpu] orthogonalize {shape} products={products}")
+    F.fp16_orthogonalize(d, [x], [x], 2, None, products, ws)
+    torch.cuda.synchronize()
+    s = v.double() / v.double().norm()
+    for _ in range(2):
+        s = QUINTIC[0] * s + QUINTIC[1] * s ** 3 + QUINTIC[2] * s ** 5
+    got = x.view(-1)[at]
+    assert off(got, s.cuda()) <= BAR[products]
+    x.view(-1)[at] = 0
+    assert not x.view(torch.int16).any()
+
+
 # ---- the update --------------------------------------------------------------------
 
 def step(ws_, gs, ms, scales, lr, mu, wd, nesterov, products, steps=5):
