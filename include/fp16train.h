@@ -503,7 +503,7 @@ typedef struct {
 size_t fp16_muon_workspace_bytes(int32_t count, const fp16_muon_desc* descs, int32_t products);
 
 /* Sides of the tiles that A, B and X of such a call run on, e.g. "192, 192, 256"
- * ("128 in 7": the reduction in 7 parts), for tests and profiles; "" for an
+ * ("128 in 7": the reduction in 7 parts), or "one workgroup each", for tests and profiles; "" for an
  * invalid list.  No contract; valid until the thread's next call. */
 const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_t products);
 

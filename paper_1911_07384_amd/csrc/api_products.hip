@@ -203,6 +203,7 @@ const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_
   if (!ns_list_ok(count, descs, products)) return "";
   NsPlan plan;
   ns_make_plan(count, descs, products, &plan);
+  if (plan.small) return "one workgroup each";
   char* at = name;
   for (const NsTile& k : plan.kind) {
     at += snprintf(at, sizeof(name) - (size_t)(at - name), "%s%s", at == name ? "" : ", ", k.name);

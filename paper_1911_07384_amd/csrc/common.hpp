@@ -6,6 +6,7 @@
 
 typedef _Float16 h16;
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
@@ -41,6 +42,26 @@ __device__ __forceinline__ V8 zero8() {
   V8 v;
   v.u = u32x4{0u, 0u, 0u, 0u};
   return v;
+}
+
+// Eight elements from p of a row that ends `left` elements further on: zeros past
+// it, and nothing stored there.
+__device__ __forceinline__ V8 load8_upto(const h16* p, int left) {
+  if (left >= 8) return load16u(p);
+  V8 v = zero8();
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) v.h[e] = p[e];
+  return v;
+}
+__device__ __forceinline__ void store8_upto(h16* p, const V8& v, int left) {
+  if (left >= 8) {
+    store16u(p, v);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) p[e] = v.h[e];
 }
 
 // float32 -> binary16, round to nearest even (v_cvt_f16_f32 in the default

@@ -93,16 +93,6 @@ __device__ __forceinline__ uint32_t i8_half_max(uint32_t v) {
   return r[0] > r[1] ? r[0] : r[1];
 }
 
-// Eight elements from p of a row that ends `left` elements further on, zeros past it.
-__device__ __forceinline__ V8 i8_load8(const h16* p, int left) {
-  if (left >= 8) return load16u(p);
-  V8 v = zero8();
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < left) v.h[e] = p[e];
-  return v;
-}
-
 __device__ __forceinline__ uint2 i8_pack(const V8& v, const I8Quant& k) {
   uint32_t b[8];
 #pragma unroll
@@ -125,12 +115,12 @@ __global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __re
 #pragma unroll
   for (int i = 0; i < kRowKeep; ++i) {
     const int c = (i * 256 + tid) * 8;
-    keep[i] = i8_load8(xr + (c < cols ? c : 0), cols - c);
+    keep[i] = load8_upto(xr + (c < cols ? c : 0), cols - c);
   }
 #pragma unroll
   for (int i = 0; i < kRowKeep; ++i) mag = i8_mag8(keep[i], mag);
   for (int c = (kRowKeep * 256 + tid) * 8; c < cols; c += 2048)
-    mag = i8_mag8(i8_load8(xr + c, cols - c), mag);
+    mag = i8_mag8(load8_upto(xr + c, cols - c), mag);
   mag = i8_wave_max(mag);
   if ((tid & 63) == 0) red[tid >> 6] = mag;
   __syncthreads();
@@ -143,7 +133,7 @@ __global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __re
     if (c < ld) *reinterpret_cast<uint2*>(qr + c) = i8_pack(keep[i], k);
   }
   for (int c = (kRowKeep * 256 + tid) * 8; c < ld; c += 2048)
-    *reinterpret_cast<uint2*>(qr + c) = i8_pack(i8_load8(xr + (c < cols ? c : 0), cols - c), k);
+    *reinterpret_cast<uint2*>(qr + c) = i8_pack(load8_upto(xr + (c < cols ? c : 0), cols - c), k);
 }
 
 // Columns, or rows and columns, of up to two matrices (blockIdx.z) in two passes.
@@ -168,7 +158,7 @@ __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
     V8 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      v[u] = c < j.cols && r + 8 * u < r1 ? i8_load8(j.x + (int64_t)(r + 8 * u) * j.cols + c, j.cols - c)
+      v[u] = c < j.cols && r + 8 * u < r1 ? load8_upto(j.x + (int64_t)(r + 8 * u) * j.cols + c, j.cols - c)
                                           : zero8();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -224,7 +214,7 @@ __global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = r0 + rg * R + i;
-    v[i] = r < j.rows && c < j.cols ? i8_load8(j.x + (int64_t)r * j.cols + c, j.cols - c) : zero8();
+    v[i] = r < j.rows && c < j.cols ? load8_upto(j.x + (int64_t)r * j.cols + c, j.cols - c) : zero8();
   }
   if (tid < T) {
     const int k = c0 + tid;
@@ -344,14 +334,7 @@ struct I8Epi {
   }
   __device__ __forceinline__ void store(int p, int q, const V8 (&out)[1]) const {
     if (p >= g.n || q >= g.m) return;
-    h16* yp = g.y + (int64_t)q * g.n + p;
-    if (p + 8 <= g.n) {
-      store16u(yp, out[0]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (p + k < g.n) yp[k] = out[0].h[k];
-    }
+    store8_upto(g.y + (int64_t)q * g.n + p, out[0], g.n - p);
   }
 };
 
@@ -420,7 +403,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, cons
       const h16* xr = x + (int64_t)r * g.k;
       uint32_t mag = 0;
       for (int c = (w * 64 + lane) * 8; c < g.k; c += 512 * wpr)
-        mag = i8_mag8(i8_load8(xr + c, g.k - c), mag);
+        mag = i8_mag8(load8_upto(xr + c, g.k - c), mag);
       mag = i8_wave_max(mag);
       if (lane == 0) top[r][w] = mag;
     }
@@ -435,7 +418,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, cons
       const I8Quant k = i8_quant(mag);
       for (int c = (w * 64 + lane) * 8; c < ld; c += 512 * wpr)
         *reinterpret_cast<uint2*>(dyn + r * lq + c) =
-            i8_pack(i8_load8(xr + (c < g.k ? c : 0), g.k - c), k);
+            i8_pack(load8_upto(xr + (c < g.k ? c : 0), g.k - c), k);
     }
     __syncthreads();
   }

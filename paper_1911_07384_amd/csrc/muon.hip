@@ -107,6 +107,14 @@ __device__ __forceinline__ double ns_block_sum(double v, double* red) {
   return ((red[0] + red[1]) + red[2]) + red[3];
 }
 
+// The factor of X from the sum of squares: 0 for a zero matrix (no epsilon, since
+// gradients trained without loss scaling are small), not a number where an element
+// is not finite.
+__device__ __forceinline__ float ns_rsqrt(double s) {
+  if (s > 0.0 && s < __builtin_inf()) return (float)((double)kSx / sqrt(s));
+  return s == 0.0 ? 0.0f : __builtin_nanf("");
+}
+
 // the float32 update direction before normalisation
 __device__ __forceinline__ float ns_dir(h16 g, h16 m, float mu, bool has_m, bool nesterov) {
   if (!has_m) return to_f32(g);
@@ -194,10 +202,7 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
   double s = 0.0;
   for (int i = tid; i < j.nparts; i += 256) s += at<double>(dv.ws, j.part)[i];
   s = ns_block_sum(s, red);
-  // 0 for a zero matrix; no epsilon, since gradients trained without loss scaling
-  // are small.  Not a number where an element is not finite.
-  const float rs = s > 0.0 && s < __builtin_inf() ? (float)((double)kSx / sqrt(s))
-                                                  : (s == 0.0 ? 0.0f : __builtin_nanf(""));
+  const float rs = ns_rsqrt(s);
   const int local = blockIdx.x - j.t_pre, tc = j.cp / 64;
   const int r0 = (local / tc) * 64, c0 = (local % tc) * 64;
   const bool has_m = j.m != nullptr;
@@ -211,17 +216,8 @@ __global__ __launch_bounds__(256) void ns_split(const NsDev dv, float mu, int ne
     V8 g = zero8(), m = zero8(), hi, lo;
     const int64_t o = (int64_t)row * j.cols + col;
     if (row < j.rows && col < j.cols) {
-      if (col + 8 <= j.cols) {
-        g = load16u(j.g + o);
-        if (has_m) m = load16u(j.m + o);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (col + e < j.cols) {
-            g.h[e] = j.g[o + e];
-            if (has_m) m.h[e] = j.m[o + e];
-          }
-      }
+      g = load8_upto(j.g + o, j.cols - col);
+      if (has_m) m = load8_upto(j.m + o, j.cols - col);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -471,14 +467,7 @@ struct NsXEpi {
       return;
     }
     if (p >= cols || q >= rows) return;
-    h16* const wp = w + (int64_t)q * cols + p;
-    if (p + 8 <= cols) {
-      store16u(wp, out[0]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (p + k < cols) wp[k] = out[0].h[k];
-    }
+    store8_upto(w + (int64_t)q * cols + p, out[0], cols - p);
   }
 };
 
@@ -603,6 +592,372 @@ __global__ __launch_bounds__(256) void ns_sum(const NsDev dv, int parts) {
   ns_sym_out<O, 0, PROD>(dv, j, 0.0f, 0.0f, acc, lds,
                          ti * C::BP + (w / C::WQ) * 64 + (wave / 2) * 32,
                          tj * C::BQ + (w % C::WQ) * 64 + (wave % 2) * 32, ti != tj);
+}
+
+// ---- few small matrices: one workgroup each, one launch --------------------------
+//
+// With a short side of at most 64 and a long one of at most 1024, X stays in registers,
+// high and low part of an element in one, from the first read to the last store: a wave holds tiles of 32 n x 64 m
+// (n along the longer side), lane l column m = l % 32 of each half and 16 values of n.
+// For A, which reduces over n, that is an operand's layout already (any order of n
+// serves if both operands share it); for B'X each wave turns its own tiles around
+// through LDS.  Only the waves' shares of A are exchanged.  Bound by latency, the
+// barriers and the one CU's products and LDS.  Against the same as launches over all
+// CUs, five steps, in us (1 to 24 matrices take the same time here):
+//                       products 1     products 3
+//     64 x 64             20 / 57        26 / 63
+//     64 x 576            37 / 69        52 / 81
+//     64 x 1024           53 / 77        78 / 91
+//     24 of 64 x 1024     54 / 94        79 / 111
+constexpr int kSmallWaves = 8, kSmallTiles = 4;           // tiles of a wave at most
+constexpr int kSmallShort = 64, kSmallLong = 32 * kSmallWaves * kSmallTiles;
+
+struct NsSmall {
+  float coef[3 * kNsMaxSteps];
+  int steps, nesterov;
+  float mu, keep;
+};
+static_assert(sizeof(NsChunk) + sizeof(NsSmall) <= 4096, "kernel arguments");
+
+// half of (row, k) of an operand of rows of 64 halves, in the order of nt_product
+__device__ __forceinline__ int ns_at(int row, int k) {
+  return row * 64 + (((k >> 3) ^ ((row >> 1) & 7)) * 8) + (k & 7);
+}
+
+template <int PROD>
+__global__ __launch_bounds__(64 * kSmallWaves) void ns_small(const NsChunk c, const NsSmall a) {
+  constexpr int H = PROD == 3 ? 2 : 1, W = kSmallWaves, T = kSmallTiles;
+  constexpr int WAVE = 12288;                 // bytes of a wave's own region
+  constexpr int GLD = 36, TLD = 72, FLD = 36, ULD = 68;  // strides: 64 m x 32 n, 32 n x 64 m
+  static_assert(2 * 64 * GLD * 2 <= WAVE && 2 * 32 * TLD * 2 <= WAVE, "inputs");
+  static_assert(64 * FLD * 4 <= WAVE && 32 * ULD * 4 <= WAVE, "outputs");
+  static_assert(H * 32 * 64 * 2 <= WAVE && 3 * 4096 <= WAVE, "operands, sums");
+  __shared__ __attribute__((aligned(1024))) char region[W][WAVE];
+  __shared__ __attribute__((aligned(1024))) h16 la[H][64 * 64], lb[H][64 * 64];
+  __shared__ __attribute__((aligned(16))) float ld[64], le[64];
+  __shared__ double red[W];
+  const NsJob& j = c.job[blockIdx.x];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lrow = lane & 31, lhi = lane >> 5;
+  const bool tall = j.tall, has_m = j.m != nullptr;
+  const int nlen = tall ? j.rows : j.cols;
+  char* const own = region[wave];
+  h16* const oh = reinterpret_cast<h16*>(own);
+  float* const of = reinterpret_cast<float*>(own);
+
+  // an element of X, v * f: its high and low part
+  auto pack = [](float v, float f) {
+    const h16 h = (h16)(v * f);
+    return half2{h, (h16)__builtin_fmaf(v, f, -to_f32(h))};
+  };
+  // chunk i of this lane of a tile from n0: its offset in the matrix, the elements of
+  // it that are there, and its place in a tile laid out by rows of ld elements
+  auto chunk = [&](int n0, int i, int ld, int64_t* off, int* left, int* at) {
+    const int r = tall ? 8 * i + (lane >> 3) : 16 * i + (lane >> 2);
+    const int k = tall ? 8 * (lane & 7) : 8 * (lane & 3);
+    const int row = tall ? n0 + r : r, col = tall ? k : n0 + k;
+    *off = (int64_t)row * j.cols + col;
+    *left = row < j.rows ? j.cols - col : 0;
+    *at = r * ld + k;
+  };
+
+  // momentum, and X in registers.  u = cm m' + cg g is any of ns_dir's, exactly.
+  const float cm = !has_m ? 0.0f : a.nesterov ? a.mu : 1.0f;
+  const float cg = has_m && !a.nesterov ? 0.0f : 1.0f;
+  half2 x[T][2][16];
+  double s = 0.0;
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][b][e] = half2{0, 0};
+  constexpr int IN = 64 * GLD;  // halves of one staged input
+  static_assert(32 * TLD <= IN, "staging");
+  V8 g[4], m[4];
+  // (one copy of the code for all tiles: fetching it is what a launch waits for)
+#pragma unroll 1
+  for (int t = -1; t < T; ++t) {
+    const int n0 = 32 * (wave + W * t);
+    if (n0 >= nlen) break;
+    if (t >= 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int64_t off;
+        int left, at;
+        chunk(n0, i, tall ? TLD : GLD, &off, &left, &at);
+        if (has_m) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            m[i].h[e] = to_h16(__builtin_fmaf(a.mu, to_f32(m[i].h[e]), to_f32(g[i].h[e])));
+          if (left > 0) store8_upto(j.m + off, m[i], left);
+        }
+        uint2* pg = reinterpret_cast<uint2*>(oh + at);
+        uint2* pm = reinterpret_cast<uint2*>(oh + IN + at);
+        pg[0] = make_uint2(g[i].u[0], g[i].u[1]);
+        pg[1] = make_uint2(g[i].u[2], g[i].u[3]);
+        pm[0] = make_uint2(m[i].u[0], m[i].u[1]);
+        pm[1] = make_uint2(m[i].u[2], m[i].u[3]);
+      }
+      nt_wave_sync();
+    }
+    // the next tile's loads
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int64_t off;
+      int left, at;
+      chunk(n0 + 32 * W, i, 0, &off, &left, &at);
+      g[i] = m[i] = zero8();
+      if (t + 1 < T && left > 0) {
+        g[i] = load8_upto(j.g + off, left);
+        if (has_m) m[i] = load8_upto(j.m + off, left);
+      }
+    }
+    if (t >= 0) {
+      const h16* const from = oh + (tall ? 4 * lhi * TLD + lrow : lrow * GLD + 4 * lhi);
+      float u[2][16], sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (eight squares each in float32)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int n = 8 * (e / 4) + e % 4, at = tall ? n * TLD + 32 * b : 32 * b * GLD + n;
+          // (elements past the matrix were read as zeros)
+          u[b][e] = __builtin_fmaf(cm, to_f32(from[IN + at]), cg * to_f32(from[at]));
+          sq[e / 4] = __builtin_fmaf(u[b][e], u[b][e], sq[e / 4]);
+        }
+      s += ((double)sq[0] + (double)sq[1]) + ((double)sq[2] + (double)sq[3]);
+#pragma unroll
+      for (int k = 0; k < T; ++k) {
+        if (k != t) continue;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[k][b][e] = __builtin_bit_cast(half2, u[b][e]);
+      }
+      nt_wave_sync();
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+  if (lane == 0) red[wave] = s;
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) s += red[i];
+  const float rs = ns_rsqrt(s);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    if (32 * (wave + W * t) >= nlen) continue;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][b][e] = pack(__builtin_bit_cast(float, x[t][b][e]), rs);
+  }
+
+  auto frag = [&](const h16* rows, int row, int ks) {
+    return *reinterpret_cast<const half8*>(rows + ns_at(row, ks * 16 + lhi * 8));
+  };
+  // four elements k .. k + 3 of a row of A or B, and their mirror images
+  auto put = [&](h16* hi, h16* lo, int q, int p, const float (&v)[4], bool mirror) {
+    h16 th[4], tl[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      th[r] = to_h16(v[r]);
+      tl[r] = to_h16(v[r] - to_f32(th[r]));
+    }
+    __builtin_memcpy(__builtin_assume_aligned(hi + ns_at(q, p), 8), th, 8);
+    if (H == 2) __builtin_memcpy(__builtin_assume_aligned(lo + ns_at(q, p), 8), tl, 8);
+    if (mirror) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        hi[ns_at(p + r, q)] = th[r];
+        if (H == 2) lo[ns_at(p + r, q)] = tl[r];
+      }
+    }
+  };
+
+  for (int step = 0; step < a.steps; ++step) {
+    const float ca = a.coef[3 * step], cb = a.coef[3 * step + 1], cc = a.coef[3 * step + 2];
+    // A = X X^T of the wave's tiles: its 32 x 32 tiles (0, 0), (1, 0) and (1, 1)
+    floatx16 acc[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (32 * (wave + W * t) >= nlen) continue;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        half8 f[H][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            f[0][b][e] = x[t][b][8 * k + e][0];
+            if (H == 2) f[H - 1][b][e] = x[t][b][8 * k + e][1];
+          }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const int p = i > 0, q = i > 1;
+          if (H == 2) {
+            acc[i] = NtHalf::mma(f[H - 1][p], f[0][q], acc[i]);
+            acc[i] = NtHalf::mma(f[0][p], f[H - 1][q], acc[i]);
+          }
+          acc[i] = NtHalf::mma(f[0][p], f[0][q], acc[i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const floatx4 v = {acc[i][4 * e], acc[i][4 * e + 1], acc[i][4 * e + 2], acc[i][4 * e + 3]};
+        reinterpret_cast<floatx4*>(own)[(i * 4 + e) * 64 + lane] = v;
+      }
+    __syncthreads();
+    for (int o = tid; o < 768; o += 64 * W) {
+      floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < W; ++w) v += reinterpret_cast<const floatx4*>(region[w])[o];
+      const int i = o / 256, e = o / 64 % 4, l = o % 64;
+      const int p = 32 * (i > 0) + 8 * e + 4 * (l / 32), q = 32 * (i > 1) + l % 32;
+      float r[4], dq = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        dq = p + k == q ? v[k] * (1.0f / (kSx * kSx)) : dq;
+        r[k] = p + k == q ? 0.0f : v[k] * (kSa / (kSx * kSx));
+      }
+      if ((unsigned)(q - p) < 4u) ld[q] = dq;
+      put(la[0], la[H - 1], q, p, r, i == 1);
+    }
+    __syncthreads();
+    // B = bA + cA^2, a tile each of the first four waves
+    if (wave < 4) {
+      const int p0 = 32 * (wave / 2), q0 = 32 * (wave % 2);
+      floatx16 b;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) b[e] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const half8 ph = frag(la[0], p0 + lrow, ks), qh = frag(la[0], q0 + lrow, ks);
+        if (H == 2) {
+          b = NtHalf::mma(frag(la[H - 1], p0 + lrow, ks), qh, b);
+          b = NtHalf::mma(ph, frag(la[H - 1], q0 + lrow, ks), b);
+        }
+        b = NtHalf::mma(ph, qh, b);
+      }
+      const int q = q0 + lrow;
+      const float dq = ld[q];
+      float b2 = 0.0f;  // of the diagonal
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int p = p0 + 8 * e + 4 * lhi;
+        h16 ah[4], al[4] = {0, 0, 0, 0};
+        __builtin_memcpy(ah, __builtin_assume_aligned(la[0] + ns_at(q, p), 8), 8);
+        if (H == 2) __builtin_memcpy(al, __builtin_assume_aligned(la[H - 1] + ns_at(q, p), 8), 8);
+        const floatx4 dp = *reinterpret_cast<const floatx4*>(ld + p);
+        float r[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float av = (to_f32(ah[k]) + to_f32(al[k])) * (1.0f / kSa);
+          const float a2 = b[4 * e + k] * (1.0f / (kSa * kSa));
+          b2 = p + k == q ? a2 : b2;
+          r[k] = kSb * __builtin_fmaf(cc, __builtin_fmaf(dq + dp[k], av, a2), cb * av);
+          r[k] = p + k == q ? 0.0f : r[k];
+        }
+        put(lb[0], lb[H - 1], q, p, r, false);
+      }
+      if (p0 == q0 && lhi == (lrow >> 2 & 1))
+        le[q] = __builtin_fmaf(cc, __builtin_fmaf(dq, dq, b2), cb * dq);
+    }
+    __syncthreads();
+    // X = (a + E) X + B'X, tile by tile
+    const float kE[2] = {kSb * (ca + le[lrow]), kSb * (ca + le[32 + lrow])};
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (32 * (wave + W * t) >= nlen) continue;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          // ns_at(8 (e / 4) + 4 lhi + e % 4, 32 b + lrow), lanes and constants apart
+          const int lanes = lhi * 256 + (((lrow >> 3) ^ (2 * lhi) ^ (e % 4 / 2)) * 8) + (lrow & 7);
+          h16* const to = oh + lanes + (8 * (e / 4) + e % 4) * 64 + 32 * (b ^ (e / 4 & 1));
+          to[0] = x[t][b][e][0];
+          if (H == 2) to[2048] = x[t][b][e][1];
+        }
+      nt_wave_sync();
+      floatx16 y[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[b][e] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const half8 ph = frag(oh, lrow, ks);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const half8 qh = frag(lb[0], 32 * b + lrow, ks);
+          if (H == 2) {
+            y[b] = NtHalf::mma(frag(oh + 2048, lrow, ks), qh, y[b]);
+            y[b] = NtHalf::mma(ph, frag(lb[H - 1], 32 * b + lrow, ks), y[b]);
+          }
+          y[b] = NtHalf::mma(ph, qh, y[b]);
+        }
+      }
+      nt_wave_sync();
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          // (see NsXEpi)
+          const float h = to_f32(x[t][b][e][0]), l = to_f32(x[t][b][e][1]);
+          const float f = __builtin_fmaf(H == 2 ? kE[b] : kSb * ca, l, y[b][e]);
+          x[t][b][e] = pack(__builtin_fmaf(kE[b], h, f), 1.0f / kSb);
+        }
+    }
+  }
+
+  // the weights' update or the result, rows whole
+#pragma unroll 1
+  for (int t = 0; t < T; ++t) {
+    const int n0 = 32 * (wave + W * t);
+    if (n0 >= nlen) break;
+    float* const to = of + (tall ? 4 * lhi * ULD + lrow : lrow * FLD + 4 * lhi);
+#pragma unroll
+    for (int k = 0; k < T; ++k) {
+      if (k != t) continue;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int n = 8 * (e / 4) + e % 4;
+          to[tall ? n * ULD + 32 * b : 32 * b * FLD + n] =
+              (to_f32(x[k][b][e][0]) + to_f32(x[k][b][e][1])) * (1.0f / kSx);
+        }
+    }
+    nt_wave_sync();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int64_t off;
+      int left, at;
+      chunk(n0, i, tall ? ULD : FLD, &off, &left, &at);
+      if (left <= 0) continue;
+      const floatx4 lo = *reinterpret_cast<const floatx4*>(of + at);
+      const floatx4 hi = *reinterpret_cast<const floatx4*>(of + at + 4);
+      const V8 w = has_m ? load8_upto(j.w + off, left) : zero8();
+      V8 out;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float o = e < 4 ? lo[e & 3] : hi[e & 3];
+        out.h[e] = to_h16(has_m ? __builtin_fmaf(-j.alpha, o, a.keep * to_f32(w.h[e])) : j.alpha * o);
+      }
+      store8_upto(j.w + off, out, left);
+    }
+    nt_wave_sync();
+  }
 }
 
 // ---- the plan ------------------------------------------------------------------
@@ -735,6 +1090,10 @@ hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
 void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, NsPlan* plan) {
   NsPlan& P = *plan;
   P.count = count;
+  P.small = count <= kJobsPerLaunch;
+  for (int i = 0; i < count; ++i)
+    P.small = P.small && std::min(rows[i], cols[i]) <= kSmallShort &&
+              std::max(rows[i], cols[i]) <= kSmallLong;
   for (int stage = 0; stage < 3; ++stage)
     P.variant[stage] = ns_choose(stage, count, rows, cols, products, &P.kind[stage]);
   // the longest products first
@@ -790,11 +1149,27 @@ void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, 
   for (int stage = 0; stage < 3; ++stage) P.map[stage] = take((uint64_t)P.tiles[stage] * 2);
   P.map_pre = take((uint64_t)P.n_pre * 2);
   P.sums = take(P.kind[0].parts > 1 ? (uint64_t)P.tiles[0] * P.kind[0].parts * 65536 : 0);
-  P.bytes = (size_t)off * 256;
+  P.bytes = P.small ? 256 : (size_t)off * 256;  // (not used; 0 would mean a bad list)
 }
 
 hipError_t launch_ns(const NsPlan& p, const NsArgs& a, void* ws, hipStream_t st) {
   char* w = static_cast<char*>(ws);
+  if (p.small) {
+    NsChunk c{};
+    std::copy(p.jobs, p.jobs + p.count, c.job);
+    NsSmall s{};
+    std::copy(a.coef, a.coef + 3 * a.steps, s.coef);
+    s.steps = a.steps;
+    s.nesterov = a.nesterov;
+    s.mu = a.momentum;
+    s.keep = a.keep;
+    const dim3 grid((unsigned)p.count), block(64 * kSmallWaves);
+    if (a.products == 3)
+      hipLaunchKernelGGL(ns_small<3>, grid, block, 0, st, c, s);
+    else
+      hipLaunchKernelGGL(ns_small<1>, grid, block, 0, st, c, s);
+    return hipGetLastError();
+  }
   const NsPlaces pl{p.table, {p.map[0], p.map[1], p.map[2]}, p.map_pre,
                     {p.kind[0].side, p.kind[1].side, p.kind[2].side}};
   for (int first = 0; first < p.count; first += kJobsPerLaunch) {

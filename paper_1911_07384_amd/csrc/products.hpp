@@ -45,6 +45,7 @@ struct NsPlan {
   NsTile kind[3];              // of A, B and X'
   int variant[3];              // their places in the list of tiles
   int count;
+  bool small;                  // one workgroup a matrix, none of the rest
   int tiles[3], n_pre;         // in all
   uint32_t table, map[3], map_pre, sums;  // in the workspace
   size_t bytes;

@@ -75,7 +75,10 @@ def orth(xs, products, steps=5, coef=None, scales=None, ws=None, out=None):
 
 SHAPES = [(1, 1), (1, 7), (5, 1), (2, 2), (3, 3), (8, 8), (16, 200), (200, 16), (63, 65), (64, 64),
           (65, 63), (64, 147), (147, 64), (64, 576), (129, 300), (256, 256), (300, 520), (1000, 257),
-          (257, 1000), (512, 512)]
+          (257, 1000), (512, 512),
+          # one workgroup each: up to 64 by 1024, tiles of 32 by the longer side
+          (64, 31), (33, 32), (32, 33), (64, 65), (1, 1024), (1023, 1), (64, 1024), (1024, 64),
+          (576, 64), (40, 999), (999, 40), (64, 1025)]
 
 
 @pytest.mark.parametrize("products", [1, 3])
@@ -276,6 +279,41 @@ def test_update(products, nesterov):
             err = (W[i].double() - ref).norm().item()
             bar = BAR[products] * upd.norm().item() + (2.0 ** -11 + 2.0 ** -20) * ref.norm().item()
             assert err <= bar + 2.0 ** -25 * math.sqrt(ref.numel())
+
+
+@pytest.mark.parametrize("products", [1, 3])
+def test_update_of_small_matrices(products):
+    """The same on one workgroup each, views of odd alignment with borders, and the
+    momentum and weights beside them left alone."""
+    shapes = [(64, 147), (147, 64), (5, 3), (64, 1024), (1024, 64), (33, 1000), (1000, 33), (1, 9)]
+    assert F.fp16_muon_kernels(F.muon_descs(shapes), products) == "one workgroup each"
+    lr, mu, wd = 0.02, 0.95, 0.1
+
+    def place(l):
+        out = []
+        for i, t in enumerate(l):
+            flat = torch.full((t.numel() + 40,), 7.0, dtype=torch.float16, device="cuda")
+            v = flat[1 + i:1 + i + t.numel()].view(t.shape)
+            v.copy_(t)
+            out.append((flat, v))
+        return [f for f, _ in out], [v for _, v in out]
+
+    g = [matrix(*s, seed=10 + i) for i, s in enumerate(shapes)]
+    m = [matrix(*s, seed=20 + i) for i, s in enumerate(shapes)]
+    w = [matrix(*s, seed=30 + i, kind="normal", scale=0.1) for i, s in enumerate(shapes)]
+    (GF, G), (MF, M), (WF, W) = place(g), place(m), place(w)
+    step(W, G, M, [1.0] * len(shapes), lr, mu, wd, True, products)
+    for i, s in enumerate(shapes):
+        _, mr = oracle.sgd_f32(np.zeros(g[i].numel(), np.float16), g[i].numpy().ravel(),
+                               m[i].numpy().ravel(), 0.1, mu, 0.0)
+        assert np.array_equal(host(M[i]).ravel().view(np.uint16), mr.view(np.uint16))
+        upd = lr * ns64(g[i].double() + float(np.float32(mu)) * torch.from_numpy(mr).view(*s).double())
+        ref = (1 - lr * wd) * w[i].double().cuda() - upd
+        bar = BAR[products] * upd.norm().item() + (2.0 ** -11 + 2.0 ** -20) * ref.norm().item()
+        assert (W[i].double() - ref).norm().item() <= bar + 2.0 ** -25 * math.sqrt(ref.numel()), s
+        assert torch.equal(G[i].cpu(), g[i])
+        for f in (GF[i], MF[i], WF[i]):
+            assert (f[:1 + i] == 7).all() and (f[1 + i + g[i].numel():] == 7).all()
 
 
 def test_update_alone():

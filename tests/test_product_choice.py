@@ -20,6 +20,14 @@ def test_every_tile_of_the_products_is_covered():
         assert seen[2] == plain | ({"64 deep"} if products == 3 else set()), (products, seen[2])
 
 
+def test_small_sets_take_one_workgroup_each():
+    name = lambda *shapes: F.fp16_muon_kernels(F.muon_descs(list(shapes)), 1)
+    small = "one workgroup each"
+    assert name((64, 1024)) == name((1024, 64)) == name(*[(64, 576)] * 24) == small
+    assert small not in (name((65, 65)), name((64, 1025)), name(*[(8, 8)] * 25),
+                         name((64, 64), (128, 128)))
+
+
 def test_every_tile_of_the_8_bit_product_is_covered():
     got = {F.fp16_int8_kernel(*c) for c in int8.PRODUCTS}
     assert got == {"few rows", "tile 64", "tile 128", "tile 128 deep", "tile 256"}
