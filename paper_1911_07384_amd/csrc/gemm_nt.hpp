@@ -6,15 +6,20 @@
 // a slice of the reduction is 128 bytes of every row.
 //
 // A workgroup owns BP x BQ outputs, WP x WQ waves TP x TQ tiles of 32 x 32 each, over
-// the whole reduction or one of several parts of it.  The slices go through S stages of LDS, loaded past the registers
-// (8 rows of one slice, 1 KB, an instruction and wave) S - 1 slices ahead and a
-// few between the products of every sub-step, one barrier a slice.  Rows of LDS
+// the whole reduction or one of several parts of it.  The slices go through S stages
+// of LDS, loaded past the registers (8 rows of one slice, 1 KB, an instruction and
+// wave) S - 1 slices ahead and a few between the products of every sub-step, one
+// barrier a slice.  Rows of LDS
 // are whole 128-byte lines; the 16-byte chunk c of row r lies at c ^ ((r/2) % 8),
 // so that the 16 rows a fragment read touches at a time lie in different banks.
 //
 // What bounds it: each sub-step reads (TP + TQ) KB of LDS a wave for TP * TQ
-// products of 32 cycles.  At TP = TQ = 4 with four waves that is 64 bytes a cycle
-// (and 32 written) of the 128 that the LDS gives, at TP = TQ = 2 all of them.
+// products of 32 cycles, of 128 bytes a cycle that the LDS gives: 96 with eight waves
+// of 2 x 4 tiles (Nt256), 85 with four of 3 x 3 (Nt192), all of them with 2 x 2, and
+// the 64 x 64 tiles' loads take what the L2 gives (17 to 20 TB/s over all CUs).
+// 8-bit, m x n x k = 8192 x 4096 x 4096: 126 us with its epilogue, 2180 TOP/s; 4096
+// each: 65.6 us (a library product of 4096: 67.0).  Binary16: about 1500 TFLOP/s in
+// the loop of the 4096 x 4096 x 4096 product, 900 with a float32 epilogue.
 #pragma once
 
 #include "common.hpp"
@@ -247,7 +252,9 @@ __device__ __forceinline__ void nt_wave_sync() {
 // rows a lane), where p < plim and q < qlim.
 // A workgroup runs this once, at one wave a SIMD for the large tiles: the passes of
 // a group are done side by side without branches, so that they hide each other's
-// latency (one at a time with a test each: 4 us a pass of a 256 x 256 tile).
+// latency (one at a time with a test each: 4 us a pass of a 256 x 256 tile; twice as
+// many side by side no longer fit the registers of two workgroups a CU: the 8-bit
+// product of 4096 each 65 -> 81 us).
 template <class C, int PARTS>
 struct NtEpi {
   static constexpr int TP = C::TP, TQ = C::TQ, U = TP;

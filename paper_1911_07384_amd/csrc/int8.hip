@@ -102,7 +102,7 @@ __device__ __forceinline__ uint2 i8_pack(const V8& v, const I8Quant& k) {
 
 // One workgroup a row; up to 8192 elements stay in registers between the maximum
 // and the quantising, further ones are read again.  Bandwidth-bound: 3 bytes an
-// element.
+// element, 5.7 TB/s at 8192 x 4096 (17.6 us).
 constexpr int kRowKeep = 4;
 __global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __restrict__ x,
                                                int8_t* __restrict__ q, float* __restrict__ scale) {
@@ -140,7 +140,8 @@ __global__ __launch_bounds__(256) void i8_rows(int cols, int ld, const h16* __re
 //
 // First pass: 256 columns of a range of rows a workgroup, a thread 8 columns of
 // every eighth row: the largest magnitude (and the sum) of each column over the
-// range and, for the rows, of each row over the 256 columns.
+// range and, for the rows, of each row over the 256 columns.  Bandwidth-bound: two
+// matrices of 4096 x 4096 at 4.8 TB/s (13.9 us).
 constexpr int kColChunks = 32, kColRows = 32;  // ranges of rows at most, rows of one at least
 __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
   const I8Cols& j = both.job[blockIdx.z];
@@ -195,8 +196,9 @@ __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
 
 // Second pass: T rows x T columns quantised and written transposed, a run of T bytes
 // of each column through LDS, and as laid out, a run of each row.  T = 128 writes
-// whole lines, T = 64 has four times the workgroups for small matrices (128 x 1000
-// and 128 x 2048: 9.0 us on 128).
+// whole lines (two matrices of 4096 x 4096, one by rows too: 117 MB in 25 us, 4.7
+// TB/s); T = 64 has four times the workgroups for small matrices (128 x 1000 and
+// 128 x 2048: 6.3 us, 9.0 on T = 128).
 template <int T>
 __global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
   const I8Cols& j = both.job[blockIdx.z];
@@ -368,19 +370,32 @@ __global__ __launch_bounds__(C::THREADS, C::OCC) void i8_product(const I8Product
 // Few rows (at most 16 tokens): bound by reading b once.  A workgroup takes 16
 // outputs; its eight waves split the reduction, each lane loading 16 bytes of one
 // row of b straight into the operand (the first kFewAhead of them before anything
-// else), and add their 32-bit sums in LDS.  FUSED: the rows of x are quantised by
-// every workgroup for itself into LDS (they are small and come from the L2), which
-// saves a launch; otherwise a is read from memory.
-constexpr int kFewRows = 16, kFewWaves = 8, kFewLds = 48 * 1024, kFewAhead = 8;
+// else), and add their 32-bit sums in LDS.  One token, 4096 x 4096: 5.0 us, 3.4 TB/s.
+// Up to two workgroups a CU: past them every one reads a again, and the 64 x 64 tiles
+// are faster.  Product alone, few rows / tiles of 64, in us, of 1 and of 16 tokens:
+//     n x k       1000 x 2048   4096 x 4096   8192 x 4096   16384 x 1024   16384 x 4096
+//     1             3.3/5.9       5.0/9.0       7.1/9.4        4.7/4.5       14.5/12.2
+//     16            3.8/6.0       5.8/9.0       9.6/9.6        5.7/4.6       18.4/12.4
+//
+// FUSED: the rows of x are quantised by every workgroup for itself into LDS (they are
+// small and come from the L2), which saves a launch; that pays for up to 4 tokens of
+// 16384 elements together.  One launch / two, in us:
+//     n x k         1000 x 2048   2048 x 8192   4096 x 4096   8192 x 4096
+//     1 token         4.2/6.1       8.2/10.8      5.7/7.8       7.7/9.9
+//     2               4.6/6.1       9.5/10.9      6.4/8.1       8.7/10.1
+//     4               4.8/6.1      11.7/11.1      7.5/8.2      10.3/10.4
+//     12              7.8/6.4         -          13.7/8.4         -
+constexpr int kFewRows = 16, kFewOut = 16, kFewWaves = 8, kFewAhead = 8, kFewGroups = 512;
+constexpr int kFusedRows = 4, kFusedElems = 16384;
 template <bool FUSED>
 __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, const h16* __restrict__ x) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];  // FUSED: [m][ld + 16]
   __shared__ int part[kFewWaves][16][17];
-  __shared__ uint32_t top[kFewRows][kFewWaves];
+  __shared__ uint32_t top[kFusedRows][kFewWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ld = (g.k + 15) & ~15, lq = ld + 16;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * kFewOut;
   const int row = lane & 15, kc = (lane >> 4) * 16;
   const bool ain = row < g.m;
   const int8_t* bp = g.b + (int64_t)(n0 + row < g.n ? n0 + row : 0) * ld;
@@ -396,23 +411,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void i8_few(const I8Product g, cons
     }
   };
   load(s0);
-  const int wpr = g.m >= 8 ? 1 : g.m >= 3 ? 2 : g.m == 2 ? 4 : 8;  // waves to a row of x
+  const int wpr = kFewWaves / (g.m >= 3 ? 4 : g.m);  // waves to a row of x
   if (FUSED) {
-    const int w = wave % wpr;
-    for (int r = wave / wpr; r < g.m; r += kFewWaves / wpr) {
-      const h16* xr = x + (int64_t)r * g.k;
+    const int w = wave % wpr, r = wave / wpr;
+    const h16* xr = x + (int64_t)r * g.k;
+    if (r < g.m) {
       uint32_t mag = 0;
       for (int c = (w * 64 + lane) * 8; c < g.k; c += 512 * wpr)
         mag = i8_mag8(load8_upto(xr + c, g.k - c), mag);
       mag = i8_wave_max(mag);
       if (lane == 0) top[r][w] = mag;
     }
-    if (wpr > 1)
-      __syncthreads();
-    else
-      nt_wave_sync();
-    for (int r = wave / wpr; r < g.m; r += kFewWaves / wpr) {
-      const h16* xr = x + (int64_t)r * g.k;
+    __syncthreads();
+    if (r < g.m) {
       uint32_t mag = 0;
       for (int i = 0; i < wpr; ++i) mag = std::max(mag, top[r][i]);
       const I8Quant k = i8_quant(mag);
@@ -538,12 +549,13 @@ hipError_t launch_i8_cols(const I8Cols* jobs, int count, hipStream_t st) {
 }
 
 bool i8_fused_ok(int m, int n, int k) {
-  return m <= kFewRows && (int64_t)m * (i8_row(k) + 16) <= kFewLds;
+  return m <= kFusedRows && (int64_t)m * k <= kFusedElems &&
+         ceil_div(n, kFewOut) <= kFewGroups;
 }
 
 hipError_t launch_i8_fused(const I8Product& a, const h16* x, hipStream_t st) {
   const size_t lds = (size_t)a.m * (i8_row(a.k) + 16);
-  hipLaunchKernelGGL((i8_few<true>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), lds,
+  hipLaunchKernelGGL((i8_few<true>), dim3((unsigned)ceil_div(a.n, kFewOut)), dim3(64 * kFewWaves), lds,
                      st, a, x);
   return hipGetLastError();
 }
@@ -571,9 +583,9 @@ constexpr I8Tile kI8Tiles[kI8Kinds + 1] = {{256, 1, 1.02, 1.72, 1.5, 11.1, "tile
                                            {64, 2, 0.18, 0.20, 2.7, 2.4, "tile 64"},
                                            {0, 0, 0.0, 0.0, 0.0, 0.0, "few rows"}};
 
-// The one that finishes soonest by that estimate.
+// The one that finishes soonest by that estimate, or few rows (see i8_few).
 int i8_tile(int m, int n, int k) {
-  if (m <= kFewRows) return kI8Kinds;
+  if (m <= kFewRows && ceil_div(n, kFewOut) <= kFewGroups) return kI8Kinds;
   int best = 0;
   double bt = 0;
   for (int i = 0; i < kI8Kinds; ++i) {
@@ -600,7 +612,7 @@ hipError_t launch_i8_product(const I8Product& a, hipStream_t st) {
     case 2: return i8_launch<Nt128d>(a, st);
     case 3: return i8_launch<Nt64>(a, st);
   }
-  hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, 16)), dim3(64 * kFewWaves), 0, st,
+  hipLaunchKernelGGL((i8_few<false>), dim3((unsigned)ceil_div(a.n, kFewOut)), dim3(64 * kFewWaves), 0, st,
                      a, (const h16*)nullptr);
   return hipGetLastError();
 }

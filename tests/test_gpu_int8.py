@@ -119,7 +119,7 @@ def test_halfway_and_special_values(by):
 PRODUCTS = [(1, 1, 1), (1, 33, 100), (3, 1000, 2048), (16, 130, 4111), (2, 40, 131071),
             (17, 1, 15), (17, 40, 16), (64, 64, 128), (65, 129, 129), (128, 1000, 2048),
             (200, 77, 1337), (900, 700, 200), (2049, 2047, 300), (2100, 2056, 64),
-            (1111, 2501, 1337), (2900, 3000, 700), (4001, 3601, 257), (3585, 3700, 128)]
+            (1, 8192, 301), (16, 8193, 301), (1111, 2501, 1337), (2900, 3000, 700), (4001, 3601, 257), (3585, 3700, 128)]
 
 
 @pytest.mark.parametrize("case", PRODUCTS, ids=lambda c: "x".join(map(str, c)))
@@ -152,7 +152,10 @@ def test_products(case):
 
 
 DENSE = [(1, 64, 40), (1, 4096, 130), (3, 100, 1000), (13, 2048, 1000), (16, 9000, 33),
-         (17, 72, 50), (100, 333, 77), (128, 2048, 1000), (515, 129, 300), (1111, 130, 257)]
+         # rows quantised by the product's workgroups up to 4 tokens, 16384 elements and
+         # 8192 outputs, and just past that
+         (4, 4096, 100), (4, 4097, 20), (2, 8192, 33), (3, 1000, 77), (5, 300, 20), (1, 65, 8192),
+         (1, 65, 8193), (17, 72, 50), (100, 333, 77), (128, 2048, 1000), (515, 129, 300), (1111, 130, 257)]
 
 
 def layer(t, i, o, seed=0):

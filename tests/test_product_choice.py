@@ -30,4 +30,5 @@ def test_small_sets_take_one_workgroup_each():
 
 def test_every_tile_of_the_8_bit_product_is_covered():
     got = {F.fp16_int8_kernel(*c) for c in int8.PRODUCTS}
+    assert F.fp16_int8_kernel(16, 8192, 300) == "few rows" != F.fp16_int8_kernel(16, 8193, 300)
     assert got == {"few rows", "tile 64", "tile 128", "tile 128 deep", "tile 256"}
