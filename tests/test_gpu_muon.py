@@ -148,8 +148,9 @@ def test_many_matrices_at_once_as_one_by_one(products):
         assert torch.isfinite(y).all(), shapes[i]
 
 
-def test_steps_and_coefficients():
-    x = matrix(100, 160, 3)
+@pytest.mark.parametrize("shape", [(100, 160), (50, 90)], ids=["tiles", "workgroup"])
+def test_steps_and_coefficients(shape):
+    x = matrix(*shape, 3)
     cubic = [(1.5, -0.5, 0.0)] * 8
     mixed = [(3.0, -3.2, 1.2), (2.5, -2.0, 0.5), (1.875, -1.25, 0.375)]
     for steps, coef in [(1, None), (2, QUINTIC), (8, cubic), (3, mixed)]:
@@ -157,45 +158,48 @@ def test_steps_and_coefficients():
         assert off(y, ns64(x, steps, coef)) <= BAR[3], (steps, coef)
 
 
-def test_scale_and_size_of_the_input():
+@pytest.mark.parametrize("shape", [(70, 80), (48, 80)], ids=["tiles", "workgroup"])
+def test_scale_and_size_of_the_input(shape):
     """The result does not depend on the input's size, down to subnormal entries."""
     for scale in (3e4, 1.0, 2.0 ** -20):
-        x = matrix(48, 80, 5, "normal", scale)
+        x = matrix(*shape, 5, "normal", scale)
         x = x.clamp(-65504, 65504)
         y, = orth([x], 3, scales=[0.25])
         assert off(y, ns64(x, scale=0.25)) <= BAR[3], scale
-    one = torch.zeros((3, 5), dtype=torch.float16)
+    one = torch.zeros((shape[0] - 45, 5), dtype=torch.float16)
     one[1, 2] = 2.0 ** -24
     y, = orth([one], 3)
     assert off(y, ns64(one)) <= BAR[3]
 
 
-def test_zero_and_not_finite():
-    z = torch.zeros((70, 90), dtype=torch.float16)
-    rows = matrix(70, 90, 1)
-    rows[10:60] = 0
-    cols = matrix(70, 90, 2)
+@pytest.mark.parametrize("shape", [(70, 90), (60, 91)], ids=["tiles", "workgroup"])
+def test_zero_and_not_finite(shape):
+    z = torch.zeros(shape, dtype=torch.float16)
+    rows = matrix(*shape, 1)
+    rows[10:50] = 0
+    cols = matrix(*shape, 2)
     cols[:, 3:] = 0
-    nan, inf = matrix(70, 90, 3), matrix(70, 90, 4)
+    nan, inf = matrix(*shape, 3), matrix(*shape, 4)
     nan[4, 5] = float("nan")
-    inf[69, 89] = float("-inf")
+    inf[-1, -1] = float("-inf")
     for products in (1, 3):
         y = orth([z, rows, nan, cols, inf, rows], products)
         assert (y[0] == 0).all()
-        assert (y[1][10:60] == 0).all() and off(y[1], ns64(rows)) <= BAR[products]
+        assert (y[1][10:50] == 0).all() and off(y[1], ns64(rows)) <= BAR[products]
         assert (y[3][:, 3:] == 0).all() and off(y[3], ns64(cols)) <= BAR[products]
         assert torch.isnan(y[2]).all() and torch.isnan(y[4]).all()
         assert torch.equal(y[5], y[1])
 
 
-def test_in_place_and_nothing_else_written():
-    x = matrix(37, 41, 7)
+@pytest.mark.parametrize("shape", [(137, 141), (37, 41)], ids=["tiles", "workgroup"])
+def test_in_place_and_nothing_else_written(shape):
+    x = matrix(*shape, 7)
     ref = ns64(x)
     n = x.numel()
     buf = torch.full((n + 64,), 3.0, dtype=torch.float16, device="cuda")
-    v = buf[8:8 + n].view(37, 41)
+    v = buf[8:8 + n].view(shape)
     v.copy_(x)
-    d = F.muon_descs([(37, 41)])
+    d = F.muon_descs([shape])
     need = F.fp16_muon_workspace_bytes(d, 3)
     ws = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device="cuda")
     F.fp16_orthogonalize(d, [v], [v], products=3, ws=ws, ws_bytes=need)
@@ -204,8 +208,9 @@ def test_in_place_and_nothing_else_written():
     assert (buf[:8] == 3).all() and (buf[8 + n:] == 3).all() and (ws[need:] == 0xA5).all()
 
 
-def test_same_bits_again_and_on_another_stream():
-    xs = [matrix(300, 200, 1), matrix(64, 576, 2)]
+@pytest.mark.parametrize("rows", [300, 30], ids=["tiles", "workgroup"])
+def test_same_bits_again_and_on_another_stream(rows):
+    xs = [matrix(rows, 200, 1), matrix(64, 576, 2)]
     a, b = orth(xs, 1), orth(xs, 1)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
@@ -326,11 +331,12 @@ def test_update_alone():
         assert off(W, -ns64(g)) <= BAR[1]
 
 
-def test_update_in_a_graph():
+@pytest.mark.parametrize("wide", [128, 60], ids=["tiles", "workgroup"])
+def test_update_in_a_graph(wide):
     """Captured once, replayed with eager work between the replays: each replay as
     the eager update from the same state."""
     require_gpu()
-    shapes = [(64, 147), (256, 128), (40, 700)]
+    shapes = [(64, 147), (256, wide), (40, 700)]
     d = F.muon_descs([(*s, 1.0) for s in shapes])
     mk = lambda o, sc: [matrix(*s, seed=o + i, scale=sc).cuda() for i, s in enumerate(shapes)]
     W, G, M = mk(1, 0.1), mk(2, 1e-3), mk(3, 1e-3)
