@@ -17,6 +17,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fp16k {
 namespace {
@@ -155,26 +156,38 @@ __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
   uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   constexpr int U = 4;
-  for (int r = r0 + rg; r < r1; r += 8 * U) {
-    V8 v[U];
+  // (whole: rows of whole vectors; one loop for both took 1 us more at 4096 x 4096)
+  auto rows = [&](auto whole) {
+    for (int r = r0 + rg; r < r1; r += 8 * U) {
+      V8 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      v[u] = c < j.cols && r + 8 * u < r1 ? load8_upto(j.x + (int64_t)(r + 8 * u) * j.cols + c, j.cols - c)
-                                          : zero8();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t b = i8_mag(v[u].s[e]);
-        m[e] = b > m[e] ? b : m[e];
-        if (want_sum) s[e] += to_f32(v[u].h[e]);
+      for (int u = 0; u < U; ++u) {
+        const int ru = r + 8 * u;
+        const h16* const row = j.x + (int64_t)(ru < r1 ? ru : r) * j.cols;
+        if constexpr (decltype(whole)::value)
+          v[u] = c < j.cols && ru < r1 ? load16u(row + c) : zero8();
+        else
+          v[u] = load8_row(row, c, j.cols, ru < r1);
       }
-      if (want_rows) {
-        const uint32_t top = i8_half_max(i8_mag8(v[u], 0));
-        if (cg == 0 && r + 8 * u < r1) j.rmag[(int64_t)blockIdx.x * j.rows + r + 8 * u] = top;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t b = i8_mag(v[u].s[e]);
+          m[e] = b > m[e] ? b : m[e];
+          if (want_sum) s[e] += to_f32(v[u].h[e]);
+        }
+        if (want_rows) {
+          const uint32_t top = i8_half_max(i8_mag8(v[u], 0));
+          if (cg == 0 && r + 8 * u < r1) j.rmag[(int64_t)blockIdx.x * j.rows + r + 8 * u] = top;
+        }
       }
     }
-  }
+  };
+  if (j.cols & 7)
+    rows(std::false_type{});
+  else
+    rows(std::true_type{});
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     rm[rg][cg * 8 + e] = m[e];
@@ -196,7 +209,7 @@ __global__ __launch_bounds__(256) void i8_cols_max(const I8Both both) {
 
 // Second pass: T rows x T columns quantised and written transposed, a run of T bytes
 // of each column through LDS, and as laid out, a run of each row.  T = 128 writes
-// whole lines (two matrices of 4096 x 4096, one by rows too: 117 MB in 25 us, 4.7
+// whole lines (two matrices of 4096 x 4096, one by rows too: 117 MB in 22 us, 5.3
 // TB/s); T = 64 has four times the workgroups for small matrices (128 x 1000 and
 // 128 x 2048: 6.3 us, 9.0 on T = 128).
 template <int T>
@@ -216,7 +229,7 @@ __global__ __launch_bounds__(256) void i8_cols_write(const I8Both both) {
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = r0 + rg * R + i;
-    v[i] = r < j.rows && c < j.cols ? load8_upto(j.x + (int64_t)r * j.cols + c, j.cols - c) : zero8();
+    v[i] = load8_row(j.x + (int64_t)(r < j.rows ? r : 0) * j.cols, c, j.cols, r < j.rows);
   }
   if (tid < T) {
     const int k = c0 + tid;
