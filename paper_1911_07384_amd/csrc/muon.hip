@@ -537,15 +537,28 @@ __device__ __forceinline__ void ns_x_out(const NsDev& dv, const NsJob& j, int cu
   nt_store<C, PARTS>(acc, lds, p0, q0, j.cp, j.rp, !LAST, mir, j.rp, epi);
 }
 
+// The XCDs take the tiles of X' of a set of matrices in groups of 32 in turn: with an
+// eighth of the list each, which is sorted, the first has the longest reductions
+// (ResNet-50's 54 matrices 95 us, 81 so; groups of 8 81, of 16 82).
+constexpr int kNsGroup = 32;
+__host__ __device__ inline int ns_group(int n, bool single) {
+  const int e = (n + 7) >> 3;
+  return single || e < kNsGroup ? e : kNsGroup;
+}
+__device__ __forceinline__ int ns_xcd(const NsDev& dv) {
+  const int g = ns_group(dv.tiles, dv.single), i = blockIdx.x >> 3;
+  return (i / g * 8 + (blockIdx.x & 7)) * g + i % g;
+}
+
 // X' = (a + E) X + B'X.  Bound by the products where m is long (4096 x 4096: 152 us,
 // 137 GFLOP; about 90 us of them the products) and by the epilogue's 10 bytes an element
-// where it is short (ResNet-50's 54 matrices, 25.5 million elements: 90 to 94 us,
-// 345 MB moved).  A low part in 8 bits, 8 bytes an element, measured the same (93 us).
+// where it is short (ResNet-50's 54 matrices, 25.5 million elements: 81 us, 345 MB
+// moved).  A low part in 8 bits, 8 bytes an element, measured the same.
 template <class C, int PROD, bool LAST>
 __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int cur, float ca,
                                                            float keep) {
   __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, PROD == 3 ? 2 : 1>::LDS];
-  const int t = nt_xcd(blockIdx.x, dv.tiles);
+  const int t = ns_xcd(dv);
   if (t >= dv.tiles) return;
   const NsJob& j = ns_job(dv, t);
   int pt, qt;
@@ -1050,7 +1063,9 @@ struct NsStep {
 
 template <class C, int PROD>
 void ns_launch(const NsStep& s, const NsDev& d, hipStream_t st) {
-  const dim3 grid((unsigned)(8 * ((d.tiles + 7) / 8))), block(C::THREADS);
+  // (a multiple of the XCDs' groups, see ns_xcd and nt_xcd)
+  const int gr = 8 * ns_group(d.tiles, s.stage < 2 || d.single);
+  const dim3 grid((unsigned)ceil_div(d.tiles, gr) * gr), block(C::THREADS);
   if (s.stage == 0)
     hipLaunchKernelGGL((ns_sym<C, 0, PROD>), grid, block, 0, st, d, s.cb, s.cc);
   else if (s.stage == 1)
