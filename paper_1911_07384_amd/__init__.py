@@ -182,9 +182,31 @@ def _ptr(t):
 def _check_dtype(t) -> None:
     global _DTYPES
     import torch
-    _DTYPES = frozenset((torch.float16, torch.float32, torch.uint8, torch.int8, torch.int32))
+    _DTYPES = frozenset((torch.float16, torch.float32, torch.uint8, torch.int32))
     if t.dtype not in _DTYPES:
-        raise TypeError(f"expected float16/float32/uint8/int8/int32 tensor, got {t.dtype}")
+        raise TypeError(f"expected float16/float32/uint8/int32 tensor, got {t.dtype}")
+
+
+def _ptr_of(dtype):
+    """A _ptr for arguments of one element type, named as in torch."""
+    want = None
+
+    def ptr(t):
+        nonlocal want
+        if t is None or isinstance(t, int):
+            return t
+        if t.dtype != want:
+            import torch
+            want = getattr(torch, dtype)
+            if t.dtype != want:
+                raise TypeError(f"expected {dtype} tensor, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+        return t.data_ptr()
+    return ptr
+
+
+_ptr_half, _ptr_float, _ptr_int8 = _ptr_of("float16"), _ptr_of("float32"), _ptr_of("int8")
 
 
 def _first_current_stream():
@@ -531,7 +553,7 @@ def int8_operand(rows, n, device="cuda"):
 
 def fp16_int8_quant_rows(rows, cols, x, q, scale, stream=None) -> None:
     _check("fp16_int8_quant_rows", lib().fp16_int8_quant_rows(
-        int(rows), int(cols), _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+        int(rows), int(cols), _ptr_half(x), _ptr_int8(q), _ptr_float(scale), _stream(stream)))
 
 
 def fp16_int8_quant_workspace_bytes(rows, cols) -> int:
@@ -540,14 +562,14 @@ def fp16_int8_quant_workspace_bytes(rows, cols) -> int:
 
 def fp16_int8_quant_cols(rows, cols, x, q, scale, ws=None, ws_bytes=None, stream=None) -> None:
     _check("fp16_int8_quant_cols", lib().fp16_int8_quant_cols(
-        int(rows), int(cols), _ptr(x), _ptr(q), _ptr(scale), _ptr(ws), _wsb(ws, ws_bytes),
-        _stream(stream)))
+        int(rows), int(cols), _ptr_half(x), _ptr_int8(q), _ptr_float(scale), _ptr(ws),
+        _wsb(ws, ws_bytes), _stream(stream)))
 
 
 def fp16_int8_matmul(m, n, k, a, sa, b, sb, bias, y, stream=None) -> None:
     _check("fp16_int8_matmul", lib().fp16_int8_matmul(
-        int(m), int(n), int(k), _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), _ptr(bias), _ptr(y),
-        _stream(stream)))
+        int(m), int(n), int(k), _ptr_int8(a), _ptr_float(sa), _ptr_int8(b), _ptr_float(sb),
+        _ptr_half(bias), _ptr_half(y), _stream(stream)))
 
 
 def fp16_int8_kernel(m, n, k) -> str:
@@ -564,21 +586,22 @@ def fp16_int8_dense_workspace_bytes(desc: Int8DenseDesc, call=None) -> int:
 def fp16_int8_dense_weights(desc, w, wq, sw, wqt=None, swt=None, ws=None, ws_bytes=None,
                             stream=None) -> None:
     _check("fp16_int8_dense_weights", lib().fp16_int8_dense_weights(
-        ctypes.byref(desc), _ptr(w), _ptr(wq), _ptr(sw), _ptr(wqt), _ptr(swt), _ptr(ws),
-        _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _ptr_half(w), _ptr_int8(wq), _ptr_float(sw), _ptr_int8(wqt),
+        _ptr_float(swt), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
 
 
 def fp16_int8_dense_fwd(desc, x, wq, sw, bias, y, ws=None, ws_bytes=None, stream=None) -> None:
     _check("fp16_int8_dense_fwd", lib().fp16_int8_dense_fwd(
-        ctypes.byref(desc), _ptr(x), _ptr(wq), _ptr(sw), _ptr(bias), _ptr(y), _ptr(ws),
-        _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _ptr_half(x), _ptr_int8(wq), _ptr_float(sw), _ptr_half(bias),
+        _ptr_half(y), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
 
 
 def fp16_int8_dense_bwd(desc, x, dy, wqt, swt, dx, dw, dbias=None, ws=None, ws_bytes=None,
                         stream=None) -> None:
     _check("fp16_int8_dense_bwd", lib().fp16_int8_dense_bwd(
-        ctypes.byref(desc), _ptr(x), _ptr(dy), _ptr(wqt), _ptr(swt), _ptr(dx), _ptr(dw),
-        _ptr(dbias), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _ptr_half(x), _ptr_half(dy), _ptr_int8(wqt), _ptr_float(swt),
+        _ptr_half(dx), _ptr_half(dw), _ptr_half(dbias), _ptr(ws), _wsb(ws, ws_bytes),
+        _stream(stream)))
 
 
 def _wsb(ws, ws_bytes):
