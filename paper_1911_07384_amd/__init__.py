@@ -13,6 +13,7 @@ nonzero status raises ``Fp16Error``.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -195,10 +196,10 @@ def _ptr_of(dtype):
         nonlocal want
         if t is None or isinstance(t, int):
             return t
-        if t.dtype != want:
+        if t.dtype is not want:
             import torch
             want = getattr(torch, dtype)
-            if t.dtype != want:
+            if t.dtype is not want:
                 raise TypeError(f"expected {dtype} tensor, got {t.dtype}")
         if not t.is_contiguous():
             raise ValueError("tensor must be contiguous")
@@ -484,11 +485,21 @@ def muon_descs(shapes):
 
 
 def _muon_list(descs, *lists):
-    """The number of matrices and an array of pointers for each list of tensors."""
+    """The number of matrices and an array of pointers for each list of tensors, which
+    are binary16 and of their matrices' sizes at least."""
     n = len(lists[0])
     if any(len(l) != n for l in (descs, *lists)):
         raise ValueError("descs and the lists of tensors differ in length")
-    return [n] + [(_P * n)(*[_ptr(t) for t in l]) for l in lists]
+    v = memoryview(descs).cast("B").cast("i").tolist()  # rows, cols and the scale's bits
+    need = [r * c for r, c in zip(v[::3], v[1::3])]
+    for l in lists:
+        try:
+            have = [t.numel() for t in l]
+        except AttributeError:  # addresses among them, which are taken as they are
+            have = [t.numel() if hasattr(t, "numel") else k for t, k in zip(l, need)]
+        if any(map(operator.lt, have, need)):
+            raise ValueError(f"matrices of {need} elements, tensors of {have}")
+    return [n] + [(_P * n)(*map(_ptr_half, l)) for l in lists]
 
 
 def _coef(coef, steps):

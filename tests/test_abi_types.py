@@ -72,3 +72,29 @@ def test_8_bit_layers_take_each_argument_in_its_type(call):
         if good[i].dim() == 2:
             with pytest.raises(ValueError):
                 f(*good[:i], torch.zeros(good[i].shape[::-1], dtype=good[i].dtype).t(), *good[i + 1:])
+
+
+def test_lists_of_matrices_fit_their_descriptors():
+    """Each tensor of a list in binary16 and of its matrix's size at least, in every
+    list and at every place of it."""
+    shapes = [(8, 8), (16, 4), (5, 7)]
+    d = F.muon_descs(shapes)
+    good = [half(*s) for s in shapes]
+    orth = lambda x, y: F.fp16_orthogonalize(d, x, y, ws=WS, stream=0)
+    step = lambda w, g, m: F.fp16_muon_step(d, w, g, m, ws=WS, stream=0)
+    for f, lists in ((orth, 2), (step, 3)):
+        with pytest.raises(pytest.fail.Exception):
+            f(*[good] * lists)
+        with pytest.raises(pytest.fail.Exception):  # part of a larger buffer
+            f(*[[half(100)] * 3] * lists)
+        with pytest.raises(pytest.fail.Exception):  # addresses are the caller's matter
+            f(*[[4096] * 3] * lists)
+        for i in range(lists):
+            for k in range(3):
+                for bad, error in ((good[k].float(), TypeError), (good[k].to(torch.int8), TypeError),
+                                   (good[k].flatten()[:-1], ValueError), (half(0), ValueError),
+                                   (half(*shapes[k][::-1], 2)[:, :, 0].t(), ValueError)):
+                    l = [list(good) for _ in range(lists)]
+                    l[i][k] = bad
+                    with pytest.raises(error):
+                        f(*l)
