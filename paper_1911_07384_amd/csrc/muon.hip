@@ -736,7 +736,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small(const NsChunk c, co
     }
     if (t >= 0) {
       const h16* const from = oh + (tall ? 4 * lhi * TLD + lrow : lrow * GLD + 4 * lhi);
-      float u[2][16], sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (eight squares each in float32)
+      // (squares in float64: those of a finite float32 need not be finite in float32)
+      float u[2][16];
+      double sq[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -744,9 +746,9 @@ __global__ __launch_bounds__(64 * kSmallWaves) void ns_small(const NsChunk c, co
           const int n = 8 * (e / 4) + e % 4, at = tall ? n * TLD + 32 * b : 32 * b * GLD + n;
           // (elements past the matrix were read as zeros)
           u[b][e] = __builtin_fmaf(cm, to_f32(from[IN + at]), cg * to_f32(from[at]));
-          sq[e / 4] = __builtin_fmaf(u[b][e], u[b][e], sq[e / 4]);
+          sq[e / 4] = __builtin_fma((double)u[b][e], (double)u[b][e], sq[e / 4]);
         }
-      s += ((double)sq[0] + (double)sq[1]) + ((double)sq[2] + (double)sq[3]);
+      s += (sq[0] + sq[1]) + (sq[2] + sq[3]);
 #pragma unroll
       for (int k = 0; k < T; ++k) {
         if (k != t) continue;

@@ -1,5 +1,5 @@
 """The momentum of fp16_muon_step on both of its paths (one workgroup a matrix; tiles
-over all CUs) without Nesterov's look-ahead."""
+over all CUs): without Nesterov's look-ahead, and with one whose squares pass float32."""
 
 import numpy as np
 import pytest
@@ -7,7 +7,7 @@ import torch
 
 import oracle
 import paper_1911_07384_amd as F
-from gpu_util import host, require_gpu
+from gpu_util import host, note, require_gpu
 from test_gpu_muon import BAR, matrix, ns64, off, step
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +40,18 @@ def test_plain_momentum(path, products):
         ref = -0.5 * ns64(torch.from_numpy(mr).view(*s))
         assert off(W[i], ref) <= BAR[products], s
         assert torch.equal(G[i].cpu(), g[i])
+
+
+@pytest.mark.parametrize("path", SETS)
+def test_momentum_whose_squares_pass_float32(path):
+    """From a zero momentum the direction is (mu + 1) g whatever mu: with mu = 2^80
+    its squares, about 2^138, are finite in float64 only."""
+    require_gpu()
+    shapes = SETS[path]
+    g = [matrix(*s, seed=30 + i) for i, s in enumerate(shapes)]
+    W, M = ([torch.zeros(s, dtype=torch.float16, device="cuda") for s in shapes] for _ in range(2))
+    note("[gpu] a momentum of 2^80")
+    step(W, [t.cuda() for t in g], M, [1.0] * len(shapes), 0.5, 2.0 ** 80, 0.0, True, 3)
+    for i, s in enumerate(shapes):
+        assert torch.equal(M[i].cpu(), g[i])
+        assert off(W[i], -0.5 * ns64(g[i])) <= BAR[3], s
