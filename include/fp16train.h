@@ -524,7 +524,8 @@ const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_
  * Coefficients have to keep |X| < 16 and |b A + c A^2| < 32 elementwise; beyond,
  * operands overflow.
  * 1 <= steps <= FP16_MUON_MAX_STEPS, products 1 or 3, finite coef (FP16_ERR_SHAPE);
- * count = 0 is a no-op.  y[i] may equal x[i]; no y[i] may overlap anything else. */
+ * FP16_ERR_HIP also if the host has no memory for the list's plan (about 240 bytes a
+ * matrix, for the call only); count = 0 is a no-op.  y[i] may equal x[i]; no y[i] may overlap anything else. */
 fp16_status fp16_orthogonalize(int32_t count, const fp16_muon_desc* descs, const fp16_t* const* x,
                                fp16_t* const* y, int32_t steps, const float* coef,
                                int32_t products, void* ws, size_t ws_bytes, fp16_stream_t stream);

@@ -8,6 +8,7 @@
 
 #include <math.h>
 #include <stdio.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -29,21 +30,42 @@ bool ns_list_ok(int32_t count, const fp16_muon_desc* d, int32_t products) {
   return true;
 }
 
-void ns_make_plan(int32_t count, const fp16_muon_desc* d, int32_t products, NsPlan* plan) {
-  int32_t rows[kNsMaxJobs], cols[kNsMaxJobs];
-  for (int i = 0; i < count; ++i) {
-    rows[i] = d[i].rows;
-    cols[i] = d[i].cols;
-  }
-  ns_plan(count, rows, cols, products, plan);
-}
-
 // Buffers of one call: a written one may overlap no other.
 struct Span {
   uintptr_t at;
   size_t bytes;
   bool written;
 };
+
+// A list's plan and spans, in one allocation of the list's size: a thread's stack need
+// not hold a list of kNsMaxJobs.  false if the host has no memory for it.
+struct NsHost {
+  NsPlan plan;
+  Span* spans = nullptr;  // [3 count + 1]
+  void* block = nullptr;
+  NsHost() = default;
+  NsHost(const NsHost&) = delete;
+  NsHost& operator=(const NsHost&) = delete;
+  ~NsHost() { free(block); }
+
+  bool make(int32_t count, const fp16_muon_desc* d, int32_t products) {
+    static_assert(alignof(NsJob) <= 8 && sizeof(NsJob) % 8 == 0 && alignof(Span) == 8, "places");
+    const size_t n = (size_t)count;
+    block = malloc(n * (sizeof(NsJob) + 3 * sizeof(Span) + 3 * sizeof(int32_t)) + sizeof(Span));
+    if (!block) return false;
+    plan.jobs = static_cast<NsJob*>(block);
+    spans = reinterpret_cast<Span*>(plan.jobs + n);
+    plan.order = reinterpret_cast<int*>(spans + 3 * n + 1);
+    int32_t *rows = plan.order + n, *cols = rows + n;
+    for (int i = 0; i < count; ++i) {
+      rows[i] = d[i].rows;
+      cols[i] = d[i].cols;
+    }
+    ns_plan(count, rows, cols, products, &plan);
+    return true;
+  }
+};
+
 bool spans_clash(Span* s, int n) {
   std::sort(s, s + n, [](const Span& a, const Span& b) { return a.at < b.at; });
   uintptr_t wend = 0, rend = 0;  // furthest end of a written and of a read span so far
@@ -77,11 +99,12 @@ fp16_status ns_call(int32_t count, const fp16_muon_desc* descs, fp16_t* const* w
     if (((uintptr_t)w[i] | (uintptr_t)g[i] | (update ? (uintptr_t)m[i] : 0)) & 1u)
       return FP16_ERR_MISALIGNED;
   }
-  NsPlan plan;
-  ns_make_plan(count, descs, products, &plan);
+  NsHost host;
+  if (!host.make(count, descs, products)) return FP16_ERR_HIP;
+  NsPlan& plan = host.plan;
   if (!ws || ws_bytes < plan.bytes) return FP16_ERR_WORKSPACE;
   if (!aligned16(ws)) return FP16_ERR_MISALIGNED;
-  Span spans[3 * kNsMaxJobs + 1];
+  Span* const spans = host.spans;
   int n = 0;
   for (int i = 0; i < count; ++i) {
     const size_t b = (size_t)descs[i].rows * descs[i].cols * 2;
@@ -193,16 +216,16 @@ extern "C" {
 
 size_t fp16_muon_workspace_bytes(int32_t count, const fp16_muon_desc* descs, int32_t products) {
   if (!ns_list_ok(count, descs, products)) return 0;
-  NsPlan plan;
-  ns_make_plan(count, descs, products, &plan);
-  return plan.bytes;
+  NsHost host;
+  return host.make(count, descs, products) ? host.plan.bytes : 0;
 }
 
 const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_t products) {
   thread_local char name[64];
   if (!ns_list_ok(count, descs, products)) return "";
-  NsPlan plan;
-  ns_make_plan(count, descs, products, &plan);
+  NsHost host;
+  if (!host.make(count, descs, products)) return "";
+  const NsPlan& plan = host.plan;
   if (plan.small) return "one workgroup each";
   char* at = name;
   for (const NsTile& k : plan.kind) {

@@ -49,11 +49,12 @@ struct NsPlan {
   int tiles[3], n_pre;         // in all
   uint32_t table, map[3], map_pre, sums;  // in the workspace
   size_t bytes;
-  int order[kNsMaxJobs];       // jobs[i] is the caller's matrix order[i]
-  NsJob jobs[kNsMaxJobs];
+  int* order;                  // [count]: jobs[i] is the caller's matrix order[i]
+  NsJob* jobs;                 // [count]
 };
 
-// Fills the plan's sizes, tiles and workspace places from rows[i], cols[i].
+// Fills the plan's sizes, tiles and workspace places from rows[i], cols[i], and order
+// and jobs, which are the caller's (a list may be long, and its stack short).
 void ns_plan(int count, const int32_t* rows, const int32_t* cols, int products, NsPlan* plan);
 
 struct NsArgs {
