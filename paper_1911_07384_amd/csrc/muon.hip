@@ -999,22 +999,26 @@ int up(int v, int t) { return (v + t - 1) / t * t; }
 //  3: 4096 x 4096      280/398   193/433   294/430   272/463   319/511   338/544       -
 //     1024 x 4096       227/92    117/54    100/47     67/39     45/40     27/46   26/-
 //     3 of 512 x 4608   258/67    128/43    109/37     75/46     49/45     29/53   24/-
+// a_only: rows that are offered to A alone.  The last cuts reductions, which only A's
+// are long enough for.  64 deep wins by its shorter `alone` time where one reduction
+// bounds the launch; with one product that takes more than 16 slices (12 for X'), and
+// B and X' of a side that long have tiles enough to bound it by `cu`.
 constexpr int kNsKinds = 7;
 constexpr NsTile kNsTiles[2][kNsKinds] = {
-    {{"256", 256, 1, 1, 1.23, 1.87, {11.1, 19.3}, 0.0},
-     {"192", 192, 1, 1, 0.68, 1.09, {11.8, 21.0}, 0.0},
-     {"128", 128, 1, 2, 0.68, 0.57, {6.4, 13.0}, 0.0},
-     {"128 deep", 128, 1, 1, 0.31, 0.74, {7.7, 8.5}, 0.0},
-     {"64", 64, 1, 2, 0.19, 0.29, {4.7, 6.3}, 0.0},
-     {"64 deep", 64, 1, 1, 0.165, 0.37, {5.1, 6.6}, 0.0},
-     {"128", 128, 2, 1, 0.31, 0.30, {9.0, 8.0}, 0.036}},
-    {{"256", 256, 1, 1, 3.80, 5.50, {15.7, 31.8}, 0.0},
-     {"192", 192, 1, 1, 1.71, 2.82, {14.6, 23.1}, 0.0},
-     {"128", 128, 1, 2, 1.53, 1.76, {7.8, 12.9}, 0.0},
-     {"128 deep", 128, 1, 1, 1.04, 1.72, {8.1, 11.6}, 0.0},
-     {"64", 64, 1, 2, 0.62, 0.53, {5.0, 6.9}, 0.0},
-     {"64 deep", 64, 1, 1, 0.30, 0.60, {5.5, 7.0}, 0.0},
-     {"128", 128, 2, 1, 0.44, 0.59, {11.0, 11.9}, 0.033}}};
+    {{"256", 256, 1, 1, 1.23, 1.87, {11.1, 19.3}, 0.0, false},
+     {"192", 192, 1, 1, 0.68, 1.09, {11.8, 21.0}, 0.0, false},
+     {"128", 128, 1, 2, 0.68, 0.57, {6.4, 13.0}, 0.0, false},
+     {"128 deep", 128, 1, 1, 0.31, 0.74, {7.7, 8.5}, 0.0, false},
+     {"64", 64, 1, 2, 0.19, 0.29, {4.7, 6.3}, 0.0, false},
+     {"64 deep", 64, 1, 1, 0.165, 0.37, {5.1, 0.0}, 0.0, true},
+     {"128", 128, 2, 1, 0.31, 0.30, {9.0, 0.0}, 0.036, true}},
+    {{"256", 256, 1, 1, 3.80, 5.50, {15.7, 31.8}, 0.0, false},
+     {"192", 192, 1, 1, 1.71, 2.82, {14.6, 23.1}, 0.0, false},
+     {"128", 128, 1, 2, 1.53, 1.76, {7.8, 12.9}, 0.0, false},
+     {"128 deep", 128, 1, 1, 1.04, 1.72, {8.1, 11.6}, 0.0, false},
+     {"64", 64, 1, 2, 0.62, 0.53, {5.0, 6.9}, 0.0, false},
+     {"64 deep", 64, 1, 1, 0.30, 0.60, {5.5, 7.0}, 0.0, false},
+     {"128", 128, 2, 1, 0.44, 0.59, {11.0, 0.0}, 0.033, true}}};
 
 // The tile that a product of the set finishes soonest on, by that estimate: the
 // work spread over the CUs (and half of the longest reduction for the last round),
@@ -1028,6 +1032,7 @@ int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, in
   double bt = 0;
   for (int i = 0; i < kNsKinds; ++i) {
     NsTile c = kNsTiles[products == 3][i];
+    if (c.a_only && stage != 0) continue;
     double tiles = 0, work = 0, longest = 0;
     for (int n = 0; n < count; ++n) {
       const int r = up(rows[n], 64), l = up(cols[n], 64), m = std::min(r, l);
@@ -1040,7 +1045,6 @@ int ns_choose(int stage, int count, const int32_t* rows, const int32_t* cols, in
     }
     double t = c.fixed[stage == 2];
     if (c.parts > 1) {
-      if (stage != 0) continue;
       c.parts = (int)std::min(std::min(cus / tiles, longest / 2), 16.0);
       if (c.parts < 2) continue;
       longest = ceil(longest / c.parts);
@@ -1063,19 +1067,24 @@ struct NsStep {
   float ca, cb, cc, keep;
 };
 
-template <class C, int PROD>
+// (A_ONLY: a tile of A alone, see kNsTiles)
+template <class C, int PROD, bool A_ONLY = false>
 void ns_launch(const NsStep& s, const NsDev& d, hipStream_t st) {
   // (a multiple of the XCDs' groups, see ns_xcd and nt_xcd)
   const int gr = 8 * ns_group(d.tiles, s.stage < 2 || d.single);
   const dim3 grid((unsigned)ceil_div(d.tiles, gr) * gr), block(C::THREADS);
-  if (s.stage == 0)
+  if constexpr (A_ONLY) {
     hipLaunchKernelGGL((ns_sym<C, 0, PROD>), grid, block, 0, st, d, s.cb, s.cc);
-  else if (s.stage == 1)
-    hipLaunchKernelGGL((ns_sym<C, 1, PROD>), grid, block, 0, st, d, s.cb, s.cc);
-  else if (!s.last)
-    hipLaunchKernelGGL((ns_x<C, PROD, false>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
-  else
-    hipLaunchKernelGGL((ns_x<C, PROD, true>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
+  } else {
+    if (s.stage == 0)
+      hipLaunchKernelGGL((ns_sym<C, 0, PROD>), grid, block, 0, st, d, s.cb, s.cc);
+    else if (s.stage == 1)
+      hipLaunchKernelGGL((ns_sym<C, 1, PROD>), grid, block, 0, st, d, s.cb, s.cc);
+    else if (!s.last)
+      hipLaunchKernelGGL((ns_x<C, PROD, false>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
+    else
+      hipLaunchKernelGGL((ns_x<C, PROD, true>), grid, block, 0, st, d, s.cur, s.ca, s.keep);
+  }
 }
 
 template <int PROD>
@@ -1095,7 +1104,7 @@ hipError_t ns_run(const NsPlan& p, const NsArgs& a, char* ws, hipStream_t st) {
         case 2: ns_launch<typename NsTiles<PROD>::T128, PROD>(s, d, st); break;
         case 3: ns_launch<typename NsTiles<PROD>::T128d, PROD>(s, d, st); break;
         case 4: ns_launch<typename NsTiles<PROD>::T64, PROD>(s, d, st); break;
-        case 5: ns_launch<typename NsTiles<PROD>::T64d, PROD>(s, d, st); break;
+        case 5: ns_launch<typename NsTiles<PROD>::T64d, PROD, PROD == 1>(s, d, st); break;
         default:
           hipLaunchKernelGGL((ns_part<PROD>), dim3((unsigned)(8 * ((d.tiles * parts + 7) / 8))),
                              dim3(256), 0, st, d, parts);

@@ -39,6 +39,7 @@ struct NsTile {
   const char* name;
   int side, parts, occ;
   double alone, cu, fixed[2], sums;
+  bool a_only;
 };
 
 struct NsPlan {
