@@ -994,9 +994,13 @@ int up(int v, int t) { return (v + t - 1) / t * t; }
 // The tiles a product may run on, with one product and with three.  Times of a
 // 128-byte slice of the reduction in microseconds, for one workgroup alone (alone)
 // and for a CU whatever it holds (cu); of a launch besides, for A or B and for X',
-// whose outputs read more; and of the sums of a workgroup to memory and back.  Fits
-// (to 10 %) to what each tile took on ten sets of 256 to 8192 rows and columns, e.g.
-// A / X' in us:
+// whose outputs read more; and of the sums of a workgroup to memory and back.  Fitted
+// to what each tile took on ten sets of 256 to 8192 rows and columns.  Of the times
+// below (A / X' in us) four in five are met within 13 %; X' of the three matrices is
+// estimated 15 to 34 % low on 64, 64 deep and 128 deep (what a tile stores counts for
+// the launch only), X' of 4096 x 4096 up to 20 % high on tiles below 192, A in parts up
+// to 28 % high.  The choice costs 7 us at most there (X' of the three matrices, one
+// product: 128 deep):
 //                          256       192       128  128 deep        64   64 deep  128 in parts
 //  1: 4096 x 4096      101/136    79/171   114/150   110/177   166/275   184/346       -
 //     1024 x 4096        80/40     49/34     46/25     30/23     18/26     17/33   18/-
