@@ -514,8 +514,10 @@ def _coef(coef, steps):
     return (_F * max(len(flat), 1))(*flat)
 
 
-def fp16_muon_workspace_bytes(descs, products=1) -> int:
-    return int(lib().fp16_muon_workspace_bytes(len(descs), descs, int(products)))
+def fp16_muon_workspace_bytes(descs, products=None) -> int:
+    """Workspace with this many products, or (None) enough for one and for three."""
+    return max(int(lib().fp16_muon_workspace_bytes(len(descs), descs, p))
+               for p in ((1, 3) if products is None else (int(products),)))
 
 
 def fp16_muon_kernels(descs, products=1) -> str:

@@ -181,3 +181,18 @@ def test_the_quantisers_oracle():
             want = round(127 * Fraction(float(x[i, j])) / top) if top else 0
             assert q[i, j] == want
         assert s[i] == np.float32(np.float32(float(top)) / np.float32(127))
+
+
+def test_a_workspace_by_default_serves_either_call_by_default():
+    """Queried without a number of products it holds one or three: each call, with its
+    own default, gets past the workspace to the next refusal (an overlap)."""
+    for shapes in ([(64, 64)], [(512, 4608)] * 3, [(1024, 4096)], [(70, 80), (700, 300)]):
+        d = F.muon_descs(shapes)
+        need = F.fp16_muon_workspace_bytes(d)
+        assert need == max(F.fp16_muon_workspace_bytes(d, 1), F.fp16_muon_workspace_bytes(d, 3))
+        far = lambda base: [base + (1 << 28) * i for i in range(len(shapes))]
+        with pytest.raises(F.Fp16Error, match="FP16_ERR_ALIASING"):
+            F.fp16_orthogonalize(d, far(1 << 40), far(2 << 40), ws=1 << 40, ws_bytes=need, stream=0)
+        with pytest.raises(F.Fp16Error, match="FP16_ERR_ALIASING"):
+            F.fp16_muon_step(d, far(1 << 40), far(2 << 40), far(3 << 40), ws=1 << 40, ws_bytes=need,
+                             stream=0)
