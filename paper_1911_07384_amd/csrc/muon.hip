@@ -376,7 +376,7 @@ __device__ __forceinline__ void ns_sym_out(const NsDev& dv, const NsJob& j, floa
 }
 
 // A = X X^T (STEP 0) or B = bA + cA^2 (STEP 1), off the diagonal, and the diagonal.
-// One product, 4096 x 4096, tiles of 192: 86 and 90 us for the 69 GFLOP of a triangle
+// One product, 4096 x 4096, tiles of 192: 88 and 91 us for the 69 GFLOP of a triangle
 // (253 tiles, one a CU: 63 us of products and an epilogue that nothing hides).
 template <class C, int STEP, int PROD>
 __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_sym(const NsDev dv, float cb, float cc) {
@@ -555,10 +555,10 @@ __device__ __forceinline__ int ns_xcd(const NsDev& dv) {
   return (i / g * 8 + (blockIdx.x & 7)) * g + i % g;
 }
 
-// X' = (a + E) X + B'X.  Bound by the products where m is long (4096 x 4096: 152 us,
+// X' = (a + E) X + B'X.  Bound by the products where m is long (4096 x 4096: 153 us,
 // 137 GFLOP; about 90 us of them the products) and by the epilogue's 10 bytes an element
-// where it is short (ResNet-50's 54 matrices, 25.5 million elements: 81 us, 345 MB
-// moved).  A low part in 8 bits, 8 bytes an element, measured the same.
+// where it is short (ResNet-50's 54 matrices, 25.5 million elements: 79 us, 358 MB
+// moved, the matrix cores 18 % busy).  A low part in 8 bits, 8 bytes an element, measured the same.
 template <class C, int PROD, bool LAST>
 __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int cur, float ca,
                                                            float keep) {
@@ -634,6 +634,7 @@ __global__ __launch_bounds__(256) void ns_sum(const NsDev dv, int parts) {
 //     64 x 576            37 / 69        52 / 81
 //     64 x 1024           53 / 77        78 / 91
 //     24 of 64 x 1024     54 / 94        79 / 111
+// (25 of them, which the arguments do not hold, take 108 and 131 over all CUs.)
 constexpr int kSmallWaves = 8, kSmallTiles = 4;           // tiles of a wave at most
 constexpr int kSmallShort = 64, kSmallLong = 32 * kSmallWaves * kSmallTiles;
 
