@@ -523,20 +523,21 @@ const char* fp16_muon_kernels(int32_t count, const fp16_muon_desc* descs, int32_
  * Relative error (2-norm) of the result before its rounding to binary16, after five
  * steps of the default coefficients:
  *                                                products 1     products 3
- *   random matrices and gradients, the shorter
- *     side 16 or more                              2.5e-3          1e-5
+ *   random matrices, gradients with noise in
+ *     every entry, the shorter side 16 or more     2.5e-3          1e-5
  *   rank one, equal rows, entries of one
  *     magnitude, the shorter side up to 2500       5e-2            3e-4
  * The second row is for roundings that all have one sign, as such entries' may (with
- * products 1, 1e-2 is the most that was measured: a constant matrix).  More steps
- * multiply an error by up to 1.6 each, and in the directions of zero singular values
- * by a, 3.4 each, with any number of bits: a matrix of low rank is off by 2e-3 after
- * eight steps with products 3, and by 0.2 after twelve.
+ * products 1, 1e-2 is the most that was measured: a constant matrix).  Each further
+ * step multiplies an error by up to about 1.6, and in the directions of zero singular
+ * values by a, 3.4, with any number of bits: matrices of low rank were off by up to
+ * 2e-3 after eight steps with products 3, and by 0.2 after twelve.
  * Coefficients have to keep |X| < 16 and |b A + c A^2| < 32 elementwise; beyond,
  * operands overflow.
  * 1 <= steps <= FP16_MUON_MAX_STEPS, products 1 or 3, finite coef (FP16_ERR_SHAPE);
  * FP16_ERR_HIP also if the host has no memory for the list's plan (about 240 bytes a
- * matrix, for the call only); count = 0 is a no-op.  y[i] may equal x[i]; no y[i] may overlap anything else. */
+ * matrix, for the call only); count = 0 is a no-op.  y[i] may equal x[i]; no y[i] may
+ * overlap anything else. */
 fp16_status fp16_orthogonalize(int32_t count, const fp16_muon_desc* descs, const fp16_t* const* x,
                                fp16_t* const* y, int32_t steps, const float* coef,
                                int32_t products, void* ws, size_t ws_bytes, fp16_stream_t stream);

@@ -536,7 +536,9 @@ def fp16_orthogonalize(descs, xs, ys, steps=5, coef=None, products=3, ws=None, w
 
 def fp16_muon_step(descs, ws_, gs, ms, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True,
                    steps=5, coef=None, products=1, ws=None, ws_bytes=None, stream=None) -> None:
-    """One update of the weights ws_ from the gradients gs with the momenta ms."""
+    """One update of the weights ws_ from the gradients gs with the momenta ms.
+    products: operands of the orthogonalisation rounded to binary16 (1) or of 22 bits
+    (3), see the header for what either keeps."""
     n, w, g, m = _muon_list(descs, ws_, gs, ms)
     _check("fp16_muon_step", lib().fp16_muon_step(
         n, descs, w, g, m, float(lr), float(momentum), float(weight_decay), int(bool(nesterov)),

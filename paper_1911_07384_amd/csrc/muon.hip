@@ -558,7 +558,8 @@ __device__ __forceinline__ int ns_xcd(const NsDev& dv) {
 // X' = (a + E) X + B'X.  Bound by the products where m is long (4096 x 4096: 153 us,
 // 137 GFLOP; about 90 us of them the products) and by the epilogue's 10 bytes an element
 // where it is short (ResNet-50's 54 matrices, 25.5 million elements: 79 us, 358 MB
-// moved, the matrix cores 18 % busy).  A low part in 8 bits, 8 bytes an element, measured the same.
+// moved, the matrix cores 18 % busy).  A low part in 8 bits, 8 bytes an element,
+// measured the same.
 template <class C, int PROD, bool LAST>
 __global__ __launch_bounds__(C::THREADS, C::OCC) void ns_x(const NsDev dv, int cur, float ca,
                                                            float keep) {

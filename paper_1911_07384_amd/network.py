@@ -19,7 +19,9 @@ block-last gamma at 0 (the initialisation of Section 5.1; with the swap it
 also zeroes the shortcut's contribution at the start); ``optimizer="muon"``
 updates the convolution filters and the classifier's weights by orthogonalised
 momentum (fp16_muon_step, each filter as a [K, R*S*C] matrix) in one call, and
-the classifier's bias and the BN parameters by SGD as before;
+the classifier's bias and the BN parameters by SGD as before (``muon_products``: 1
+rounds the products' operands to binary16, 3 keeps 22 bits of them and takes twice as
+long);
 ``classifier="int8"`` runs the classifier's products in 8-bit integers
 (fp16_int8_dense_*), its weights quantised anew in every step.
 
