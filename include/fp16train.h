@@ -10,9 +10,9 @@
  * rounded once to binary16, to nearest with ties to even, at its store
  * (Section 4.2 leaves the rounding method open; this library uses the IEEE
  * default).  Binary16 subnormals are kept (gradual underflow) and overflow
- * rounds to +-infinity.  The exceptions are statistics, losses and masks, and the
- * quantised operands of the 8-bit dense layers, which say so where they are
- * declared.
+ * rounds to +-infinity.  The exceptions are statistics, losses, log probabilities and
+ * masks, and the quantised operands of the 8-bit dense layers, which say so where they
+ * are declared.
  *
  * Conventions shared by every entry point:
  *   - Buffers are device pointers owned by the caller.  The library never
@@ -633,6 +633,117 @@ fp16_status fp16_int8_dense_fwd(const fp16_int8_dense_desc* desc, const fp16_t* 
 fp16_status fp16_int8_dense_bwd(const fp16_int8_dense_desc* desc, const fp16_t* x, const fp16_t* dy,
                                 const int8_t* wqt, const float* swt, fp16_t* dx, fp16_t* dw,
                                 fp16_t* dbias, void* ws, size_t ws_bytes, fp16_stream_t stream);
+
+/* ---- dropout from a counter-based generator ----
+ * Random numbers of the calls below come from Philox4x32-10 (Salmon, Moraes, Dror,
+ * Shaw, 2011) and a state of two 64-bit numbers in device memory, rng[0] the seed and
+ * rng[1] the step, which the calls read and never write.  A `site` tells the dropouts
+ * of one step apart.  Element i of a call (row-major) takes 16-bit word i % 8, the low
+ * half of each 32-bit word first, of the block with counter (i / 8, site, step low,
+ * step high) and key (seed low, seed high); it is kept if the word is at least
+ * t = round(65536 p), ties up.  The drop probability is thus a multiple of 2^-16, and
+ * kept values are multiplied by 65536 / (65536 - t), rounded to float32.  No mask is
+ * stored: a backward pass with the same state, site and p makes the same choice.  A
+ * program that is captured in a graph advances the step in the graph. */
+
+/* rng[1] += steps (8-byte aligned, FP16_ERR_MISALIGNED). */
+fp16_status fp16_rng_advance(uint64_t* rng, uint64_t steps, fp16_stream_t stream);
+
+/* y[i] = round_to_binary16((kept_i ? fl(x[i] * scale) : +0) + residual[i]), in float32;
+ * residual may be NULL.  The gradient of x is the same call on dy without a residual
+ * (that of the residual is dy).  What is dropped is not looked at: a NaN or an infinity
+ * there gives 0.  y may equal x or residual, and overlaps nothing otherwise.
+ * 0 <= p <= 1, n < 2^35 (FP16_ERR_SHAPE); n = 0 is a no-op. */
+fp16_status fp16_dropout(size_t n, const fp16_t* x, const fp16_t* residual, fp16_t* y, float p,
+                         const uint64_t* rng, uint32_t site, fp16_stream_t stream);
+
+/* ---- dense layers with bias, activation, dropout and residual in the product ----
+ * A dense layer over `tokens` rows: x [tokens][inputs], W [outputs][inputs],
+ * y [tokens][outputs]. */
+typedef enum {
+  FP16_ACT_NONE = 0,
+  FP16_ACT_RELU = 1,
+  FP16_ACT_GELU = 2, /* z Phi(z), with the normal distribution's Phi (no tanh form) */
+  FP16_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} fp16_act;
+
+typedef struct {
+  int32_t tokens, inputs, outputs; /* each 1 to 2^20, each matrix < 2^35 elements */
+  int32_t act;                     /* fp16_act */
+  float drop;                      /* drop probability in [0, 1]; 0: no dropout */
+  uint32_t site;                   /* the dropout's, see above */
+} fp16_dense_desc;
+
+typedef enum { FP16_DENSE_FWD = 0, FP16_DENSE_BWD = 1 } fp16_dense_call;
+
+/* Bytes of workspace of one of the two calls below; 0 if it needs none or invalid. */
+size_t fp16_dense_workspace_bytes(const fp16_dense_desc* desc, int32_t call);
+
+/* Forward:
+ *   v = x W^T + bias                                   (float32 sums)
+ *   z = round_to_binary16(v)                           (unless NULL: kept for a backward)
+ *   y = round_to_binary16(drop(act(v)) + residual)
+ * with the dropout of fp16_dropout over y's elements.  act is taken of the float32
+ * value; at -inf GELU and SiLU are 0, their limit.  bias [outputs] and residual
+ * [tokens][outputs] may be NULL, rng too without a dropout.  y may equal residual; y
+ * and z overlap nothing otherwise. */
+fp16_status fp16_dense_fwd(const fp16_dense_desc* desc, const fp16_t* x, const fp16_t* w,
+                           const fp16_t* bias, const fp16_t* residual, const uint64_t* rng,
+                           fp16_t* y, fp16_t* z, void* ws, size_t ws_bytes, fp16_stream_t stream);
+
+/* Backward, from the z that the forward kept (not read without an activation):
+ *   u  = drop(dy) * act'(z)                            (float32)
+ *   dz = round_to_binary16(u)                          (in the workspace, or dy itself)
+ *   dx = round_to_binary16(dz W)
+ *   dw = round_to_binary16(dz^T x)
+ *   dbias[j] = round_to_binary16(sum_i u[i][j])        (float32 partial sums, added in
+ *              float64)
+ * The residual's gradient is dy.  The ReLU's slope at 0 is 0.  dx (with w), dw (with
+ * x) and dbias may each be NULL if not wanted, and overlap nothing. */
+fp16_status fp16_dense_bwd(const fp16_dense_desc* desc, const fp16_t* x, const fp16_t* w,
+                           const fp16_t* z, const fp16_t* dy, const uint64_t* rng, fp16_t* dx,
+                           fp16_t* dw, fp16_t* dbias, void* ws, size_t ws_bytes,
+                           fp16_stream_t stream);
+
+/* ---- log probabilities of given classes, entropies, most probable classes ----
+ * Logits z, `rows` rows of `classes`, a row's first `stride` elements after the one
+ * before's; l = scale * z (scale: one over a temperature). */
+#define FP16_LOGPROB_TOP_MAX 64
+typedef struct {
+  int32_t rows, classes; /* 1 <= rows < 2^24, 1 <= classes <= 2^20 */
+  int32_t stride;        /* classes <= stride <= 2^21, rows * stride < 2^35 */
+  float scale;           /* positive, finite */
+  int32_t top;           /* most probable classes: 0 to FP16_LOGPROB_TOP_MAX, <= classes */
+} fp16_logprob_desc;
+
+/* Bytes of workspace for fp16_logprobs; 0 if it needs none or invalid. */
+size_t fp16_logprobs_workspace_bytes(const fp16_logprob_desc* desc);
+
+/* For each row, in float32:
+ *   logp     = l_t - log(sum_j exp(l_j)), t the row's entry of tokens
+ *   stats[3] = the largest z, log(sum_j exp(l_j - its l)), the entropy
+ *              H = -sum_j p_j log p_j
+ *   top_id, top_logp [top]: the classes of the largest logits, the largest first (of
+ *              equal ones the lower class first), and their log probabilities
+ * A negative token asks for nothing: its logp is 0; one past the classes gives NaN.  A
+ * logit of -inf has probability 0 and takes no part.  In a row with nothing but -inf
+ * every log probability is -inf and H is 0.  A row with a NaN or +inf gives NaN, and
+ * NaN counts as the largest logit.  logp (with tokens) may be NULL; top_id and
+ * top_logp are needed where top > 0. */
+fp16_status fp16_logprobs(const fp16_logprob_desc* desc, const fp16_t* z, const int32_t* tokens,
+                          float* logp, float* stats, int32_t* top_id, float* top_logp, void* ws,
+                          size_t ws_bytes, fp16_stream_t stream);
+
+/* The logits' gradient, from the stats of fp16_logprobs with the same z, tokens and
+ * scale and the gradients of logp and of the entropies (either may be NULL: 0; the
+ * first needs tokens):
+ *   dz_j = round_to_binary16(scale * (dlogp ([j = t] - p_j) - dentropy p_j (log p_j + H)))
+ * with dlogp taken as 0 for a negative token; a token past the classes has no [j = t].
+ * A row with nothing but -inf gets zeros.  dz has z's stride, elements past the classes
+ * are not written; it may equal z and overlaps nothing otherwise. */
+fp16_status fp16_logprobs_bwd(const fp16_logprob_desc* desc, const fp16_t* z,
+                              const int32_t* tokens, const float* stats, const float* dlogp,
+                              const float* dentropy, fp16_t* dz, fp16_stream_t stream);
 
 /* Human-readable name of a status code (static string). */
 const char* fp16_status_string(fp16_status status);

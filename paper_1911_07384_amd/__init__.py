@@ -42,7 +42,9 @@ EXPORTS = ["fp16_conv_out_dims", "fp16_conv_workspace_bytes", "fp16_conv_fwd", "
            "fp16_muon_step", "fp16_int8_row_bytes", "fp16_int8_quant_rows",
            "fp16_int8_quant_workspace_bytes", "fp16_int8_quant_cols", "fp16_int8_matmul",
            "fp16_int8_kernel", "fp16_int8_dense_workspace_bytes", "fp16_int8_dense_weights",
-           "fp16_int8_dense_fwd", "fp16_int8_dense_bwd"]
+           "fp16_int8_dense_fwd", "fp16_int8_dense_bwd", "fp16_rng_advance", "fp16_dropout",
+           "fp16_dense_workspace_bytes", "fp16_dense_fwd", "fp16_dense_bwd",
+           "fp16_logprobs_workspace_bytes", "fp16_logprobs", "fp16_logprobs_bwd"]
 
 
 class Fp16Error(RuntimeError):
@@ -75,6 +77,17 @@ class MuonDesc(ctypes.Structure):
 
 class Int8DenseDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "inputs", "outputs")]
+
+
+class DenseDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("inputs", ctypes.c_int32),
+                ("outputs", ctypes.c_int32), ("act", ctypes.c_int32), ("drop", ctypes.c_float),
+                ("site", ctypes.c_uint32)]
+
+
+class LogprobDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("classes", ctypes.c_int32), ("stride", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("top", ctypes.c_int32)]
 
 
 _lib = None
@@ -132,6 +145,14 @@ _SIGS = {
     "fp16_int8_dense_weights": (ctypes.c_int, [_P] * 7 + [_SZ, _P]),
     "fp16_int8_dense_fwd": (ctypes.c_int, [_P] * 7 + [_SZ, _P]),
     "fp16_int8_dense_bwd": (ctypes.c_int, [_P] * 9 + [_SZ, _P]),
+    "fp16_rng_advance": (ctypes.c_int, [_P, ctypes.c_uint64, _P]),
+    "fp16_dropout": (ctypes.c_int, [_SZ, _P, _P, _P, _F, _P, ctypes.c_uint32, _P]),
+    "fp16_dense_workspace_bytes": (_SZ, [_P, _I32]),
+    "fp16_dense_fwd": (ctypes.c_int, [_P] * 9 + [_SZ, _P]),
+    "fp16_dense_bwd": (ctypes.c_int, [_P] * 10 + [_SZ, _P]),
+    "fp16_logprobs_workspace_bytes": (_SZ, [_P]),
+    "fp16_logprobs": (ctypes.c_int, [_P] * 8 + [_SZ, _P]),
+    "fp16_logprobs_bwd": (ctypes.c_int, [_P] * 8),
     "fp16_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "fp16_version": (ctypes.c_char_p, []),
 }
@@ -208,6 +229,15 @@ def _ptr_of(dtype):
 
 
 _ptr_half, _ptr_float, _ptr_int8 = _ptr_of("float16"), _ptr_of("float32"), _ptr_of("int8")
+_ptr_int, _ptr_long = _ptr_of("int32"), _ptr_of("int64")
+
+
+def _held(**tensors):
+    """Raises for a tensor with fewer elements than its call reads or writes; values are
+    (tensor or address or None, elements)."""
+    for name, (t, n) in tensors.items():
+        if hasattr(t, "numel") and t.numel() < n:
+            raise ValueError(f"{name} has {t.numel()} elements of {n}")
 
 
 def _first_current_stream():
@@ -617,6 +647,107 @@ def fp16_int8_dense_bwd(desc, x, dy, wqt, swt, dx, dw, dbias=None, ws=None, ws_b
         ctypes.byref(desc), _ptr_half(x), _ptr_half(dy), _ptr_int8(wqt), _ptr_float(swt),
         _ptr_half(dx), _ptr_half(dw), _ptr_half(dbias), _ptr(ws), _wsb(ws, ws_bytes),
         _stream(stream)))
+
+
+# ---- dropout from a counter-based generator ---------------------------------
+
+def rng_state(seed, step=0, device="cuda"):
+    """The generator's state, [seed, step] (64 bits each, the step advanced by
+    fp16_rng_advance or by a program's own arithmetic on element 1)."""
+    import torch
+    wrap = lambda v: (int(v) + (1 << 63)) % (1 << 64) - (1 << 63)
+    return torch.tensor([wrap(seed), wrap(step)], dtype=torch.int64, device=device)
+
+
+def fp16_rng_advance(rng, steps=1, stream=None) -> None:
+    _held(rng=(rng, 2))
+    _check("fp16_rng_advance", lib().fp16_rng_advance(_ptr_long(rng), int(steps) % (1 << 64),
+                                                      _stream(stream)))
+
+
+def fp16_dropout(x, residual, y, p, rng, site=0, n=None, stream=None) -> None:
+    """y = dropout of x (+ residual); the gradient is the same call on dy."""
+    if n is None:
+        n = x.numel()
+    _held(x=(x, n), residual=(residual, n), y=(y, n), rng=(rng, 2))
+    _check("fp16_dropout", lib().fp16_dropout(
+        int(n), _ptr_half(x), _ptr_half(residual), _ptr_half(y), float(p), _ptr_long(rng),
+        int(site), _stream(stream)))
+
+
+# ---- dense layers with bias, activation, dropout and residual ----------------
+
+DENSE_FWD, DENSE_BWD = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, None: 0}
+
+
+def dense_desc(tokens, inputs, outputs, act="none", drop=0.0, site=0) -> DenseDesc:
+    """act: a name ("none", "relu", "gelu", "silu") or one of the ACT_ numbers."""
+    return DenseDesc(int(tokens), int(inputs), int(outputs),
+                     act if isinstance(act, int) else _ACTS[act], float(drop), int(site))
+
+
+def fp16_dense_workspace_bytes(desc: DenseDesc, call=None) -> int:
+    """Workspace of one of the layer's calls, or (None) enough for both."""
+    calls = (DENSE_FWD, DENSE_BWD) if call is None else (int(call),)
+    return max(int(lib().fp16_dense_workspace_bytes(ctypes.byref(desc), c)) for c in calls)
+
+
+def fp16_dense_fwd(desc, x, w, bias, residual, y, z=None, rng=None, ws=None, ws_bytes=None,
+                   stream=None) -> None:
+    t, i, o = desc.tokens, desc.inputs, desc.outputs
+    _held(x=(x, t * i), w=(w, o * i), bias=(bias, o), residual=(residual, t * o), y=(y, t * o),
+          z=(z, t * o), rng=(rng, 2))
+    _check("fp16_dense_fwd", lib().fp16_dense_fwd(
+        ctypes.byref(desc), _ptr_half(x), _ptr_half(w), _ptr_half(bias), _ptr_half(residual),
+        _ptr_long(rng), _ptr_half(y), _ptr_half(z), _ptr(ws), _wsb(ws, ws_bytes),
+        _stream(stream)))
+
+
+def fp16_dense_bwd(desc, x, w, z, dy, dx, dw, dbias=None, rng=None, ws=None, ws_bytes=None,
+                   stream=None) -> None:
+    t, i, o = desc.tokens, desc.inputs, desc.outputs
+    _held(x=(x, t * i), w=(w, o * i), z=(z, t * o), dy=(dy, t * o), dx=(dx, t * i),
+          dw=(dw, o * i), dbias=(dbias, o), rng=(rng, 2))
+    _check("fp16_dense_bwd", lib().fp16_dense_bwd(
+        ctypes.byref(desc), _ptr_half(x), _ptr_half(w), _ptr_half(z), _ptr_half(dy),
+        _ptr_long(rng), _ptr_half(dx), _ptr_half(dw), _ptr_half(dbias), _ptr(ws),
+        _wsb(ws, ws_bytes), _stream(stream)))
+
+
+# ---- log probabilities -------------------------------------------------------
+
+def logprob_desc(rows, classes, stride=None, scale=1.0, top=0) -> LogprobDesc:
+    """stride: elements from row to row (None: classes); scale: one over a temperature."""
+    return LogprobDesc(int(rows), int(classes), int(classes if stride is None else stride),
+                       float(scale), int(top))
+
+
+def fp16_logprobs_workspace_bytes(desc: LogprobDesc) -> int:
+    return int(lib().fp16_logprobs_workspace_bytes(ctypes.byref(desc)))
+
+
+def fp16_logprobs(desc, z, tokens, logp, stats, top_id=None, top_logp=None, ws=None,
+                  ws_bytes=None, stream=None) -> None:
+    """logp, stats [rows][3] (largest logit, log of the sum, entropy) and the desc.top
+    most probable classes of each row."""
+    n, k = desc.rows, desc.top
+    _held(z=(z, (n - 1) * desc.stride + desc.classes), tokens=(tokens, n), logp=(logp, n),
+          stats=(stats, 3 * n), top_id=(top_id, n * k), top_logp=(top_logp, n * k))
+    _check("fp16_logprobs", lib().fp16_logprobs(
+        ctypes.byref(desc), _ptr_half(z), _ptr_int(tokens), _ptr_float(logp), _ptr_float(stats),
+        _ptr_int(top_id), _ptr_float(top_logp), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
+
+
+def fp16_logprobs_bwd(desc, z, tokens, stats, dlogp, dentropy, dz, stream=None) -> None:
+    n = desc.rows
+    size = (n - 1) * desc.stride + desc.classes
+    _held(z=(z, size), tokens=(tokens, n), stats=(stats, 3 * n), dlogp=(dlogp, n),
+          dentropy=(dentropy, n), dz=(dz, size))
+    _check("fp16_logprobs_bwd", lib().fp16_logprobs_bwd(
+        ctypes.byref(desc), _ptr_half(z), _ptr_int(tokens), _ptr_float(stats), _ptr_float(dlogp),
+        _ptr_float(dentropy), _ptr_half(dz), _stream(stream)))
 
 
 def _wsb(ws, ws_bytes):

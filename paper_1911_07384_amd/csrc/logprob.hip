@@ -1,0 +1,441 @@
+// Log probabilities of given classes, the entropy of each row's distribution and its
+// most probable classes, and the logits' gradient from the gradients of the first two.
+//
+// For a row of logits z, with m its largest and d_j = scale (z_j - m):
+//   S = sum_j exp(d_j),  T = sum_j exp(d_j) d_j
+//   logp_j = d_j - log S,  H = log S - T / S   (every term of T is <= 0: no
+//   cancellation), and, with p_j = exp(logp_j) and t the given class,
+//   dz_j = scale (dlogp ([j = t] - p_j) - dH p_j (logp_j + H)).
+// One pass over the row holds m, S and T by lane (each further group of elements may
+// raise m, which scales S and T down), and they are joined over the lanes and, where
+// few long rows are split over workgroups, over the parts.  The differences z_j - m
+// of binary16 values are taken before the scale, which keeps logits of any size.
+//
+// The most probable classes: the top-th largest of the lanes' maxima bounds the top-th
+// largest element from below, so that a second look at the row (from the caches)
+// gathers the few elements at or above it; those are ranked by counting, with the
+// value and then the lower class as the key.  Where equal values make them more than
+// kCand, the value itself is found by bisection over its 16 bits.
+
+#include "head.hpp"
+
+namespace fp16k {
+namespace {
+
+constexpr int kNT = 256, kWaves = kNT / 64, kU = 4;
+constexpr int kCand = 1024;
+constexpr int kPart = 4096, kMaxParts = 64;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFloor = -1e30f;
+
+typedef unsigned long long u64;
+
+// 16-bit keys in the order of the values: NaN above all, +0 and -0 the same, 0 below all
+__device__ __forceinline__ uint32_t value_key(uint16_t b) {
+  if ((b & 0x7FFF) > 0x7C00) return 0xFFFF;
+  if (b == 0x8000) return 0x8000;
+  return (b & 0x8000) ? (uint16_t)~b : (b | 0x8000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  const uint16_t b = (k & 0x8000) ? (uint16_t)(k ^ 0x8000) : (uint16_t)~k;
+  return k == 0xFFFF ? __builtin_nanf("") : to_f32(__builtin_bit_cast(h16, b));
+}
+__device__ __forceinline__ u64 full_key(uint32_t value, int cls) {
+  return ((u64)value << 32) | (0xFFFFFFFFu - (uint32_t)cls);
+}
+
+struct Sums {
+  float m, s, t;  // m: a binary16 value; t in units of ln 2
+};
+
+// exponent by which sums of maximum m count towards a maximum of top
+__device__ __forceinline__ float shift(float m, float top, float c) {
+  return __builtin_fmaxf((m - top) * c, kFloor);  // (the floor also where both are -inf)
+}
+__device__ __forceinline__ void rescale(Sums& a, float top, float c) {
+  const float d = shift(a.m, top, c), f = __builtin_amdgcn_exp2f(d);
+  a.t = f * (a.t + d * a.s);
+  a.s *= f;
+  a.m = top;
+}
+
+__device__ __forceinline__ V8 low8() {
+  V8 v;
+  v.u = u32x4{0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
+  return v;
+}
+__device__ __forceinline__ V8 load8_low(const h16* p, int left) {
+  if (left >= 8) return load16u(p);
+  V8 v = low8();
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) v.h[e] = p[e];
+  return v;
+}
+
+// This lane's sums over z[0 .. n).
+__device__ __forceinline__ Sums lane_sums(const h16* z, int n, float c) {
+  Sums a = {-__builtin_inff(), 0.0f, 0.0f};
+  for (int i = threadIdx.x * 8; i < n; i += kNT * 8 * kU) {
+    V8 v[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int at = i + u * kNT * 8;
+      v[u] = at < n ? load8_low(z + at, n - at) : low8();
+    }
+    half2 top = __builtin_bit_cast(half2, v[0].d[0]);
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(half2, v[u].d[k]));
+    // (a NaN is no maximum here; it reaches the sums below)
+    float m = __builtin_fmaxf(to_f32(top[0]), to_f32(top[1]));
+    m = __builtin_fmaxf(m, a.m);
+    rescale(a, m, c);
+    const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float d = (to_f32(v[u].h[k]) - base) * c;
+        const float e = __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        a.t += e * __builtin_fmaxf(d, kFloor);
+      }
+  }
+  return a;
+}
+
+// Joined over the workgroup, the same in every lane.
+__device__ __forceinline__ Sums block_sums(Sums a, float c, float (*red)[3]) {
+  float m = a.m;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, o, 64));
+  rescale(a, m, c);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    a.s += __shfl_xor(a.s, o, 64);
+    a.t += __shfl_xor(a.t, o, 64);
+  }
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[wave][0] = a.m;
+    red[wave][1] = a.s;
+    red[wave][2] = a.t;
+  }
+  __syncthreads();
+  m = red[0][0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) m = __builtin_fmaxf(m, red[w][0]);
+  Sums r = {m, 0.0f, 0.0f};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    Sums b = {red[w][0], red[w][1], red[w][2]};
+    rescale(b, m, c);
+    r.s += b.s;
+    r.t += b.t;
+  }
+  __syncthreads();
+  return r;
+}
+
+struct TopLds {
+  u64 cand[kCand];
+  u64 best[kTopMax];
+  uint32_t lane[kNT];
+  int count, scan[kWaves];
+};
+
+// A workgroup's `top` largest keys into l.best, in order, from `count` distinct ones
+// in l.cand (0s where there are fewer).
+__device__ __forceinline__ void rank_candidates(TopLds& l, int count, int top) {
+  for (int i = threadIdx.x; i < top; i += kNT) l.best[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < count; i += kNT) {
+    const u64 k = l.cand[i];
+    int r = 0;
+    for (int j = 0; j < count; ++j) r += l.cand[j] > k;
+    if (r < top) l.best[r] = k;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int block_count(int n, TopLds& l) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) l.scan[threadIdx.x >> 6] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) n += l.scan[w];
+  __syncthreads();
+  return n;
+}
+
+// The `top` largest elements of z[0 .. n), classes first + i, into l.best.  m: the
+// largest of this lane's elements.
+__device__ __forceinline__ void block_top(const h16* z, int n, int first, int top, float m,
+                                          TopLds& l) {
+  // the lanes' maxima with the lane's number as the lower key: distinct, and the one of
+  // rank top - 1 is the bound
+  const uint32_t mine =
+      (value_key(__builtin_bit_cast(uint16_t, (h16)m)) << 16) | (kNT - 1 - threadIdx.x);
+  l.lane[threadIdx.x] = mine;
+  if (threadIdx.x == 0) l.count = 0;
+  __syncthreads();
+  int r = 0;
+  for (int j = 0; j < kNT; ++j) r += l.lane[j] > mine;
+  __syncthreads();
+  if (r == top - 1) l.lane[0] = mine >> 16;
+  __syncthreads();
+  const uint32_t bound = l.lane[0];
+  for (int i = threadIdx.x * 8; i < n; i += kNT * 8) {
+    const V8 v = load8_low(z + i, n - i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t k = value_key(v.s[e]);
+      if (k >= bound && i + e < n) {
+        const int at = atomicAdd(&l.count, 1);
+        if (at < kCand) l.cand[at] = full_key(k, first + i + e);
+      }
+    }
+  }
+  __syncthreads();
+  int count = l.count;
+  __syncthreads();
+  if (count > kCand) {
+    // the largest value that `top` elements reach, bit by bit
+    uint32_t value = 0;
+    for (int b = 15; b >= 0; --b) {
+      const uint32_t up = value | (1u << b);
+      int c = 0;
+      for (int i = threadIdx.x * 8; i < n; i += kNT * 8) {
+        const V8 v = load8_low(z + i, n - i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c += value_key(v.s[e]) >= up && i + e < n;
+      }
+      if (block_count(c, l) >= top) value = up;
+    }
+    // those above it (fewer than top) ..
+    if (threadIdx.x == 0) l.count = 0;
+    __syncthreads();
+    for (int i = threadIdx.x * 8; i < n; i += kNT * 8) {
+      const V8 v = load8_low(z + i, n - i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t k = value_key(v.s[e]);
+        if (k > value && i + e < n) l.cand[atomicAdd(&l.count, 1)] = full_key(k, first + i + e);
+      }
+    }
+    __syncthreads();
+    count = l.count;
+    // .. and the first of those equal to it, in the order of the classes
+    for (int i0 = 0; i0 < n && count < top; i0 += kNT * 8) {
+      const int i = i0 + threadIdx.x * 8;
+      const V8 v = i < n ? load8_low(z + i, n - i) : low8();
+      uint32_t eq = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) eq |= (uint32_t)(value_key(v.s[e]) == value && i + e < n) << e;
+      const int mine8 = __popc(eq);
+      int before = mine8;  // inclusive, over the wave
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int other = __shfl_up(before, o, 64);
+        if ((int)(threadIdx.x & 63) >= o) before += other;
+      }
+      if ((threadIdx.x & 63) == 63) l.scan[threadIdx.x >> 6] = before;
+      __syncthreads();
+      int at = count + before - mine8, all = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < (int)(threadIdx.x >> 6)) at += l.scan[w];
+        all += l.scan[w];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if ((eq >> e) & 1) {
+          if (at < top) l.cand[at] = full_key(value, first + i + e);
+          ++at;
+        }
+      count = count + all < top ? count + all : top;
+      __syncthreads();
+    }
+  }
+  rank_candidates(l, count, top);
+}
+
+// What a row's sums and largest keys give.
+__device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums& r,
+                                       const u64* best) {
+  const bool none = r.s == 0.0f;  // every class is at -inf
+  const float log_s = logf(r.s);
+  if (threadIdx.x == 0) {
+    a.stats[3 * (int64_t)row] = r.m;
+    a.stats[3 * (int64_t)row + 1] = none ? -__builtin_inff() : log_s;
+    a.stats[3 * (int64_t)row + 2] = none ? 0.0f : log_s - kLn2 * (r.t / r.s);
+    if (a.logp) {
+      const int t = a.token[row];
+      float lp = 0.0f;
+      if (t >= a.classes)
+        lp = __builtin_nanf("");
+      else if (t >= 0)
+        lp = none ? -__builtin_inff()
+                  : (to_f32(a.z[row * a.stride + t]) - r.m) * a.scale - log_s;
+      a.logp[row] = lp;
+    }
+  }
+  for (int i = threadIdx.x; i < a.top; i += kNT) {
+    const u64 k = best[i];
+    const float v = key_value((uint32_t)(k >> 32));
+    a.top_id[(int64_t)row * a.top + i] = (int32_t)(0xFFFFFFFFu - (uint32_t)k);
+    a.top_logp[(int64_t)row * a.top + i] =
+        none ? -__builtin_inff() : (v - r.m) * a.scale - log_s;
+  }
+}
+
+// What a part of a row leaves for the join.
+__host__ __device__ inline size_t part_bytes(int top) { return 16 + (size_t)top * 8; }
+
+template <bool PARTS>
+__global__ __launch_bounds__(kNT) void logprob_kernel(const LogprobArgs a, int parts, int per) {
+  __shared__ float red[kWaves][3];
+  __shared__ TopLds l;
+  const int row = PARTS ? blockIdx.x / parts : blockIdx.x;
+  const int first = PARTS ? (blockIdx.x % parts) * per : 0;
+  const int n = PARTS && a.classes - first > per ? per : a.classes - first;
+  const h16* z = a.z + row * a.stride + first;
+  const float c = a.scale * kLog2e;
+  const Sums mine = lane_sums(z, n, c);
+  const Sums r = block_sums(mine, c, red);
+  if (a.top) block_top(z, n, first, a.top, mine.m, l);
+  if (!PARTS) {
+    finish(a, row, r, l.best);
+  } else {
+    char* to = static_cast<char*>(a.ws) + blockIdx.x * part_bytes(a.top);
+    if (threadIdx.x == 0) {
+      float* f = reinterpret_cast<float*>(to);
+      f[0] = r.m;
+      f[1] = r.s;
+      f[2] = r.t;
+    }
+    u64* k = reinterpret_cast<u64*>(to + 16);
+    for (int i = threadIdx.x; i < a.top; i += kNT) k[i] = l.best[i];
+  }
+}
+
+__global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int parts) {
+  __shared__ float red[kWaves][3];
+  __shared__ TopLds l;
+  const int row = blockIdx.x;
+  const float c = a.scale * kLog2e;
+  const char* from = static_cast<const char*>(a.ws) + (int64_t)row * parts * part_bytes(a.top);
+  Sums mine = {-__builtin_inff(), 0.0f, 0.0f};
+  if ((int)threadIdx.x < parts) {
+    const float* f = reinterpret_cast<const float*>(from + threadIdx.x * part_bytes(a.top));
+    mine = {f[0], f[1], f[2]};
+  }
+  const Sums r = block_sums(mine, c, red);
+  if (a.top) {
+    // a lane holds up to kPer of the parts' keys; as in block_top, the lanes' maxima
+    // bound what is ranked, and only `top` lanes reach the bound
+    constexpr int kPer = kMaxParts * kTopMax / kNT;
+    static_assert(kPer * kTopMax <= kCand, "candidates");
+    const int all = parts * a.top;
+    u64 key[kPer], most = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int at = i * kNT + threadIdx.x;
+      key[i] = at < all ? reinterpret_cast<const u64*>(from + (at / a.top) * part_bytes(a.top) +
+                                                       16)[at % a.top]
+                        : 0;
+      most = key[i] > most ? key[i] : most;
+    }
+    l.cand[threadIdx.x] = most;
+    if (threadIdx.x == 0) {
+      l.count = 0;
+      l.best[0] = 0;
+    }
+    __syncthreads();
+    int rank = 0;
+    for (int j = 0; j < kNT; ++j) rank += l.cand[j] > most;
+    if (rank == a.top - 1 && most) l.best[0] = most;  // (lanes without keys share 0)
+    __syncthreads();
+    const u64 bound = l.best[0];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (key[i] && key[i] >= bound) {
+        const int at = atomicAdd(&l.count, 1);
+        if (at < kCand) l.cand[at] = key[i];
+      }
+    __syncthreads();
+    rank_candidates(l, l.count < kCand ? l.count : kCand, a.top);
+  }
+  finish(a, row, r, l.best);
+}
+
+// The gradient: each lane 8 classes of a row at a time.
+__global__ __launch_bounds__(kNT) void logprob_bwd_kernel(const LogprobArgs a, int parts, int per) {
+  const int row = blockIdx.x / parts, first = (blockIdx.x % parts) * per;
+  const int end = a.classes - first > per ? first + per : a.classes;
+  const float m = a.stats[3 * (int64_t)row], log_s = a.stats[3 * (int64_t)row + 1],
+              h = a.stats[3 * (int64_t)row + 2];
+  const int t = a.token ? a.token[row] : -1;
+  const float dl = a.dlogp && t >= 0 ? a.dlogp[row] : 0.0f;
+  const float dh = a.dentropy ? a.dentropy[row] : 0.0f;
+  const bool none = m == -__builtin_inff() && log_s == -__builtin_inff();
+  const h16* z = a.z + row * a.stride;
+  h16* dz = a.dz + row * a.stride;
+  for (int i = first + threadIdx.x * 8; i < end; i += kNT * 8) {
+    const V8 v = load8_upto(z + i, end - i);
+    V8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float lp = (to_f32(v.h[e]) - m) * a.scale - log_s;
+      const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+      float g = -(dl + dh * (__builtin_fmaxf(lp, kFloor) + h)) * p;
+      if (i + e == t) g += dl;
+      o.h[e] = to_h16(none ? 0.0f : g * a.scale);
+    }
+    store8_upto(dz + i, o, end - i);
+  }
+}
+
+// Parts of a row: as many as fill the device, of kPart classes at least.
+int row_parts(int rows, int classes) {
+  const int fill = (512 + rows - 1) / rows, most = (classes + kPart - 1) / kPart;
+  const int parts = fill < most ? fill : most;
+  return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : parts;
+}
+int part_len(int classes, int parts) { return ((classes + parts - 1) / parts + 7) & ~7; }
+
+}  // namespace
+
+size_t logprob_ws_bytes(int rows, int classes, int top) {
+  const int parts = row_parts(rows, classes);
+  return parts == 1 ? 0 : (size_t)rows * parts * part_bytes(top);
+}
+
+hipError_t launch_logprob(const LogprobArgs& a, hipStream_t st) {
+  int parts = row_parts(a.rows, a.classes);
+  if (parts == 1) {
+    logprob_kernel<false><<<a.rows, kNT, 0, st>>>(a, 1, a.classes);
+    return hipGetLastError();
+  }
+  const int per = part_len(a.classes, parts);
+  parts = (a.classes + per - 1) / per;  // (none is empty)
+  logprob_kernel<true><<<(unsigned)((int64_t)a.rows * parts), kNT, 0, st>>>(a, parts, per);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  logprob_join<<<a.rows, kNT, 0, st>>>(a, parts);
+  return hipGetLastError();
+}
+
+hipError_t launch_logprob_bwd(const LogprobArgs& a, hipStream_t st) {
+  const int per = 8 * kNT * 4, parts = (a.classes + per - 1) / per;
+  logprob_bwd_kernel<<<(unsigned)((int64_t)a.rows * parts), kNT, 0, st>>>(a, parts, per);
+  return hipGetLastError();
+}
+
+}  // namespace fp16k

@@ -1,0 +1,222 @@
+"""GPU parity of dense layers with their epilogue, and of their gradients, with the
+definition in 64 bits; the bounds are derived in head_oracle.Dense."""
+
+import numpy as np
+import pytest
+import torch
+
+import head_oracle as O
+import paper_1911_07384_amd as F
+from gpu_util import dev, host, note, require_gpu
+
+pytestmark = pytest.mark.gpu
+
+RNG = (1234567890123, 1 << 33)
+SITE = 6
+
+
+def half(r, *s, std=1.0):
+    return (std * r.standard_normal(s)).astype(np.float16)
+
+
+class Case:
+    def __init__(self, tokens, inputs, outputs, act="none", p=0.0, bias=True, residual=True, seed=0):
+        r = np.random.default_rng(seed + tokens * 3 + inputs * 5 + outputs)
+        self.d = F.dense_desc(tokens, inputs, outputs, act, p, SITE)
+        self.act, self.p = act, p
+        self.x = half(r, tokens, inputs)
+        self.w = half(r, outputs, inputs, std=inputs ** -0.5)
+        self.bias = half(r, outputs, std=0.3) if bias else None
+        self.residual = half(r, tokens, outputs) if residual else None
+        self.z = half(r, tokens, outputs)
+        self.dy = half(r, tokens, outputs, std=0.1)
+        self.label = f"{tokens}x{inputs}x{outputs} {act} p={p} bias={bias} residual={residual}"
+
+    def ws(self, call):
+        # poisoned: what is not written must not be read
+        t = F.workspace(F.fp16_dense_workspace_bytes(self.d, call))
+        return t.fill_(255)
+
+    def forward(self, keep_z=True, inplace=False):
+        require_gpu()
+        t, o = self.d.tokens, self.d.outputs
+        g = lambda a: None if a is None else dev(a)
+        res = g(self.residual)
+        full = torch.full((t * o + 64,), 5.0, dtype=torch.float16, device="cuda")
+        y = res if inplace else full[:t * o].view(t, o)
+        z = torch.full_like(y, 9.0) if keep_z else None
+        note(f"[gpu] dense fwd {self.label}")
+        F.fp16_dense_fwd(self.d, dev(self.x), dev(self.w), g(self.bias), res, y, z,
+                         rng=F.rng_state(*RNG), ws=self.ws(F.DENSE_FWD))
+        torch.cuda.synchronize()
+        assert bool((full[t * o:] == 5.0).all())
+        return host(y), None if z is None else host(z)
+
+    def backward(self, dx=True, dw=True, db=True):
+        require_gpu()
+        t, i, o = self.d.tokens, self.d.inputs, self.d.outputs
+        new = lambda on, *s: torch.full(s, 5.0, dtype=torch.float16, device="cuda") if on else None
+        out = [new(dx, t, i), new(dw, o, i), new(db, o)]
+        note(f"[gpu] dense bwd {self.label}")
+        F.fp16_dense_bwd(self.d, dev(self.x), dev(self.w), dev(self.z), dev(self.dy), *out,
+                         rng=F.rng_state(*RNG), ws=self.ws(F.DENSE_BWD))
+        torch.cuda.synchronize()
+        return [None if v is None else host(v) for v in out]
+
+    def want(self):
+        return O.Dense(self.x, self.w, self.bias, self.residual, self.act, self.p, RNG, SITE,
+                       self.z, self.dy)
+
+    def check(self):
+        w = self.want()
+        y, z = self.forward()
+        O.close(y, w.y, w.y_err, f"y {self.label}")
+        O.close(z, w.z, w.z_err, f"z {self.label}")
+        dx, dw, db = self.backward()
+        O.close(dx, w.dx, w.dx_err, f"dx {self.label}")
+        O.close(dw, w.dw, w.dw_err, f"dw {self.label}")
+        O.close(db, w.db, w.db_err, f"dbias {self.label}")
+        # and on the whole no worse than the roundings that are declared
+        rms = lambda g, v: float((torch.from_numpy(g).double() - v).square().mean().sqrt()
+                                 / max(float(v.square().mean().sqrt()), 1e-30))
+        if y.size > 4000:
+            assert rms(y, w.y) < O.HALF and rms(dx, w.dx) < 2 * O.HALF and rms(dw, w.dw) < 2 * O.HALF
+
+
+SIZES = [(1, 1, 1), (1, 2, 3), (2, 8, 8), (3, 5, 7), (1, 2048, 1000), (5, 100, 33), (13, 64, 40),
+         (16, 512, 16), (17, 33, 65), (24, 4096, 72), (32, 40, 300), (33, 7, 129), (64, 64, 64),
+         (65, 65, 65), (100, 129, 31), (130, 72, 200), (128, 256, 1000), (257, 40, 513),
+         (1111, 37, 24), (200, 1337, 300), (9, 4111, 520)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("act,p", [("none", 0.0), ("gelu", 0.1)])
+def test_sizes(size, act, p):
+    Case(*size, act=act, p=p).check()
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("p", [0.0, 0.5])
+@pytest.mark.parametrize("bias,residual", [(False, False), (True, False), (False, True)])
+def test_epilogues(act, p, bias, residual):
+    for size in [(3, 96, 45), (70, 50, 90)]:
+        Case(*size, act=act, p=p, bias=bias, residual=residual).check()
+
+
+@pytest.mark.parametrize("size", [(1, 64, 48), (70, 64, 130), (300, 136, 520)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_residual_in_place_and_no_z(size):
+    c = Case(*size, act="silu", p=0.2)
+    y, z = c.forward()
+    y2, z2 = c.forward(keep_z=False, inplace=True)
+    assert z2 is None and np.array_equal(y, y2)
+
+
+def test_parts_of_the_gradients():
+    for size in [(40, 72, 56), (40, 71, 57)]:
+        c = Case(*size, act="gelu", p=0.1)
+        whole = c.backward()
+        for k in range(1, 8):
+            on = [bool(k & 1), bool(k & 2), bool(k & 4)]
+            for a, b, want in zip(c.backward(*on), whole, on):
+                assert (a is None) != want and (a is None or np.array_equal(a, b))
+        c = Case(*size)
+        whole = c.backward()
+        for a, b in zip(c.backward(True, False, True), whole):
+            assert a is None or np.array_equal(a, b)
+
+
+def test_all_dropped():
+    c = Case(20, 40, 64, act="relu", p=1.0)
+    y, _ = c.forward()
+    assert np.array_equal(y, c.residual)
+    dx, dw, db = c.backward()
+    assert not dx.any() and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+def test_activations_over_all_values(act):
+    """Every finite binary16 value through an identity, and its slope."""
+    v = np.arange(0x7C00, dtype=np.uint16).view(np.float16)
+    v = np.concatenate([v, -v])
+    v = np.concatenate([v, np.zeros(-v.size % 64, np.float16)]).reshape(-1, 64)
+    c = Case(v.shape[0], 64, 64, act=act, bias=False, residual=False)
+    c.x, c.w = v, np.eye(64, dtype=np.float16)
+    c.z, c.dy = v, np.ones_like(v)
+    y, z = c.forward()
+    assert np.array_equal(z, v + np.float16(0)) or np.array_equal(np.abs(z), np.abs(v))
+    V = O.t64(v)
+    want = O.activate(V, act)
+    err = O.Dense.EPS * want.abs()
+    O.close(y, want, err + O.HALF * (want.abs() + err) + O.TINY, act)
+    dx, _, _ = c.backward()
+    s = O.slope(V, act)
+    err = O.Dense.EPS * torch.ones_like(s)
+    O.close(dx, s, err + O.HALF * (s.abs() + err) + O.TINY, act + " slope")
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("size", [(5, 64, 40), (90, 64, 72)], ids=lambda s: "x".join(map(str, s)))
+def test_values_that_are_not_finite(act, size):
+    c = Case(*size, act=act, residual=False)
+    c.w = np.abs(c.w) + np.float16(0.01)  # (an infinity keeps its sign)
+    c.x[0, 3], c.x[1, 2], c.x[2, 1] = np.nan, np.inf, -np.inf
+    y, z = c.forward()
+    assert np.isnan(y[0]).all() and np.isnan(z[0]).all()
+    assert np.isposinf(y[1]).all() and np.isposinf(z[1]).all() and np.isneginf(z[2]).all()
+    assert np.isneginf(y[2]).all() if act == "none" else (y[2] == 0).all()
+    assert np.isfinite(y[3:]).all()
+    c.z[0, 0], c.z[1, 1], c.z[2, 2] = np.nan, np.inf, -np.inf
+    c.x = np.nan_to_num(c.x, nan=0.0, posinf=1.0, neginf=1.0)
+    dx, dw, db = c.backward()
+    if act == "none":
+        assert np.isfinite(dx).all()
+    else:
+        assert np.isnan(dx[0]).all() and np.isfinite(dx[1:]).all()
+        assert np.isnan(dw[0]).all() and np.isfinite(dw[1:]).all()
+        assert np.isnan(db[0]) and np.isfinite(db[1:]).all()
+
+
+def test_overflow_rounds_to_infinity():
+    c = Case(30, 64, 40, bias=False, residual=False)
+    c.x[:], c.w[:] = 300.0, 10.0  # 192000
+    c.w[0] = -10.0
+    y, _ = c.forward()
+    assert np.isneginf(y[:, 0]).all() and np.isposinf(y[:, 1:]).all()
+
+
+def test_same_bits_every_time():
+    for size in [(3, 300, 50), (200, 520, 264)]:
+        c = Case(*size, act="gelu", p=0.1)
+        y, z = c.forward()
+        g = c.backward()
+        for _ in range(3):
+            y2, z2 = c.forward()
+            assert np.array_equal(y, y2) and np.array_equal(z, z2)
+            assert all(np.array_equal(a, b) for a, b in zip(g, c.backward()))
+
+
+def test_gradients_against_differences():
+    """The loss sum(y dy) along a direction of x, of W and of the bias, from the kernel's
+    own forward (smooth activations; y without a rounding that matters: large steps)."""
+    c = Case(6, 24, 20, act="silu", p=0.25, residual=False)
+    _, c.z = c.forward()
+    dx, dw, db = (g.astype(np.float64) for g in c.backward())
+    r = np.random.default_rng(0)
+    for name, g in [("x", dx), ("w", dw), ("bias", db)]:
+        at = getattr(c, name)
+        dirn = r.choice([-1.0, 1.0], at.shape)
+        h = 2.0 ** -4
+        loss = []
+        for s in (1, -1):
+            setattr(c, name, (at.astype(np.float64) + s * h * dirn).astype(np.float16))
+            moved = getattr(c, name).astype(np.float64)
+            loss.append((c.forward()[0].astype(np.float64) * c.dy.astype(np.float64)).sum())
+            if s == 1:
+                up = moved
+        num = (loss[0] - loss[1])
+        exact = (g * (up - moved)).sum()
+        setattr(c, name, at)
+        # each y is off by 2^-11 of itself, the third order by h^2 / 6 of a slope's change
+        scale = np.abs(c.dy.astype(np.float64)).sum() * 2
+        assert abs(num - exact) < scale * 2.0 ** -10 + 0.1 * abs(exact) + 0.02 * np.abs(g).sum() * h
