@@ -2,216 +2,534 @@
 // gradients of x, W and bias.
 //
 //   forward   z = x W^T + bias       rows of both operands run along the reduction
-//   dx        dz W                   W's columns do
-//   dW        dz^T x                 both operands' columns do
+//   dx        dz W                   W lies along its rows (see NtTile)
+//   dW        dz^T x                 both operands do
 //   with dz = drop(dy) act'(z), a pass over the elements that also sums its columns for
 //   dbias.
+//
+// Tile rows p run along the output's rows in memory, tile columns q are its rows.
 
+#include "gemm_nt.hpp"
 #include "head.hpp"
+
+#include <type_traits>
 
 namespace fp16k {
 namespace {
 
 // ---- activations -------------------------------------------------------------------
 
-// (Past these the values are their limits: -0 and z, slopes 0 and 1; the formulas would
-// multiply an infinity by 0.)
-__device__ __forceinline__ float act_value(int act, float z) {
-  if (act == kActRelu) return relu_keep_nan(z);
-  if (act == kActGelu) return z < -15.0f ? -0.0f : 0.5f * z * erfcf(z * -0.70710678f);
-  if (act == kActSilu) return z < -110.0f ? -0.0f : z / (1.0f + expf(-z));
+// Phi(-u) exp(u^2 / 2) for u >= 0: a polynomial of t = 1 / (1 + 0.3 u) whose largest
+// relative error on [0, 6.2] is 2^-19 (least squares reweighted towards the largest
+// error, in 64 bits); past 6.2 u Phi(-u) is below binary16's smallest.  erfcf takes
+// about three times the instructions, a quarter of a 4096-deep product's time.
+__device__ __forceinline__ float normal_tail(float u) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, u, 1.0f));
+  float g = -0.08251488231f;
+  g = __builtin_fmaf(g, t, 0.23263196995f);
+  g = __builtin_fmaf(g, t, -0.03640279134f);
+  g = __builtin_fmaf(g, t, 0.15505104012f);
+  g = __builtin_fmaf(g, t, 0.11087362581f);
+  g = __builtin_fmaf(g, t, 0.12036026875f);
+  return g * t;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
+// GELU z Phi(z) = max(z, 0) - |z| Phi(-|z|), whose terms do not cancel.  An infinity
+// times 0 is kept out: the limits are -0 and z.
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+  if (ACT == kActRelu) return relu_keep_nan(z);
+  if (ACT == kActGelu) {
+    const float u = __builtin_fabsf(z);
+    const float e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+    const float tail = u * e * normal_tail(u);
+    const float top = z > 0.0f ? z : 0.0f;
+    return u > 15.0f ? top : top - tail;
+  }
+  if (ACT == kActSilu) {
+    const float v = z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2e));
+    return z < -110.0f ? 0.0f : v;
+  }
   return z;
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
-  if (act == kActRelu) return z > 0.0f ? 1.0f : __builtin_isnan(z) ? z : 0.0f;
-  if (act == kActGelu) {
-    if (__builtin_fabsf(z) > 15.0f) return z > 0.0f ? 1.0f : 0.0f;
-    return 0.5f * erfcf(z * -0.70710678f) + z * (0.39894228f * expf(-0.5f * z * z));
+// .. and the slopes, Phi(z) + z phi(z) with 1 - Phi(-z) for positive z, and
+// s (1 + z (1 - s)).
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if (ACT == kActRelu) return z > 0.0f ? 1.0f : __builtin_isnan(z) ? z : 0.0f;
+  if (ACT == kActGelu) {
+    const float u = __builtin_fabsf(z);
+    const float e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+    const float h = e * __builtin_fmaf(u, -0.3989422804f, normal_tail(u));
+    const float s = z > 0.0f ? 1.0f - h : h;
+    return u > 15.0f ? (z > 0.0f ? 1.0f : 0.0f) : s;
   }
-  if (act == kActSilu) {
-    if (__builtin_fabsf(z) > 110.0f) return z > 0.0f ? 1.0f : 0.0f;
-    const float s = 1.0f / (1.0f + expf(-z));
-    return s * (1.0f + z * (1.0f - s));
+  if (ACT == kActSilu) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2e));
+    const float v = s * __builtin_fmaf(z, 1.0f - s, 1.0f);
+    return __builtin_fabsf(z) > 110.0f ? (z > 0.0f ? 1.0f : 0.0f) : v;
   }
   return 1.0f;
 }
 
-// ---- the product -------------------------------------------------------------------
+// Eight elements from element i on (any i) under the dropout's mask.
+__device__ __forceinline__ void drop8(float (&v)[8], int64_t i, const Drop& d) {
+  const uint64_t seed = d.state[0], step = d.state[1];
+  const uint32_t g = (uint32_t)(i >> 3);
+  const int s = (int)(i & 7);
+  PhiloxBlock b = philox(g, d.site, step, seed);
+  if (s) {  // the words s .. 7 of one block and 0 .. s - 1 of the next
+    const PhiloxBlock n = philox(g + 1, d.site, step, seed);
+    const uint32_t w[8] = {b.w[0], b.w[1], b.w[2], b.w[3], n.w[0], n.w[1], n.w[2], n.w[3]};
+    uint32_t h[5];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      const uint32_t w0 = w[k], w1 = w[k + 1], w2 = w[k + 2], w3 = w[k + 3 < 8 ? k + 3 : 7];
+      const uint32_t x = s & 4 ? w2 : w0, y = s & 4 ? w3 : w1;
+      h[k] = s & 2 ? y : x;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      b.w[k] = s & 1 ? __builtin_amdgcn_alignbit(h[k + 1], h[k], 16) : h[k];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = kept(b, e, d.threshold) ? v[e] * d.scale : 0.0f;
+}
 
-// D[q][p] = sum_k P(p, k) Q(q, k), P(p, k) = P[p * ldp + k], or P[k * ldp + p] with PS
-// (likewise Q), D's rows ldd apart.
+// ---- what a tile stores (see nt_store) -----------------------------------------------
+
+// Rounded, [q][p].
+struct HalfEpi {
+  h16* d;
+  int np, nq;
+  static constexpr int OUTS = 1;
+  static constexpr bool DIAGONAL = false;
+  struct Pre {};
+  __device__ __forceinline__ Pre load(int, int) const { return {}; }
+  __device__ __forceinline__ void compute(int, int, const float (&v)[8], const Pre&,
+                                          V8 (&out)[1]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) out[0].h[k] = to_h16(v[k]);
+  }
+  __device__ __forceinline__ void store(int p, int q, const V8 (&out)[1]) const {
+    if (p < np && q < nq) store8_upto(d + (int64_t)q * np + p, out[0], np - p);
+  }
+};
+
+// The float32 sums of one part of a reduction, [q][p] with rows of whole eights.
+struct PartEpi {
+  float* d;
+  int np, nq, ld;
+  static constexpr int OUTS = 2;
+  static constexpr bool DIAGONAL = false;
+  struct Pre {};
+  __device__ __forceinline__ Pre load(int, int) const { return {}; }
+  __device__ __forceinline__ void compute(int, int, const float (&v)[8], const Pre&,
+                                          V8 (&out)[2]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) out[k / 4].d[k % 4] = __builtin_bit_cast(uint32_t, v[k]);
+  }
+  __device__ __forceinline__ void store(int p, int q, const V8 (&out)[2]) const {
+    if (p < np && q < nq) {
+      float* to = d + (int64_t)q * ld + p;
+      store16(to, out[0]);
+      store16(to + 4, out[1]);
+    }
+  }
+};
+
+// The layer's outputs.
+template <int ACT>
+struct LayerEpi {
+  const h16 *bias, *residual;
+  h16 *y, *z;
+  int np, nq;
+  Drop drop;
+  static constexpr int OUTS = 2;
+  static constexpr bool DIAGONAL = false;
+  struct Pre {
+    V8 bias, residual;
+  };
+  __device__ __forceinline__ Pre load(int p, int q) const {
+    Pre r;
+    r.bias = r.residual = zero8();
+    if (p < np && q < nq) {
+      if (bias) r.bias = load8_upto(bias + p, np - p);
+      if (residual) r.residual = load8_upto(residual + (int64_t)q * np + p, np - p);
+    }
+    return r;
+  }
+  __device__ __forceinline__ void compute(int p, int q, const float (&sum)[8], const Pre& pre,
+                                          V8 (&out)[2]) const {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      v[k] = sum[k] + to_f32(pre.bias.h[k]);
+      out[1].h[k] = to_h16(v[k]);
+      v[k] = act_value<ACT>(v[k]);
+    }
+    if (drop.threshold) drop8(v, (int64_t)q * np + p, drop);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) out[0].h[k] = to_h16(v[k] + to_f32(pre.residual.h[k]));
+  }
+  __device__ __forceinline__ void store(int p, int q, const V8 (&out)[2]) const {
+    if (p < np && q < nq) {
+      const int64_t i = (int64_t)q * np + p;
+      store8_upto(y + i, out[0], np - p);
+      if (z) store8_upto(z + i, out[1], np - p);
+    }
+  }
+};
+
+// ---- the product -----------------------------------------------------------------------
+
+// D[q][p] = sum_k P(p, k) Q(q, k), the operands' rows ldp and ldq elements apart,
+// multiples of 8: P[p * ldp + k], or P[k * ldp + p] along its rows; likewise Q.
 struct Product {
   const h16 *p, *q;
   int64_t ldp, ldq;
   int np, nq, nk;
+  int parts;
 };
 
-struct ToHalf {  // rounded and stored
-  h16* d;
-  int64_t ldd;
-  __device__ __forceinline__ void operator()(int p, int q, float v) const {
-    d[q * ldd + p] = to_h16(v);
-  }
-};
-
-struct Forward {
-  const h16 *bias, *residual;
-  h16 *y, *z;
-  int64_t ldd;
-  int act;
-  Drop drop;
-  __device__ __forceinline__ void operator()(int p, int q, float v) const {
-    if (bias) v = v + to_f32(bias[p]);
-    const int64_t i = q * ldd + p;
-    if (z) z[i] = to_h16(v);
-    v = act_value(act, v);
-    if (drop.threshold) {
-      const PhiloxBlock b = philox((uint32_t)(i >> 3), drop.site, drop.state[1], drop.state[0]);
-      v = kept(b, (int)(i & 7), drop.threshold) ? v * drop.scale : 0.0f;
-    }
-    if (residual) v = v + to_f32(residual[i]);
-    y[i] = to_h16(v);
-  }
-};
-
-constexpr int kSide = 64, kDeep = 32, kLd = kDeep + 8;
-
-// A tile's 64 rows x 32 of one operand into LDS, [row][k], zeros past its ends.
-template <bool S>
-__device__ __forceinline__ void stage(h16* to, const h16* m, int64_t ld, int r0, int rows, int k0,
-                                      int nk) {
-  const int t = threadIdx.x;
-  if (!S) {
-    const int r = t >> 2, k = (t & 3) * 8;
-    const V8 v = r0 + r < rows && k0 + k < nk ? load8_upto(m + (r0 + r) * ld + k0 + k, nk - k0 - k)
-                                              : zero8();
-    store16(to + r * kLd + k, v);
-  } else {
-    const int k = t >> 3, r = (t & 7) * 8;
-    const V8 v = k0 + k < nk && r0 + r < rows ? load8_upto(m + (k0 + k) * ld + r0 + r, rows - r0 - r)
-                                              : zero8();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) to[(r + e) * kLd + k] = v.h[e];
-  }
+// Tiles in groups of 8 tile columns, within a group column by column: the 32 tiles that
+// an XCD holds at a time share 8 + 4 tiles' rows in its L2.
+template <class C, class Epi>
+__global__ __launch_bounds__(C::THREADS, (C::OCC * C::WAVES + 3) / 4) void dense_product(const Product a, Epi epi) {
+  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, 1>::LDS];
+  const int tp = (a.np + C::BP - 1) / C::BP, tq = (a.nq + C::BQ - 1) / C::BQ;
+  const int all = tp * tq * a.parts;
+  int t = nt_xcd(blockIdx.x, all);
+  if (t >= all) return;
+  const int part = t / (tp * tq);
+  t -= part * tp * tq;
+  const int g = t / (8 * tp), w = t - g * 8 * tp;
+  const int gw = tq - 8 * g < 8 ? tq - 8 * g : 8;
+  const int p0 = (w / gw) * C::BP, q0 = (8 * g + w % gw) * C::BQ;
+  NtTile nt;
+  nt.ldp = (uint32_t)(a.ldp * 2);
+  nt.ldq = (uint32_t)(a.ldq * 2);
+  nt.p[0] = nt.p[1] = a.p + (C::PS ? (int64_t)p0 : p0 * a.ldp);
+  nt.q[0] = nt.q[1] = a.q + (C::QS ? (int64_t)q0 : q0 * a.ldq);
+  nt.prows = a.np - p0;
+  nt.qrows = a.nq - q0;
+  nt.kbytes = a.nk * 2;
+  nt.part = part;
+  nt.parts = a.parts;
+  floatx16 acc[C::TP][C::TQ];
+  nt_product<NtHalf, C>(nt, lds, acc);
+  if constexpr (std::is_same<Epi, PartEpi>::value) epi.d += (int64_t)part * epi.nq * epi.ld;
+  const int wave = threadIdx.x >> 6;
+  h16* none[1] = {nullptr};
+  nt_store<C, 1>(acc, lds, p0 + (wave / C::WQ) * 32 * C::TP, q0 + (wave % C::WQ) * 32 * C::TQ, a.np,
+                 a.nq, false, none, 0, epi);
 }
 
-template <bool PS, bool QS, class Epi>
-__global__ __launch_bounds__(256) void product_kernel(const Product a, const Epi epi) {
-  __shared__ __attribute__((aligned(16))) h16 lp[kSide * kLd], lq[kSide * kLd];
-  const int tp = (a.np + kSide - 1) / kSide;
-  const int p0 = (blockIdx.x % tp) * kSide, q0 = (blockIdx.x / tp) * kSide;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int lrow = lane & 31, lhi = lane >> 5, wp = (wave & 1) * 32, wq = (wave >> 1) * 32;
-  floatx16 acc;
+// The parts' sums added in their order, and the product's epilogue.
+template <class Epi>
+__global__ __launch_bounds__(256) void dense_join(const float* from, int parts, int np, int nq,
+                                                  int ld, const Epi epi) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per = ld / 8, q = (int)(i / per), p = (int)(i - (int64_t)q * per) * 8;
+  if (q >= nq) return;
+  const typename Epi::Pre pre = epi.load(p, q);
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const float* f = from + (int64_t)q * ld + p;
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s, f += (int64_t)nq * ld) {
+    const floatx4 x = reinterpret_cast<const floatx4*>(f)[0];
+    const floatx4 y = reinterpret_cast<const floatx4*>(f)[1];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-  for (int k0 = 0; k0 < a.nk; k0 += kDeep) {
-    stage<PS>(lp, a.p, a.ldp, p0, a.np, k0, a.nk);
-    stage<QS>(lq, a.q, a.ldq, q0, a.nq, k0, a.nk);
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const V8 fp = load16(lp + (wp + lrow) * kLd + s * 16 + lhi * 8);
-      const V8 fq = load16(lq + (wq + lrow) * kLd + s * 16 + lhi * 8);
-      acc = mfma32x32x16(fp.h, fq.h, acc);
+    for (int k = 0; k < 4; ++k) {
+      v[k] += x[k];
+      v[4 + k] += y[k];
     }
-    __syncthreads();
   }
-  const int q = q0 + wq + lrow;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int p = p0 + wp + 8 * (e >> 2) + 4 * lhi + (e & 3);
-    if (p < a.np && q < a.nq) epi(p, q, acc[e]);
-  }
+  V8 out[Epi::OUTS];
+  epi.compute(p, q, v, pre, out);
+  epi.store(p, q, out);
 }
 
-template <bool PS, bool QS, class Epi>
-hipError_t launch_product(const Product& a, const Epi& epi, hipStream_t st) {
-  const int64_t tiles = ceil_div64(a.np, kSide) * ceil_div64(a.nq, kSide);
-  product_kernel<PS, QS><<<(unsigned)tiles, 256, 0, st>>>(a, epi);
+enum Layout { kForward, kDx, kDw };  // which operands lie along their rows: none, P, both
+
+template <Layout L, int WP, int WQ, int TP, int TQ, int S, int OCC>
+using Cfg = NtCfg<WP, WQ, TP, TQ, 128, S, OCC, 1, L != kForward, L == kDw>;
+
+//                            waves  tile  stages  workgroups a CU
+template <Layout L> using Cfg256 = Cfg<L, 4, 2, 2, 4, 2, 1>;  // 256 x 256
+template <Layout L> using Cfg128 = Cfg<L, 2, 2, 2, 2, 2, 2>;  // 128 x 128
+template <Layout L> using Cfg32 = Cfg<L, 2, 1, 2, 1, 4, 2>;   // 128 x 32: few tokens
+
+template <class C, class Epi>
+hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {
+  const int64_t all = ceil_div64(a.np, C::BP) * ceil_div64(a.nq, C::BQ) * a.parts;
+  const unsigned grid = (unsigned)(8 * ceil_div64(all, 8));
+  if (a.parts == 1) {
+    dense_product<C><<<grid, C::THREADS, 0, st>>>(a, epi);
+    return hipGetLastError();
+  }
+  const int ld = (a.np + 7) & ~7;
+  dense_product<C><<<grid, C::THREADS, 0, st>>>(a, PartEpi{sums, a.np, a.nq, ld});
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  dense_join<<<(unsigned)ceil_div64((int64_t)a.nq * (ld / 8), 256), 256, 0, st>>>(
+      sums, a.parts, a.np, a.nq, ld, epi);
   return hipGetLastError();
 }
 
-// ---- dz and dbias --------------------------------------------------------------------
-
-constexpr int kRows = 64;  // of a workgroup's partial sums
-
-// dz (unless null) and its columns' sums over kRows rows (unless null), 256 columns a
-// workgroup.
-__global__ __launch_bounds__(256) void dz_kernel(int tokens, int outputs, int act, Drop drop,
-                                                 const h16* z, const h16* dy, h16* dz, float* part) {
-  const int c = blockIdx.x * 256 + threadIdx.x, r0 = blockIdx.y * kRows;
-  if (c >= outputs) return;
-  float sum = 0.0f;
-  for (int r = r0; r < r0 + kRows && r < tokens; ++r) {
-    const int64_t i = (int64_t)r * outputs + c;
-    float v = to_f32(dy[i]);
-    if (drop.threshold) {
-      const PhiloxBlock b = philox((uint32_t)(i >> 3), drop.site, drop.state[1], drop.state[0]);
-      v = kept(b, (int)(i & 7), drop.threshold) ? v * drop.scale : 0.0f;
-    }
-    if (act != kActNone) v *= act_slope(act, to_f32(z[i]));
-    if (dz) dz[i] = to_h16(v);
-    sum += v;
+// The tile a product runs on, and the parts its reduction is split into: enough
+// workgroups for every CU, of four slices of 64 at least.
+struct Choice {
+  int side, parts;
+};
+Choice choose(Layout l, int64_t np, int64_t nq, int64_t nk) {
+  Choice c;
+  const int64_t big = ceil_div64(np, 256) * ceil_div64(nq, 256);
+  int64_t tiles;
+  if (l != kDw && nq <= 32) {
+    c.side = 32;
+    tiles = ceil_div64(np, 128) * ceil_div64(nq, 32);
+  } else if (big >= 192) {
+    c.side = 256;
+    tiles = big;
+  } else {
+    c.side = 128;
+    tiles = ceil_div64(np, 128) * ceil_div64(nq, 128);
   }
-  if (part) part[(int64_t)blockIdx.y * outputs + c] = sum;
+  const int64_t slices = ceil_div64(nk, 64), fill = (c.side == 256 ? 256 : 512) / tiles;
+  int64_t parts = fill < slices / 4 ? fill : slices / 4;
+  parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
+  // (whole slices a part, none without)
+  c.parts = (int)ceil_div64(slices, ceil_div64(slices, parts));
+  return c;
 }
 
+size_t sums_bytes(const Choice& c, int64_t np, int64_t nq) {
+  return c.parts == 1 ? 0 : (size_t)c.parts * nq * ((np + 7) & ~(int64_t)7) * sizeof(float);
+}
+
+template <Layout L, class Epi>
+hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st) {
+  const Choice c = choose(L, a.np, a.nq, a.nk);
+  a.parts = c.parts;
+  float* f = static_cast<float*>(sums);
+  if constexpr (L != kDw)
+    if (c.side == 32) return run<Cfg32<L>>(a, epi, f, st);
+  if (c.side == 256) return run<Cfg256<L>>(a, epi, f, st);
+  return run<Cfg128<L>>(a, epi, f, st);
+}
+
+// ---- rows laid out anew ------------------------------------------------------------------
+
+// Rows whose length is no multiple of 8, to rows that are, zeros behind them.
+__global__ __launch_bounds__(256) void repack_kernel(int rows, int cols, int ld, const h16* from,
+                                                     h16* to) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per = ld / 8;
+  const int64_t r = i / per;
+  const int c = (int)(i - r * per) * 8;
+  if (r < rows) store16(to + r * ld + c, load8_row(from + r * cols, c, cols, true));
+}
+hipError_t launch_repack(int rows, int cols, const h16* from, h16* to, hipStream_t st) {
+  const int ld = (cols + 7) & ~7;
+  repack_kernel<<<(unsigned)ceil_div64((int64_t)rows * (ld / 8), 256), 256, 0, st>>>(rows, cols, ld,
+                                                                                 from, to);
+  return hipGetLastError();
+}
+
+// ---- dz and dbias --------------------------------------------------------------------------
+
+constexpr int kRows = 32;  // of a workgroup's partial sums
+
+// dz [tokens][ld] (unless null) with zeros past its columns, and its columns' sums over
+// kRows rows (unless null): 256 columns a workgroup, a lane 8 of them in every eighth
+// row.
+template <int ACT>
+__global__ __launch_bounds__(256) void dz_kernel(int tokens, int outputs, int ld, Drop drop,
+                                                 const h16* z, const h16* dy, h16* dz,
+                                                 float* part) {
+  __shared__ float sums[8][256];
+  const int cg = threadIdx.x & 31, rg = threadIdx.x >> 5;
+  const int c = blockIdx.x * 256 + cg * 8, r0 = blockIdx.y * kRows;
+  constexpr int U = kRows / 8;
+  V8 vy[U], vz[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = r0 + rg + 8 * u;
+    const int64_t row = (int64_t)(r < tokens ? r : 0) * outputs;
+    vy[u] = load8_row(dy + row, c, outputs, r < tokens);
+    if (ACT != kActNone) vz[u] = load8_row(z + row, c, outputs, r < tokens);
+  }
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = r0 + rg + 8 * u;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(vy[u].h[e]);
+    if (drop.threshold) drop8(v, (int64_t)r * outputs + c, drop);
+    V8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (ACT != kActNone) v[e] *= act_slope<ACT>(to_f32(vz[u].h[e]));
+      s[e] += v[e];
+      o.h[e] = to_h16(v[e]);
+    }
+    if (dz && r < tokens && c < ld) store16(dz + (int64_t)r * ld + c, o);
+  }
+  if (!part) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[rg][cg * 8 + e] = s[e];
+  __syncthreads();
+  float t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
+  const int cc = blockIdx.x * 256 + threadIdx.x;
+  if (cc < outputs) part[(int64_t)blockIdx.y * outputs + cc] = t;
+}
+
+// 64 columns a workgroup, the parts dealt to its four waves.
 __global__ __launch_bounds__(256) void dbias_kernel(int outputs, int parts, const float* part,
                                                     h16* dbias) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= outputs) return;
+  __shared__ double sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   double s = 0.0;
-  for (int i = 0; i < parts; ++i) s += (double)part[(int64_t)i * outputs + c];
-  dbias[c] = dbl_to_h16(s);
+  if (c < outputs) {
+#pragma unroll 8
+    for (int i = wave; i < parts; i += 4) s += (double)part[(int64_t)i * outputs + c];
+  }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < outputs)
+    dbias[c] = dbl_to_h16((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
 }
 
-size_t dz_bytes(int tokens, int outputs) {
-  return ((size_t)tokens * outputs * 2 + 255) & ~(size_t)255;
+template <int ACT>
+hipError_t launch_dz(const DenseArgs& a, int ld, h16* dz, float* part, hipStream_t st) {
+  const int parts = ceil_div(a.tokens, kRows);
+  dz_kernel<ACT><<<dim3((unsigned)ceil_div(ld, 256), (unsigned)parts), 256, 0, st>>>(
+      a.tokens, a.outputs, ld, a.drop, a.kept, a.dy, dz, a.dbias ? part : nullptr);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.dbias) return e;
+  dbias_kernel<<<(unsigned)ceil_div(a.outputs, 64), 256, 0, st>>>(a.outputs, parts, part, a.dbias);
+  return hipGetLastError();
+}
+
+// ---- workspace -------------------------------------------------------------------------------
+
+int whole8(int n) { return (n + 7) & ~7; }
+size_t rows_bytes(int rows, int cols) {
+  return ((size_t)rows * whole8(cols) * 2 + 255) & ~(size_t)255;
+}
+
+// Places: x and W with rows of whole vectors (where theirs are not), dz, the parts' sums
+// (of one product at a time) and dbias's.
+struct Places {
+  size_t x = 0, w = 0, dz = 0, part = 0, sums = 0, total = 0;
+};
+size_t take(Places& p, size_t bytes) {
+  const size_t at = p.total;
+  p.total += (bytes + 255) & ~(size_t)255;
+  return at;
+}
+Places places(int T, int I, int O, bool backward, bool makes) {
+  Places p;
+  if (I & 7) {
+    p.x = take(p, rows_bytes(T, I));
+    p.w = take(p, rows_bytes(O, I));
+  }
+  if (!backward) {
+    p.sums = take(p, sums_bytes(choose(kForward, O, T, I), O, T));
+    return p;
+  }
+  if (makes || (O & 7)) p.dz = take(p, rows_bytes(T, O));
+  p.part = take(p, (size_t)ceil_div(T, kRows) * O * sizeof(float));
+  const size_t dx = sums_bytes(choose(kDx, I, T, O), I, T);
+  const size_t dw = sums_bytes(choose(kDw, I, O, T), I, O);
+  p.sums = take(p, dx > dw ? dx : dw);
+  return p;
+}
+
+template <class T>
+T* at(void* ws, size_t off) {
+  return reinterpret_cast<T*>(static_cast<char*>(ws) + off);
 }
 
 }  // namespace
 
-size_t dense_fwd_ws_bytes(int, int, int) { return 0; }
-
-size_t dense_bwd_ws_bytes(int tokens, int inputs, int outputs, bool dz) {
-  return (dz ? dz_bytes(tokens, outputs) : 0) +
-         (size_t)ceil_div(tokens, kRows) * outputs * sizeof(float);
+size_t dense_fwd_ws_bytes(int tokens, int inputs, int outputs) {
+  return places(tokens, inputs, outputs, false, false).total;
 }
 
+size_t dense_bwd_ws_bytes(int tokens, int inputs, int outputs, bool dz) {
+  return places(tokens, inputs, outputs, true, dz).total;
+}
+
+#define RUN(expr)                     \
+  do {                                \
+    const hipError_t e_ = (expr);     \
+    if (e_ != hipSuccess) return e_;  \
+  } while (0)
+
 hipError_t launch_dense_fwd(const DenseArgs& a, hipStream_t st) {
-  const Product p = {a.w, a.x, a.inputs, a.inputs, a.outputs, a.tokens, a.inputs};
-  return launch_product<false, false>(
-      p, Forward{a.bias, a.residual, a.y, a.z, a.outputs, a.act, a.drop}, st);
+  const int T = a.tokens, I = a.inputs, O = a.outputs, ld = whole8(I);
+  const Places at_ = places(T, I, O, false, false);
+  const h16 *x = a.x, *w = a.w;
+  if (ld != I) {
+    RUN(launch_repack(T, I, a.x, at<h16>(a.ws, at_.x), st));
+    RUN(launch_repack(O, I, a.w, at<h16>(a.ws, at_.w), st));
+    x = at<h16>(a.ws, at_.x);
+    w = at<h16>(a.ws, at_.w);
+  }
+  const Product p = {w, x, ld, ld, O, T, I, 1};
+  void* sums = at<void>(a.ws, at_.sums);
+  const auto go = [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    return launch_product<kForward>(
+        p, LayerEpi<ACT>{a.bias, a.residual, a.y, a.z, O, T, a.drop}, sums, st);
+  };
+  switch (a.act) {
+    case kActRelu: return go(std::integral_constant<int, kActRelu>{});
+    case kActGelu: return go(std::integral_constant<int, kActGelu>{});
+    case kActSilu: return go(std::integral_constant<int, kActSilu>{});
+    default: return go(std::integral_constant<int, kActNone>{});
+  }
 }
 
 hipError_t launch_dense_bwd(const DenseArgs& a, hipStream_t st) {
+  const int T = a.tokens, I = a.inputs, O = a.outputs, ldi = whole8(I), ldo = whole8(O);
   const bool makes = a.act != kActNone || a.drop.threshold;
-  const h16* dz = a.dy;
-  h16* made = makes ? static_cast<h16*>(a.ws) : nullptr;
-  float* part = reinterpret_cast<float*>(static_cast<char*>(a.ws) +
-                                         (makes ? dz_bytes(a.tokens, a.outputs) : 0));
-  if (makes || a.dbias) {
-    const int parts = ceil_div(a.tokens, kRows);
-    dz_kernel<<<dim3((unsigned)ceil_div(a.outputs, 256), (unsigned)parts), 256, 0, st>>>(
-        a.tokens, a.outputs, a.act, a.drop, a.kept, a.dy, made, a.dbias ? part : nullptr);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (a.dbias) {
-      dbias_kernel<<<(unsigned)ceil_div(a.outputs, 256), 256, 0, st>>>(a.outputs, parts, part,
-                                                                       a.dbias);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+  const Places at_ = places(T, I, O, true, makes);
+  const h16 *x = a.x, *w = a.w, *dz = a.dy;
+  h16* made = nullptr;
+  if (makes || ldo != O) dz = made = at<h16>(a.ws, at_.dz);
+  if (!a.dx && !a.dw) made = nullptr;
+  if (made || a.dbias) {
+    float* part = at<float>(a.ws, at_.part);
+    switch (a.act) {
+      case kActRelu: RUN(launch_dz<kActRelu>(a, ldo, made, part, st)); break;
+      case kActGelu: RUN(launch_dz<kActGelu>(a, ldo, made, part, st)); break;
+      case kActSilu: RUN(launch_dz<kActSilu>(a, ldo, made, part, st)); break;
+      default: RUN(launch_dz<kActNone>(a, ldo, made, part, st));
     }
   }
-  if (makes) dz = made;
+  void* sums = at<void>(a.ws, at_.sums);
   if (a.dx) {
-    const Product p = {a.w, dz, a.inputs, a.outputs, a.inputs, a.tokens, a.outputs};
-    const hipError_t e = launch_product<true, false>(p, ToHalf{a.dx, a.inputs}, st);
-    if (e != hipSuccess) return e;
+    if (ldi != I) {
+      RUN(launch_repack(O, I, a.w, at<h16>(a.ws, at_.w), st));
+      w = at<h16>(a.ws, at_.w);
+    }
+    const Product p = {w, dz, ldi, ldo, I, T, O, 1};
+    RUN(launch_product<kDx>(p, HalfEpi{a.dx, I, T}, sums, st));
   }
   if (a.dw) {
-    const Product p = {a.x, dz, a.inputs, a.outputs, a.inputs, a.outputs, a.tokens};
-    return launch_product<true, true>(p, ToHalf{a.dw, a.inputs}, st);
+    if (ldi != I) {
+      RUN(launch_repack(T, I, a.x, at<h16>(a.ws, at_.x), st));
+      x = at<h16>(a.ws, at_.x);
+    }
+    const Product p = {x, dz, ldi, ldo, I, O, T, 1};
+    RUN(launch_product<kDw>(p, HalfEpi{a.dw, I, O}, sums, st));
   }
   return hipSuccess;
 }
