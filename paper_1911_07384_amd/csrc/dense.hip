@@ -2,14 +2,14 @@
 // gradients of x, W and bias.
 //
 //   forward   z = x W^T + bias       rows of both operands run along the reduction
-//   dx        dz W                   W lies along its rows (see NtTile)
-//   dW        dz^T x                 both operands do
+//   dx        dz W                   W's columns do
+//   dW        dz^T x                 both operands' columns do
 //   with dz = drop(dy) act'(z), a pass over the elements that also sums its columns for
 //   dbias.
 //
 // Tile rows p run along the output's rows in memory, tile columns q are its rows.
 
-#include "gemm_nt.hpp"
+#include "gemm_dense.hpp"
 #include "head.hpp"
 
 #include <type_traits>
@@ -97,17 +97,18 @@ __device__ __forceinline__ void drop8(float (&v)[8], int64_t i, const Drop& d) {
   for (int e = 0; e < 8; ++e) v[e] = kept(b, e, d.threshold) ? v[e] * d.scale : 0.0f;
 }
 
-// ---- what a tile stores (see nt_store) -----------------------------------------------
+// ---- what a tile stores (see dense_store) -----------------------------------------------
 
 // Rounded, [q][p].
 struct HalfEpi {
   h16* d;
   int np, nq;
   static constexpr int OUTS = 1;
-  static constexpr bool DIAGONAL = false;
+  struct Col {};
   struct Pre {};
+  __device__ __forceinline__ Col column(int) const { return {}; }
   __device__ __forceinline__ Pre load(int, int) const { return {}; }
-  __device__ __forceinline__ void compute(int, int, const float (&v)[8], const Pre&,
+  __device__ __forceinline__ void compute(int, int, const float (&v)[8], Col, Pre,
                                           V8 (&out)[1]) const {
 #pragma unroll
     for (int k = 0; k < 8; ++k) out[0].h[k] = to_h16(v[k]);
@@ -122,10 +123,11 @@ struct PartEpi {
   float* d;
   int np, nq, ld;
   static constexpr int OUTS = 2;
-  static constexpr bool DIAGONAL = false;
+  struct Col {};
   struct Pre {};
+  __device__ __forceinline__ Col column(int) const { return {}; }
   __device__ __forceinline__ Pre load(int, int) const { return {}; }
-  __device__ __forceinline__ void compute(int, int, const float (&v)[8], const Pre&,
+  __device__ __forceinline__ void compute(int, int, const float (&v)[8], Col, Pre,
                                           V8 (&out)[2]) const {
 #pragma unroll
     for (int k = 0; k < 8; ++k) out[k / 4].d[k % 4] = __builtin_bit_cast(uint32_t, v[k]);
@@ -147,25 +149,25 @@ struct LayerEpi {
   int np, nq;
   Drop drop;
   static constexpr int OUTS = 2;
-  static constexpr bool DIAGONAL = false;
-  struct Pre {
-    V8 bias, residual;
+  struct Col {
+    V8 bias;
   };
-  __device__ __forceinline__ Pre load(int p, int q) const {
-    Pre r;
-    r.bias = r.residual = zero8();
-    if (p < np && q < nq) {
-      if (bias) r.bias = load8_upto(bias + p, np - p);
-      if (residual) r.residual = load8_upto(residual + (int64_t)q * np + p, np - p);
-    }
-    return r;
+  struct Pre {
+    V8 residual;
+  };
+  __device__ __forceinline__ Col column(int p) const {
+    return {bias && p < np ? load8_upto(bias + p, np - p) : zero8()};
   }
-  __device__ __forceinline__ void compute(int p, int q, const float (&sum)[8], const Pre& pre,
-                                          V8 (&out)[2]) const {
+  __device__ __forceinline__ Pre load(int p, int q) const {
+    return {residual && p < np && q < nq ? load8_upto(residual + (int64_t)q * np + p, np - p)
+                                         : zero8()};
+  }
+  __device__ __forceinline__ void compute(int p, int q, const float (&sum)[8], const Col& col,
+                                          const Pre& pre, V8 (&out)[2]) const {
     float v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      v[k] = sum[k] + to_f32(pre.bias.h[k]);
+      v[k] = sum[k] + to_f32(col.bias.h[k]);
       out[1].h[k] = to_h16(v[k]);
       v[k] = act_value<ACT>(v[k]);
     }
@@ -196,34 +198,32 @@ struct Product {
 // Tiles in groups of 8 tile columns, within a group column by column: the 32 tiles that
 // an XCD holds at a time share 8 + 4 tiles' rows in its L2.
 template <class C, class Epi>
-__global__ __launch_bounds__(C::THREADS, (C::OCC * C::WAVES + 3) / 4) void dense_product(const Product a, Epi epi) {
-  __shared__ __attribute__((aligned(1024))) char lds[NtEpi<C, 1>::LDS];
+__global__ __launch_bounds__(C::BOUND, 2) void dense_product(const Product a, Epi epi) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int tp = (a.np + C::BP - 1) / C::BP, tq = (a.nq + C::BQ - 1) / C::BQ;
   const int all = tp * tq * a.parts;
-  int t = nt_xcd(blockIdx.x, all);
+  int t = dense_xcd(blockIdx.x, all);
   if (t >= all) return;
   const int part = t / (tp * tq);
   t -= part * tp * tq;
   const int g = t / (8 * tp), w = t - g * 8 * tp;
   const int gw = tq - 8 * g < 8 ? tq - 8 * g : 8;
   const int p0 = (w / gw) * C::BP, q0 = (8 * g + w % gw) * C::BQ;
-  NtTile nt;
-  nt.ldp = (uint32_t)(a.ldp * 2);
-  nt.ldq = (uint32_t)(a.ldq * 2);
-  nt.p[0] = nt.p[1] = a.p + (C::PS ? (int64_t)p0 : p0 * a.ldp);
-  nt.q[0] = nt.q[1] = a.q + (C::QS ? (int64_t)q0 : q0 * a.ldq);
-  nt.prows = a.np - p0;
-  nt.qrows = a.nq - q0;
-  nt.kbytes = a.nk * 2;
-  nt.part = part;
-  nt.parts = a.parts;
-  floatx16 acc[C::TP][C::TQ];
-  nt_product<NtHalf, C>(nt, lds, acc);
+  DenseTile d;
+  d.ldp = (uint32_t)(a.ldp * 2);
+  d.ldq = (uint32_t)(a.ldq * 2);
+  d.p = a.p + (C::PS ? (int64_t)p0 : p0 * a.ldp);
+  d.q = a.q + (C::QS ? (int64_t)q0 : q0 * a.ldq);
+  d.prows = a.np - p0;
+  d.qrows = a.nq - q0;
+  d.nk = a.nk;
+  d.part = part;
+  d.parts = a.parts;
+  floatx4 acc[C::TP][C::TQ];
+  dense_loop<C>(d, lds, acc);
   if constexpr (std::is_same<Epi, PartEpi>::value) epi.d += (int64_t)part * epi.nq * epi.ld;
   const int wave = threadIdx.x >> 6;
-  h16* none[1] = {nullptr};
-  nt_store<C, 1>(acc, lds, p0 + (wave / C::WQ) * 32 * C::TP, q0 + (wave % C::WQ) * 32 * C::TQ, a.np,
-                 a.nq, false, none, 0, epi);
+  dense_store<C>(acc, p0 + (wave / C::WQ) * 16 * C::TP, q0 + (wave % C::WQ) * 16 * C::TQ, epi);
 }
 
 // The parts' sums added in their order, and the product's epilogue.
@@ -233,6 +233,7 @@ __global__ __launch_bounds__(256) void dense_join(const float* from, int parts, 
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int per = ld / 8, q = (int)(i / per), p = (int)(i - (int64_t)q * per) * 8;
   if (q >= nq) return;
+  const typename Epi::Col col = epi.column(p);
   const typename Epi::Pre pre = epi.load(p, q);
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   const float* f = from + (int64_t)q * ld + p;
@@ -247,19 +248,19 @@ __global__ __launch_bounds__(256) void dense_join(const float* from, int parts, 
     }
   }
   V8 out[Epi::OUTS];
-  epi.compute(p, q, v, pre, out);
+  epi.compute(p, q, v, col, pre, out);
   epi.store(p, q, out);
 }
 
 enum Layout { kForward, kDx, kDw };  // which operands lie along their rows: none, P, both
 
-template <Layout L, int WP, int WQ, int TP, int TQ, int S, int OCC>
-using Cfg = NtCfg<WP, WQ, TP, TQ, 128, S, OCC, 1, L != kForward, L == kDw>;
+template <Layout L, int WP, int WQ, int TQ, int S, int OCC>
+using Cfg = DenseCfg<WP, WQ, 8, TQ, S, OCC, L != kForward, L == kDw>;
 
-//                            waves  tile  stages  workgroups a CU
-template <Layout L> using Cfg256 = Cfg<L, 4, 2, 2, 4, 2, 1>;  // 256 x 256
-template <Layout L> using Cfg128 = Cfg<L, 2, 2, 2, 2, 2, 2>;  // 128 x 128
-template <Layout L> using Cfg32 = Cfg<L, 2, 1, 2, 1, 4, 2>;   // 128 x 32: few tokens
+//                                 waves  tiles  stages  workgroups a CU
+template <Layout L> using Cfg256 = Cfg<L, 2, 4, 4, 2, 1>;
+template <Layout L> using Cfg128 = Cfg<L, 1, 2, 4, 2, 2>;
+template <Layout L> using Cfg32 = Cfg<L, 1, 1, 2, 4, 2>;   // 128 x 32: few tokens
 
 template <class C, class Epi>
 hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {

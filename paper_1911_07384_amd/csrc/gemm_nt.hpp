@@ -45,12 +45,9 @@ struct NtByte {  // 8-bit integers, 32-bit sums (exact below 2^31)
   }
 };
 
-// H = 2: operands in a high and a low part each (see nt_product).  PS, QS: the operand is
-// laid out along its rows (see NtTile).
-template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int OCC_, int H_ = 1,
-          bool PS_ = false, bool QS_ = false>
+// H = 2: operands in a high and a low part each (see nt_product).
+template <int WP_, int WQ_, int TP_, int TQ_, int SB_, int S_, int OCC_, int H_ = 1>
 struct NtCfg {
-  static constexpr bool PS = PS_, QS = QS_;
   static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, SB = SB_, S = S_, OCC = OCC_, H = H_;
   static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES;
   static constexpr int BP = 32 * TP * WP, BQ = 32 * TQ * WQ;
@@ -59,10 +56,6 @@ struct NtCfg {
   static_assert(SB == 64 || (SB == 128 && IP % 2 == 0 && IQ % 2 == 0), "the chunks' order");
   static_assert(IP * 1024 * WAVES == BP * SB && IQ * 1024 * WAVES == BQ * SB, "whole loads");
   static_assert(LDS * OCC <= 160 * 1024, "LDS");
-  static_assert(!(PS || QS) || (H == 1 && SB == 128), "operands along their rows");
-  static_assert((!PS || ((TP == 2 || TP == 4) && 1024 % (BP * 2) == 0 && BP >= 128)) &&
-                    (!QS || ((TQ == 2 || TQ == 4) && 1024 % (BQ * 2) == 0 && BQ >= 128)),
-                "whole loads and reads of operands along their rows");
 };
 
 // One 16-byte-per-lane load from a buffer resource into LDS (1 KB a wave).
@@ -77,8 +70,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t nt_rsrc(const void* p, int byt
 __device__ __forceinline__ void nt_barrier() { __asm__ volatile("s_barrier" ::: "memory"); }
 
 // The rows of one tile, each operand from the tile's first row (with H = 2 its high
-// and its low part).  An operand that is laid out along its rows (binary16, PS or QS:
-// P[k][p] in memory) has ldp bytes from one k to the next.
+// and its low part).
 struct NtTile {
   const void* p[2];
   const void* q[2];
@@ -87,31 +79,6 @@ struct NtTile {
   int kbytes;          // of a row; a last chunk's bytes past it are multiplied too
   int part, parts;     // which of so many ranges of the slices
 };
-
-// An operand along its rows, binary16: LDS holds a slice as 64 lines of the tile's rows,
-// one a k, whose 128-byte blocks are exchanged in pairs where k has its bit 3 set.  A
-// lane reads its T rows T (l % 32) .. + T - 1 at eight k, and permutes bytes into the
-// fragments of T tiles of 32 rows, every T-th row each: eight reads of 2 T bytes and
-// 4 T permutes for T fragments (gfx950's transposing read would need none, but through
-// the compiler's builtin each waits for all loads in flight).
-template <int T>
-struct NtRaw {
-  uint32_t d[8][T / 2];
-};
-template <int T>
-__device__ __forceinline__ half8 nt_rows(const NtRaw<T>& r, int a) {
-  const uint32_t sel = a & 1 ? 0x07060302u : 0x05040100u;
-  V8 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v.d[i] = __builtin_amdgcn_perm(r.d[2 * i + 1][a >> 1], r.d[2 * i][a >> 1], sel);
-  return v.h;
-}
-// Which row of its wave's 32 T a tile's row m is: tile a's own, or every T-th.
-template <int T, bool S>
-__device__ __forceinline__ int nt_row(int a, int m) {
-  return S ? T * m + a : 32 * a + m;
-}
 
 // acc = the sums of P[p][k] Q[q][k]; with H = 2 of Ph Ql + Pl Qh + Ph Qh, every part
 // loaded once for the three products.
@@ -132,10 +99,6 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
   constexpr int RI = 1024 / SB;
   const int prec = (t.prows < C::BP ? t.prows : C::BP) * (int)t.ldp;
   const int qrec = (t.qrows < C::BQ ? t.qrows : C::BQ) * (int)t.ldq;
-  // an operand along its rows: the slice's first k, and a lane's place in one load
-  constexpr int PK = 1024 / (C::BP * 2), QK = 1024 / (C::BQ * 2);  // k of a load
-  const char* ps = static_cast<const char*>(t.p[0]);
-  const char* qs = static_cast<const char*>(t.q[0]);
   int ck[2];           // byte of the chunk in its row's slice, even and odd instructions
   uint32_t pv[2], qv[2];
 #pragma unroll
@@ -156,18 +119,7 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
   const int slices = (t.kbytes + SB - 1) / SB, KT = (slices + t.parts - 1) / t.parts;
   int k0 = t.part * KT * SB;
   const int kend = t.kbytes < k0 + KT * SB ? t.kbytes : k0 + KT * SB;
-  if (C::PS) ps += (uint64_t)(k0 >> 1) * t.ldp;
-  if (C::QS) qs += (uint64_t)(k0 >> 1) * t.ldq;
   bool in[2];
-  // bytes of a slice of an operand along its rows, up to its last row's last chunk
-  auto slice_bytes = [&](uint32_t ld, int rows) {
-    const int n = (kend - k0) >> 1;
-    return n <= 0 ? 0 : ((n < 64 ? n : 64) - 1) * (int)ld + ((rows + 7) & ~7) * 2;
-  };
-  auto slice_at = [&](int line, int per, uint32_t ld) {
-    const int k = line * per + lane / (64 / per);
-    return (uint32_t)k * ld + (uint32_t)((lane % (64 / per)) ^ (k & 8)) * 16u;
-  };
   auto begin = [&]() {
 #pragma unroll
     for (int h = 0; h < 2; ++h) in[h] = k0 + ck[h] < kend;
@@ -175,15 +127,7 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
   auto load = [&](char* buf, int n) {
     const int h = n / I1, i = n % I1;
     buf += h * C::PART;
-    if (C::PS && i < IP) {
-      const int line = wave * IP + i;
-      nt_load(nt_rsrc(ps, slice_bytes(t.ldp, t.prows)), buf + line * 1024,
-              slice_at(line, PK, t.ldp));
-    } else if (C::QS && i >= IP) {
-      const int line = wave * IQ + i - IP;
-      nt_load(nt_rsrc(qs, slice_bytes(t.ldq, t.qrows)), buf + C::BP * SB + line * 1024,
-              slice_at(line, QK, t.ldq));
-    } else if (i < IP) {
+    if (i < IP) {
       const uint32_t off = pv[i & 1] + ((uint32_t)(i * RI) * t.ldp + (uint32_t)k0);
       nt_load(nt_rsrc(t.p[h], prec), buf + (wave * IP + i) * 1024, in[i & 1] ? off : OOB);
     } else {
@@ -193,11 +137,7 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
               in[j & 1] ? off : OOB);
     }
   };
-  auto advance = [&]() {
-    k0 += SB;
-    if (C::PS) ps += 64ull * t.ldp;
-    if (C::QS) qs += 64ull * t.ldq;
-  };
+  auto advance = [&]() { k0 += SB; };
 
 #pragma unroll
   for (int a = 0; a < TP; ++a)
@@ -206,49 +146,14 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[a][b][e] = 0;
 
-  // an operand along its rows is held as it was read until its products
   Frag fp[2][H][TP], fq[2][H][TQ];
-  NtRaw<C::PS ? TP : 2> rp[2];
-  NtRaw<C::QS ? TQ : 2> rq[2];
   // byte of this lane's fragment of sub-step ks in a block of 32 rows
   auto place = [&](int ks) {
     if (SB == 128) return lrow * 128 + ((ks * 2 + lhi) ^ ((lrow >> 1) & 7)) * 16;
     return (lrow >> 1) * 128 + (((lrow & 1) * 4 + ks * 2 + lhi) ^ ((lrow >> 2) & 3)) * 16;
   };
-  auto fetch_raw = [&](const char* line, int row, int width, int j, auto& raw) {
-    // k = 16 ks + 8 lhi + j: the blocks' exchange is lhi's
-    constexpr int W = sizeof(raw.d[0]);
-    const char* from = line + (8 * lhi + j) * width * 2 + ((row * 2) ^ (lhi * 128));
-    if constexpr (W == 4) {
-      raw.d[j][0] = *reinterpret_cast<const uint32_t*>(from);
-    } else {
-      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-      const u32x2 v = *reinterpret_cast<const u32x2*>(from);
-      raw.d[j][0] = v[0];
-      raw.d[j][W / 4 - 1] = v[1];
-    }
-  };
   // read r of the fragments of sub-step ks, in the order they are used in
-  constexpr int RQ = C::QS ? 8 : TQ, RP = C::PS ? 8 : TP;
-  auto fetch = [&](const char* buf, int ks, int r, int set) {
-    auto &p = fp[set];
-    auto &q = fq[set];
-    if constexpr (C::PS || C::QS) {
-      const char* const bq = buf + C::BP * SB;
-      if (r < RQ) {
-        if constexpr (C::QS)
-          fetch_raw(bq + ks * 16 * C::BQ * 2, (wq * 32 + lrow) * TQ, C::BQ, r, rq[set]);
-        else
-          q[0][r] = *reinterpret_cast<const Frag*>(bq + (wq * TQ + r) * 32 * SB + place(ks));
-      } else {
-        if constexpr (C::PS)
-          fetch_raw(buf + ks * 16 * C::BP * 2, (wp * 32 + lrow) * TP, C::BP, r - RQ, rp[set]);
-        else
-          p[0][r - RQ] =
-              *reinterpret_cast<const Frag*>(buf + (wp * TP + r - RQ) * 32 * SB + place(ks));
-      }
-      return;
-    }
+  auto fetch = [&](const char* buf, int ks, int r, Frag (&p)[H][TP], Frag (&q)[H][TQ]) {
     const bool isq = r < TQ || r >= TQ + H * TP;
     const int h = H == 1 ? 0 : r < TQ ? 1 : r < TQ + TP ? 0 : r < TQ + 2 * TP ? 1 : 0;
     const int i = r < TQ ? r : r < TQ + TP ? r - TQ : r < TQ + 2 * TP ? r - TQ - TP : r - TQ - 2 * TP;
@@ -260,26 +165,20 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
     else
       p[h][i < TP ? i : 0] = *from;
   };
-  constexpr int R = C::PS || C::QS ? RP + RQ : H * (TP + TQ);  // reads
-  constexpr int M = (H == 2 ? 3 : 1) * TP * TQ;                // products
+  constexpr int R = H * (TP + TQ), M = (H == 2 ? 3 : 1) * TP * TQ;  // reads, products
   // One sub-step: the products of one set of fragments, between them the reads of
   // the next set (sub-step ks of `from`) and loads L0 .. L1 - 1 into `to`, an
   // instruction or two after each product (kept there by the scheduling barriers;
   // left to itself the compiler issues them in bursts that hold the products up).
-  auto substep = [&](int set, const char* from, int ks, char* to, auto l0, auto l1) {
+  auto substep = [&](const Frag (&p)[H][TP], const Frag (&q)[H][TQ], const char* from, int ks,
+                     Frag (&np)[H][TP], Frag (&nq)[H][TQ], char* to, auto l0, auto l1) {
     constexpr int L0 = decltype(l0)::value, V = decltype(l1)::value - L0;
-    auto &p = fp[set];
-    auto &q = fq[set];
 #pragma unroll
     for (int i = 0; i < M; ++i) {
       const int a = i / TQ % TP, b = i % TQ, term = i / (TP * TQ);
-      if constexpr (C::PS)
-        if (b == 0) p[0][a] = nt_rows(rp[set], a);
-      if constexpr (C::QS)
-        if (a == 0) q[0][b] = nt_rows(rq[set], b);
       acc[a][b] = T::mma(p[H == 2 && term == 1][a], q[H == 2 && term == 0][b], acc[a][b]);
 #pragma unroll
-      for (int r = R * i / M; r < R * (i + 1) / M; ++r) fetch(from, ks, r, set ^ 1);
+      for (int r = R * i / M; r < R * (i + 1) / M; ++r) fetch(from, ks, r, np, nq);
 #pragma unroll
       for (int v = V * i / M; v < V * (i + 1) / M; ++v) load(to, L0 + v);
       __builtin_amdgcn_sched_barrier(0);
@@ -300,7 +199,7 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
   __builtin_amdgcn_s_waitcnt(WAIT);
   nt_barrier();
 #pragma unroll
-  for (int r = 0; r < R; ++r) fetch(lds, 0, r, 0);
+  for (int r = 0; r < R; ++r) fetch(lds, 0, r, fp[0], fq[0]);
   int rd = 0, wr = S - 1;
   for (int kt = 0; kt < KT; ++kt) {
     const char* cur = lds + rd * C::STAGE;
@@ -309,10 +208,10 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
     constexpr std::integral_constant<int, SB == 64 ? I : (I + 1) / 2> L1{};
     constexpr std::integral_constant<int, I> L2{};
     begin();
-    substep(0, cur, 1, nxt, L0, L1);
+    substep(fp[0], fq[0], cur, 1, fp[1], fq[1], nxt, L0, L1);
     if constexpr (SB == 128) {
-      substep(1, cur, 2, nxt, L1, L2);
-      substep(0, cur, 3, nxt, L2, L2);
+      substep(fp[1], fq[1], cur, 2, fp[0], fq[0], nxt, L1, L2);
+      substep(fp[0], fq[0], cur, 3, fp[1], fq[1], nxt, L2, L2);
     }
     advance();
     // this wave's reads of the stage are complete and its part of the next one
@@ -321,7 +220,7 @@ __device__ __forceinline__ void nt_product(const NtTile& t, char* lds,
     nt_barrier();
     rd = rd + 1 == S ? 0 : rd + 1;
     wr = wr + 1 == S ? 0 : wr + 1;
-    substep(1, lds + rd * C::STAGE, 0, nxt, L2, L2);
+    substep(fp[1], fq[1], lds + rd * C::STAGE, 0, fp[0], fq[0], nxt, L2, L2);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // every load has landed and every read is done: LDS is free
@@ -384,8 +283,7 @@ __device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* l
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = (n % 2) * U + u;
-      pre[u] = epi.load(p0 + 8 * ((i * 64 + lane) % CPR),
-                        q0 + nt_row<TQ, C::QS>(n / 2, (i * 64 + lane) / CPR));
+      pre[u] = epi.load(p0 + 8 * ((i * 64 + lane) % CPR), q0 + 32 * (n / 2) + (i * 64 + lane) / CPR);
     }
   };
   load(0);
@@ -398,19 +296,9 @@ __device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* l
       for (int a = 0; a < TP; ++a)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if constexpr (C::PS && TP == 4) {  // rows 4 m + 0 .. 3, m = 8 e + 4 lhi + a
-            const V4 v = {acc[0][s][4 * e + a], acc[1][s][4 * e + a], acc[2][s][4 * e + a],
-                          acc[3][s][4 * e + a]};
-            *reinterpret_cast<V4*>(f + lrow * FLD + 4 * (8 * e + 4 * lhi + a)) = v;
-          } else if constexpr (C::PS) {  // rows 2 m + 0 .. 3, m = 8 e + 4 lhi + 2 a
-            const V4 v = {acc[0][s][4 * e + 2 * a], acc[1][s][4 * e + 2 * a],
-                          acc[0][s][4 * e + 2 * a + 1], acc[1][s][4 * e + 2 * a + 1]};
-            *reinterpret_cast<V4*>(f + lrow * FLD + 2 * (8 * e + 4 * lhi + 2 * a)) = v;
-          } else {
-            const V4 v = {acc[a][s][4 * e], acc[a][s][4 * e + 1], acc[a][s][4 * e + 2],
-                          acc[a][s][4 * e + 3]};
-            *reinterpret_cast<V4*>(f + lrow * FLD + 32 * a + 8 * e + 4 * lhi) = v;
-          }
+          const V4 v = {acc[a][s][4 * e], acc[a][s][4 * e + 1], acc[a][s][4 * e + 2],
+                        acc[a][s][4 * e + 3]};
+          *reinterpret_cast<V4*>(f + lrow * FLD + 32 * a + 8 * e + 4 * lhi) = v;
         }
     }
     nt_wave_sync();
@@ -441,7 +329,7 @@ __device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* l
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int r = ((h * U + u) * 64 + lane) / CPR, c = ((h * U + u) * 64 + lane) % CPR;
-        epi.compute(p0 + 8 * c, q0 + nt_row<TQ, C::QS>(b, r), v[u], now[u], out[u]);
+        epi.compute(p0 + 8 * c, qb + r, v[u], now[u], out[u]);
         if (mirror) {
 #pragma unroll
           for (int s = 0; s < PARTS; ++s)
@@ -454,7 +342,7 @@ __device__ __forceinline__ void nt_store(const Acc (&acc)[C::TP][C::TQ], char* l
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int r = ((h * U + u) * 64 + lane) / CPR, c = ((h * U + u) * 64 + lane) % CPR;
-        epi.store(p0 + 8 * c, q0 + nt_row<TQ, C::QS>(b, r), out[u]);
+        epi.store(p0 + 8 * c, qb + r, out[u]);
       }
     }
     nt_wave_sync();
