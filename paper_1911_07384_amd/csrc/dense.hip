@@ -258,9 +258,17 @@ template <Layout L, int WP, int WQ, int TQ, int S, int OCC>
 using Cfg = DenseCfg<WP, WQ, 8, TQ, S, OCC, L != kForward, L == kDw>;
 
 //                                 waves  tiles  stages  workgroups a CU
-template <Layout L> using Cfg256 = Cfg<L, 2, 4, 4, 2, 1>;
-template <Layout L> using Cfg128 = Cfg<L, 1, 2, 4, 2, 2>;
-template <Layout L> using Cfg32 = Cfg<L, 1, 1, 2, 4, 2>;   // 128 x 32: few tokens
+template <Layout L> using Cfg256 = Cfg<L, 2, 4, 4, 2, 1>;  // 256 x 256
+template <Layout L> using Cfg128 = Cfg<L, 1, 4, 2, 2, 2>;  // 128 x 128
+template <Layout L> using Cfg64 = Cfg<L, 1, 4, 1, 3, 2>;   // 128 x 64
+
+template <class Epi>
+hipError_t launch_join(const Product& a, const float* sums, int ld, const Epi& epi,
+                       hipStream_t st) {
+  dense_join<<<(unsigned)ceil_div64((int64_t)a.nq * (ld / 8), 256), 256, 0, st>>>(
+      sums, a.parts, a.np, a.nq, ld, epi);
+  return hipGetLastError();
+}
 
 template <class C, class Epi>
 hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {
@@ -274,36 +282,54 @@ hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {
   dense_product<C><<<grid, C::THREADS, 0, st>>>(a, PartEpi{sums, a.np, a.nq, ld});
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  dense_join<<<(unsigned)ceil_div64((int64_t)a.nq * (ld / 8), 256), 256, 0, st>>>(
-      sums, a.parts, a.np, a.nq, ld, epi);
-  return hipGetLastError();
+  return launch_join(a, sums, ld, epi, st);
 }
 
-// The tile a product runs on, and the parts its reduction is split into: enough
-// workgroups for every CU, of four slices of 64 at least.
+// The tile a product runs on, and the parts its reduction is split into: the least of
+// the times below, in microseconds: of a slice with one workgroup a CU and with two, and
+// of a workgroup's start and end, for each layout, fitted to 14 products of 32 to 8192
+// tokens and 512 to 4096 inputs and outputs in three layouts, each on every tile and
+// with up to 32 parts.  What it chooses for them takes 1.4 % longer than the best choice
+// (geometric mean; 13 % at most).  For the largest the 256 x 256 tile's slices cost 1.5
+// us for four times the outputs that the others do in 0.49 (128 x 128) or 0.62 us.
 struct Choice {
   int side, parts;
 };
+struct Tile {
+  int side, occ;
+  double one, two, ends;
+};
 Choice choose(Layout l, int64_t np, int64_t nq, int64_t nk) {
-  Choice c;
-  const int64_t big = ceil_div64(np, 256) * ceil_div64(nq, 256);
-  int64_t tiles;
-  if (l != kDw && nq <= 32) {
-    c.side = 32;
-    tiles = ceil_div64(np, 128) * ceil_div64(nq, 32);
-  } else if (big >= 192) {
-    c.side = 256;
-    tiles = big;
-  } else {
-    c.side = 128;
-    tiles = ceil_div64(np, 128) * ceil_div64(nq, 128);
+  static const Tile tiles[3][3] = {
+      {{256, 1, 1.48, 0, 12}, {128, 2, 0.58, 0.97, 5.5}, {64, 2, 0.30, 0.62, 4.7}},
+      {{256, 1, 1.55, 0, 12}, {128, 2, 0.70, 1.12, 5.5}, {64, 2, 0.42, 0.79, 4.7}},
+      {{256, 1, 1.60, 0, 12}, {128, 2, 0.78, 1.20, 5.5}, {0, 0, 0, 0, 0}}};
+  const double launch = 4.0, join = 2.5, bytes = 4.5e6;  // (bytes a microsecond)
+  const int64_t slices = ceil_div64(nk, 64);
+  Choice best = {128, 1};
+  double least = 1e300;
+  for (const Tile& t : tiles[l]) {
+    if (!t.side) continue;
+    const int64_t n1 = ceil_div64(np, t.side < 128 ? 128 : t.side) * ceil_div64(nq, t.side);
+    for (int64_t want = 1; want <= 32 && want <= slices; want += 1 + want / 4) {
+      const int64_t sl = ceil_div64(slices, want), parts = ceil_div64(slices, sl);
+      if (parts > 1 && sl < 2) break;
+      // rounds of workgroups on the busiest CU
+      const int64_t n = n1 * parts, cu = ceil_div64(n, 256);
+      const double full = (double)(cu / t.occ), rest = (double)(cu % t.occ);
+      const double end = t.ends - launch;
+      double us = launch + full * ((double)sl * (t.occ == 2 ? t.two : t.one) + t.occ * end) +
+                  rest * ((double)sl * t.one + end);
+      // (a device that is not full runs at a higher clock)
+      if (n < 256) us -= 0.2 * (1.0 - (double)n / 256.0) * (double)sl * t.one;
+      if (parts > 1) us += join + (double)(parts * np * nq * 8) / bytes;
+      if (us < least) {
+        least = us;
+        best = {t.side, (int)parts};
+      }
+    }
   }
-  const int64_t slices = ceil_div64(nk, 64), fill = (c.side == 256 ? 256 : 512) / tiles;
-  int64_t parts = fill < slices / 4 ? fill : slices / 4;
-  parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
-  // (whole slices a part, none without)
-  c.parts = (int)ceil_div64(slices, ceil_div64(slices, parts));
-  return c;
+  return best;
 }
 
 size_t sums_bytes(const Choice& c, int64_t np, int64_t nq) {
@@ -316,9 +342,183 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
   a.parts = c.parts;
   float* f = static_cast<float*>(sums);
   if constexpr (L != kDw)
-    if (c.side == 32) return run<Cfg32<L>>(a, epi, f, st);
+    if (c.side == 64) return run<Cfg64<L>>(a, epi, f, st);
   if (c.side == 256) return run<Cfg256<L>>(a, epi, f, st);
   return run<Cfg128<L>>(a, epi, f, st);
+}
+
+// ---- few tokens ------------------------------------------------------------------------------
+
+// The forward of at most 32 tokens, bound by reading W once: a workgroup takes 16 RF rows
+// of W, its sixteen waves the reduction in turns of 64, each lane 16 bytes of a row
+// straight into the operand (the next turn's before this one's products), with no regard
+// to a row's alignment; the waves' sums are added in LDS in their order.  One token, W
+// 16384 x 4096 from memory: 24.1 us, 5.6 TB/s; rows that are not aligned take twice as
+// long.  (Turns of 128: 34.5 us; starting each workgroup at another turn: 25.7, and 39
+// for 31 with rows of 32 KB.)
+constexpr int kFewTokens = 32, kFewWaves = 16, kFewSteps = 2, kFewTurn = 32 * kFewSteps;
+
+template <int RF, int NT, class Epi>
+__global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi epi) {
+  constexpr int U = kFewSteps, TURN = kFewTurn;
+  __shared__ floatx4 sums[kFewWaves][RF * NT * 64];
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.np + 16 * RF - 1) / (16 * RF);
+  const int part = blockIdx.x / groups, p0 = (blockIdx.x - part * groups) * 16 * RF;
+  // this part's range of the reduction, in whole turns of all waves
+  const int per = ((a.nk + a.parts - 1) / a.parts + 7) & ~7;
+  const int kbeg = part * per, kend = a.nk < kbeg + per ? a.nk : kbeg + per;
+  const h16* pr[RF];  // (rows and tokens that are not there read the last one)
+  const h16* qr[NT];
+#pragma unroll
+  for (int f = 0; f < RF; ++f) {
+    const int r = p0 + 16 * f + m;
+    pr[f] = a.p + (int64_t)(r < a.np ? r : a.np - 1) * a.ldp + 8 * g;
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = 16 * n + m;
+    qr[n] = a.q + (int64_t)(r < a.nq ? r : a.nq - 1) * a.ldq + 8 * g;
+  }
+  V8 w[2][U][RF], x[2][U][NT];
+  auto load = [&](int k, V8 (&wv)[U][RF], V8 (&xv)[U][NT]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int f = 0; f < RF; ++f) wv[u][f] = load16u(pr[f] + k + 32 * u);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) xv[u][n] = load16u(qr[n] + k + 32 * u);
+    }
+  };
+  floatx4 acc[RF][NT];
+#pragma unroll
+  for (int f = 0; f < RF; ++f)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[f][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto mma = [&](const V8 (&wv)[U][RF], const V8 (&xv)[U][NT]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          acc[f][n] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(wv[u][f].h, xv[u][n].h, acc[f][n], 0, 0, 0);
+  };
+  constexpr int STEP = TURN * kFewWaves;
+  // this wave's whole turns, and the one that the range ends in
+  const int whole = (kend - kbeg) / TURN, turns = (whole - wave + kFewWaves - 1) / kFewWaves;
+  int k = kbeg + wave * TURN;
+  if (turns > 0) {
+    load(k, w[0], x[0]);
+    int i = turns;
+    for (; i > 2; i -= 2, k += 2 * STEP) {
+      load(k + STEP, w[1], x[1]);
+      mma(w[0], x[0]);
+      load(k + 2 * STEP, w[0], x[0]);
+      mma(w[1], x[1]);
+    }
+    if (i == 2) load(k + STEP, w[1], x[1]);
+    mma(w[0], x[0]);
+    if (i == 2) mma(w[1], x[1]);
+  }
+  if (wave == whole % kFewWaves) {
+#pragma unroll 1
+    for (int at = kbeg + whole * TURN; at < kend; at += 32) {
+      const int left = kend - at - 8 * g;
+      V8 wt[RF], xt[NT];
+#pragma unroll
+      for (int f = 0; f < RF; ++f) wt[f] = left > 0 ? load8_upto(pr[f] + at, left) : zero8();
+#pragma unroll
+      for (int n = 0; n < NT; ++n) xt[n] = left > 0 ? load8_upto(qr[n] + at, left) : zero8();
+#pragma unroll
+      for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          acc[f][n] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(wt[f].h, xt[n].h, acc[f][n], 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < RF; ++f)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sums[wave][(f * NT + n) * 64 + lane] = acc[f][n];
+  __syncthreads();
+  // 8 rows c of one token t a thread; a sum's rows are 4 (lane / 16) + 0 .. 3
+  if constexpr (std::is_same<Epi, PartEpi>::value) epi.d += (int64_t)part * epi.nq * epi.ld;
+  const int c = threadIdx.x % (2 * RF), t = threadIdx.x / (2 * RF);
+  if (t >= a.nq || p0 + 8 * c >= a.np) return;
+  const typename Epi::Col col = epi.column(p0 + 8 * c);
+  const typename Epi::Pre pre = epi.load(p0 + 8 * c, t);
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int at = ((c / 2) * NT + t / 16) * 64 + (c % 2) * 32 + t % 16;
+#pragma unroll
+  for (int s = 0; s < kFewWaves; ++s) {
+    const floatx4 lo = sums[s][at], hi = sums[s][at + 16];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] += lo[e];
+      v[4 + e] += hi[e];
+    }
+  }
+  V8 out[Epi::OUTS];
+  epi.compute(p0 + 8 * c, t, v, col, pre, out);
+  epi.store(p0 + 8 * c, t, out);
+}
+
+// Rows of W a workgroup takes, over 16: every workgroup reads the tokens again, so two
+// groups where tokens are several and workgroups many, or tokens and the reduction long
+// (16 tokens of 16384 x 4096: 29 us, 34 with one; 24 of 4096 x 16384: 37 and 45).
+int few_rows(int64_t np, int64_t nq, int64_t nk) {
+  return (nq > 4 && np >= 8192) || (nq > 16 && nk >= 8192) ? 2 : 1;
+}
+// Past 16 tokens of wide layers the tiles read each token less often (24 tokens of 4096 x
+// 4096: 12.1 us, 13.0 here; of 4096 x 2048: 10.2 and 8.0).
+bool few_ok(int64_t np, int64_t nq, int64_t nk) {
+  return nq <= 16 || (nq <= kFewTokens && (few_rows(np, nq, nk) == 2 || np * nk <= 1 << 23));
+}
+// Parts: a workgroup alone on its CU reads about 32 KB a microsecond; joining parts takes a
+// launch, 4 us.
+int few_parts(int np, int nq, int nk) {
+  const int rf = few_rows(np, nq, nk), groups = ceil_div(np, 16 * rf);
+  const double alone = (double)nk / 1024.0;
+  int best = 1;
+  double least = alone;
+  for (int p = 2; p * groups <= 256 && nk / p >= 1024; ++p)
+    if (alone / p + 4.0 + 0.05 * p < least) {
+      least = alone / p + 4.0 + 0.05 * p;
+      best = p;
+    }
+  return best;
+}
+
+template <class Epi>
+hipError_t launch_few(Product a, const Epi& epi, void* sums, hipStream_t st) {
+  const int rf = few_rows(a.np, a.nq, a.nk);
+  a.parts = few_parts(a.np, a.nq, a.nk);
+  const unsigned grid = (unsigned)(ceil_div(a.np, 16 * rf) * a.parts);
+  auto go = [&](auto e) {
+    typedef decltype(e) E;
+    constexpr int T = 64 * kFewWaves;
+    if (a.nq <= 16) {
+      if (rf == 2)
+        dense_few<2, 1, E><<<grid, T, 0, st>>>(a, e);
+      else
+        dense_few<1, 1, E><<<grid, T, 0, st>>>(a, e);
+    } else if (rf == 2) {
+      dense_few<2, 2, E><<<grid, T, 0, st>>>(a, e);
+    } else {
+      dense_few<1, 2, E><<<grid, T, 0, st>>>(a, e);
+    }
+    return hipGetLastError();
+  };
+  if (a.parts == 1) return go(epi);
+  const int ld = (a.np + 7) & ~7;
+  float* f = static_cast<float*>(sums);
+  const hipError_t e = go(PartEpi{f, a.np, a.nq, ld});
+  if (e != hipSuccess) return e;
+  return launch_join(a, f, ld, epi, st);
 }
 
 // ---- rows laid out anew ------------------------------------------------------------------
@@ -436,6 +636,11 @@ size_t take(Places& p, size_t bytes) {
 }
 Places places(int T, int I, int O, bool backward, bool makes) {
   Places p;
+  if (!backward && few_ok(O, T, I)) {  // (takes rows as they are)
+    const Choice c = {0, few_parts(O, T, I)};
+    p.sums = take(p, sums_bytes(c, O, T));
+    return p;
+  }
   if (I & 7) {
     p.x = take(p, rows_bytes(T, I));
     p.w = take(p, rows_bytes(O, I));
@@ -474,7 +679,9 @@ size_t dense_bwd_ws_bytes(int tokens, int inputs, int outputs, bool dz) {
   } while (0)
 
 hipError_t launch_dense_fwd(const DenseArgs& a, hipStream_t st) {
-  const int T = a.tokens, I = a.inputs, O = a.outputs, ld = whole8(I);
+  const int T = a.tokens, I = a.inputs, O = a.outputs;
+  const bool few = few_ok(O, T, I);
+  const int ld = few ? I : whole8(I);
   const Places at_ = places(T, I, O, false, false);
   const h16 *x = a.x, *w = a.w;
   if (ld != I) {
@@ -487,8 +694,8 @@ hipError_t launch_dense_fwd(const DenseArgs& a, hipStream_t st) {
   void* sums = at<void>(a.ws, at_.sums);
   const auto go = [&](auto act) {
     constexpr int ACT = decltype(act)::value;
-    return launch_product<kForward>(
-        p, LayerEpi<ACT>{a.bias, a.residual, a.y, a.z, O, T, a.drop}, sums, st);
+    const LayerEpi<ACT> epi = {a.bias, a.residual, a.y, a.z, O, T, a.drop};
+    return few ? launch_few(p, epi, sums, st) : launch_product<kForward>(p, epi, sums, st);
   };
   switch (a.act) {
     case kActRelu: return go(std::integral_constant<int, kActRelu>{});
