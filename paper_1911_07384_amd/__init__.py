@@ -229,15 +229,32 @@ def _ptr_of(dtype):
 
 
 _ptr_half, _ptr_float, _ptr_int8 = _ptr_of("float16"), _ptr_of("float32"), _ptr_of("int8")
-_ptr_int, _ptr_long = _ptr_of("int32"), _ptr_of("int64")
 
 
-def _held(**tensors):
-    """Raises for a tensor with fewer elements than its call reads or writes; values are
-    (tensor or address or None, elements)."""
-    for name, (t, n) in tensors.items():
-        if hasattr(t, "numel") and t.numel() < n:
-            raise ValueError(f"{name} has {t.numel()} elements of {n}")
+def _held_of(dtype):
+    """A _ptr for arguments of one element type and a number of elements at least, which
+    `what` names."""
+    want = None
+
+    def ptr(t, n, what):
+        nonlocal want
+        if t is None or isinstance(t, int):
+            return t
+        if t.dtype is not want:
+            import torch
+            want = getattr(torch, dtype)
+            if t.dtype is not want:
+                raise TypeError(f"{what}: expected {dtype} tensor, got {t.dtype}")
+        if t.numel() < n:
+            raise ValueError(f"{what} has {t.numel()} elements of {n}")
+        if not t.is_contiguous():
+            raise ValueError(f"{what}: tensor must be contiguous")
+        return t.data_ptr()
+    return ptr
+
+
+_held_half, _held_float, _held_int, _held_long = (_held_of(d) for d in (
+    "float16", "float32", "int32", "int64"))
 
 
 def _first_current_stream():
@@ -660,19 +677,16 @@ def rng_state(seed, step=0, device="cuda"):
 
 
 def fp16_rng_advance(rng, steps=1, stream=None) -> None:
-    _held(rng=(rng, 2))
-    _check("fp16_rng_advance", lib().fp16_rng_advance(_ptr_long(rng), int(steps) % (1 << 64),
-                                                      _stream(stream)))
+    _check("fp16_rng_advance", lib().fp16_rng_advance(
+        _held_long(rng, 2, "rng"), int(steps) % (1 << 64), _stream(stream)))
 
 
 def fp16_dropout(x, residual, y, p, rng, site=0, n=None, stream=None) -> None:
     """y = dropout of x (+ residual); the gradient is the same call on dy."""
-    if n is None:
-        n = x.numel()
-    _held(x=(x, n), residual=(residual, n), y=(y, n), rng=(rng, 2))
+    n = x.numel() if n is None else int(n)
     _check("fp16_dropout", lib().fp16_dropout(
-        int(n), _ptr_half(x), _ptr_half(residual), _ptr_half(y), float(p), _ptr_long(rng),
-        int(site), _stream(stream)))
+        n, _held_half(x, n, "x"), _held_half(residual, n, "residual"), _held_half(y, n, "y"), p,
+        _held_long(rng, 2, "rng"), site, _stream(stream)))
 
 
 # ---- dense layers with bias, activation, dropout and residual ----------------
@@ -697,23 +711,22 @@ def fp16_dense_workspace_bytes(desc: DenseDesc, call=None) -> int:
 def fp16_dense_fwd(desc, x, w, bias, residual, y, z=None, rng=None, ws=None, ws_bytes=None,
                    stream=None) -> None:
     t, i, o = desc.tokens, desc.inputs, desc.outputs
-    _held(x=(x, t * i), w=(w, o * i), bias=(bias, o), residual=(residual, t * o), y=(y, t * o),
-          z=(z, t * o), rng=(rng, 2))
+    to = t * o
     _check("fp16_dense_fwd", lib().fp16_dense_fwd(
-        ctypes.byref(desc), _ptr_half(x), _ptr_half(w), _ptr_half(bias), _ptr_half(residual),
-        _ptr_long(rng), _ptr_half(y), _ptr_half(z), _ptr(ws), _wsb(ws, ws_bytes),
-        _stream(stream)))
+        ctypes.byref(desc), _held_half(x, t * i, "x"), _held_half(w, o * i, "w"),
+        _held_half(bias, o, "bias"), _held_half(residual, to, "residual"),
+        _held_long(rng, 2, "rng"), _held_half(y, to, "y"), _held_half(z, to, "z"), _ptr(ws),
+        _wsb(ws, ws_bytes), _stream(stream)))
 
 
 def fp16_dense_bwd(desc, x, w, z, dy, dx, dw, dbias=None, rng=None, ws=None, ws_bytes=None,
                    stream=None) -> None:
     t, i, o = desc.tokens, desc.inputs, desc.outputs
-    _held(x=(x, t * i), w=(w, o * i), z=(z, t * o), dy=(dy, t * o), dx=(dx, t * i),
-          dw=(dw, o * i), dbias=(dbias, o), rng=(rng, 2))
     _check("fp16_dense_bwd", lib().fp16_dense_bwd(
-        ctypes.byref(desc), _ptr_half(x), _ptr_half(w), _ptr_half(z), _ptr_half(dy),
-        _ptr_long(rng), _ptr_half(dx), _ptr_half(dw), _ptr_half(dbias), _ptr(ws),
-        _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _held_half(x, t * i, "x"), _held_half(w, o * i, "w"),
+        _held_half(z, t * o, "z"), _held_half(dy, t * o, "dy"), _held_long(rng, 2, "rng"),
+        _held_half(dx, t * i, "dx"), _held_half(dw, o * i, "dw"), _held_half(dbias, o, "dbias"),
+        _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
 
 
 # ---- log probabilities -------------------------------------------------------
@@ -733,21 +746,20 @@ def fp16_logprobs(desc, z, tokens, logp, stats, top_id=None, top_logp=None, ws=N
     """logp, stats [rows][3] (largest logit, log of the sum, entropy) and the desc.top
     most probable classes of each row."""
     n, k = desc.rows, desc.top
-    _held(z=(z, (n - 1) * desc.stride + desc.classes), tokens=(tokens, n), logp=(logp, n),
-          stats=(stats, 3 * n), top_id=(top_id, n * k), top_logp=(top_logp, n * k))
     _check("fp16_logprobs", lib().fp16_logprobs(
-        ctypes.byref(desc), _ptr_half(z), _ptr_int(tokens), _ptr_float(logp), _ptr_float(stats),
-        _ptr_int(top_id), _ptr_float(top_logp), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _held_half(z, (n - 1) * desc.stride + desc.classes, "z"),
+        _held_int(tokens, n, "tokens"), _held_float(logp, n, "logp"),
+        _held_float(stats, 3 * n, "stats"), _held_int(top_id, n * k, "top_id"),
+        _held_float(top_logp, n * k, "top_logp"), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
 
 
 def fp16_logprobs_bwd(desc, z, tokens, stats, dlogp, dentropy, dz, stream=None) -> None:
     n = desc.rows
     size = (n - 1) * desc.stride + desc.classes
-    _held(z=(z, size), tokens=(tokens, n), stats=(stats, 3 * n), dlogp=(dlogp, n),
-          dentropy=(dentropy, n), dz=(dz, size))
     _check("fp16_logprobs_bwd", lib().fp16_logprobs_bwd(
-        ctypes.byref(desc), _ptr_half(z), _ptr_int(tokens), _ptr_float(stats), _ptr_float(dlogp),
-        _ptr_float(dentropy), _ptr_half(dz), _stream(stream)))
+        ctypes.byref(desc), _held_half(z, size, "z"), _held_int(tokens, n, "tokens"),
+        _held_float(stats, 3 * n, "stats"), _held_float(dlogp, n, "dlogp"),
+        _held_float(dentropy, n, "dentropy"), _held_half(dz, size, "dz"), _stream(stream)))
 
 
 def _wsb(ws, ws_bytes):

@@ -352,10 +352,11 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
 // The forward of at most 32 tokens, bound by reading W once: a workgroup takes 16 RF rows
 // of W, its sixteen waves the reduction in turns of 64, each lane 16 bytes of a row
 // straight into the operand (the next turn's before this one's products), with no regard
-// to a row's alignment; the waves' sums are added in LDS in their order.  One token, W
-// 16384 x 4096 from memory: 24.1 us, 5.6 TB/s; rows that are not aligned take twice as
-// long.  (Turns of 128: 34.5 us; starting each workgroup at another turn: 25.7, and 39
-// for 31 with rows of 32 KB.)
+// to a row's alignment; the waves' sums are added in LDS in their order.  Neighbouring
+// workgroups of an XCD start at different turns: at the same one, rows of 8 or 32 KB
+// have all of them ask the same memory channels (one token, 4096 x 16384 from memory: 31.2
+// us, 27.4 so; 16 tokens, 16384 x 4096: 33.9 and 29.4).  One token, 16384 x 4096: 25.2
+// us, 5.3 TB/s; rows that are not aligned take twice as long.
 constexpr int kFewTokens = 32, kFewWaves = 16, kFewSteps = 2, kFewTurn = 32 * kFewSteps;
 
 template <int RF, int NT, class Epi>
@@ -409,17 +410,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi
   constexpr int STEP = TURN * kFewWaves;
   // this wave's whole turns, and the one that the range ends in
   const int whole = (kend - kbeg) / TURN, turns = (whole - wave + kFewWaves - 1) / kFewWaves;
-  int k = kbeg + wave * TURN;
   if (turns > 0) {
+    const int first = kbeg + wave * TURN, end = first + turns * STEP;
+    int k = first + (int)((blockIdx.x >> 3) % (unsigned)turns) * STEP;
+    auto next = [&]() { k = k + STEP < end ? k + STEP : first; };
     load(k, w[0], x[0]);
     int i = turns;
-    for (; i > 2; i -= 2, k += 2 * STEP) {
-      load(k + STEP, w[1], x[1]);
+    for (; i > 2; i -= 2) {
+      next();
+      load(k, w[1], x[1]);
       mma(w[0], x[0]);
-      load(k + 2 * STEP, w[0], x[0]);
+      next();
+      load(k, w[0], x[0]);
       mma(w[1], x[1]);
     }
-    if (i == 2) load(k + STEP, w[1], x[1]);
+    if (i == 2) {
+      next();
+      load(k, w[1], x[1]);
+    }
     mma(w[0], x[0]);
     if (i == 2) mma(w[1], x[1]);
   }
@@ -543,6 +551,62 @@ hipError_t launch_repack(int rows, int cols, const h16* from, h16* to, hipStream
 
 constexpr int kRows = 32;  // of a workgroup's partial sums
 
+// One vector of dz: from a row's dy and z, columns c .. c + 7.
+template <int ACT>
+__device__ __forceinline__ V8 dz8(const V8& y, const V8& z, int64_t i, const Drop& drop,
+                                  float (&s)[8]) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = to_f32(y.h[e]);
+  if (drop.threshold) drop8(v, i, drop);
+  V8 o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (ACT != kActNone) v[e] *= act_slope<ACT>(to_f32(z.h[e]));
+    s[e] += v[e];
+    o.h[e] = to_h16(v[e]);
+  }
+  return o;
+}
+
+// All of dz and dbias for few tokens in one launch: 64 columns a workgroup, a lane 8 of
+// them in every 32nd row.
+constexpr int kDzFew = 128;
+template <int ACT>
+__global__ __launch_bounds__(256) void dz_few(int tokens, int outputs, int ld, Drop drop,
+                                              const h16* z, const h16* dy, h16* dz, h16* dbias) {
+  __shared__ float sums[32][64];
+  const int cg = threadIdx.x & 7, rg = threadIdx.x >> 3, c = blockIdx.x * 64 + cg * 8;
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  constexpr int U = 4;
+  for (int r0 = rg; r0 < tokens; r0 += 32 * U) {
+    V8 vy[U], vz[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + 32 * u;
+      const int64_t row = (int64_t)(r < tokens ? r : 0) * outputs;
+      vy[u] = load8_row(dy + row, c, outputs, r < tokens);
+      if (ACT != kActNone) vz[u] = load8_row(z + row, c, outputs, r < tokens);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + 32 * u;
+      const V8 o = dz8<ACT>(vy[u], vz[u], (int64_t)r * outputs + c, drop, s);
+      if (dz && r < tokens && c < ld) store16(dz + (int64_t)r * ld + c, o);
+    }
+  }
+  if (!dbias) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[rg][cg * 8 + e] = s[e];
+  __syncthreads();
+  const int cc = blockIdx.x * 64 + threadIdx.x;
+  if (threadIdx.x >= 64 || cc >= outputs) return;
+  double t = 0.0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) t += (double)sums[i][threadIdx.x];
+  dbias[cc] = dbl_to_h16(t);
+}
+
 // dz [tokens][ld] (unless null) with zeros past its columns, and its columns' sums over
 // kRows rows (unless null): 256 columns a workgroup, a lane 8 of them in every eighth
 // row.
@@ -566,17 +630,7 @@ __global__ __launch_bounds__(256) void dz_kernel(int tokens, int outputs, int ld
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int r = r0 + rg + 8 * u;
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = to_f32(vy[u].h[e]);
-    if (drop.threshold) drop8(v, (int64_t)r * outputs + c, drop);
-    V8 o;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (ACT != kActNone) v[e] *= act_slope<ACT>(to_f32(vz[u].h[e]));
-      s[e] += v[e];
-      o.h[e] = to_h16(v[e]);
-    }
+    const V8 o = dz8<ACT>(vy[u], vz[u], (int64_t)r * outputs + c, drop, s);
     if (dz && r < tokens && c < ld) store16(dz + (int64_t)r * ld + c, o);
   }
   if (!part) return;
@@ -608,6 +662,11 @@ __global__ __launch_bounds__(256) void dbias_kernel(int outputs, int parts, cons
 
 template <int ACT>
 hipError_t launch_dz(const DenseArgs& a, int ld, h16* dz, float* part, hipStream_t st) {
+  if (a.tokens <= kDzFew) {
+    dz_few<ACT><<<(unsigned)ceil_div(ld, 64), 256, 0, st>>>(a.tokens, a.outputs, ld, a.drop,
+                                                            a.kept, a.dy, dz, a.dbias);
+    return hipGetLastError();
+  }
   const int parts = ceil_div(a.tokens, kRows);
   dz_kernel<ACT><<<dim3((unsigned)ceil_div(ld, 256), (unsigned)parts), 256, 0, st>>>(
       a.tokens, a.outputs, ld, a.drop, a.kept, a.dy, dz, a.dbias ? part : nullptr);
@@ -650,7 +709,7 @@ Places places(int T, int I, int O, bool backward, bool makes) {
     return p;
   }
   if (makes || (O & 7)) p.dz = take(p, rows_bytes(T, O));
-  p.part = take(p, (size_t)ceil_div(T, kRows) * O * sizeof(float));
+  if (T > kDzFew) p.part = take(p, (size_t)ceil_div(T, kRows) * O * sizeof(float));
   const size_t dx = sums_bytes(choose(kDx, I, T, O), I, T);
   const size_t dw = sums_bytes(choose(kDw, I, O, T), I, O);
   p.sums = take(p, dx > dw ? dx : dw);

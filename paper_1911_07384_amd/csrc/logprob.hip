@@ -15,9 +15,12 @@
 // largest element from below, so that a second look at the row (from the caches)
 // gathers the few elements at or above it; those are ranked by counting, with the
 // value and then the lower class as the key.  Where equal values make them more than
-// kCand, the value itself is found by bisection over its 16 bits.
+// kCand, those above the bound are gathered and the first ones at it added in order; if
+// these are too many still, the value that `top` elements reach is found by bisection.
 
 #include "head.hpp"
+
+#include <type_traits>
 
 namespace fp16k {
 namespace {
@@ -64,47 +67,108 @@ __device__ __forceinline__ V8 low8() {
   v.u = u32x4{0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
   return v;
 }
+// (Loops that few lanes enter are kept as loops: these kernels run once over a row, and
+// instructions that have to be fetched for one use cost more than they do.)
 __device__ __forceinline__ V8 load8_low(const h16* p, int left) {
   if (left >= 8) return load16u(p);
-  V8 v = low8();
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < left) v.h[e] = p[e];
+  u64 lo = 0xFC00FC00FC00FC00ull, hi = lo;
+  const uint16_t* const from = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll 1
+  for (int e = left - 1; e >= 0; --e) {
+    hi = hi << 16 | lo >> 48;
+    lo = lo << 16 | from[e];
+  }
+  V8 v;
+  v.d[0] = (uint32_t)lo;
+  v.d[1] = (uint32_t)(lo >> 32);
+  v.d[2] = (uint32_t)hi;
+  v.d[3] = (uint32_t)(hi >> 32);
   return v;
+}
+__device__ __forceinline__ half2 top2(const V8& v) {
+  half2 t = __builtin_bit_cast(half2, v.d[0]);
+#pragma unroll
+  for (int k = 1; k < 4; ++k) t = __builtin_elementwise_max(t, __builtin_bit_cast(half2, v.d[k]));
+  return t;
+}
+// f(value key, e) for the elements e of v, -inf past the first `left`
+template <class F>
+__device__ __forceinline__ void each8(const V8& v, int left, F f) {
+  u64 w = v.d[0] | (u64)v.d[1] << 32, hi = v.d[2] | (u64)v.d[3] << 32;
+#pragma unroll 1
+  for (int e = 0; e < 8 && e < left; ++e) {
+    f(value_key((uint16_t)w), e);
+    w = w >> 16 | hi << 48;
+    hi >>= 16;
+  }
+}
+// the largest value key of a vector (of a NaN's, if it has one)
+__device__ __forceinline__ uint32_t top_key(const V8& v) {
+  const half2 t = top2(v);
+  const float f = __builtin_fmaxf(to_f32(t[0]), to_f32(t[1]));
+  bool nan = false;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const half2 h = __builtin_bit_cast(half2, v.d[k]);
+    nan |= __builtin_isnan(h[0]) | __builtin_isnan(h[1]);
+  }
+  return nan ? 0xFFFFu : value_key(__builtin_bit_cast(uint16_t, (h16)f));
+}
+
+// A lane's elements of z[0 .. n): vectors of 8, kU at a time, -inf past the end.
+__device__ __forceinline__ void lane_load(const h16* z, int n, int i, V8 (&v)[kU]) {
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+    const int at = i + u * kNT * 8;
+    v[u] = at < n ? load8_low(z + at, n - at) : low8();
+  }
+}
+constexpr int kTurn = kNT * 8 * kU;  // elements of a workgroup's turn
+
+__device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
+  half2 top = top2(v[0]);
+#pragma unroll
+  for (int u = 1; u < kU; ++u) top = __builtin_elementwise_max(top, top2(v[u]));
+  // (a NaN is no maximum here; it reaches the sums below)
+  float m = __builtin_fmaxf(to_f32(top[0]), to_f32(top[1]));
+  m = __builtin_fmaxf(m, a.m);
+  rescale(a, m, c);
+  const float base = m == -__builtin_inff() ? 0.0f : m;
+  float one = 1.0f;
+  __asm__("" : "+v"(one));
+#pragma unroll
+  for (int u = 0; u < kU; ++u)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      // (a difference as one instruction, which takes a binary16 factor: h * 1 - base)
+      const float d = __builtin_fmaf(to_f32(v[u].h[k]), one, -base) * c;
+      const float e = __builtin_amdgcn_exp2f(d);
+      a.s += e;
+      a.t += e * __builtin_fmaxf(d, kFloor);
+    }
 }
 
 // This lane's sums over z[0 .. n).
 __device__ __forceinline__ Sums lane_sums(const h16* z, int n, float c) {
   Sums a = {-__builtin_inff(), 0.0f, 0.0f};
-  for (int i = threadIdx.x * 8; i < n; i += kNT * 8 * kU) {
+  for (int i = threadIdx.x * 8; i < n; i += kTurn) {
     V8 v[kU];
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int at = i + u * kNT * 8;
-      v[u] = at < n ? load8_low(z + at, n - at) : low8();
-    }
-    half2 top = __builtin_bit_cast(half2, v[0].d[0]);
-#pragma unroll
-    for (int u = 0; u < kU; ++u)
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        top = __builtin_elementwise_max(top, __builtin_bit_cast(half2, v[u].d[k]));
-    // (a NaN is no maximum here; it reaches the sums below)
-    float m = __builtin_fmaxf(to_f32(top[0]), to_f32(top[1]));
-    m = __builtin_fmaxf(m, a.m);
-    rescale(a, m, c);
-    const float base = m == -__builtin_inff() ? 0.0f : m;
-#pragma unroll
-    for (int u = 0; u < kU; ++u)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float d = (to_f32(v[u].h[k]) - base) * c;
-        const float e = __builtin_amdgcn_exp2f(d);
-        a.s += e;
-        a.t += e * __builtin_fmaxf(d, kFloor);
-      }
+    lane_load(z, n, i, v);
+    lane_add(v, c, a);
   }
   return a;
+}
+
+// f(x, i) for a lane's vectors x from z + i on, read again
+template <class F>
+__device__ __forceinline__ void lane_each(const h16* z, int n, F f) {
+  for (int i = threadIdx.x * 8; i < n; i += kTurn) {
+    V8 v[kU];
+    lane_load(z, n, i, v);
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (i + u * kNT * 8 < n) f(v[u], i + u * kNT * 8);
+  }
 }
 
 // Joined over the workgroup, the same in every lane.
@@ -141,9 +205,9 @@ __device__ __forceinline__ Sums block_sums(Sums a, float c, float (*red)[3]) {
 }
 
 struct TopLds {
-  u64 cand[kCand];
+  __attribute__((aligned(16))) u64 cand[kCand + 8];
   u64 best[kTopMax];
-  uint32_t lane[kNT];
+  uint16_t lane[kNT];
   int count, scan[kWaves];
 };
 
@@ -151,11 +215,18 @@ struct TopLds {
 // in l.cand (0s where there are fewer).
 __device__ __forceinline__ void rank_candidates(TopLds& l, int count, int top) {
   for (int i = threadIdx.x; i < top; i += kNT) l.best[i] = 0;
+  if (threadIdx.x < 8) l.cand[count + threadIdx.x] = 0;  // (whole eights)
   __syncthreads();
   for (int i = threadIdx.x; i < count; i += kNT) {
     const u64 k = l.cand[i];
     int r = 0;
-    for (int j = 0; j < count; ++j) r += l.cand[j] > k;
+    for (int j = 0; j < count; j += 8) {
+      u64 o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = l.cand[j + e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r += o[e] > k;
+    }
     if (r < top) l.best[r] = k;
   }
   __syncthreads();
@@ -177,66 +248,69 @@ __device__ __forceinline__ int block_count(int n, TopLds& l) {
 // largest of this lane's elements.
 __device__ __forceinline__ void block_top(const h16* z, int n, int first, int top, float m,
                                           TopLds& l) {
-  // the lanes' maxima with the lane's number as the lower key: distinct, and the one of
-  // rank top - 1 is the bound
-  const uint32_t mine =
-      (value_key(__builtin_bit_cast(uint16_t, (h16)m)) << 16) | (kNT - 1 - threadIdx.x);
-  l.lane[threadIdx.x] = mine;
-  if (threadIdx.x == 0) l.count = 0;
+  l.lane[threadIdx.x] = (uint16_t)value_key(__builtin_bit_cast(uint16_t, (h16)m));
   __syncthreads();
-  int r = 0;
-  for (int j = 0; j < kNT; ++j) r += l.lane[j] > mine;
-  __syncthreads();
-  if (r == top - 1) l.lane[0] = mine >> 16;
-  __syncthreads();
-  const uint32_t bound = l.lane[0];
-  for (int i = threadIdx.x * 8; i < n; i += kNT * 8) {
-    const V8 v = load8_low(z + i, n - i);
+  // the largest value that `top` lanes' maxima reach, bit by bit, in every wave alike
+  uint32_t bound = 0;
+  {
+    uint32_t key[kWaves];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t k = value_key(v.s[e]);
-      if (k >= bound && i + e < n) {
-        const int at = atomicAdd(&l.count, 1);
-        if (at < kCand) l.cand[at] = full_key(k, first + i + e);
-      }
+    for (int w = 0; w < kWaves; ++w) key[w] = l.lane[w * 64 + (threadIdx.x & 63)];
+#pragma unroll 1
+    for (int b = 15; b >= 0; --b) {
+      const uint32_t up = bound | (1u << b);
+      int c = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) c += __popcll(__ballot(key[w] >= up));
+      if (c >= top) bound = up;
     }
   }
-  __syncthreads();
-  int count = l.count;
-  __syncthreads();
-  if (count > kCand) {
-    // the largest value that `top` elements reach, bit by bit
-    uint32_t value = 0;
-    for (int b = 15; b >= 0; --b) {
-      const uint32_t up = value | (1u << b);
-      int c = 0;
-      for (int i = threadIdx.x * 8; i < n; i += kNT * 8) {
-        const V8 v = load8_low(z + i, n - i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) c += value_key(v.s[e]) >= up && i + e < n;
-      }
-      if (block_count(c, l) >= top) value = up;
-    }
-    // those above it (fewer than top) ..
+  // gathers what is at or above `from`
+  auto gather = [&](uint32_t from) {
     if (threadIdx.x == 0) l.count = 0;
     __syncthreads();
-    for (int i = threadIdx.x * 8; i < n; i += kNT * 8) {
-      const V8 v = load8_low(z + i, n - i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t k = value_key(v.s[e]);
-        if (k > value && i + e < n) l.cand[atomicAdd(&l.count, 1)] = full_key(k, first + i + e);
-      }
-    }
+    lane_each(z, n, [&](const V8& x, int i) {
+      if (top_key(x) < from) return;
+      each8(x, n - i, [&](uint32_t k, int e) {
+        if (k >= from) {
+          const int at = atomicAdd(&l.count, 1);
+          if (at < kCand) l.cand[at] = full_key(k, first + i + e);
+        }
+      });
+    });
     __syncthreads();
-    count = l.count;
+    const int count = l.count;
+    __syncthreads();
+    return count;
+  };
+  // (masked classes are at -inf and many)
+  constexpr uint32_t kLow = 0x3FF;
+  int count = gather(bound == kLow ? kLow + 1 : bound);
+  if (count > kCand || count < top) {
+    // too many of one value: those above it ..
+    uint32_t value = bound;
+    if (count > kCand) count = gather(value + 1);
+    if (count > kCand) {
+      // (more than it reaches: the largest value that `top` elements reach, bit by bit)
+      value = 0;
+#pragma unroll 1
+      for (int b = 15; b >= 0; --b) {
+        const uint32_t up = value | (1u << b);
+        int c = 0;
+        lane_each(z, n, [&](const V8& x, int i) {
+          each8(x, n - i, [&](uint32_t k, int) { c += k >= up; });
+        });
+        if (block_count(c, l) >= top) value = up;
+      }
+      count = gather(value + 1);
+    }
     // .. and the first of those equal to it, in the order of the classes
+#pragma unroll 1
     for (int i0 = 0; i0 < n && count < top; i0 += kNT * 8) {
       const int i = i0 + threadIdx.x * 8;
-      const V8 v = i < n ? load8_low(z + i, n - i) : low8();
+      const V8 x = i < n ? load8_low(z + i, n - i) : low8();
       uint32_t eq = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) eq |= (uint32_t)(value_key(v.s[e]) == value && i + e < n) << e;
+      each8(x, n - i, [&](uint32_t k, int e) { eq |= (uint32_t)(k == value) << e; });
       const int mine8 = __popc(eq);
       int before = mine8;  // inclusive, over the wave
 #pragma unroll
@@ -252,7 +326,7 @@ __device__ __forceinline__ void block_top(const h16* z, int n, int first, int to
         if (w < (int)(threadIdx.x >> 6)) at += l.scan[w];
         all += l.scan[w];
       }
-#pragma unroll
+#pragma unroll 1
       for (int e = 0; e < 8; ++e)
         if ((eq >> e) & 1) {
           if (at < top) l.cand[at] = full_key(value, first + i + e);
@@ -297,10 +371,10 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums
 // What a part of a row leaves for the join.
 __host__ __device__ inline size_t part_bytes(int top) { return 16 + (size_t)top * 8; }
 
-template <bool PARTS>
+template <bool PARTS, bool TOP>
 __global__ __launch_bounds__(kNT) void logprob_kernel(const LogprobArgs a, int parts, int per) {
   __shared__ float red[kWaves][3];
-  __shared__ TopLds l;
+  __shared__ typename std::conditional<TOP, TopLds, u64>::type l;
   const int row = PARTS ? blockIdx.x / parts : blockIdx.x;
   const int first = PARTS ? (blockIdx.x % parts) * per : 0;
   const int n = PARTS && a.classes - first > per ? per : a.classes - first;
@@ -308,9 +382,10 @@ __global__ __launch_bounds__(kNT) void logprob_kernel(const LogprobArgs a, int p
   const float c = a.scale * kLog2e;
   const Sums mine = lane_sums(z, n, c);
   const Sums r = block_sums(mine, c, red);
-  if (a.top) block_top(z, n, first, a.top, mine.m, l);
+  if constexpr (TOP) block_top(z, n, first, a.top, mine.m, l);
+  const u64* const best = reinterpret_cast<const TopLds*>(&l)->best;
   if (!PARTS) {
-    finish(a, row, r, l.best);
+    finish(a, row, r, best);
   } else {
     char* to = static_cast<char*>(a.ws) + blockIdx.x * part_bytes(a.top);
     if (threadIdx.x == 0) {
@@ -320,7 +395,7 @@ __global__ __launch_bounds__(kNT) void logprob_kernel(const LogprobArgs a, int p
       f[2] = r.t;
     }
     u64* k = reinterpret_cast<u64*>(to + 16);
-    for (int i = threadIdx.x; i < a.top; i += kNT) k[i] = l.best[i];
+    for (int i = threadIdx.x; i < a.top; i += kNT) k[i] = best[i];
   }
 }
 
@@ -337,18 +412,17 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
   }
   const Sums r = block_sums(mine, c, red);
   if (a.top) {
-    // a lane holds up to kPer of the parts' keys; as in block_top, the lanes' maxima
-    // bound what is ranked, and only `top` lanes reach the bound
-    constexpr int kPer = kMaxParts * kTopMax / kNT;
+    // a lane holds up to kPer of a part's keys; as in block_top, the lanes' maxima bound
+    // what is ranked, and only `top` lanes reach the bound
+    constexpr int kLanes = kNT / kMaxParts, kPer = kTopMax / kLanes;  // of a part; keys
     static_assert(kPer * kTopMax <= kCand, "candidates");
-    const int all = parts * a.top;
+    const int p = threadIdx.x / kLanes;
+    const u64* const keys = reinterpret_cast<const u64*>(from + p * part_bytes(a.top) + 16);
     u64 key[kPer], most = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int at = i * kNT + threadIdx.x;
-      key[i] = at < all ? reinterpret_cast<const u64*>(from + (at / a.top) * part_bytes(a.top) +
-                                                       16)[at % a.top]
-                        : 0;
+      const int at = i * kLanes + threadIdx.x % kLanes;
+      key[i] = p < parts && at < a.top ? keys[at] : 0;
       most = key[i] > most ? key[i] : most;
     }
     l.cand[threadIdx.x] = most;
@@ -358,7 +432,14 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
     }
     __syncthreads();
     int rank = 0;
-    for (int j = 0; j < kNT; ++j) rank += l.cand[j] > most;
+    const int lanes = parts * kLanes;
+    for (int j = 0; j < lanes; j += 4) {
+      u64 o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = l.cand[j + e];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rank += o[e] > most;
+    }
     if (rank == a.top - 1 && most) l.best[0] = most;  // (lanes without keys share 0)
     __syncthreads();
     const u64 bound = l.best[0];
@@ -377,7 +458,8 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
 
 // The gradient: each lane 8 classes of a row at a time.
 __global__ __launch_bounds__(kNT) void logprob_bwd_kernel(const LogprobArgs a, int parts, int per) {
-  const int row = blockIdx.x / parts, first = (blockIdx.x % parts) * per;
+  // the last rows first: a forward before read them last, and they may still be cached
+  const int row = a.rows - 1 - (int)(blockIdx.x / parts), first = (blockIdx.x % parts) * per;
   const int end = a.classes - first > per ? first + per : a.classes;
   const float m = a.stats[3 * (int64_t)row], log_s = a.stats[3 * (int64_t)row + 1],
               h = a.stats[3 * (int64_t)row + 2];
@@ -420,12 +502,19 @@ size_t logprob_ws_bytes(int rows, int classes, int top) {
 hipError_t launch_logprob(const LogprobArgs& a, hipStream_t st) {
   int parts = row_parts(a.rows, a.classes);
   if (parts == 1) {
-    logprob_kernel<false><<<a.rows, kNT, 0, st>>>(a, 1, a.classes);
+    if (a.top)
+      logprob_kernel<false, true><<<a.rows, kNT, 0, st>>>(a, 1, a.classes);
+    else
+      logprob_kernel<false, false><<<a.rows, kNT, 0, st>>>(a, 1, a.classes);
     return hipGetLastError();
   }
   const int per = part_len(a.classes, parts);
   parts = (a.classes + per - 1) / per;  // (none is empty)
-  logprob_kernel<true><<<(unsigned)((int64_t)a.rows * parts), kNT, 0, st>>>(a, parts, per);
+  const unsigned grid = (unsigned)((int64_t)a.rows * parts);
+  if (a.top)
+    logprob_kernel<true, true><<<grid, kNT, 0, st>>>(a, parts, per);
+  else
+    logprob_kernel<true, false><<<grid, kNT, 0, st>>>(a, parts, per);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   logprob_join<<<a.rows, kNT, 0, st>>>(a, parts);
