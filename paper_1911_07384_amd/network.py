@@ -23,7 +23,12 @@ the classifier's bias and the BN parameters by SGD as before (``muon_products``:
 rounds the products' operands to binary16, 3 keeps 22 bits of them and takes twice as
 long);
 ``classifier="int8"`` runs the classifier's products in 8-bit integers
-(fp16_int8_dense_*), its weights quantised anew in every step.
+(fp16_int8_dense_*), its weights quantised anew in every step;
+``classifier="dense"`` runs them as one dense layer whose bias joins the product
+before its rounding (fp16_dense_*); ``dropout`` drops that share of the features
+before the classifier (fp16_dropout), its generator seeded with ``seed`` and advanced
+by one in every update.  ``predict`` and ``evaluate`` give the log probabilities, most
+probable classes and accuracies of the batch just loaded, without dropout.
 
 The step is an explicit program: a list of ``Op`` records, each one ABI call
 with named device buffers.  Running the list in order is one training step.
@@ -74,9 +79,13 @@ class ResNet50:
                  post_scale: float = 0.25, eps: float = 1e-5, stages=STAGES, device="cuda",
                  bn_swap: bool = False, zero_gamma_last: bool = False,
                  fuse_bn_stats: bool = True, optimizer: str = "sgd", classifier: str = "fp16",
-                 muon_lr: float = 0.02, muon_momentum: float = 0.95, muon_products: int = 1):
-        if optimizer not in ("sgd", "muon") or classifier not in ("fp16", "int8"):
+                 muon_lr: float = 0.02, muon_momentum: float = 0.95, muon_products: int = 1,
+                 dropout: float = 0.0):
+        if optimizer not in ("sgd", "muon") or classifier not in ("fp16", "int8", "dense"):
             raise ValueError(f"optimizer {optimizer!r}, classifier {classifier!r}")
+        if not 0.0 <= dropout <= 1.0:
+            raise ValueError(f"dropout {dropout}")
+        self.dropout = float(dropout)
         self.optimizer, self.classifier = optimizer, classifier
         self.muon_lr, self.muon_momentum, self.muon_products = muon_lr, muon_momentum, muon_products
         self.n, self.image, self.classes = n, image, classes
@@ -186,13 +195,25 @@ class ResNet50:
         gd = F.pool_desc(n, cin, h, h, h, h, 1, 0)
         self._buf("gap.y", (n, 1, 1, cin))
         self.fwd.append(Op("avgpool_fwd", "gap", {"desc": gd, "x": xname, "y": "gap.y"}))
-        self._conv("fc", self.buffers["gap.y"], "gap.y", cin, self.classes, 1, 1, 0)
+        self._feat = "gap.y"  # what the classifier reads
+        if self.dropout:
+            self._feat = "drop.y"
+            self._buf("drop.y", (n, 1, 1, cin))
+            self.buffers["rng"] = F.rng_state(self.seed, 0, self.dev)
+            self.fwd.append(Op("dropout", "drop", {"x": "gap.y", "y": "drop.y"}))
+        self._conv("fc", self.buffers[self._feat], self._feat, cin, self.classes, 1, 1, 0)
         if self.classifier == "int8":
             self._int8_classifier(cin)
+        elif self.classifier == "dense":
+            self._dense_classifier(cin)
         self._buf("loss", (n,), torch.float32)
         self._buf("fc.dy", (n, 1, 1, self.classes))
+        bias = "fc.bias"
+        if self.classifier == "dense":  # (joined the product)
+            bias = "fc.zero"
+            self._buf(bias, (self.classes,)).zero_()
         self.fwd.append(Op("softmax_ce", "loss", {"n": n, "k": self.classes, "z": "fc.y",
-                                                  "bias": "fc.bias", "labels": "labels",
+                                                  "bias": bias, "labels": "labels",
                                                   "loss": "loss", "dz": "fc.dy",
                                                   "dbias": "fc.dbias"}))
         self._last = xname
@@ -213,8 +234,17 @@ class ResNet50:
         self.fwd.append(Op("int8_weights", "fc", {"desc": d, "w": "fc", "wq": "fc.wq",
                                                   "sw": "fc.wq.scale", "wqt": "fc.wqt",
                                                   "swt": "fc.wqt.scale"}))
-        self.fwd.append(Op("int8_fwd", "fc", {"desc": d, "x": "gap.y", "wq": "fc.wq",
+        self.fwd.append(Op("int8_fwd", "fc", {"desc": d, "x": self._feat, "wq": "fc.wq",
                                               "sw": "fc.wq.scale", "y": "fc.y"}))
+
+    def _dense_classifier(self, cin):
+        """The classifier's forward as a dense layer (in place of the convolution just
+        planned)."""
+        d = F.dense_desc(self.n, cin, self.classes)
+        self._ws_need = max(self._ws_need, F.fp16_dense_workspace_bytes(d))
+        self.fwd.pop()
+        self.fwd.append(Op("dense_fwd", "fc", {"desc": d, "x": self._feat, "w": "fc",
+                                               "bias": "fc.bias", "y": "fc.y"}))
 
     def _fuse_bn_pool(self):
         """A BN + ReLU whose output only feeds the max pool that follows it
@@ -338,14 +368,20 @@ class ResNet50:
 
     def _plan_backward(self, gd, pd):
         # classifier: the loss kernel wrote fc.dy and the bias gradient
-        dgap = self._grad("gap.y")
+        dgap, dfeat = self._grad("gap.y"), self._grad(self._feat)
         if self.classifier == "int8":
             a = next(o for o in self.fwd if o.kind == "int8_weights").a
-            self.bwd.append(Op("int8_bwd", "fc", {"desc": a["desc"], "x": "gap.y", "dy": "fc.dy",
-                                                  "wqt": a["wqt"], "swt": a["swt"], "dx": dgap,
-                                                  "dw": "d:fc"}))
+            self.bwd.append(Op("int8_bwd", "fc", {"desc": a["desc"], "x": self._feat,
+                                                  "dy": "fc.dy", "wqt": a["wqt"], "swt": a["swt"],
+                                                  "dx": dfeat, "dw": "d:fc"}))
+        elif self.classifier == "dense":
+            a = next(o for o in self.fwd if o.kind == "dense_fwd").a
+            self.bwd.append(Op("dense_bwd", "fc", {"desc": a["desc"], "x": self._feat, "w": "fc",
+                                                   "dy": "fc.dy", "dx": dfeat, "dw": "d:fc"}))
         else:
             self._conv_bwd("fc", "fc.dy")
+        if self.dropout:
+            self.bwd.append(Op("dropout_bwd", "drop", {"dy": dfeat, "dx": dgap}))
         dlast = self._grad(self._last)
         self.bwd.append(Op("avgpool_bwd", "gap", {"desc": gd, "dy": dgap, "dx": dlast}))
         dout = dlast
@@ -451,6 +487,8 @@ class ResNet50:
             Op("sgd", "sgd_bn", {"w": self.bn_arena, "g": self.dbn_arena, "m": self.mbn_arena,
                                  "wd": 0.0}),
         ]
+        if self.dropout:
+            self.upd.append(Op("rng_advance", "rng", {}))
         self.n_weights, self.n_bn = nw, nb
 
     def _muon_op(self):
@@ -557,6 +595,17 @@ class ResNet50:
         elif k == "int8_bwd":
             F.fp16_int8_dense_bwd(a["desc"], t(a["x"]), t(a["dy"]), t(a["wqt"]), t(a["swt"]),
                                   t(a["dx"]), t(a["dw"]), None, ws)
+        elif k == "dense_fwd":
+            F.fp16_dense_fwd(a["desc"], t(a["x"]), t(a["w"]), t(a["bias"]), None, t(a["y"]), ws=ws)
+        elif k == "dense_bwd":
+            F.fp16_dense_bwd(a["desc"], t(a["x"]), t(a["w"]), None, t(a["dy"]), t(a["dx"]),
+                             t(a["dw"]), ws=ws)
+        elif k == "dropout":
+            F.fp16_dropout(t(a["x"]), None, t(a["y"]), self.dropout, t("rng"))
+        elif k == "dropout_bwd":
+            F.fp16_dropout(t(a["dy"]), None, t(a["dx"]), self.dropout, t("rng"))
+        elif k == "rng_advance":
+            F.fp16_rng_advance(t("rng"))
         elif k == "muon":
             F.fp16_muon_step(a["descs"], a["w"], a["g"], a["m"], self.muon_lr, self.muon_momentum,
                              self.wd, products=self.muon_products, ws=a["ws"])
@@ -583,7 +632,8 @@ class ResNet50:
                 "bn_maxpool_fwd": ("stats", "y", "idx"),
                 "softmax_ce": ("loss", "dz", "dbias"), "dgrad_filter": ("wf",),
                 "int8_weights": ("wq", "sw", "wqt", "swt"), "int8_fwd": ("y",),
-                "int8_bwd": ("dx", "dw")}
+                "int8_bwd": ("dx", "dw"), "dense_fwd": ("y",), "dense_bwd": ("dx", "dw"),
+                "dropout": ("y",), "dropout_bwd": ("dx",)}
 
     def _schedule(self):
         """For each weight gradient of the backward, the index (in bwd) of the
@@ -683,6 +733,40 @@ class ResNet50:
         self.backward()
         self.update()
 
+    # ---- predictions -----------------------------------------------------------------
+
+    def predict(self, top: int = 5):
+        """The forward of the loaded batch and what its logits say, as tensors: "logits"
+        [n, classes] (the classifier's dense layer on the features, without dropout),
+        "logp" [n] (of the labels), "stats" [n, 3] (largest logit, log of the sum,
+        entropy), "top_id" and "top_logp" [n, top].  BN uses this batch's statistics, as
+        in training."""
+        self.forward()
+        if self.side is not None:  # (the backward's filters, which no backward waits for)
+            torch.cuda.current_stream().wait_event(self._wf_ready)
+        n, k, cin = self.n, self.classes, self.buffers["gap.y"].shape[-1]
+        dense, lp = F.dense_desc(n, cin, k), F.logprob_desc(n, k, top=top)
+        ws = F.workspace(max(F.fp16_dense_workspace_bytes(dense, F.DENSE_FWD),
+                             F.fp16_logprobs_workspace_bytes(lp)), self.dev)
+        new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=self.dev)
+        out = {"logits": new(torch.float16, n, k), "logp": new(torch.float32, n),
+               "stats": new(torch.float32, n, 3), "top_id": new(torch.int32, n, top),
+               "top_logp": new(torch.float32, n, top)}
+        F.fp16_dense_fwd(dense, self.buffers["gap.y"], self.buffers["fc"], self.buffers["fc.bias"],
+                         None, out["logits"], ws=ws)
+        F.fp16_logprobs(lp, out["logits"], self.buffers["labels"], out["logp"], out["stats"],
+                        out["top_id"], out["top_logp"], ws=ws)
+        return out
+
+    def evaluate(self):
+        """Mean loss and entropy, and the shares of images whose label is the most
+        probable class and among the five most probable ones."""
+        out = self.predict(min(5, self.classes))
+        hit = out["top_id"] == self.buffers["labels"][:, None]
+        return {"loss": -out["logp"].mean().item(), "entropy": out["stats"][:, 2].mean().item(),
+                "top1": hit[:, 0].float().mean().item(),
+                "top5": hit.any(1).float().mean().item()}
+
     def calls(self):
         """(name, thunk) for every ABI call of one step, in order."""
         return [(f"{op.name}:{op.kind}", (lambda o=op: self.run(o))) for op in self.program()]
@@ -706,8 +790,12 @@ class ResNet50:
         return 3 * self.conv_flops() - 2 * stem.n * p * q * stem.k * stem.c * stem.r * stem.s
 
     def state(self):
-        return [t.clone() for t in (self.w_arena, self.mw_arena, self.bn_arena, self.mbn_arena)]
+        return [t.clone() for t in self._state()]
+
+    def _state(self):
+        kept = [self.w_arena, self.mw_arena, self.bn_arena, self.mbn_arena]
+        return kept + ([self.buffers["rng"]] if self.dropout else [])
 
     def load_state(self, st):
-        for t, v in zip((self.w_arena, self.mw_arena, self.bn_arena, self.mbn_arena), st):
+        for t, v in zip(self._state(), st):
             t.copy_(v)
