@@ -712,7 +712,7 @@ fp16_status fp16_dense_bwd(const fp16_dense_desc* desc, const fp16_t* x, const f
 typedef struct {
   int32_t rows, classes; /* 1 <= rows < 2^24, 1 <= classes <= 2^20 */
   int32_t stride;        /* classes <= stride <= 2^21, rows * stride < 2^35 */
-  float scale;           /* positive, finite */
+  float scale;           /* positive, at most 1e30 */
   int32_t top;           /* most probable classes: 0 to FP16_LOGPROB_TOP_MAX, <= classes */
 } fp16_logprob_desc;
 

@@ -6,8 +6,6 @@
 #include "api_util.hpp"
 #include "head.hpp"
 
-#include <math.h>
-
 using namespace fp16k;
 
 namespace {
@@ -77,7 +75,7 @@ DenseArgs dense_args(const fp16_dense_desc* d, const uint64_t* rng, void* ws) {
 bool logprob_ok(const fp16_logprob_desc* d) {
   return d->rows >= 1 && d->rows < (1 << 24) && d->classes >= 1 && d->classes <= kMaxSide &&
          d->stride >= d->classes && d->stride <= 2 * kMaxSide &&
-         (int64_t)d->rows * d->stride < kMaxElems && isfinite(d->scale) && d->scale > 0.0f &&
+         (int64_t)d->rows * d->stride < kMaxElems && d->scale > 0.0f && d->scale <= 1e30f &&
          d->top >= 0 && d->top <= FP16_LOGPROB_TOP_MAX && d->top <= d->classes;
 }
 

@@ -9,7 +9,7 @@
 // One pass over the row holds m, S and T by lane (each further group of elements may
 // raise m, which scales S and T down), and they are joined over the lanes and, where
 // few long rows are split over workgroups, over the parts.  The differences z_j - m
-// of binary16 values are taken before the scale, which keeps logits of any size.
+// lose nothing to the size of the logits (see Sums).
 //
 // The most probable classes: the top-th largest of the lanes' maxima bounds the top-th
 // largest element from below, so that a second look at the row (from the caches)
@@ -47,13 +47,17 @@ __device__ __forceinline__ u64 full_key(uint32_t value, int cls) {
   return ((u64)value << 32) | (0xFFFFFFFFu - (uint32_t)cls);
 }
 
+// The sums are taken relative to r = fl(m c), c = fl(scale / ln 2), not to m c: with it a
+// term's exponent z c - r is one instruction with one rounding (a factor may be
+// binary16), and what r is off by, known exactly, is put right at the end:
+//   log sum exp(scale (z - m)) = log s + ln 2 (r - m c),  H = log s - ln 2 t / s.
 struct Sums {
   float m, s, t;  // m: a binary16 value; t in units of ln 2
 };
 
 // exponent by which sums of maximum m count towards a maximum of top
 __device__ __forceinline__ float shift(float m, float top, float c) {
-  return __builtin_fmaxf((m - top) * c, kFloor);  // (the floor also where both are -inf)
+  return __builtin_fmaxf(m * c - top * c, kFloor);  // (the floor also where both are -inf)
 }
 __device__ __forceinline__ void rescale(Sums& a, float top, float c) {
   const float d = shift(a.m, top, c), f = __builtin_amdgcn_exp2f(d);
@@ -133,18 +137,15 @@ __device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
   float m = __builtin_fmaxf(to_f32(top[0]), to_f32(top[1]));
   m = __builtin_fmaxf(m, a.m);
   rescale(a, m, c);
-  const float base = m == -__builtin_inff() ? 0.0f : m;
-  float one = 1.0f;
-  __asm__("" : "+v"(one));
+  const float r = m == -__builtin_inff() ? 0.0f : m * c;
 #pragma unroll
   for (int u = 0; u < kU; ++u)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      // (a difference as one instruction, which takes a binary16 factor: h * 1 - base)
-      const float d = __builtin_fmaf(to_f32(v[u].h[k]), one, -base) * c;
+      const float d = __builtin_fmaf(to_f32(v[u].h[k]), c, -r);
       const float e = __builtin_amdgcn_exp2f(d);
       a.s += e;
-      a.t += e * __builtin_fmaxf(d, kFloor);
+      a.t = __builtin_fmaf(e, __builtin_fmaxf(d, kFloor), a.t);
     }
 }
 
@@ -343,11 +344,12 @@ __device__ __forceinline__ void block_top(const h16* z, int n, int first, int to
 __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums& r,
                                        const u64* best) {
   const bool none = r.s == 0.0f;  // every class is at -inf
-  const float log_s = logf(r.s);
+  const float c = a.scale * kLog2e, ln = logf(r.s);
+  const float log_s = __builtin_fmaf(kLn2, __builtin_fmaf(-r.m, c, r.m * c), ln);
   if (threadIdx.x == 0) {
     a.stats[3 * (int64_t)row] = r.m;
     a.stats[3 * (int64_t)row + 1] = none ? -__builtin_inff() : log_s;
-    a.stats[3 * (int64_t)row + 2] = none ? 0.0f : log_s - kLn2 * (r.t / r.s);
+    a.stats[3 * (int64_t)row + 2] = none ? 0.0f : ln - kLn2 * (r.t / r.s);
     if (a.logp) {
       const int t = a.token[row];
       float lp = 0.0f;

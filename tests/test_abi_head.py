@@ -115,7 +115,7 @@ def test_logprob_refusals():
     L = F.logprob_desc
     for d in [L(0, 10), L(10, 0), L(-1, 5), L(1 << 24, 1), L(1, (1 << 20) + 1), L(4, 10, stride=9),
               L(4, 10, stride=(1 << 21) + 1), L((1 << 24) - 1, 4096), L(4, 10, scale=0.0),
-              L(4, 10, scale=-1.0), L(4, 10, scale=NAN), L(4, 10, scale=INF), L(4, 10, top=-1),
+              L(4, 10, scale=-1.0), L(4, 10, scale=NAN), L(4, 10, scale=INF), L(4, 10, scale=2e30), L(4, 10, top=-1),
               L(4, 10, top=11), L(4, 100, top=65)]:
         assert logp(d, ti=E, tl=G) == SHAPE and logb(d) == SHAPE
         assert F.lib().fp16_logprobs_workspace_bytes(ctypes.byref(d)) == 0
