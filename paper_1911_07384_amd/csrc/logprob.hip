@@ -15,8 +15,8 @@
 // largest element from below, so that a second look at the row (from the caches)
 // gathers the few elements at or above it; those are ranked by counting, with the
 // value and then the lower class as the key.  Where equal values make them more than
-// kCand, those above the bound are gathered and the first ones at it added in order; if
-// these are too many still, the value that `top` elements reach is found by bisection.
+// kCand, the value that `top` elements reach is found by bisection, those above it are
+// gathered and the first ones at it added in order.
 
 #include "head.hpp"
 
@@ -25,7 +25,9 @@
 namespace fp16k {
 namespace {
 
-constexpr int kNT = 256, kWaves = kNT / 64, kU = 4;
+// Threads of a workgroup, NT: 256, and 512 for whole rows of more than kLong classes, of
+// which fewer are then read at a time (4096 x 50001: 96 us with 256, 89 with 512).
+constexpr int kNT = 256, kU = 4, kLong = 16384;
 constexpr int kCand = 1024;
 constexpr int kPart = 4096, kMaxParts = 64;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -120,14 +122,14 @@ __device__ __forceinline__ uint32_t top_key(const V8& v) {
 }
 
 // A lane's elements of z[0 .. n): vectors of 8, kU at a time, -inf past the end.
+template <int NT>
 __device__ __forceinline__ void lane_load(const h16* z, int n, int i, V8 (&v)[kU]) {
 #pragma unroll
   for (int u = 0; u < kU; ++u) {
-    const int at = i + u * kNT * 8;
+    const int at = i + u * NT * 8;
     v[u] = at < n ? load8_low(z + at, n - at) : low8();
   }
 }
-constexpr int kTurn = kNT * 8 * kU;  // elements of a workgroup's turn
 
 __device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
   half2 top = top2(v[0]);
@@ -149,40 +151,59 @@ __device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
     }
 }
 
-// This lane's sums over z[0 .. n).
-__device__ __forceinline__ Sums lane_sums(const h16* z, int n, float c) {
+// This lane's sums over z[0 .. n); v holds the last turn's elements.
+template <int NT>
+__device__ __forceinline__ Sums lane_sums(const h16* z, int n, float c, V8 (&v)[kU]) {
   Sums a = {-__builtin_inff(), 0.0f, 0.0f};
-  for (int i = threadIdx.x * 8; i < n; i += kTurn) {
-    V8 v[kU];
-    lane_load(z, n, i, v);
+  for (int i = threadIdx.x * 8; i < n; i += NT * 8 * kU) {
+    lane_load<NT>(z, n, i, v);
     lane_add(v, c, a);
   }
   return a;
 }
 
-// f(x, i) for a lane's vectors x from z + i on, read again
-template <class F>
-__device__ __forceinline__ void lane_each(const h16* z, int n, F f) {
-  for (int i = threadIdx.x * 8; i < n; i += kTurn) {
-    V8 v[kU];
-    lane_load(z, n, i, v);
+// f(x, i) for a lane's vectors x from z + i on, read again if they are not all in v
+template <int NT, class F>
+__device__ __forceinline__ void lane_each(const h16* z, int n, V8 (&v)[kU], F f) {
+  for (int i = threadIdx.x * 8; i < n; i += NT * 8 * kU) {
+    if (n > NT * 8 * kU) lane_load<NT>(z, n, i, v);
 #pragma unroll
     for (int u = 0; u < kU; ++u)
-      if (i + u * kNT * 8 < n) f(v[u], i + u * kNT * 8);
+      if (i + u * NT * 8 < n) f(v[u], i + u * NT * 8);
   }
 }
 
+// Over the 64 lanes of a wave, in every one of them, by register permutes alone: quads,
+// eights, sixteens, the rows of 16 and the halves.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL,
+                                                               0xf, 0xf, false));
+}
+template <class F>
+__device__ __forceinline__ float wave_all(float v, F f) {
+  v = f(v, dpp<0xB1>(v));   // lanes 1 0 3 2 of each quad
+  v = f(v, dpp<0x4E>(v));   // 2 3 0 1
+  v = f(v, dpp<0x141>(v));  // 7 .. 0 of each eight
+  v = f(v, dpp<0x140>(v));  // 15 .. 0 of each sixteen
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  v = f(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+  const uint32_t d = __builtin_bit_cast(uint32_t, v);
+  const auto q = __builtin_amdgcn_permlane32_swap(d, d, false, false);
+  return f(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
+
 // Joined over the workgroup, the same in every lane.
+template <int NT>
 __device__ __forceinline__ Sums block_sums(Sums a, float c, float (*red)[3]) {
-  float m = a.m;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, o, 64));
+  constexpr int kWaves = NT / 64;
+  const auto larger = [](float x, float y) { return __builtin_fmaxf(x, y); };
+  const auto sum = [](float x, float y) { return x + y; };
+  float m = wave_all(a.m, larger);
   rescale(a, m, c);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    a.s += __shfl_xor(a.s, o, 64);
-    a.t += __shfl_xor(a.t, o, 64);
-  }
+  a.s = wave_all(a.s, sum);
+  a.t = wave_all(a.t, sum);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
     red[wave][0] = a.m;
@@ -205,20 +226,22 @@ __device__ __forceinline__ Sums block_sums(Sums a, float c, float (*red)[3]) {
   return r;
 }
 
+template <int NT>
 struct TopLds {
   __attribute__((aligned(16))) u64 cand[kCand + 8];
   u64 best[kTopMax];
-  uint16_t lane[kNT];
-  int count, scan[kWaves];
+  uint16_t lane[NT];
+  int count, scan[NT / 64];
 };
 
 // A workgroup's `top` largest keys into l.best, in order, from `count` distinct ones
 // in l.cand (0s where there are fewer).
-__device__ __forceinline__ void rank_candidates(TopLds& l, int count, int top) {
-  for (int i = threadIdx.x; i < top; i += kNT) l.best[i] = 0;
+template <int NT>
+__device__ __forceinline__ void rank_candidates(TopLds<NT>& l, int count, int top) {
+  for (int i = threadIdx.x; i < top; i += NT) l.best[i] = 0;
   if (threadIdx.x < 8) l.cand[count + threadIdx.x] = 0;  // (whole eights)
   __syncthreads();
-  for (int i = threadIdx.x; i < count; i += kNT) {
+  for (int i = threadIdx.x; i < count; i += NT) {
     const u64 k = l.cand[i];
     int r = 0;
     for (int j = 0; j < count; j += 8) {
@@ -233,32 +256,36 @@ __device__ __forceinline__ void rank_candidates(TopLds& l, int count, int top) {
   __syncthreads();
 }
 
-__device__ __forceinline__ int block_count(int n, TopLds& l) {
+template <int NT>
+__device__ __forceinline__ int block_count(int n, TopLds<NT>& l) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
   if ((threadIdx.x & 63) == 0) l.scan[threadIdx.x >> 6] = n;
   __syncthreads();
   n = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) n += l.scan[w];
+  for (int w = 0; w < NT / 64; ++w) n += l.scan[w];
   __syncthreads();
   return n;
 }
 
 // The `top` largest elements of z[0 .. n), classes first + i, into l.best.  m: the
-// largest of this lane's elements.
+// largest of this lane's elements, v as lane_sums left it.
+template <int NT>
 __device__ __forceinline__ void block_top(const h16* z, int n, int first, int top, float m,
-                                          TopLds& l) {
+                                          V8 (&v)[kU], TopLds<NT>& l) {
+  constexpr int kWaves = NT / 64;
   l.lane[threadIdx.x] = (uint16_t)value_key(__builtin_bit_cast(uint16_t, (h16)m));
   __syncthreads();
-  // the largest value that `top` lanes' maxima reach, bit by bit, in every wave alike
+  // the largest value that `top` lanes' maxima reach, to its highest twelve bits (1.6 %,
+  // and a few more candidates), bit by bit, in every wave alike
   uint32_t bound = 0;
   {
     uint32_t key[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) key[w] = l.lane[w * 64 + (threadIdx.x & 63)];
 #pragma unroll 1
-    for (int b = 15; b >= 0; --b) {
+    for (int b = 15; b >= 4; --b) {
       const uint32_t up = bound | (1u << b);
       int c = 0;
 #pragma unroll
@@ -270,7 +297,7 @@ __device__ __forceinline__ void block_top(const h16* z, int n, int first, int to
   auto gather = [&](uint32_t from) {
     if (threadIdx.x == 0) l.count = 0;
     __syncthreads();
-    lane_each(z, n, [&](const V8& x, int i) {
+    lane_each<NT>(z, n, v, [&](const V8& x, int i) {
       if (top_key(x) < from) return;
       each8(x, n - i, [&](uint32_t k, int e) {
         if (k >= from) {
@@ -286,28 +313,28 @@ __device__ __forceinline__ void block_top(const h16* z, int n, int first, int to
   };
   // (masked classes are at -inf and many)
   constexpr uint32_t kLow = 0x3FF;
+  if (bound <= kLow) bound = kLow;  // (no value is below)
   int count = gather(bound == kLow ? kLow + 1 : bound);
   if (count > kCand || count < top) {
     // too many of one value: those above it ..
     uint32_t value = bound;
-    if (count > kCand) count = gather(value + 1);
     if (count > kCand) {
-      // (more than it reaches: the largest value that `top` elements reach, bit by bit)
+      // (the largest value that `top` elements reach, bit by bit)
       value = 0;
 #pragma unroll 1
       for (int b = 15; b >= 0; --b) {
         const uint32_t up = value | (1u << b);
         int c = 0;
-        lane_each(z, n, [&](const V8& x, int i) {
+        lane_each<NT>(z, n, v, [&](const V8& x, int i) {
           each8(x, n - i, [&](uint32_t k, int) { c += k >= up; });
         });
-        if (block_count(c, l) >= top) value = up;
+        if (block_count<NT>(c, l) >= top) value = up;
       }
       count = gather(value + 1);
     }
     // .. and the first of those equal to it, in the order of the classes
 #pragma unroll 1
-    for (int i0 = 0; i0 < n && count < top; i0 += kNT * 8) {
+    for (int i0 = 0; i0 < n && count < top; i0 += NT * 8) {
       const int i = i0 + threadIdx.x * 8;
       const V8 x = i < n ? load8_low(z + i, n - i) : low8();
       uint32_t eq = 0;
@@ -337,10 +364,11 @@ __device__ __forceinline__ void block_top(const h16* z, int n, int first, int to
       __syncthreads();
     }
   }
-  rank_candidates(l, count, top);
+  rank_candidates<NT>(l, count, top);
 }
 
 // What a row's sums and largest keys give.
+template <int NT>
 __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums& r,
                                        const u64* best) {
   const bool none = r.s == 0.0f;  // every class is at -inf
@@ -361,7 +389,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums
       a.logp[row] = lp;
     }
   }
-  for (int i = threadIdx.x; i < a.top; i += kNT) {
+  for (int i = threadIdx.x; i < a.top; i += NT) {
     const u64 k = best[i];
     const float v = key_value((uint32_t)(k >> 32));
     a.top_id[(int64_t)row * a.top + i] = (int32_t)(0xFFFFFFFFu - (uint32_t)k);
@@ -373,21 +401,25 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums
 // What a part of a row leaves for the join.
 __host__ __device__ inline size_t part_bytes(int top) { return 16 + (size_t)top * 8; }
 
-template <bool PARTS, bool TOP>
-__global__ __launch_bounds__(kNT) void logprob_kernel(const LogprobArgs a, int parts, int per) {
-  __shared__ float red[kWaves][3];
-  __shared__ typename std::conditional<TOP, TopLds, u64>::type l;
+template <int NT, bool PARTS, bool TOP>
+__global__ __launch_bounds__(NT) void logprob_kernel(const LogprobArgs a, int parts, int per) {
+  __shared__ float red[NT / 64][3];
+  __shared__ typename std::conditional<TOP, TopLds<NT>, u64>::type l;
   const int row = PARTS ? blockIdx.x / parts : blockIdx.x;
   const int first = PARTS ? (blockIdx.x % parts) * per : 0;
   const int n = PARTS && a.classes - first > per ? per : a.classes - first;
   const h16* z = a.z + row * a.stride + first;
   const float c = a.scale * kLog2e;
-  const Sums mine = lane_sums(z, n, c);
-  const Sums r = block_sums(mine, c, red);
-  if constexpr (TOP) block_top(z, n, first, a.top, mine.m, l);
-  const u64* const best = reinterpret_cast<const TopLds*>(&l)->best;
+  V8 v[kU];
+  const Sums mine = lane_sums<NT>(z, n, c, v);
+  const Sums r = block_sums<NT>(mine, c, red);
+  const u64* best = nullptr;
+  if constexpr (TOP) {
+    block_top<NT>(z, n, first, a.top, mine.m, v, l);
+    best = l.best;
+  }
   if (!PARTS) {
-    finish(a, row, r, best);
+    finish<NT>(a, row, r, best);
   } else {
     char* to = static_cast<char*>(a.ws) + blockIdx.x * part_bytes(a.top);
     if (threadIdx.x == 0) {
@@ -397,13 +429,13 @@ __global__ __launch_bounds__(kNT) void logprob_kernel(const LogprobArgs a, int p
       f[2] = r.t;
     }
     u64* k = reinterpret_cast<u64*>(to + 16);
-    for (int i = threadIdx.x; i < a.top; i += kNT) k[i] = best[i];
+    for (int i = threadIdx.x; i < a.top; i += NT) k[i] = best[i];
   }
 }
 
 __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int parts) {
-  __shared__ float red[kWaves][3];
-  __shared__ TopLds l;
+  __shared__ float red[kNT / 64][3];
+  __shared__ TopLds<kNT> l;
   const int row = blockIdx.x;
   const float c = a.scale * kLog2e;
   const char* from = static_cast<const char*>(a.ws) + (int64_t)row * parts * part_bytes(a.top);
@@ -412,7 +444,7 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
     const float* f = reinterpret_cast<const float*>(from + threadIdx.x * part_bytes(a.top));
     mine = {f[0], f[1], f[2]};
   }
-  const Sums r = block_sums(mine, c, red);
+  const Sums r = block_sums<kNT>(mine, c, red);
   if (a.top) {
     // a lane holds up to kPer of a part's keys; as in block_top, the lanes' maxima bound
     // what is ranked, and only `top` lanes reach the bound
@@ -435,12 +467,12 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
     __syncthreads();
     int rank = 0;
     const int lanes = parts * kLanes;
-    for (int j = 0; j < lanes; j += 4) {
-      u64 o[4];
+    for (int j = 0; j < lanes; j += 16) {  // (parts past the last hold zeros)
+      u64 o[16];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = l.cand[j + e];
+      for (int e = 0; e < 16; ++e) o[e] = l.cand[j + e];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) rank += o[e] > most;
+      for (int e = 0; e < 16; ++e) rank += o[e] > most;
     }
     if (rank == a.top - 1 && most) l.best[0] = most;  // (lanes without keys share 0)
     __syncthreads();
@@ -453,9 +485,9 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
         if (at < kCand) l.cand[at] = key[i];
       }
     __syncthreads();
-    rank_candidates(l, l.count < kCand ? l.count : kCand, a.top);
+    rank_candidates<kNT>(l, l.count < kCand ? l.count : kCand, a.top);
   }
-  finish(a, row, r, l.best);
+  finish<kNT>(a, row, r, l.best);
 }
 
 // The gradient: each lane 8 classes of a row at a time.
@@ -503,20 +535,29 @@ size_t logprob_ws_bytes(int rows, int classes, int top) {
 
 hipError_t launch_logprob(const LogprobArgs& a, hipStream_t st) {
   int parts = row_parts(a.rows, a.classes);
-  if (parts == 1) {
-    if (a.top)
-      logprob_kernel<false, true><<<a.rows, kNT, 0, st>>>(a, 1, a.classes);
-    else
-      logprob_kernel<false, false><<<a.rows, kNT, 0, st>>>(a, 1, a.classes);
-    return hipGetLastError();
-  }
   const int per = part_len(a.classes, parts);
   parts = (a.classes + per - 1) / per;  // (none is empty)
   const unsigned grid = (unsigned)((int64_t)a.rows * parts);
-  if (a.top)
-    logprob_kernel<true, true><<<grid, kNT, 0, st>>>(a, parts, per);
-  else
-    logprob_kernel<true, false><<<grid, kNT, 0, st>>>(a, parts, per);
+  const auto go = [&](auto nt, auto split, auto top) {
+    constexpr int NT = decltype(nt)::value;
+    logprob_kernel<NT, decltype(split)::value, decltype(top)::value>
+        <<<grid, NT, 0, st>>>(a, parts, per);
+  };
+  const auto pick = [&](auto nt, auto split) {
+    if (a.top)
+      go(nt, split, std::true_type{});
+    else
+      go(nt, split, std::false_type{});
+  };
+  constexpr std::integral_constant<int, 256> small{};
+  if (parts == 1) {
+    if (a.classes > kLong)
+      pick(std::integral_constant<int, 512>{}, std::false_type{});
+    else
+      pick(small, std::false_type{});
+    return hipGetLastError();
+  }
+  pick(small, std::true_type{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   logprob_join<<<a.rows, kNT, 0, st>>>(a, parts);
