@@ -260,6 +260,7 @@ using Cfg = DenseCfg<WP, WQ, 8, TQ, S, OCC, L != kForward, L == kDw>;
 //                                 waves  tiles  stages  workgroups a CU
 template <Layout L> using Cfg256 = Cfg<L, 2, 4, 4, 2, 1>;  // 256 x 256
 template <Layout L> using Cfg128 = Cfg<L, 1, 4, 2, 2, 2>;  // 128 x 128
+template <Layout L> using Cfg128d = Cfg<L, 1, 4, 2, 4, 1>;  // .. loads further ahead
 template <Layout L> using Cfg64 = Cfg<L, 1, 4, 1, 3, 2>;   // 128 x 64
 
 template <class Epi>
@@ -292,21 +293,25 @@ hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {
 // with up to 32 parts.  What it chooses for them takes 1.4 % longer than the best choice
 // (geometric mean; 13 % at most).  For the largest the 256 x 256 tile's slices cost 1.5
 // us for four times the outputs that the others do in 0.49 (128 x 128) or 0.62 us.
+// One workgroup a CU of 128 x 128 is held up by its loads with two stages: with four a
+// forward's slice takes 0.50 us (2048 x 2048 x 2048 26.0 -> 22.7 us; the other layouts
+// gain nothing).
 struct Choice {
-  int side, parts;
+  int side, stages, parts;
 };
 struct Tile {
-  int side, occ;
+  int side, stages, occ;
   double one, two, ends;
 };
 Choice choose(Layout l, int64_t np, int64_t nq, int64_t nk) {
-  static const Tile tiles[3][3] = {
-      {{256, 1, 1.48, 0, 12}, {128, 2, 0.58, 0.97, 5.5}, {64, 2, 0.30, 0.62, 4.7}},
-      {{256, 1, 1.55, 0, 12}, {128, 2, 0.70, 1.12, 5.5}, {64, 2, 0.42, 0.79, 4.7}},
-      {{256, 1, 1.60, 0, 12}, {128, 2, 0.78, 1.20, 5.5}, {0, 0, 0, 0, 0}}};
+  static const Tile tiles[3][4] = {
+      {{256, 2, 1, 1.48, 0, 12}, {128, 2, 2, 0.58, 0.97, 5.5}, {64, 3, 2, 0.30, 0.62, 4.7},
+       {128, 4, 1, 0.50, 0, 5.5}},
+      {{256, 2, 1, 1.55, 0, 12}, {128, 2, 2, 0.70, 1.12, 5.5}, {64, 3, 2, 0.42, 0.79, 4.7}},
+      {{256, 2, 1, 1.60, 0, 12}, {128, 2, 2, 0.78, 1.20, 5.5}}};
   const double launch = 4.0, join = 2.5, bytes = 4.5e6;  // (bytes a microsecond)
   const int64_t slices = ceil_div64(nk, 64);
-  Choice best = {128, 1};
+  Choice best = {128, 2, 1};
   double least = 1e300;
   for (const Tile& t : tiles[l]) {
     if (!t.side) continue;
@@ -325,7 +330,7 @@ Choice choose(Layout l, int64_t np, int64_t nq, int64_t nk) {
       if (parts > 1) us += join + (double)(parts * np * nq * 8) / bytes;
       if (us < least) {
         least = us;
-        best = {t.side, (int)parts};
+        best = {t.side, t.stages, (int)parts};
       }
     }
   }
@@ -343,6 +348,8 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
   float* f = static_cast<float*>(sums);
   if constexpr (L != kDw)
     if (c.side == 64) return run<Cfg64<L>>(a, epi, f, st);
+  if constexpr (L == kForward)
+    if (c.side == 128 && c.stages == 4) return run<Cfg128d<L>>(a, epi, f, st);
   if (c.side == 256) return run<Cfg256<L>>(a, epi, f, st);
   return run<Cfg128<L>>(a, epi, f, st);
 }
@@ -531,19 +538,29 @@ hipError_t launch_few(Product a, const Epi& epi, void* sums, hipStream_t st) {
 
 // ---- rows laid out anew ------------------------------------------------------------------
 
-// Rows whose length is no multiple of 8, to rows that are, zeros behind them.
-__global__ __launch_bounds__(256) void repack_kernel(int rows, int cols, int ld, const h16* from,
-                                                     h16* to) {
+// Rows whose length is no multiple of 8, to rows that are, zeros behind them; of up to two
+// matrices with rows of one length in a launch (a second one took 3 us).
+struct Repack {
+  int rows;
+  const h16* from;
+  h16* to;
+};
+__global__ __launch_bounds__(256) void repack_kernel(int cols, int ld, const Repack one,
+                                                     const Repack two) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int per = ld / 8;
-  const int64_t r = i / per;
+  int64_t r = i / per;
   const int c = (int)(i - r * per) * 8;
-  if (r < rows) store16(to + r * ld + c, load8_row(from + r * cols, c, cols, true));
+  const bool second = r >= one.rows;
+  const Repack m = second ? two : one;
+  if (second) r -= one.rows;
+  if (r < m.rows) store16(m.to + r * ld + c, load8_row(m.from + r * cols, c, cols, true));
 }
-hipError_t launch_repack(int rows, int cols, const h16* from, h16* to, hipStream_t st) {
+hipError_t launch_repack(int cols, const Repack& one, const Repack& two, hipStream_t st) {
   const int ld = (cols + 7) & ~7;
-  repack_kernel<<<(unsigned)ceil_div64((int64_t)rows * (ld / 8), 256), 256, 0, st>>>(rows, cols, ld,
-                                                                                 from, to);
+  const int64_t n = ((int64_t)one.rows + two.rows) * (ld / 8);
+  if (n == 0) return hipSuccess;
+  repack_kernel<<<(unsigned)ceil_div64(n, 256), 256, 0, st>>>(cols, ld, one, two);
   return hipGetLastError();
 }
 
@@ -696,7 +713,7 @@ size_t take(Places& p, size_t bytes) {
 Places places(int T, int I, int O, bool backward, bool makes) {
   Places p;
   if (!backward && few_ok(O, T, I)) {  // (takes rows as they are)
-    const Choice c = {0, few_parts(O, T, I)};
+    const Choice c = {0, 0, few_parts(O, T, I)};
     p.sums = take(p, sums_bytes(c, O, T));
     return p;
   }
@@ -744,10 +761,10 @@ hipError_t launch_dense_fwd(const DenseArgs& a, hipStream_t st) {
   const Places at_ = places(T, I, O, false, false);
   const h16 *x = a.x, *w = a.w;
   if (ld != I) {
-    RUN(launch_repack(T, I, a.x, at<h16>(a.ws, at_.x), st));
-    RUN(launch_repack(O, I, a.w, at<h16>(a.ws, at_.w), st));
-    x = at<h16>(a.ws, at_.x);
-    w = at<h16>(a.ws, at_.w);
+    h16 *xs = at<h16>(a.ws, at_.x), *ws = at<h16>(a.ws, at_.w);
+    RUN(launch_repack(I, {T, a.x, xs}, {O, a.w, ws}, st));
+    x = xs;
+    w = ws;
   }
   const Product p = {w, x, ld, ld, O, T, I, 1};
   void* sums = at<void>(a.ws, at_.sums);
@@ -782,19 +799,17 @@ hipError_t launch_dense_bwd(const DenseArgs& a, hipStream_t st) {
     }
   }
   void* sums = at<void>(a.ws, at_.sums);
+  if (ldi != I) {
+    h16 *xs = at<h16>(a.ws, at_.x), *ws = at<h16>(a.ws, at_.w);
+    RUN(launch_repack(I, {a.dw ? T : 0, a.x, xs}, {a.dx ? O : 0, a.w, ws}, st));
+    x = xs;
+    w = ws;
+  }
   if (a.dx) {
-    if (ldi != I) {
-      RUN(launch_repack(O, I, a.w, at<h16>(a.ws, at_.w), st));
-      w = at<h16>(a.ws, at_.w);
-    }
     const Product p = {w, dz, ldi, ldo, I, T, O, 1};
     RUN(launch_product<kDx>(p, HalfEpi{a.dx, I, T}, sums, st));
   }
   if (a.dw) {
-    if (ldi != I) {
-      RUN(launch_repack(T, I, a.x, at<h16>(a.ws, at_.x), st));
-      x = at<h16>(a.ws, at_.x);
-    }
     const Product p = {x, dz, ldi, ldo, I, O, T, 1};
     RUN(launch_product<kDw>(p, HalfEpi{a.dw, I, O}, sums, st));
   }
