@@ -705,6 +705,12 @@ fp16_status fp16_dense_bwd(const fp16_dense_desc* desc, const fp16_t* x, const f
                            fp16_t* dw, fp16_t* dbias, void* ws, size_t ws_bytes,
                            fp16_stream_t stream);
 
+/* The kernel that a layer's product runs on (0 the forward's, 1 dx's, 2 dw's), e.g. "128 x
+ * 64 in 4" (a tile, its reduction in 4 parts) or "few tokens, 16 rows", for tests and
+ * profiles; "" for an invalid descriptor.  No contract; valid until the thread's next
+ * call. */
+const char* fp16_dense_kernel(const fp16_dense_desc* desc, int32_t product);
+
 /* ---- log probabilities of given classes, entropies, most probable classes ----
  * Logits z, `rows` rows of `classes`, a row's first `stride` elements after the one
  * before's; l = scale * z (scale: one over a temperature). */

@@ -43,7 +43,7 @@ EXPORTS = ["fp16_conv_out_dims", "fp16_conv_workspace_bytes", "fp16_conv_fwd", "
            "fp16_int8_quant_workspace_bytes", "fp16_int8_quant_cols", "fp16_int8_matmul",
            "fp16_int8_kernel", "fp16_int8_dense_workspace_bytes", "fp16_int8_dense_weights",
            "fp16_int8_dense_fwd", "fp16_int8_dense_bwd", "fp16_rng_advance", "fp16_dropout",
-           "fp16_dense_workspace_bytes", "fp16_dense_fwd", "fp16_dense_bwd",
+           "fp16_dense_workspace_bytes", "fp16_dense_fwd", "fp16_dense_bwd", "fp16_dense_kernel",
            "fp16_logprobs_workspace_bytes", "fp16_logprobs", "fp16_logprobs_bwd"]
 
 
@@ -150,6 +150,7 @@ _SIGS = {
     "fp16_dense_workspace_bytes": (_SZ, [_P, _I32]),
     "fp16_dense_fwd": (ctypes.c_int, [_P] * 9 + [_SZ, _P]),
     "fp16_dense_bwd": (ctypes.c_int, [_P] * 10 + [_SZ, _P]),
+    "fp16_dense_kernel": (ctypes.c_char_p, [_P, _I32]),
     "fp16_logprobs_workspace_bytes": (_SZ, [_P]),
     "fp16_logprobs": (ctypes.c_int, [_P] * 8 + [_SZ, _P]),
     "fp16_logprobs_bwd": (ctypes.c_int, [_P] * 8),
@@ -706,6 +707,11 @@ def fp16_dense_workspace_bytes(desc: DenseDesc, call=None) -> int:
     """Workspace of one of the layer's calls, or (None) enough for both."""
     calls = (DENSE_FWD, DENSE_BWD) if call is None else (int(call),)
     return max(int(lib().fp16_dense_workspace_bytes(ctypes.byref(desc), c)) for c in calls)
+
+
+def fp16_dense_kernel(desc: DenseDesc, product=0) -> str:
+    """The kernel that a product runs on (0 forward, 1 dx, 2 dW; for tests and profiles)."""
+    return lib().fp16_dense_kernel(ctypes.byref(desc), int(product)).decode()
 
 
 def fp16_dense_fwd(desc, x, w, bias, residual, y, z=None, rng=None, ws=None, ws_bytes=None,

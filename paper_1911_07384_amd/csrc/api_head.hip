@@ -204,6 +204,13 @@ fp16_status fp16_dense_bwd(const fp16_dense_desc* desc, const fp16_t* x, const f
   return hip_status(launch_dense_bwd(a, static_cast<hipStream_t>(stream)));
 }
 
+const char* fp16_dense_kernel(const fp16_dense_desc* desc, int32_t product) {
+  thread_local char name[48];
+  if (!desc || !dense_ok(desc) || product < 0 || product > 2) return "";
+  dense_name(desc->tokens, desc->inputs, desc->outputs, product, name, sizeof(name));
+  return name;
+}
+
 size_t fp16_logprobs_workspace_bytes(const fp16_logprob_desc* desc) {
   if (!desc || !logprob_ok(desc)) return 0;
   return logprob_ws_bytes(desc->rows, desc->classes, desc->top);

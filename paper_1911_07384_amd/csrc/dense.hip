@@ -12,6 +12,8 @@
 #include "gemm_dense.hpp"
 #include "head.hpp"
 
+#include <stdio.h>
+
 #include <type_traits>
 
 namespace fp16k {
@@ -746,6 +748,23 @@ size_t dense_fwd_ws_bytes(int tokens, int inputs, int outputs) {
 
 size_t dense_bwd_ws_bytes(int tokens, int inputs, int outputs, bool dz) {
   return places(tokens, inputs, outputs, true, dz).total;
+}
+
+void dense_name(int tokens, int inputs, int outputs, int product, char* name, size_t size) {
+  const int64_t T = tokens, I = inputs, O = outputs;
+  char in[16] = "";
+  if (product == kForward && few_ok(O, T, I)) {
+    const int parts = few_parts(outputs, tokens, inputs);
+    if (parts > 1) snprintf(in, sizeof(in), " in %d", parts);
+    snprintf(name, size, "few tokens, %d rows%s", 16 * few_rows(O, T, I), in);
+    return;
+  }
+  const Choice c = product == kForward ? choose(kForward, O, T, I)
+                   : product == kDx    ? choose(kDx, I, T, O)
+                                       : choose(kDw, I, O, T);
+  if (c.parts > 1) snprintf(in, sizeof(in), " in %d", c.parts);
+  snprintf(name, size, "%d x %d%s%s", c.side < 128 ? 128 : c.side, c.side,
+           c.stages == 4 ? " deep" : "", in);
 }
 
 #define RUN(expr)                     \

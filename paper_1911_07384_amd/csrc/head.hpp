@@ -31,6 +31,8 @@ struct DenseArgs {
 };
 size_t dense_fwd_ws_bytes(int tokens, int inputs, int outputs);
 size_t dense_bwd_ws_bytes(int tokens, int inputs, int outputs, bool dz);
+// The kernel of a product (0 forward, 1 dx, 2 dW).
+void dense_name(int tokens, int inputs, int outputs, int product, char* name, size_t size);
 hipError_t launch_dense_fwd(const DenseArgs& a, hipStream_t st);
 hipError_t launch_dense_bwd(const DenseArgs& a, hipStream_t st);
 

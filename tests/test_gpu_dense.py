@@ -220,3 +220,25 @@ def test_gradients_against_differences():
         # each y is off by 2^-11 of itself, the third order by h^2 / 6 of a slope's change
         scale = np.abs(c.dy.astype(np.float64)).sum() * 2
         assert abs(num - exact) < scale * 2.0 ** -10 + 0.1 * abs(exact) + 0.02 * np.abs(g).sum() * h
+
+
+# Sizes with odd edges that run on each kernel a product has.
+KERNELS = [(0, "few tokens, 16 rows in 16", (2, 16384, 48)), (0, "few tokens, 16 rows in 5", (1, 5453, 1)),
+           (0, "few tokens, 32 rows", (5, 72, 8200)), (0, "few tokens, 32 rows", (24, 40, 8201)),
+           (0, "few tokens, 32 rows in 8", (20, 8200, 40)), (0, "few tokens, 32 rows in 8", (17, 8211, 9)),
+           (0, "128 x 64 in 7", (34, 816, 1)), (0, "128 x 128", (2600, 24, 2601)),
+           (0, "128 x 128 in 11", (5614, 3337, 1)), (0, "128 x 128 deep", (16400, 1, 1)),
+           (0, "128 x 128 deep in 11", (2716, 2060, 1)), (0, "256 x 256", (8499, 259, 1467)),
+           (0, "256 x 256 in 3", (17583, 4109, 134)), (1, "128 x 64 in 5", (1, 1, 579)),
+           (1, "128 x 128", (16400, 1, 1)), (1, "128 x 128 in 21", (1480, 1, 2605)),
+           (1, "256 x 256", (5259, 2337, 129)), (1, "256 x 256 in 14", (4146, 129, 13080)),
+           (2, "128 x 128 in 4", (385, 1, 1)), (2, "256 x 256", (129, 13307, 917)),
+           (2, "256 x 256 in 3", (1910, 139, 16895))]
+
+
+@pytest.mark.parametrize("product,name,size", KERNELS, ids=lambda v: str(v).replace(" ", ""))
+def test_every_kernel(product, name, size):
+    big = max(size[0], size[2]) > 8000 and min(size[0], size[2]) > 16
+    c = Case(*size, *([] if big else ["silu", 0.25]))
+    assert F.fp16_dense_kernel(c.d, product) == name
+    c.check()

@@ -212,3 +212,15 @@ def test_same_bits_every_time():
     for _ in range(3):
         b = run(z, t, 1.0, 20, 1, np.ones(40), np.ones(40))
         assert all(np.array_equal(p, q, equal_nan=True) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("top", [0, 20, 64])
+def test_many_long_rows(top):
+    """Whole rows of a wider workgroup's own."""
+    for k in (16385, 17003):
+        r = np.random.default_rng(k)
+        check(logits(512, k, k), given(512, k, 1), 0.9, top, 5, r.standard_normal(512),
+              r.standard_normal(512))
+        z = np.zeros((512, k))
+        z[:256, ::3] = -np.inf
+        check(z.astype(np.float16), given(512, k, 2), 1.0, top)
