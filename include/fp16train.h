@@ -653,7 +653,7 @@ fp16_status fp16_rng_advance(uint64_t* rng, uint64_t steps, fp16_stream_t stream
  * residual may be NULL.  The gradient of x is the same call on dy without a residual
  * (that of the residual is dy).  What is dropped is not looked at: a NaN or an infinity
  * there gives 0.  y may equal x or residual, and overlaps nothing otherwise.
- * 0 <= p <= 1, n < 2^35 (FP16_ERR_SHAPE); n = 0 is a no-op. */
+ * 0 <= p <= 1, n < 2^34 (FP16_ERR_SHAPE); n = 0 is a no-op. */
 fp16_status fp16_dropout(size_t n, const fp16_t* x, const fp16_t* residual, fp16_t* y, float p,
                          const uint64_t* rng, uint32_t site, fp16_stream_t stream);
 
@@ -668,7 +668,7 @@ typedef enum {
 } fp16_act;
 
 typedef struct {
-  int32_t tokens, inputs, outputs; /* each 1 to 2^20, each matrix < 2^35 elements */
+  int32_t tokens, inputs, outputs; /* each 1 to 2^20, each matrix < 2^34 elements */
   int32_t act;                     /* fp16_act */
   float drop;                      /* drop probability in [0, 1]; 0: no dropout */
   uint32_t site;                   /* the dropout's, see above */
@@ -717,7 +717,7 @@ const char* fp16_dense_kernel(const fp16_dense_desc* desc, int32_t product);
 #define FP16_LOGPROB_TOP_MAX 64
 typedef struct {
   int32_t rows, classes; /* 1 <= rows < 2^24, 1 <= classes <= 2^20 */
-  int32_t stride;        /* classes <= stride <= 2^21, rows * stride < 2^35 */
+  int32_t stride;        /* classes <= stride <= 2^21, rows * stride < 2^34 */
   float scale;           /* positive, at most 1e30 */
   int32_t top;           /* most probable classes: 0 to FP16_LOGPROB_TOP_MAX, <= classes */
 } fp16_logprob_desc;

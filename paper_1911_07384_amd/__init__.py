@@ -233,11 +233,11 @@ _ptr_half, _ptr_float, _ptr_int8 = _ptr_of("float16"), _ptr_of("float32"), _ptr_
 
 
 def _held_of(dtype):
-    """A _ptr for arguments of one element type and a number of elements at least, which
-    `what` names."""
+    """A _ptr for arguments of one element type, a number of elements at least and a
+    device, which `what` names."""
     want = None
 
-    def ptr(t, n, what):
+    def ptr(t, n, what, device):
         nonlocal want
         if t is None or isinstance(t, int):
             return t
@@ -248,6 +248,8 @@ def _held_of(dtype):
                 raise TypeError(f"{what}: expected {dtype} tensor, got {t.dtype}")
         if t.numel() < n:
             raise ValueError(f"{what} has {t.numel()} elements of {n}")
+        if t.get_device() != device:
+            raise ValueError(f"{what} is on {t.device}, which is not the current device")
         if not t.is_contiguous():
             raise ValueError(f"{what}: tensor must be contiguous")
         return t.data_ptr()
@@ -276,6 +278,34 @@ def _first_current_stream():
 
 
 _current_stream = _first_current_stream
+
+
+def _first_device():
+    """The current device (-1, a CPU tensor's, where there is none); later calls ask
+    torch's C++ side as _current_stream does."""
+    global _device
+    import torch
+    if not torch.cuda.is_available():
+        return -1
+    d = torch.cuda.current_device()
+    raw = getattr(torch._C, "_cuda_getDevice", None)
+    if raw is not None and raw() == d:
+        _device = raw
+    return d
+
+
+_device = _first_device
+
+
+def _held_ws(ws, ws_bytes, device):
+    """A workspace's address and bytes."""
+    if ws is None or isinstance(ws, int):
+        return ws, 0 if ws_bytes is None else int(ws_bytes)
+    if ws.get_device() != device:
+        raise ValueError(f"ws is on {ws.device}, which is not the current device")
+    if not ws.is_contiguous():
+        raise ValueError("ws: tensor must be contiguous")
+    return ws.data_ptr(), ws.nbytes if ws_bytes is None else int(ws_bytes)
 
 
 def _stream(stream):
@@ -678,16 +708,17 @@ def rng_state(seed, step=0, device="cuda"):
 
 
 def fp16_rng_advance(rng, steps=1, stream=None) -> None:
-    _check("fp16_rng_advance", lib().fp16_rng_advance(
-        _held_long(rng, 2, "rng"), int(steps) % (1 << 64), _stream(stream)))
+    p = _held_long(rng, 2, "rng", _device())
+    _check("fp16_rng_advance", lib().fp16_rng_advance(p, int(steps) % (1 << 64), _stream(stream)))
 
 
 def fp16_dropout(x, residual, y, p, rng, site=0, n=None, stream=None) -> None:
     """y = dropout of x (+ residual); the gradient is the same call on dy."""
     n = x.numel() if n is None else int(n)
+    dev = _device()
     _check("fp16_dropout", lib().fp16_dropout(
-        n, _held_half(x, n, "x"), _held_half(residual, n, "residual"), _held_half(y, n, "y"), p,
-        _held_long(rng, 2, "rng"), site, _stream(stream)))
+        n, _held_half(x, n, "x", dev), _held_half(residual, n, "residual", dev),
+        _held_half(y, n, "y", dev), p, _held_long(rng, 2, "rng", dev), site, _stream(stream)))
 
 
 # ---- dense layers with bias, activation, dropout and residual ----------------
@@ -717,22 +748,26 @@ def fp16_dense_kernel(desc: DenseDesc, product=0) -> str:
 def fp16_dense_fwd(desc, x, w, bias, residual, y, z=None, rng=None, ws=None, ws_bytes=None,
                    stream=None) -> None:
     t, i, o = desc.tokens, desc.inputs, desc.outputs
-    to = t * o
+    to, dev = t * o, _device()
+    work, size = _held_ws(ws, ws_bytes, dev)
     _check("fp16_dense_fwd", lib().fp16_dense_fwd(
-        ctypes.byref(desc), _held_half(x, t * i, "x"), _held_half(w, o * i, "w"),
-        _held_half(bias, o, "bias"), _held_half(residual, to, "residual"),
-        _held_long(rng, 2, "rng"), _held_half(y, to, "y"), _held_half(z, to, "z"), _ptr(ws),
-        _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _held_half(x, t * i, "x", dev), _held_half(w, o * i, "w", dev),
+        _held_half(bias, o, "bias", dev), _held_half(residual, to, "residual", dev),
+        _held_long(rng, 2, "rng", dev), _held_half(y, to, "y", dev), _held_half(z, to, "z", dev),
+        work, size, _stream(stream)))
 
 
 def fp16_dense_bwd(desc, x, w, z, dy, dx, dw, dbias=None, rng=None, ws=None, ws_bytes=None,
                    stream=None) -> None:
     t, i, o = desc.tokens, desc.inputs, desc.outputs
+    dev = _device()
+    work, size = _held_ws(ws, ws_bytes, dev)
     _check("fp16_dense_bwd", lib().fp16_dense_bwd(
-        ctypes.byref(desc), _held_half(x, t * i, "x"), _held_half(w, o * i, "w"),
-        _held_half(z, t * o, "z"), _held_half(dy, t * o, "dy"), _held_long(rng, 2, "rng"),
-        _held_half(dx, t * i, "dx"), _held_half(dw, o * i, "dw"), _held_half(dbias, o, "dbias"),
-        _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _held_half(x, t * i, "x", dev), _held_half(w, o * i, "w", dev),
+        _held_half(z, t * o, "z", dev), _held_half(dy, t * o, "dy", dev),
+        _held_long(rng, 2, "rng", dev), _held_half(dx, t * i, "dx", dev),
+        _held_half(dw, o * i, "dw", dev), _held_half(dbias, o, "dbias", dev),
+        work, size, _stream(stream)))
 
 
 # ---- log probabilities -------------------------------------------------------
@@ -751,21 +786,23 @@ def fp16_logprobs(desc, z, tokens, logp, stats, top_id=None, top_logp=None, ws=N
                   ws_bytes=None, stream=None) -> None:
     """logp, stats [rows][3] (largest logit, log of the sum, entropy) and the desc.top
     most probable classes of each row."""
-    n, k = desc.rows, desc.top
+    n, k, dev = desc.rows, desc.top, _device()
+    work, size = _held_ws(ws, ws_bytes, dev)
     _check("fp16_logprobs", lib().fp16_logprobs(
-        ctypes.byref(desc), _held_half(z, (n - 1) * desc.stride + desc.classes, "z"),
-        _held_int(tokens, n, "tokens"), _held_float(logp, n, "logp"),
-        _held_float(stats, 3 * n, "stats"), _held_int(top_id, n * k, "top_id"),
-        _held_float(top_logp, n * k, "top_logp"), _ptr(ws), _wsb(ws, ws_bytes), _stream(stream)))
+        ctypes.byref(desc), _held_half(z, (n - 1) * desc.stride + desc.classes, "z", dev),
+        _held_int(tokens, n, "tokens", dev), _held_float(logp, n, "logp", dev),
+        _held_float(stats, 3 * n, "stats", dev), _held_int(top_id, n * k, "top_id", dev),
+        _held_float(top_logp, n * k, "top_logp", dev), work, size, _stream(stream)))
 
 
 def fp16_logprobs_bwd(desc, z, tokens, stats, dlogp, dentropy, dz, stream=None) -> None:
-    n = desc.rows
+    n, dev = desc.rows, _device()
     size = (n - 1) * desc.stride + desc.classes
     _check("fp16_logprobs_bwd", lib().fp16_logprobs_bwd(
-        ctypes.byref(desc), _held_half(z, size, "z"), _held_int(tokens, n, "tokens"),
-        _held_float(stats, 3 * n, "stats"), _held_float(dlogp, n, "dlogp"),
-        _held_float(dentropy, n, "dentropy"), _held_half(dz, size, "dz"), _stream(stream)))
+        ctypes.byref(desc), _held_half(z, size, "z", dev), _held_int(tokens, n, "tokens", dev),
+        _held_float(stats, 3 * n, "stats", dev), _held_float(dlogp, n, "dlogp", dev),
+        _held_float(dentropy, n, "dentropy", dev), _held_half(dz, size, "dz", dev),
+        _stream(stream)))
 
 
 def _wsb(ws, ws_bytes):

@@ -11,7 +11,9 @@ using namespace fp16k;
 namespace {
 
 constexpr int32_t kMaxSide = 1 << 20;          // of a dense layer's sizes
-constexpr int64_t kMaxElems = (int64_t)1 << 35;  // of a tensor (a dropout's groups of 8: 2^32)
+// Elements of a tensor: below 2^32 threads of a launch over its groups of 8, for two
+// matrices in one launch (rows laid out anew) too.
+constexpr int64_t kMaxElems = (int64_t)1 << 34;
 
 const h16* hp(const fp16_t* p) { return reinterpret_cast<const h16*>(p); }
 h16* hp(fp16_t* p) { return reinterpret_cast<h16*>(p); }

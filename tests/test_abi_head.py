@@ -23,7 +23,7 @@ def test_dropout_refusals():
     assert dropout(n=0, x=None, y=None, rng=None) == OK
     for p in (-0.1, 1.1, NAN, INF):
         assert dropout(p=p) == SHAPE and dropout(n=0, p=p) == SHAPE
-    assert dropout(n=1 << 35) == SHAPE
+    assert dropout(n=1 << 34) == SHAPE
     assert dropout(x=None) == NULL and dropout(y=None) == NULL and dropout(rng=None) == NULL
     assert dropout(x=A + 2) == MISALIGNED and dropout(y=B + 8) == MISALIGNED
     assert dropout(res=C + 4) == MISALIGNED and dropout(rng=R + 4) == MISALIGNED
@@ -53,8 +53,8 @@ def bwd(d=None, x=A, w=B, z=None, dy=C, rng=None, dx=D, dw=E, db=None, ws=W, n=B
 
 BAD = [desc(tokens=0), desc(inputs=0), desc(outputs=0), desc(tokens=-1), desc(tokens=(1 << 20) + 1),
        desc(inputs=(1 << 20) + 1), desc(outputs=(1 << 20) + 1), desc(act=4), desc(act=-1),
-       desc(drop=-0.1), desc(drop=1.5), desc(drop=NAN), desc(tokens=1 << 20, inputs=1 << 15),
-       desc(tokens=1 << 20, outputs=1 << 15), desc(inputs=1 << 20, outputs=1 << 15)]
+       desc(drop=-0.1), desc(drop=1.5), desc(drop=NAN), desc(tokens=1 << 20, inputs=1 << 14),
+       desc(tokens=1 << 20, outputs=1 << 14), desc(inputs=1 << 20, outputs=1 << 14)]
 
 
 def test_dense_forward_refusals():
@@ -148,7 +148,8 @@ def test_logprob_backward_refusals():
     assert logb(dz=D) == ALIASING and logb(dz=E) == ALIASING
 
 
-def test_binding_checks():
+def test_binding_checks(monkeypatch):
+    monkeypatch.setattr(F, "_device", lambda: -1)  # (a CPU tensor's)
     cpu = lambda *s, t=torch.float16: torch.zeros(s, dtype=t)
     d = F.dense_desc(4, 8, 16)
     with pytest.raises(ValueError, match="w has"):
@@ -171,5 +172,27 @@ def test_binding_checks():
     with pytest.raises(ValueError, match="z has"):
         F.fp16_logprobs(F.logprob_desc(4, 8, stride=9), cpu(4, 8), None, None,
                         cpu(12, t=torch.float32), stream=0)
+    with pytest.raises(TypeError):
+        F.fp16_logprobs_bwd(F.logprob_desc(4, 8), cpu(4, 8), None, cpu(12, t=torch.float32), None,
+                            cpu(4), cpu(4, 8), stream=0)
     s = F.rng_state((1 << 64) - 1, 1 << 63, device="cpu")
     assert s.tolist() == [-1, -(1 << 63)]
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """Arguments that are right but for their device are refused before the call."""
+    monkeypatch.setattr(F, "_device", lambda: 0)
+    h = lambda *s: torch.zeros(s, dtype=torch.float16)
+    f = lambda *s: torch.zeros(s, dtype=torch.float32)
+    rng = F.rng_state(1, device="cpu")
+    d, lp = F.dense_desc(4, 8, 16), F.logprob_desc(4, 8)
+    for call in (lambda: F.fp16_rng_advance(rng, stream=0),
+                 lambda: F.fp16_dropout(A, None, B, 0.5, rng, n=8, stream=0),
+                 lambda: F.fp16_dropout(h(8), None, B, 0.5, R, stream=0),
+                 lambda: F.fp16_dense_fwd(d, A, B, None, h(4, 16), C, stream=0),
+                 lambda: F.fp16_dense_fwd(d, A, B, None, None, C, ws=f(8), stream=0),
+                 lambda: F.fp16_dense_bwd(d, A, B, None, C, D, h(16, 8), stream=0),
+                 lambda: F.fp16_logprobs(lp, A, None, None, f(12), stream=0),
+                 lambda: F.fp16_logprobs_bwd(lp, A, None, B, f(4), None, C, stream=0)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
