@@ -205,6 +205,14 @@ def test_gradient_against_differences():
     assert abs(num - (dz.astype(np.float64) * dirn).sum()) < 18 * 2.0 ** -10 + 1e-3
 
 
+def test_large_gradients_of_masked_classes():
+    z = logits(3, 700, 4)
+    z[:, 5:300] = -np.inf
+    z[2, 400:] = -65504  # (a probability of 0, but for the scale)
+    dz = run(z, None, scale=4.0, dentropy=np.full(3, 1e32))[-1]
+    assert (dz[:, 5:300] == 0).all() and (dz[2, 400:] == 0).all() and not np.isnan(dz).any()
+
+
 def test_same_bits_every_time():
     z, t = logits(40, 20011, 3), given(40, 20011, 5)
     z[5] = 1.0
