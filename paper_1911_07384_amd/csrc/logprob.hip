@@ -26,7 +26,8 @@ namespace fp16k {
 namespace {
 
 // Threads of a workgroup, NT: 256, and 512 for whole rows of more than kLong classes, of
-// which fewer are then read at a time (4096 x 50001: 96 us with 256, 89 with 512).
+// which fewer are then read at a time (4096 x 50001: 96 us with 256, 89 with 512: 410 MB at
+// 4.6 TB/s; 128 x 1000 with 5 alternatives 5.4 us, a launch, one trip to memory and the ranking).
 constexpr int kNT = 256, kU = 4, kLong = 16384;
 constexpr int kCand = 1024;
 constexpr int kPart = 4096, kMaxParts = 64;
@@ -490,7 +491,8 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
   finish<kNT>(a, row, r, l.best);
 }
 
-// The gradient: each lane 8 classes of a row at a time.
+// The gradient: each lane 8 classes of a row at a time, no sums, bound by its bytes: 4096 x
+// 50001 after the forward 129 us, 819 MB at 6.4 TB/s (some of them from the caches).
 __global__ __launch_bounds__(kNT) void logprob_bwd_kernel(const LogprobArgs a, int parts, int per) {
   // the last rows first: a forward before read them last, and they may still be cached
   const int row = a.rows - 1 - (int)(blockIdx.x / parts), first = (blockIdx.x % parts) * per;

@@ -30,7 +30,9 @@ struct PhiloxBlock {
   uint32_t w[4];
 };
 
-// The words of group g of 8 elements.
+// The words of group g of 8 elements.  XOR3: a round's two differences of three words in one
+// instruction each (kernels that hold many registers spill with it).
+template <bool XOR3 = false>
 __device__ __forceinline__ PhiloxBlock philox(uint32_t g, uint32_t site, uint64_t step,
                                               uint64_t seed) {
   uint32_t c0 = g, c1 = site, c2 = (uint32_t)step, c3 = (uint32_t)(step >> 32);
@@ -38,9 +40,10 @@ __device__ __forceinline__ PhiloxBlock philox(uint32_t g, uint32_t site, uint64_
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    const uint32_t bh = (uint32_t)(b >> 32), ah = (uint32_t)(a >> 32);
+    c0 = XOR3 ? __builtin_amdgcn_bitop3_b32(bh, c1, k0, 0x96) : bh ^ c1 ^ k0;
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = XOR3 ? __builtin_amdgcn_bitop3_b32(ah, c3, k1, 0x96) : ah ^ c3 ^ k1;
     c3 = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
