@@ -221,7 +221,7 @@ struct Product {
 // workgroup a CU: a residual or a kept z of 8192 x 4096 adds 15 us, its bytes' time.
 template <class C, class Epi>
 __global__ __launch_bounds__(C::BOUND, 2) void dense_product(const Product a, Epi epi) {
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  __shared__ __attribute__((aligned(1024))) char lds[C::G * C::LDS];
   const int tp = (a.np + C::BP - 1) / C::BP, tq = (a.nq + C::BQ - 1) / C::BQ;
   const int all = tp * tq * a.parts;
   int t = dense_xcd(blockIdx.x, all);
@@ -239,12 +239,18 @@ __global__ __launch_bounds__(C::BOUND, 2) void dense_product(const Product a, Ep
   d.prows = a.np - p0;
   d.qrows = a.nq - q0;
   d.nk = a.nk;
-  d.part = part;
-  d.parts = a.parts;
+  int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = C::G > 1 ? wave / C::WAVES : 0;
+  wave -= group * C::WAVES;
+  d.part = part * C::G + group;
+  d.parts = a.parts * C::G;
   floatx4 acc[C::TP][C::TQ];
-  dense_loop<C>(d, lds, acc);
+  dense_loop<C>(d, lds + group * C::LDS, wave, acc);
+  if constexpr (C::G > 1) {
+    dense_groups<C>(lds, group, wave, acc);
+    if (group > 0) return;
+  }
   if constexpr (std::is_same<Epi, PartEpi>::value) epi.d += (int64_t)part * epi.nq * epi.ld;
-  const int wave = threadIdx.x >> 6;
   dense_store<C>(acc, p0 + (wave / C::WQ) * 16 * C::TP, q0 + (wave % C::WQ) * 16 * C::TQ, epi);
 }
 
@@ -277,14 +283,15 @@ __global__ __launch_bounds__(256) void dense_join(const float* from, int parts, 
 
 enum Layout { kForward, kDx, kDw };  // which operands lie along their rows: none, P, both
 
-template <Layout L, int WP, int WQ, int TQ, int S, int OCC>
-using Cfg = DenseCfg<WP, WQ, 8, TQ, S, OCC, L != kForward, L == kDw>;
+template <Layout L, int WP, int WQ, int TQ, int S, int OCC, int G = 1>
+using Cfg = DenseCfg<WP, WQ, 8, TQ, S, OCC, L != kForward, L == kDw, G>;
 
-//                                 waves  tiles  stages  workgroups a CU
+//                                 waves  tiles  stages  workgroups a CU (groups)
 template <Layout L> using Cfg256 = Cfg<L, 2, 4, 4, 2, 1>;  // 256 x 256
 template <Layout L> using Cfg128 = Cfg<L, 1, 4, 2, 2, 2>;  // 128 x 128
 template <Layout L> using Cfg128d = Cfg<L, 1, 4, 2, 4, 1>;  // .. loads further ahead
 template <Layout L> using Cfg64 = Cfg<L, 1, 4, 1, 3, 2>;   // 128 x 64
+template <Layout L> using Cfg32 = Cfg<L, 1, 2, 1, 2, 1, 4>;  // 128 x 32, four groups
 
 template <class Epi>
 hipError_t launch_join(const Product& a, const float* sums, int ld, const Epi& epi,
@@ -319,18 +326,26 @@ hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {
 // One workgroup a CU of 128 x 128 is held up by its loads with two stages: with four a
 // forward's slice takes 0.50 us (2048 x 2048 x 2048 26.0 -> 22.7 us; the other layouts
 // gain nothing).
+// A slice of dx with few workgroups is held up by its fragments' way from LDS through the
+// permutes: four groups of two waves, each with a quarter of the reduction, take turns at it
+// and join in LDS (dx of 128 x 2048 x 1000 10.5 -> 7.8 us, 256 x 1024 x 1024 10.5 -> 7.7;
+// two groups of 128 x 64: 9.0 and 9.0); in parts besides they gain nothing, and where W's
+// bytes count they lose (8 x 4096 x 16384 29.2 -> 34.2).  The forward's is held up by its loads and gains
+// nothing (64 x 1024 x 4096: 7.9 us, 8.4 so).
 struct Choice {
   int side, stages, parts;
 };
 struct Tile {
   int side, stages, occ;
   double one, two, ends;
+  int groups = 1;  // a slice's times are of so many
 };
 Choice choose(Layout l, int64_t np, int64_t nq, int64_t nk) {
   static const Tile tiles[3][4] = {
       {{256, 2, 1, 1.48, 0, 12}, {128, 2, 2, 0.58, 0.97, 5.5}, {64, 3, 2, 0.30, 0.62, 4.7},
        {128, 4, 1, 0.50, 0, 5.5}},
-      {{256, 2, 1, 1.55, 0, 12}, {128, 2, 2, 0.70, 1.12, 5.5}, {64, 3, 2, 0.42, 0.79, 4.7}},
+      {{256, 2, 1, 1.55, 0, 12}, {128, 2, 2, 0.70, 1.12, 5.5}, {64, 3, 2, 0.42, 0.79, 4.7},
+       {32, 2, 1, 1.10, 0, 4.6, 4}},
       {{256, 2, 1, 1.60, 0, 12}, {128, 2, 2, 0.78, 1.20, 5.5}}};
   const double launch = 4.0, join = 2.5, bytes = 4.5e6;  // (bytes a microsecond)
   const int64_t slices = ceil_div64(nk, 64);
@@ -340,8 +355,9 @@ Choice choose(Layout l, int64_t np, int64_t nq, int64_t nk) {
     if (!t.side) continue;
     const int64_t n1 = ceil_div64(np, t.side < 128 ? 128 : t.side) * ceil_div64(nq, t.side);
     for (int64_t want = 1; want <= 32 && want <= slices; want += 1 + want / 4) {
-      const int64_t sl = ceil_div64(slices, want), parts = ceil_div64(slices, sl);
-      if (parts > 1 && sl < 2) break;
+      const int64_t sl = ceil_div64(slices, want * t.groups);
+      const int64_t parts = ceil_div64(slices, sl * t.groups);
+      if (parts > 1 && (sl < 2 || t.groups > 1)) break;
       // rounds of workgroups on the busiest CU
       const int64_t n = n1 * parts, cu = ceil_div64(n, 256);
       const double full = (double)(cu / t.occ), rest = (double)(cu % t.occ);
@@ -371,6 +387,8 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
   float* f = static_cast<float*>(sums);
   if constexpr (L != kDw)
     if (c.side == 64) return run<Cfg64<L>>(a, epi, f, st);
+  if constexpr (L == kDx)
+    if (c.side == 32) return run<Cfg32<L>>(a, epi, f, st);
   if constexpr (L == kForward)
     if (c.side == 128 && c.stages == 4) return run<Cfg128d<L>>(a, epi, f, st);
   if (c.side == 256) return run<Cfg256<L>>(a, epi, f, st);

@@ -6,7 +6,8 @@
 // Matrix instructions are the 16 x 16 x 32 ones: the card is bound by its power, and on
 // random operands in registers they sustain 1930 TFLOP/s, 32 x 32 x 16 ones 1650.
 //
-// A workgroup owns BP x BQ outputs, WP x WQ waves TP x TQ tiles of 16 x 16 each.  Slices
+// A workgroup owns BP x BQ outputs, WP x WQ waves TP x TQ tiles of 16 x 16 each, and G such
+// groups of waves a range of the reduction each, with LDS of their own.  Slices
 // of 64 of the reduction go through S stages of LDS, loaded past the registers (1 KB an
 // instruction and wave) S slices ahead, in the sub-step (32 of the reduction) behind the
 // barrier that frees their stage.  A sub-step's fragments are read from LDS between the
@@ -32,24 +33,26 @@
 
 namespace fp16k {
 
-template <int WP_, int WQ_, int TP_, int TQ_, int S_, int OCC_, bool PS_ = false, bool QS_ = false>
+template <int WP_, int WQ_, int TP_, int TQ_, int S_, int OCC_, bool PS_ = false, bool QS_ = false,
+          int G_ = 1>
 struct DenseCfg {
-  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, S = S_, OCC = OCC_;
+  static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, S = S_, OCC = OCC_, G = G_;
   static constexpr bool PS = PS_, QS = QS_;
-  static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES;
+  static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES * G;
   static constexpr int BP = 16 * TP * WP, BQ = 16 * TQ * WQ;
-  static constexpr int STAGE = (BP + BQ) * 128, LDS = S * STAGE;
+  static constexpr int STAGE = (BP + BQ) * 128, LDS = S * STAGE;  // of a group
   static constexpr int IP = BP / (8 * WAVES), IQ = BQ / (8 * WAVES);  // loads of a wave
   static_assert(TP == 8, "a lane's chunks of 8 rows");
   static_assert(IP % 2 == 0 && IQ % 2 == 0, "the chunks' order");
   static_assert(IP * 8 * WAVES == BP && IQ * 8 * WAVES == BQ, "whole loads");
-  static_assert(LDS * OCC <= 160 * 1024, "LDS");
+  static_assert(G * LDS * OCC <= 160 * 1024, "LDS");
+  static_assert((G - 1) * BP * BQ * 4 <= G * LDS, "the groups' sums");
   static_assert(!QS || ((TQ == 2 || TQ == 4 || TQ == 8) && 512 % BQ == 0), "lines of whole loads");
   static_assert(!PS || 512 % BP == 0, "lines of whole loads");
   // Threads for __launch_bounds__: two waves a SIMD, also where there is one, keep the
   // compiler to 256 registers, with the sums among them (with accumulator registers it
   // copied them to and fro within the loop, 96 moves for 64 products).
-  static constexpr int BOUND = 512 / OCC;
+  static constexpr int BOUND = THREADS > 512 / OCC ? THREADS : 512 / OCC;
 };
 
 // One 16-byte-per-lane load from a buffer resource into LDS (1 KB a wave).
@@ -94,13 +97,13 @@ __device__ __forceinline__ half8 dense_rows(const DenseRaw<T>& r, int t) {
   return v.h;
 }
 
+// One group's sums; lds: its own.  Every group passes the same number of barriers.
 template <class C>
-__device__ __forceinline__ void dense_loop(const DenseTile& t, char* lds,
+__device__ __forceinline__ void dense_loop(const DenseTile& t, char* lds, int wave,
                                            floatx4 (&acc)[C::TP][C::TQ]) {
   constexpr int TP = C::TP, TQ = C::TQ, S = C::S, IP = C::IP, IQ = C::IQ, I = IP + IQ;
   constexpr uint32_t OOB = 0x80000000u;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave / C::WQ, wq = wave % C::WQ;
   const int m = lane & 15, g = lane >> 4;
 
@@ -277,6 +280,30 @@ __device__ __forceinline__ void dense_loop(const DenseTile& t, char* lds,
     advance();
   }
   __builtin_amdgcn_s_waitcnt(0);  // (loads past the end are still to land in LDS)
+}
+
+// The groups' sums added in their order, in the first one's.
+template <class C>
+__device__ __forceinline__ void dense_groups(char* lds, int group, int wave,
+                                             floatx4 (&acc)[C::TP][C::TQ]) {
+  constexpr int N = C::TP * C::TQ * 64;
+  floatx4* const sums = reinterpret_cast<floatx4*>(lds) + wave * N + (threadIdx.x & 63);
+  __syncthreads();  // (the last reads of what is written over)
+  if (group > 0) {
+#pragma unroll
+    for (int a = 0; a < C::TP; ++a)
+#pragma unroll
+      for (int b = 0; b < C::TQ; ++b)
+        sums[(group - 1) * C::WAVES * N + (a * C::TQ + b) * 64] = acc[a][b];
+  }
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int g = 0; g < C::G - 1; ++g)
+#pragma unroll
+    for (int a = 0; a < C::TP; ++a)
+#pragma unroll
+      for (int b = 0; b < C::TQ; ++b) acc[a][b] += sums[g * C::WAVES * N + (a * C::TQ + b) * 64];
 }
 
 // A wave's outputs to memory: its tile's first p and q, and for a lane 8 consecutive p

@@ -229,7 +229,9 @@ KERNELS = [(0, "few tokens, 16 rows in 16", (2, 16384, 48)), (0, "few tokens, 16
            (0, "128 x 64 in 7", (34, 816, 1)), (0, "128 x 128", (2600, 24, 2601)),
            (0, "128 x 128 in 11", (5614, 3337, 1)), (0, "128 x 128 deep", (16400, 1, 1)),
            (0, "128 x 128 deep in 11", (2716, 2060, 1)), (0, "256 x 256", (8499, 259, 1467)),
-           (0, "256 x 256 in 3", (17583, 4109, 134)), (1, "128 x 64 in 5", (1, 1, 579)),
+           (0, "256 x 256 in 3", (17583, 4109, 134)), (1, "128 x 64 in 7", (1, 1, 769)),
+           (1, "128 x 32", (1, 1, 129)), (1, "128 x 32", (200, 2001, 600)),
+           (1, "128 x 32", (37, 150, 200)), (1, "128 x 64 in 6", (9, 4097, 4095)),
            (1, "128 x 128", (16400, 1, 1)), (1, "128 x 128 in 21", (1480, 1, 2605)),
            (1, "256 x 256", (5259, 2337, 129)), (1, "256 x 256 in 14", (4146, 129, 13080)),
            (2, "128 x 128 in 4", (385, 1, 1)), (2, "256 x 256", (129, 13307, 917)),
