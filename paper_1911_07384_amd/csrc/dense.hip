@@ -330,8 +330,8 @@ hipError_t run(const Product& a, const Epi& epi, float* sums, hipStream_t st) {
 // permutes: four groups of two waves, each with a quarter of the reduction, take turns at it
 // and join in LDS (dx of 128 x 2048 x 1000 10.5 -> 7.8 us, 256 x 1024 x 1024 10.5 -> 7.7;
 // two groups of 128 x 64: 9.0 and 9.0); in parts besides they gain nothing, and where W's
-// bytes count they lose (8 x 4096 x 16384 29.2 -> 34.2).  The forward's is held up by its loads and gains
-// nothing (64 x 1024 x 4096: 7.9 us, 8.4 so).
+// bytes count they lose (8 x 4096 x 16384 29.2 -> 34.2).  The forward's is held up by its
+// loads and gains nothing (64 x 1024 x 4096: 7.9 us, 8.4 so).
 struct Choice {
   int side, stages, parts;
 };
@@ -398,19 +398,21 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
 // ---- few tokens ------------------------------------------------------------------------------
 
 // The forward of at most 32 tokens, bound by reading W once: a workgroup takes 16 RF rows
-// of W, its sixteen waves the reduction in turns of 64, each lane 16 bytes of a row
-// straight into the operand (the next turn's before this one's products), with no regard
-// to a row's alignment; the waves' sums are added in LDS in their order.  Neighbouring
-// workgroups of an XCD start at different turns: at the same one, rows of 8 or 32 KB
-// have all of them ask the same memory channels (one token, 4096 x 16384 from memory: 31.2
-// us, 27.4 so; 16 tokens, 16384 x 4096: 33.9 and 29.4).  One token, 16384 x 4096: 25.2
-// us, 5.3 TB/s; rows that are not aligned take twice as long.
-constexpr int kFewTokens = 32, kFewWaves = 16, kFewSteps = 2, kFewTurn = 32 * kFewSteps;
+// of W, its sixteen waves (eight with more registers for 64 rows) the reduction in turns
+// of 64, each lane 16 bytes of a row straight into the operand (the next turn's before
+// this one's products), with no regard to a row's alignment; the waves' sums are added in
+// LDS in their order.  Neighbouring workgroups of an XCD start at different turns: at the
+// same one, rows of 8 or 32 KB have all of them ask the same memory channels (one token,
+// 4096 x 16384 from memory: 31.2 us, 27.4 so; 16 tokens, 16384 x 4096: 33.9 and 29.4).  One token, 4096 x 16384: 22.7
+// us, 5.9 TB/s; 24 tokens, 16384 x 4096: 24.0 and 3.9 for joining four parts; rows that are
+// not aligned take half as long again.
+constexpr int kFewTokens = 32, kFewSteps = 2, kFewTurn = 32 * kFewSteps;
+constexpr int few_waves(int rf) { return rf == 4 ? 8 : 16; }
 
 template <int RF, int NT, class Epi>
-__global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi epi) {
-  constexpr int U = kFewSteps, TURN = kFewTurn;
-  __shared__ floatx4 sums[kFewWaves][RF * NT * 64];
+__global__ __launch_bounds__(64 * few_waves(RF)) void dense_few(const Product a, Epi epi) {
+  constexpr int U = kFewSteps, TURN = kFewTurn, WAVES = few_waves(RF);
+  __shared__ floatx4 sums[WAVES][RF * NT * 64];
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = (a.np + 16 * RF - 1) / (16 * RF);
@@ -455,9 +457,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi
           acc[f][n] =
               __builtin_amdgcn_mfma_f32_16x16x32_f16(wv[u][f].h, xv[u][n].h, acc[f][n], 0, 0, 0);
   };
-  constexpr int STEP = TURN * kFewWaves;
+  constexpr int STEP = TURN * WAVES;
   // this wave's whole turns, and the one that the range ends in
-  const int whole = (kend - kbeg) / TURN, turns = (whole - wave + kFewWaves - 1) / kFewWaves;
+  const int whole = (kend - kbeg) / TURN, turns = (whole - wave + WAVES - 1) / WAVES;
   if (turns > 0) {
     const int first = kbeg + wave * TURN, end = first + turns * STEP;
     int k = first + (int)((blockIdx.x >> 3) % (unsigned)turns) * STEP;
@@ -479,7 +481,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi
     mma(w[0], x[0]);
     if (i == 2) mma(w[1], x[1]);
   }
-  if (wave == whole % kFewWaves) {
+  if (wave == whole % WAVES) {
 #pragma unroll 1
     for (int at = kbeg + whole * TURN; at < kend; at += 32) {
       const int left = kend - at - 8 * g;
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   const int at = ((c / 2) * NT + t / 16) * 64 + (c % 2) * 32 + t % 16;
 #pragma unroll
-  for (int s = 0; s < kFewWaves; ++s) {
+  for (int s = 0; s < WAVES; ++s) {
     const floatx4 lo = sums[s][at], hi = sums[s][at + 16];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -523,50 +525,57 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few(const Product a, Epi
   epi.store(p0 + 8 * c, t, out);
 }
 
-// Rows of W a workgroup takes, over 16: every workgroup reads the tokens again, so two
-// groups where tokens are several and workgroups many, or tokens and the reduction long
-// (16 tokens of 16384 x 4096: 29 us, 34 with one; 24 of 4096 x 16384: 37 and 45).
-int few_rows(int64_t np, int64_t nq, int64_t nk) {
-  return (nq > 4 && np >= 8192) || (nq > 16 && nk >= 8192) ? 2 : 1;
+// The rows of W a workgroup takes, over 16, and the parts of the reduction: the least of
+// the times below, in microseconds.  Every workgroup reads the tokens again from L2, which
+// adds to the time that W takes from memory (0.5 us a token of 128 workgroups and 32 KB); more
+// rows read them less often, but a workgroup alone on its CU takes longer, and joining parts
+// takes a launch.  24 tokens: 16384 x 4096 45.5, 36.6 and 32.4 us with 16, 32 and 64 rows, 4096 x
+// 16384 46.4, 36.4 and 30.1.
+struct Few {
+  int rows, parts;
+};
+Few few_choice(int64_t np, int64_t nq, int64_t nk) {
+  Few best = {1, 1};
+  double least = 1e300;
+  for (int rf = 1; rf <= 4; rf *= 2) {
+    const int64_t groups = ceil_div64(np, 16 * rf);
+    const double alone = (double)nk / 1024.0 * (0.95 * rf + 0.045 * (double)nq + 0.2);
+    const double bytes = (double)(np * nk) / 2.8e6 + (double)(groups * nq * nk) / 4.2e6;
+    for (int p = 1; p == 1 || (p * groups <= 256 && nk / p >= 1024); ++p) {
+      const double rounds = p * groups > 256 ? (double)groups / 256.0 : 1.0;
+      double us = 4.0 + alone / p * rounds;
+      if (us < bytes) us = bytes;
+      us += rf;  // (a longer start and end)
+      if (p > 1) us += 3.4 + (double)(p * np * nq * 8) / 4.5e6;
+      if (us < least) {
+        least = us;
+        best = {rf, p};
+      }
+    }
+  }
+  return best;
 }
 // Past 16 tokens of wide layers the tiles read each token less often (24 tokens of 4096 x
-// 4096: 12.1 us, 13.0 here; of 4096 x 2048: 10.2 and 8.0).
+// 4096: 12.8 us, 13.4 here; of 4096 x 2048: 10.2 and 8.0).
 bool few_ok(int64_t np, int64_t nq, int64_t nk) {
-  return nq <= 16 || (nq <= kFewTokens && (few_rows(np, nq, nk) == 2 || np * nk <= 1 << 23));
-}
-// Parts: a workgroup alone on its CU reads about 32 KB a microsecond; joining parts takes a
-// launch, 4 us.
-int few_parts(int np, int nq, int nk) {
-  const int rf = few_rows(np, nq, nk), groups = ceil_div(np, 16 * rf);
-  const double alone = (double)nk / 1024.0;
-  int best = 1;
-  double least = alone;
-  for (int p = 2; p * groups <= 256 && nk / p >= 1024; ++p)
-    if (alone / p + 4.0 + 0.05 * p < least) {
-      least = alone / p + 4.0 + 0.05 * p;
-      best = p;
-    }
-  return best;
+  return nq <= 16 ||
+         (nq <= kFewTokens && (np >= 8192 || nk >= 8192 || np * nk <= 1 << 23));
 }
 
 template <class Epi>
 hipError_t launch_few(Product a, const Epi& epi, void* sums, hipStream_t st) {
-  const int rf = few_rows(a.np, a.nq, a.nk);
-  a.parts = few_parts(a.np, a.nq, a.nk);
+  const Few c = few_choice(a.np, a.nq, a.nk);
+  const int rf = c.rows;
+  a.parts = c.parts;
   const unsigned grid = (unsigned)(ceil_div(a.np, 16 * rf) * a.parts);
   auto go = [&](auto e) {
     typedef decltype(e) E;
-    constexpr int T = 64 * kFewWaves;
-    if (a.nq <= 16) {
-      if (rf == 2)
-        dense_few<2, 1, E><<<grid, T, 0, st>>>(a, e);
-      else
-        dense_few<1, 1, E><<<grid, T, 0, st>>>(a, e);
-    } else if (rf == 2) {
-      dense_few<2, 2, E><<<grid, T, 0, st>>>(a, e);
-    } else {
-      dense_few<1, 2, E><<<grid, T, 0, st>>>(a, e);
-    }
+    const int threads = 64 * few_waves(rf);
+    const auto run = [&](auto kernel) { kernel<<<grid, threads, 0, st>>>(a, e); };
+    if (a.nq <= 16)
+      run(rf == 4 ? dense_few<4, 1, E> : rf == 2 ? dense_few<2, 1, E> : dense_few<1, 1, E>);
+    else
+      run(rf == 4 ? dense_few<4, 2, E> : rf == 2 ? dense_few<2, 2, E> : dense_few<1, 2, E>);
     return hipGetLastError();
   };
   if (a.parts == 1) return go(epi);
@@ -760,7 +769,7 @@ size_t take(Places& p, size_t bytes) {
 Places places(int T, int I, int O, bool backward, bool makes) {
   Places p;
   if (!backward && few_ok(O, T, I)) {  // (takes rows as they are)
-    const Choice c = {0, 0, few_parts(O, T, I)};
+    const Choice c = {0, 0, few_choice(O, T, I).parts};
     p.sums = take(p, sums_bytes(c, O, T));
     return p;
   }
@@ -799,9 +808,9 @@ void dense_name(int tokens, int inputs, int outputs, int product, char* name, si
   const int64_t T = tokens, I = inputs, O = outputs;
   char in[16] = "";
   if (product == kForward && few_ok(O, T, I)) {
-    const int parts = few_parts(outputs, tokens, inputs);
-    if (parts > 1) snprintf(in, sizeof(in), " in %d", parts);
-    snprintf(name, size, "few tokens, %d rows%s", 16 * few_rows(O, T, I), in);
+    const Few c = few_choice(O, T, I);
+    if (c.parts > 1) snprintf(in, sizeof(in), " in %d", c.parts);
+    snprintf(name, size, "few tokens, %d rows%s", 16 * c.rows, in);
     return;
   }
   const Choice c = product == kForward ? choose(kForward, O, T, I)

@@ -223,9 +223,19 @@ def test_gradients_against_differences():
 
 
 # Sizes with odd edges that run on each kernel a product has.
-KERNELS = [(0, "few tokens, 16 rows in 16", (2, 16384, 48)), (0, "few tokens, 16 rows in 5", (1, 5453, 1)),
-           (0, "few tokens, 32 rows", (5, 72, 8200)), (0, "few tokens, 32 rows", (24, 40, 8201)),
-           (0, "few tokens, 32 rows in 8", (20, 8200, 40)), (0, "few tokens, 32 rows in 8", (17, 8211, 9)),
+KERNELS = [(0, "few tokens, 16 rows in 16", (2, 16384, 48)),
+           (0, "few tokens, 16 rows in 5", (1, 5453, 1)),
+           (0, "few tokens, 16 rows in 8", (17, 8211, 9)),
+           (0, "few tokens, 16 rows", (24, 40, 8201)),
+           (0, "few tokens, 32 rows", (1, 3035, 11377)),
+           (0, "few tokens, 32 rows", (17, 731, 11901)),
+           (0, "few tokens, 32 rows in 5", (1, 6927, 1381)),
+           (0, "few tokens, 32 rows in 4", (19, 4319, 1371)),
+           (0, "few tokens, 64 rows", (4, 11097, 12169)),
+           (0, "few tokens, 64 rows", (17, 1785, 18155)),
+           (0, "few tokens, 64 rows in 7", (1, 16041, 2063)),
+           (0, "few tokens, 64 rows in 7", (18, 8599, 2069)),
+           (0, "few tokens, 64 rows in 8", (32, 16384, 2048)),
            (0, "128 x 64 in 7", (34, 816, 1)), (0, "128 x 128", (2600, 24, 2601)),
            (0, "128 x 128 in 11", (5614, 3337, 1)), (0, "128 x 128 deep", (16400, 1, 1)),
            (0, "128 x 128 deep in 11", (2716, 2060, 1)), (0, "256 x 256", (8499, 259, 1467)),
