@@ -403,13 +403,43 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
 // this one's products), with no regard to a row's alignment; the waves' sums are added in
 // LDS in their order.  Neighbouring workgroups of an XCD start at different turns: at the
 // same one, rows of 8 or 32 KB have all of them ask the same memory channels (one token,
-// 4096 x 16384 from memory: 31.2 us, 27.4 so; 16 tokens, 16384 x 4096: 33.9 and 29.4).  One token, 4096 x 16384: 22.7
-// us, 5.9 TB/s; 24 tokens, 16384 x 4096: 24.0 and 3.9 for joining four parts; rows that are
-// not aligned take half as long again.
+// 4096 x 16384 from memory: 31.2 us, 27.4 so; 16 tokens, 16384 x 4096: 33.9 and 29.4).
+// One token, 4096 x 16384: 22.7 us, 5.9 TB/s; 24 tokens, 16384 x 4096: 24.0 and 3.9 for joining
+// four parts; rows of even lengths that are not aligned take a tenth longer, of odd ones
+// two fifths (one token, 4097 x 16000 36.6 us, 26.1 of 4096).
 constexpr int kFewTokens = 32, kFewSteps = 2, kFewTurn = 32 * kFewSteps;
 constexpr int few_waves(int rf) { return rf == 4 ? 8 : 16; }
 
-template <int RF, int NT, class Epi>
+// Eight elements of a row.  Loads of 16 bytes at odd elements take twice the time of those
+// at even ones (one token, 4097 x 16000: 56 us, 36.6 so), so rows of odd length (ODD) are
+// read from the even element at or before the first, the eighth by itself, and put in place
+// when they are used.
+template <bool ODD>
+struct FewVec {
+  V8 v;
+  __device__ __forceinline__ void load(const h16* p, const h16*) { v = load16u(p); }
+  __device__ __forceinline__ half8 get(int) const { return v.h; }
+};
+template <>
+struct FewVec<true> {
+  V8 v;
+  uint32_t last;
+  // (p: the even element, eighth: p's, or the next one, as the row starts)
+  __device__ __forceinline__ void load(const h16* p, const h16* eighth) {
+    typedef u32x4 even __attribute__((aligned(4)));
+    v.u = *reinterpret_cast<const even*>(p);
+    last = *reinterpret_cast<const uint16_t*>(eighth);
+  }
+  __device__ __forceinline__ half8 get(int odd) const {  // (odd: the row starts at an odd one)
+    V8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r.d[i] = __builtin_amdgcn_alignbit(i < 3 ? v.d[i + 1] : last, v.d[i], 16 * odd);
+    return r.h;
+  }
+};
+
+template <int RF, int NT, bool ODD, class Epi>
 __global__ __launch_bounds__(64 * few_waves(RF)) void dense_few(const Product a, Epi epi) {
   constexpr int U = kFewSteps, TURN = kFewTurn, WAVES = few_waves(RF);
   __shared__ floatx4 sums[WAVES][RF * NT * 64];
@@ -422,24 +452,30 @@ __global__ __launch_bounds__(64 * few_waves(RF)) void dense_few(const Product a,
   const int kbeg = part * per, kend = a.nk < kbeg + per ? a.nk : kbeg + per;
   const h16* pr[RF];  // (rows and tokens that are not there read the last one)
   const h16* qr[NT];
+  int po[RF], qo[NT];  // whether a row starts at an odd element
 #pragma unroll
   for (int f = 0; f < RF; ++f) {
-    const int r = p0 + 16 * f + m;
-    pr[f] = a.p + (int64_t)(r < a.np ? r : a.np - 1) * a.ldp + 8 * g;
+    const int r = p0 + 16 * f + m, row = r < a.np ? r : a.np - 1;
+    po[f] = ODD ? row & 1 : 0;
+    pr[f] = a.p + row * a.ldp + 8 * g - po[f];
   }
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = 16 * n + m;
-    qr[n] = a.q + (int64_t)(r < a.nq ? r : a.nq - 1) * a.ldq + 8 * g;
+    const int r = 16 * n + m, row = r < a.nq ? r : a.nq - 1;
+    qo[n] = ODD ? row & 1 : 0;
+    qr[n] = a.q + row * a.ldq + 8 * g - qo[n];
   }
-  V8 w[2][U][RF], x[2][U][NT];
-  auto load = [&](int k, V8 (&wv)[U][RF], V8 (&xv)[U][NT]) {
+  typedef FewVec<ODD> Vec;
+  Vec w[2][U][RF], x[2][U][NT];
+  auto load = [&](int k, Vec (&wv)[U][RF], Vec (&xv)[U][NT]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int f = 0; f < RF; ++f) wv[u][f] = load16u(pr[f] + k + 32 * u);
+      for (int f = 0; f < RF; ++f)
+        wv[u][f].load(pr[f] + k + 32 * u, pr[f] + po[f] + (k + 32 * u + 7));
 #pragma unroll
-      for (int n = 0; n < NT; ++n) xv[u][n] = load16u(qr[n] + k + 32 * u);
+      for (int n = 0; n < NT; ++n)
+        xv[u][n].load(qr[n] + k + 32 * u, qr[n] + qo[n] + (k + 32 * u + 7));
     }
   };
   floatx4 acc[RF][NT];
@@ -447,15 +483,20 @@ __global__ __launch_bounds__(64 * few_waves(RF)) void dense_few(const Product a,
   for (int f = 0; f < RF; ++f)
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[f][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  auto mma = [&](const V8 (&wv)[U][RF], const V8 (&xv)[U][NT]) {
+  auto mma = [&](const Vec (&wv)[U][RF], const Vec (&xv)[U][NT]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      half8 xh[NT];
 #pragma unroll
-      for (int f = 0; f < RF; ++f)
+      for (int n = 0; n < NT; ++n) xh[n] = xv[u][n].get(qo[n]);
+#pragma unroll
+      for (int f = 0; f < RF; ++f) {
+        const half8 wh = wv[u][f].get(po[f]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          acc[f][n] =
-              __builtin_amdgcn_mfma_f32_16x16x32_f16(wv[u][f].h, xv[u][n].h, acc[f][n], 0, 0, 0);
+          acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, xh[n], acc[f][n], 0, 0, 0);
+      }
+    }
   };
   constexpr int STEP = TURN * WAVES;
   // this wave's whole turns, and the one that the range ends in
@@ -487,9 +528,11 @@ __global__ __launch_bounds__(64 * few_waves(RF)) void dense_few(const Product a,
       const int left = kend - at - 8 * g;
       V8 wt[RF], xt[NT];
 #pragma unroll
-      for (int f = 0; f < RF; ++f) wt[f] = left > 0 ? load8_upto(pr[f] + at, left) : zero8();
+      for (int f = 0; f < RF; ++f)
+        wt[f] = left > 0 ? load8_upto(pr[f] + po[f] + at, left) : zero8();
 #pragma unroll
-      for (int n = 0; n < NT; ++n) xt[n] = left > 0 ? load8_upto(qr[n] + at, left) : zero8();
+      for (int n = 0; n < NT; ++n)
+        xt[n] = left > 0 ? load8_upto(qr[n] + qo[n] + at, left) : zero8();
 #pragma unroll
       for (int f = 0; f < RF; ++f)
 #pragma unroll
@@ -556,10 +599,11 @@ Few few_choice(int64_t np, int64_t nq, int64_t nk) {
   return best;
 }
 // Past 16 tokens of wide layers the tiles read each token less often (24 tokens of 4096 x
-// 4096: 12.8 us, 13.4 here; of 4096 x 2048: 10.2 and 8.0).
+// 4096: 12.8 us, 13.4 here; of 4096 x 2048: 10.2 and 8.0), unless rows have to be laid out
+// anew for them (4097 x 4000: 26.1 us, 18.2 here).
 bool few_ok(int64_t np, int64_t nq, int64_t nk) {
-  return nq <= 16 ||
-         (nq <= kFewTokens && (np >= 8192 || nk >= 8192 || np * nk <= 1 << 23));
+  return nq <= 16 || (nq <= kFewTokens && (np >= 8192 || nk >= 8192 || np * nk <= 1 << 23 ||
+                                           (nk & 7)));
 }
 
 template <class Epi>
@@ -572,10 +616,23 @@ hipError_t launch_few(Product a, const Epi& epi, void* sums, hipStream_t st) {
     typedef decltype(e) E;
     const int threads = 64 * few_waves(rf);
     const auto run = [&](auto kernel) { kernel<<<grid, threads, 0, st>>>(a, e); };
+    const auto pick = [&](auto tiles, auto odd) {
+      constexpr int NT = decltype(tiles)::value;
+      constexpr bool ODD = decltype(odd)::value;
+      run(rf == 4   ? dense_few<4, NT, ODD, E>
+          : rf == 2 ? dense_few<2, NT, ODD, E>
+                    : dense_few<1, NT, ODD, E>);
+    };
+    const auto of = [&](auto tiles) {
+      if (a.ldp & 1)
+        pick(tiles, std::true_type{});
+      else
+        pick(tiles, std::false_type{});
+    };
     if (a.nq <= 16)
-      run(rf == 4 ? dense_few<4, 1, E> : rf == 2 ? dense_few<2, 1, E> : dense_few<1, 1, E>);
+      of(std::integral_constant<int, 1>{});
     else
-      run(rf == 4 ? dense_few<4, 2, E> : rf == 2 ? dense_few<2, 2, E> : dense_few<1, 2, E>);
+      of(std::integral_constant<int, 2>{});
     return hipGetLastError();
   };
   if (a.parts == 1) return go(epi);

@@ -236,6 +236,10 @@ KERNELS = [(0, "few tokens, 16 rows in 16", (2, 16384, 48)),
            (0, "few tokens, 64 rows in 7", (1, 16041, 2063)),
            (0, "few tokens, 64 rows in 7", (18, 8599, 2069)),
            (0, "few tokens, 64 rows in 8", (32, 16384, 2048)),
+           (0, "few tokens, 32 rows", (8, 4096, 16384)),
+           (0, "few tokens, 64 rows", (24, 4096, 16384)),
+           (0, "few tokens, 64 rows in 4", (12, 16386, 4093)),
+           (0, "few tokens, 32 rows in 3", (27, 4097, 2051)),
            (0, "128 x 64 in 7", (34, 816, 1)), (0, "128 x 128", (2600, 24, 2601)),
            (0, "128 x 128 in 11", (5614, 3337, 1)), (0, "128 x 128 deep", (16400, 1, 1)),
            (0, "128 x 128 deep in 11", (2716, 2060, 1)), (0, "256 x 256", (8499, 259, 1467)),
