@@ -8,8 +8,8 @@
 //   dz_j = scale (dlogp ([j = t] - p_j) - dH p_j (logp_j + H)).
 // One pass over the row holds m, S and T by lane (each further group of elements may
 // raise m, which scales S and T down), and they are joined over the lanes and, where
-// few long rows are split over workgroups, over the parts.  The differences z_j - m
-// lose nothing to the size of the logits (see Sums).
+// few long rows are split over workgroups, over the parts.  How the exponents are
+// computed, and what S and T are relative to, goes by the scale (see Sums).
 //
 // The most probable classes: the top-th largest of the lanes' maxima bounds the top-th
 // largest element from below, so that a second look at the row (from the caches)
@@ -50,20 +50,32 @@ __device__ __forceinline__ u64 full_key(uint32_t value, int cls) {
   return ((u64)value << 32) | (0xFFFFFFFFu - (uint32_t)cls);
 }
 
-// The sums are taken relative to r = fl(m c), c = fl(scale / ln 2), not to m c: with it a
-// term's exponent z c - r is one instruction with one rounding (a factor may be
-// binary16), and what r is off by, known exactly, is put right at the end:
+// With c = fl(scale / ln 2), a term's exponent is fl(z c - r), r = fl(m c), where the scale
+// allows it (!DIFF): one instruction with one rounding (a factor may be binary16).  The
+// sums are then relative to r and not to m c, and what r is off by, known exactly, is put
+// right at the end:
 //   log sum exp(scale (z - m)) = log s + ln 2 (r - m c),  H = log s - ln 2 t / s.
+// While kLargest c < 2^24 (scales up to 177) r is off by at most 1/2, for any logits: the
+// largest term is 2^-1/2 to 2^1/2, and H's two parts cancel by ln 2 / 2 at most.  Larger
+// scales let r be off by enough for the largest term to overflow or vanish: there the
+// differences are taken first (DIFF), fl(fl(z - m) c), the largest exponent is 0 and no
+// term of t is positive.  They have kernels of their own, so that usual scales do not pay
+// for them (32768 x 1000: 56 us, 49 without; 4096 x 50048: 74 and 73).
 struct Sums {
   float m, s, t;  // m: a binary16 value; t in units of ln 2
 };
+constexpr float kLargest = 65504.0f;  // of binary16
+bool differences_first(float scale) { return !(kLargest * (scale * kLog2e) < 16777216.0f); }
 
 // exponent by which sums of maximum m count towards a maximum of top
+template <bool DIFF>
 __device__ __forceinline__ float shift(float m, float top, float c) {
-  return __builtin_fmaxf(m * c - top * c, kFloor);  // (the floor also where both are -inf)
+  // (the floor also where both are -inf)
+  return __builtin_fmaxf(DIFF ? (m - top) * c : m * c - top * c, kFloor);
 }
+template <bool DIFF>
 __device__ __forceinline__ void rescale(Sums& a, float top, float c) {
-  const float d = shift(a.m, top, c), f = __builtin_amdgcn_exp2f(d);
+  const float d = shift<DIFF>(a.m, top, c), f = __builtin_amdgcn_exp2f(d);
   a.t = f * (a.t + d * a.s);
   a.s *= f;
   a.m = top;
@@ -132,6 +144,7 @@ __device__ __forceinline__ void lane_load(const h16* z, int n, int i, V8 (&v)[kU
   }
 }
 
+template <bool DIFF>
 __device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
   half2 top = top2(v[0]);
 #pragma unroll
@@ -139,13 +152,14 @@ __device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
   // (a NaN is no maximum here; it reaches the sums below)
   float m = __builtin_fmaxf(to_f32(top[0]), to_f32(top[1]));
   m = __builtin_fmaxf(m, a.m);
-  rescale(a, m, c);
-  const float r = m == -__builtin_inff() ? 0.0f : m * c;
+  rescale<DIFF>(a, m, c);
+  const float r = m == -__builtin_inff() ? 0.0f : DIFF ? m : m * c;
 #pragma unroll
   for (int u = 0; u < kU; ++u)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float d = __builtin_fmaf(to_f32(v[u].h[k]), c, -r);
+      const float z = to_f32(v[u].h[k]);
+      const float d = DIFF ? (z - r) * c : __builtin_fmaf(z, c, -r);
       const float e = __builtin_amdgcn_exp2f(d);
       a.s += e;
       a.t = __builtin_fmaf(e, __builtin_fmaxf(d, kFloor), a.t);
@@ -153,12 +167,12 @@ __device__ __forceinline__ void lane_add(const V8 (&v)[kU], float c, Sums& a) {
 }
 
 // This lane's sums over z[0 .. n); v holds the last turn's elements.
-template <int NT>
+template <int NT, bool DIFF>
 __device__ __forceinline__ Sums lane_sums(const h16* z, int n, float c, V8 (&v)[kU]) {
   Sums a = {-__builtin_inff(), 0.0f, 0.0f};
   for (int i = threadIdx.x * 8; i < n; i += NT * 8 * kU) {
     lane_load<NT>(z, n, i, v);
-    lane_add(v, c, a);
+    lane_add<DIFF>(v, c, a);
   }
   return a;
 }
@@ -196,13 +210,13 @@ __device__ __forceinline__ float wave_all(float v, F f) {
 }
 
 // Joined over the workgroup, the same in every lane.
-template <int NT>
+template <int NT, bool DIFF>
 __device__ __forceinline__ Sums block_sums(Sums a, float c, float (*red)[3]) {
   constexpr int kWaves = NT / 64;
   const auto larger = [](float x, float y) { return __builtin_fmaxf(x, y); };
   const auto sum = [](float x, float y) { return x + y; };
   float m = wave_all(a.m, larger);
-  rescale(a, m, c);
+  rescale<DIFF>(a, m, c);
   a.s = wave_all(a.s, sum);
   a.t = wave_all(a.t, sum);
   const int wave = threadIdx.x >> 6;
@@ -219,7 +233,7 @@ __device__ __forceinline__ Sums block_sums(Sums a, float c, float (*red)[3]) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     Sums b = {red[w][0], red[w][1], red[w][2]};
-    rescale(b, m, c);
+    rescale<DIFF>(b, m, c);
     r.s += b.s;
     r.t += b.t;
   }
@@ -369,12 +383,13 @@ __device__ __forceinline__ void block_top(const h16* z, int n, int first, int to
 }
 
 // What a row's sums and largest keys give.
-template <int NT>
+template <int NT, bool DIFF>
 __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums& r,
                                        const u64* best) {
-  const bool none = r.s == 0.0f;  // every class is at -inf
+  const bool none = r.m == -__builtin_inff() && r.s == 0.0f;  // every class is at -inf
   const float c = a.scale * kLog2e, ln = logf(r.s);
-  const float log_s = __builtin_fmaf(kLn2, __builtin_fmaf(-r.m, c, r.m * c), ln);
+  const float log_s =
+      DIFF ? ln : __builtin_fmaf(kLn2, __builtin_fmaf(-r.m, c, r.m * c), ln);
   if (threadIdx.x == 0) {
     a.stats[3 * (int64_t)row] = r.m;
     a.stats[3 * (int64_t)row + 1] = none ? -__builtin_inff() : log_s;
@@ -402,7 +417,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Sums
 // What a part of a row leaves for the join.
 __host__ __device__ inline size_t part_bytes(int top) { return 16 + (size_t)top * 8; }
 
-template <int NT, bool PARTS, bool TOP>
+template <int NT, bool PARTS, bool TOP, bool DIFF>
 __global__ __launch_bounds__(NT) void logprob_kernel(const LogprobArgs a, int parts, int per) {
   __shared__ float red[NT / 64][3];
   __shared__ typename std::conditional<TOP, TopLds<NT>, u64>::type l;
@@ -412,15 +427,15 @@ __global__ __launch_bounds__(NT) void logprob_kernel(const LogprobArgs a, int pa
   const h16* z = a.z + row * a.stride + first;
   const float c = a.scale * kLog2e;
   V8 v[kU];
-  const Sums mine = lane_sums<NT>(z, n, c, v);
-  const Sums r = block_sums<NT>(mine, c, red);
+  const Sums mine = lane_sums<NT, DIFF>(z, n, c, v);
+  const Sums r = block_sums<NT, DIFF>(mine, c, red);
   const u64* best = nullptr;
   if constexpr (TOP) {
     block_top<NT>(z, n, first, a.top, mine.m, v, l);
     best = l.best;
   }
   if (!PARTS) {
-    finish<NT>(a, row, r, best);
+    finish<NT, DIFF>(a, row, r, best);
   } else {
     char* to = static_cast<char*>(a.ws) + blockIdx.x * part_bytes(a.top);
     if (threadIdx.x == 0) {
@@ -436,6 +451,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(const LogprobArgs a, int pa
 
 // A row from its parts: the sums, and the largest of their keys by counting.  32 parts with 20
 // keys each 5.0 us, a launch and two dependent trips to memory and LDS.
+template <bool DIFF>
 __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int parts) {
   __shared__ float red[kNT / 64][3];
   __shared__ TopLds<kNT> l;
@@ -447,7 +463,7 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
     const float* f = reinterpret_cast<const float*>(from + threadIdx.x * part_bytes(a.top));
     mine = {f[0], f[1], f[2]};
   }
-  const Sums r = block_sums<kNT>(mine, c, red);
+  const Sums r = block_sums<kNT, DIFF>(mine, c, red);
   if (a.top) {
     // a lane holds up to kPer of a part's keys; as in block_top, the lanes' maxima bound
     // what is ranked, and only `top` lanes reach the bound
@@ -490,7 +506,7 @@ __global__ __launch_bounds__(kNT) void logprob_join(const LogprobArgs a, int par
     __syncthreads();
     rank_candidates<kNT>(l, l.count < kCand ? l.count : kCand, a.top);
   }
-  finish<kNT>(a, row, r, l.best);
+  finish<kNT, DIFF>(a, row, r, l.best);
 }
 
 // The gradient: each lane 8 classes of a row at a time, no sums, bound by its bytes: 4096 x
@@ -538,14 +554,16 @@ size_t logprob_ws_bytes(int rows, int classes, int top) {
   return parts == 1 ? 0 : (size_t)rows * parts * part_bytes(top);
 }
 
-hipError_t launch_logprob(const LogprobArgs& a, hipStream_t st) {
+namespace {
+template <bool DIFF>
+hipError_t launch_sums(const LogprobArgs& a, hipStream_t st) {
   int parts = row_parts(a.rows, a.classes);
   const int per = part_len(a.classes, parts);
   parts = (a.classes + per - 1) / per;  // (none is empty)
   const unsigned grid = (unsigned)((int64_t)a.rows * parts);
   const auto go = [&](auto nt, auto split, auto top) {
     constexpr int NT = decltype(nt)::value;
-    logprob_kernel<NT, decltype(split)::value, decltype(top)::value>
+    logprob_kernel<NT, decltype(split)::value, decltype(top)::value, DIFF>
         <<<grid, NT, 0, st>>>(a, parts, per);
   };
   const auto pick = [&](auto nt, auto split) {
@@ -565,8 +583,13 @@ hipError_t launch_logprob(const LogprobArgs& a, hipStream_t st) {
   pick(small, std::true_type{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  logprob_join<<<a.rows, kNT, 0, st>>>(a, parts);
+  logprob_join<DIFF><<<a.rows, kNT, 0, st>>>(a, parts);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_logprob(const LogprobArgs& a, hipStream_t st) {
+  return differences_first(a.scale) ? launch_sums<true>(a, st) : launch_sums<false>(a, st);
 }
 
 hipError_t launch_logprob_bwd(const LogprobArgs& a, hipStream_t st) {
