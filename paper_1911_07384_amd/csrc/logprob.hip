@@ -530,8 +530,9 @@ __global__ __launch_bounds__(kNT) void logprob_bwd_kernel(const LogprobArgs a, i
     for (int e = 0; e < 8; ++e) {
       const float lp = (to_f32(v.h[e]) - m) * a.scale - log_s;
       const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-      // (below -200 p is 0, and a large dh must not make the factor infinite)
-      float g = -(dl + dh * (__builtin_fmaxf(lp, -200.0f) + h)) * p;
+      // (p before dh: with any finite dh a class of p = 0, at any lp from -200 down, adds 0)
+      const float q = p * (__builtin_fmaxf(lp, -200.0f) + h);
+      float g = -__builtin_fmaf(dh, q, dl * p);
       if (i + e == t) g += dl;
       o.h[e] = to_h16(none ? 0.0f : g * a.scale);
     }
