@@ -298,14 +298,22 @@ _device = _first_device
 
 
 def _held_ws(ws, ws_bytes, device):
-    """A workspace's address and bytes."""
+    """A workspace's address and bytes, at most a tensor's own."""
     if ws is None or isinstance(ws, int):
-        return ws, 0 if ws_bytes is None else int(ws_bytes)
+        size = 0 if ws_bytes is None else int(ws_bytes)
+        if size < 0:
+            raise ValueError(f"ws_bytes {size}")
+        return ws, size
     if ws.get_device() != device:
         raise ValueError(f"ws is on {ws.device}, which is not the current device")
     if not ws.is_contiguous():
         raise ValueError("ws: tensor must be contiguous")
-    return ws.data_ptr(), ws.nbytes if ws_bytes is None else int(ws_bytes)
+    size = ws.nbytes
+    if ws_bytes is not None:
+        if not 0 <= ws_bytes <= size:
+            raise ValueError(f"ws has {size} bytes, ws_bytes is {ws_bytes}")
+        size = int(ws_bytes)
+    return ws.data_ptr(), size
 
 
 def _stream(stream):
