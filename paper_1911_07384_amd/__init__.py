@@ -720,8 +720,21 @@ def fp16_rng_advance(rng, steps=1, stream=None) -> None:
     _check("fp16_rng_advance", lib().fp16_rng_advance(p, int(steps) % (1 << 64), _stream(stream)))
 
 
+def _fits(what, v, low, high):
+    """v, unless a field from low to high would cut it to another number."""
+    v = int(v)
+    if not low <= v <= high:
+        raise ValueError(f"{what} {v}")
+    return v
+
+
+def _int32(**fields):
+    return [_fits(k, v, -(1 << 31), (1 << 31) - 1) for k, v in fields.items()]
+
+
 def fp16_dropout(x, residual, y, p, rng, site=0, n=None, stream=None) -> None:
     """y = dropout of x (+ residual); the gradient is the same call on dy."""
+    site = _fits("site", site, 0, 0xFFFFFFFF)
     n = x.numel() if n is None else int(n)
     dev = _device()
     _check("fp16_dropout", lib().fp16_dropout(
@@ -738,8 +751,9 @@ _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, None: 0}
 
 def dense_desc(tokens, inputs, outputs, act="none", drop=0.0, site=0) -> DenseDesc:
     """act: a name ("none", "relu", "gelu", "silu") or one of the ACT_ numbers."""
-    return DenseDesc(int(tokens), int(inputs), int(outputs),
-                     act if isinstance(act, int) else _ACTS[act], float(drop), int(site))
+    return DenseDesc(*_int32(tokens=tokens, inputs=inputs, outputs=outputs,
+                             act=act if isinstance(act, int) else _ACTS[act]),
+                     float(drop), _fits("site", site, 0, 0xFFFFFFFF))
 
 
 def fp16_dense_workspace_bytes(desc: DenseDesc, call=None) -> int:
@@ -782,8 +796,9 @@ def fp16_dense_bwd(desc, x, w, z, dy, dx, dw, dbias=None, rng=None, ws=None, ws_
 
 def logprob_desc(rows, classes, stride=None, scale=1.0, top=0) -> LogprobDesc:
     """stride: elements from row to row (None: classes); scale: one over a temperature."""
-    return LogprobDesc(int(rows), int(classes), int(classes if stride is None else stride),
-                       float(scale), int(top))
+    rows, classes, stride, top = _int32(
+        rows=rows, classes=classes, stride=classes if stride is None else stride, top=top)
+    return LogprobDesc(rows, classes, stride, float(scale), top)
 
 
 def fp16_logprobs_workspace_bytes(desc: LogprobDesc) -> int:
