@@ -794,6 +794,9 @@ def fp16_dense_bwd(desc, x, w, z, dy, dx, dw, dbias=None, rng=None, ws=None, ws_
 
 # ---- log probabilities -------------------------------------------------------
 
+LOGPROB_TOP_MAX = 64  # FP16_LOGPROB_TOP_MAX
+
+
 def logprob_desc(rows, classes, stride=None, scale=1.0, top=0) -> LogprobDesc:
     """stride: elements from row to row (None: classes); scale: one over a temperature."""
     rows, classes, stride, top = _int32(

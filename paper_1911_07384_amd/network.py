@@ -739,8 +739,10 @@ class ResNet50:
         """The forward of the loaded batch and what its logits say, as tensors: "logits"
         [n, classes] (the classifier's dense layer on the features, without dropout),
         "logp" [n] (of the labels), "stats" [n, 3] (largest logit, log of the sum,
-        entropy), "top_id" and "top_logp" [n, top].  BN uses this batch's statistics, as
-        in training."""
+        entropy), "top_id" and "top_logp" [n, top], of up to F.LOGPROB_TOP_MAX classes.  BN
+        uses this batch's statistics, as in training."""
+        if not 0 <= top <= min(F.LOGPROB_TOP_MAX, self.classes):
+            raise ValueError(f"top {top} of {self.classes} classes")
         self.forward()
         if self.side is not None:  # (the backward's filters, which no backward waits for)
             torch.cuda.current_stream().wait_event(self._wf_ready)
