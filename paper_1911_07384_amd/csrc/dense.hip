@@ -404,14 +404,15 @@ hipError_t launch_product(Product a, const Epi& epi, void* sums, hipStream_t st)
 // LDS in their order.  Neighbouring workgroups of an XCD start at different turns: at the
 // same one, rows of 8 or 32 KB have all of them ask the same memory channels (one token,
 // 4096 x 16384 from memory: 31.2 us, 27.4 so; 16 tokens, 16384 x 4096: 33.9 and 29.4).
-// One token, 4096 x 16384: 22.7 us, 5.9 TB/s; 24 tokens, 16384 x 4096: 24.0 and 3.9 for joining
-// four parts; rows of even lengths that are not aligned take a tenth longer, of odd ones
-// two fifths (one token, 4097 x 16000 36.6 us, 26.1 of 4096).
+// One token, 4096 x 16384: 22.4 us, 6.0 TB/s; 24 tokens, 16384 x 4096: 24.0 and 4.1 for joining
+// four parts.  Rows that are not aligned: one token, four matrices W in turn (from memory),
+// 4096 x 16000 27.1 us, 4098 x 16000 29.2, 4097 x 16000 36.4; one W again and again (in part
+// from the caches) 23.9, 22.7 and 29.8.
 constexpr int kFewTokens = 32, kFewSteps = 2, kFewTurn = 32 * kFewSteps;
 constexpr int few_waves(int rf) { return rf == 4 ? 8 : 16; }
 
 // Eight elements of a row.  Loads of 16 bytes at odd elements take twice the time of those
-// at even ones (one token, 4097 x 16000: 56 us, 36.6 so), so rows of odd length (ODD) are
+// at even ones (one token, 4097 x 16000 from memory: 56 us, 36.4 so), so rows of odd length (ODD) are
 // read from the even element at or before the first, the eighth by itself, and put in place
 // when they are used.
 template <bool ODD>
@@ -676,7 +677,11 @@ hipError_t launch_repack(int cols, const Repack& one, const Repack& two, hipStre
 
 constexpr int kRows = 32;  // of a workgroup's partial sums
 
-// One vector of dz: from a row's dy and z, columns c .. c + 7.
+// One vector of dz: from a row's dy and z, columns c .. c + 7.  dz is rounded to binary16, to be
+// an operand of the matrix cores in both products that follow: two parts of it would take
+// the products' time twice.  dx and dW are then off by 2.9e-4 (relative 2-norm, 4096 x 4096 x
+// 4096) where a float32 dz leaves their own rounding's 2.1e-4, and a dz past 65504 is
+// infinite.  dbias is summed before the rounding.
 template <int ACT>
 __device__ __forceinline__ V8 dz8(const V8& y, const V8& z, int64_t i, const Drop& drop,
                                   float (&s)[8]) {
